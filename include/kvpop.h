@@ -234,8 +234,8 @@ kvpop_status kvpop_prompt_attention(const void* Q_dev, const void* K_dev, const 
 
 /* First device-side error (a bounded wait that expired) recorded by the
  * cache-free calls kvpop_prompt_attention, kvpop_causal_lse,
- * kvpop_future_target and kvpop_attend_noalloc since the last call of this
- * function: KVPOP_OK, or
+ * kvpop_future_target, kvpop_attend_noalloc and the kvpop_paged_* calls (which also
+ * record bad page tables and offsets) since the last call of this function: KVPOP_OK, or
  * KVPOP_ERR_DEVICE_CHECK (details in kvpop_last_error).  Synchronises `stream`
  * and clears the record. */
 kvpop_status kvpop_standalone_status(cudaStream_t stream);
@@ -428,6 +428,91 @@ kvpop_status kvpop_attend_noalloc(const void* slotK_dev, const void* slotV_dev,
                                   int32_t n_kv_heads, int32_t q_per_kv, int32_t head_dim,
                                   int32_t budget_B, int32_t delay_D, kvpop_dtype kv_dtype,
                                   cudaStream_t stream);
+
+/* Paged 8-bit key/value cache: layers that keep every token, beside the compressed ones (no
+ * counterpart in the paper).  The caller owns all memory; a call takes what it describes.
+ *
+ * A page holds `page` consecutive positions of one sequence, for every KV head, as e4m3 bytes
+ * (1 sign, 4 exponent, 3 mantissa bits; no infinities).  Each block of 16 positions and KV head
+ * has a scale for its keys and one for its values, a power of two: a byte stands for its e4m3
+ * value times the scale.  Blocks and pages start at positions that are multiples of their size. */
+typedef struct {
+  void* k_pages_dev;       /* [n_pages][H][page][d], 16-byte aligned                  */
+  void* v_pages_dev;       /* the same                                                */
+  float* k_scale_dev;      /* [n_pages][H][page / 16], positive powers of two in use  */
+  float* v_scale_dev;      /* the same                                                */
+  int32_t n_pages;         /* >= 1                                                    */
+  int32_t n_kv_heads;      /* H >= 1                                                  */
+  int32_t head_dim;        /* d in {64, 128}                                          */
+  int32_t page;            /* a power of two, 16 .. 1024                              */
+} kvpop_paged_pool;
+
+/* New tokens of n_seq sequences.  Sequence s holds lens_dev[s] tokens before them (-1: an idle
+ * place of the batch, whose tokens are passed over) and its new tokens are the rows starts_dev[s]
+ * .. starts_dev[s + 1] - 1 of the token tensors, at the positions lens_dev[s] onwards; without
+ * starts_dev each sequence has one, row s.  Entry p / page of row s of the table is the page of
+ * position p.  An entry in use that is no page of the pool, a position past the table's row or
+ * offsets that do not ascend are recorded (kvpop_standalone_status) and what they concern is left
+ * out; nothing outside the given memory is touched.  Nothing here is changed: the caller advances
+ * lens_dev once the last layer has taken the tokens. */
+typedef struct {
+  const int32_t* table_dev;    /* [n_seq] rows of max_pages entries, table_stride apart     */
+  const int32_t* lens_dev;     /* [n_seq]                                                   */
+  const int32_t* starts_dev;   /* [n_seq + 1], starts_dev[0] = 0, ascending; or NULL        */
+  int64_t table_stride;        /* in entries, >= max_pages                                  */
+  int32_t max_pages;           /* >= 1                                                      */
+  int32_t n_seq;               /* >= 0                                                      */
+  int32_t n_tokens;            /* rows of the token tensors (n_seq without starts_dev)      */
+  int32_t max_new;             /* most new tokens of a sequence, as far as known (>= 1): it
+                                  chooses among kernels, and outputs do not rest on it      */
+} kvpop_paged_batch;
+
+/* Rows [token][head][d] with strides in elements, multiples of 16 bytes; d is contiguous. */
+typedef struct {
+  const void* data_dev;        /* 16-byte aligned */
+  int64_t token_stride;
+  int64_t head_stride;
+} kvpop_rows;
+
+/* Append: rotate the new tokens' queries and keys by their positions, and write keys and values
+ * to the cache.  With cos, sin the tables' row of the token's position, pairs (a, b) become
+ *   (a cos - b sin, b cos + a sin),  each product and sum rounded to fp32;
+ * pairs are (j, j + rot_dim / 2) for j < rot_dim / 2, or (2 j, 2 j + 1) with interleaved = 1;
+ * values from rot_dim on are not turned.  A block's scale is the least 2^e, e >= -96, with every
+ * finite magnitude of its tokens so far at most 448 * 2^e; values are rounded to the nearest e4m3
+ * (ties to even).  A token that raises the scale of a block has the block's earlier bytes moved
+ * to it: exactly, but that those which fall below 2^-6 of it are rounded again.  Infinities, NaN
+ * and magnitudes of 2^108 and more are stored as NaN.  A block's first token starts its scale
+ * anew; rows past the new tokens keep their bytes.
+ *   q [n_tokens][n_q_heads][d] with q_out_dev [n_tokens][n_q_heads][d] bf16 (contiguous, may not
+ *   overlap q), or both NULL; k, v [n_tokens][H][d]; dtype of q, k and v
+ *   cos_dev, sin_dev [max_pos][rot_dim / 2] fp32, 16-byte aligned; rot_dim a multiple of 16, 0 ..
+ *   d (0: no rotation, tables unused).  Tokens at max_pos and beyond are recorded and left out.
+ * Asynchronous on `stream`; no allocation. */
+kvpop_status kvpop_paged_append(const kvpop_paged_pool* pool, const kvpop_paged_batch* batch,
+                                const kvpop_rows* q, int32_t n_q_heads, const kvpop_rows* k,
+                                const kvpop_rows* v, kvpop_dtype dtype, const float* cos_dev,
+                                const float* sin_dev, int32_t rot_dim, int32_t max_pos,
+                                int32_t interleaved, void* q_out_dev, cudaStream_t stream);
+
+/* Bytes of device workspace kvpop_paged_attend needs on the current device (0 without one). */
+size_t kvpop_paged_workspace_bytes(void);
+
+/* Attention of the new tokens over the cache, their own keys (appended before) included: for
+ * token i of a sequence and query head h * G + g, over the positions t <= lens + i,
+ *   y = sum_t softmax_t(q.k_t / sqrt(d)) v_t,   lse = log sum_t exp(q.k_t / sqrt(d)).
+ *   q [n_tokens][n_q_heads][d] bf16, n_q_heads = H * G
+ *   out_dev [n_tokens][n_q_heads][d] contiguous, 16-byte aligned, fp32 or bf16 (out_dtype); its
+ *   type is also the precision of the softmax's weights: 22 bits for fp32, 11 for bf16
+ *   lse_dev [n_tokens][n_q_heads] fp32, or NULL
+ * An idle place's tokens get zeros and -inf.  workspace_dev: kvpop_paged_workspace_bytes()
+ * bytes, 256-byte aligned, owned by the caller and zero before its first call; every call leaves
+ * it fit for the next one, and calls that share it have to be serialised.  Asynchronous on
+ * `stream`; no allocation. */
+kvpop_status kvpop_paged_attend(const kvpop_paged_pool* pool, const kvpop_paged_batch* batch,
+                                const kvpop_rows* q, int32_t n_q_heads, void* out_dev,
+                                kvpop_dtype out_dtype, float* lse_dev, void* workspace_dev,
+                                size_t workspace_bytes, cudaStream_t stream);
 
 /* Description of the last failing CUDA call made by this library on the
  * calling thread ("" if none): call site, error name and message. */

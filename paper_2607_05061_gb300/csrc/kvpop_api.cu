@@ -7,6 +7,7 @@
 #include <vector>
 
 #include "kvpop_argmin.cuh"
+#include "kvpop_paged.cuh"
 
 using namespace kvpop;
 
@@ -798,6 +799,111 @@ kvpop_status kvpop_standalone_status(cudaStream_t stream) {
     return e == cudaSuccess ? KVPOP_ERR_DEVICE_CHECK : from_cuda(e);
   }
   return KVPOP_OK;
+}
+
+// ---- paged 8-bit cache
+static bool paged_pool_ok(const kvpop_paged_pool* p) {
+  return p && p->n_pages >= 1 && p->n_kv_heads >= 1 && p->n_kv_heads <= (1 << 20) &&
+         (p->head_dim == 64 || p->head_dim == 128) && p->page >= paged::BLK && p->page <= 1024 &&
+         (p->page & (p->page - 1)) == 0 && p->k_pages_dev && p->v_pages_dev && p->k_scale_dev && p->v_scale_dev;
+}
+static bool paged_batch_ok(const kvpop_paged_batch* b) {
+  return b && b->n_seq >= 0 && b->n_tokens >= 0 && (b->starts_dev || b->n_tokens == b->n_seq) &&
+         b->max_new >= 1 && b->max_pages >= 1 && b->table_stride >= b->max_pages;
+}
+static bool rows_aligned(const kvpop_rows* r, int esz) {
+  return aligned16(r->data_dev) && r->token_stride * esz % 16 == 0 && r->head_stride * esz % 16 == 0;
+}
+static bool paged_aligned(const kvpop_paged_pool* p, const kvpop_paged_batch* b) {
+  return aligned16(p->k_pages_dev) && aligned16(p->v_pages_dev) && aligned4(p->k_scale_dev) &&
+         aligned4(p->v_scale_dev) && aligned4(b->table_dev) && aligned4(b->lens_dev) && aligned4(b->starts_dev);
+}
+static paged::Pool paged_pool(const kvpop_paged_pool* p) {
+  paged::Pool q;
+  q.k = static_cast<unsigned char*>(p->k_pages_dev);
+  q.v = static_cast<unsigned char*>(p->v_pages_dev);
+  q.ks = p->k_scale_dev;
+  q.vs = p->v_scale_dev;
+  q.n_pages = p->n_pages;
+  q.H = p->n_kv_heads;
+  q.d = p->head_dim;
+  q.page = p->page;
+  q.page_shift = 0;
+  while ((1 << q.page_shift) < p->page) ++q.page_shift;
+  return q;
+}
+static paged::Batch paged_batch(const kvpop_paged_batch* b) {
+  paged::Batch c;
+  c.table = b->table_dev;
+  c.lens = b->lens_dev;
+  c.starts = b->starts_dev;
+  c.table_stride = b->table_stride;
+  c.max_pages = b->max_pages;
+  c.n_seq = b->n_seq;
+  c.n_tokens = b->n_tokens;
+  c.max_new = b->max_new;
+  return c;
+}
+static int device_sms() {
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+    cudaGetLastError();
+    return 0;
+  }
+  return sms;
+}
+
+kvpop_status kvpop_paged_append(const kvpop_paged_pool* pool, const kvpop_paged_batch* batch,
+                                const kvpop_rows* q, int32_t n_q_heads, const kvpop_rows* k,
+                                const kvpop_rows* v, kvpop_dtype dtype, const float* cos_dev,
+                                const float* sin_dev, int32_t rot_dim, int32_t max_pos,
+                                int32_t interleaved, void* q_out, cudaStream_t stream) {
+  if (!paged_pool_ok(pool) || !paged_batch_ok(batch) || !k || !v || (dtype != KVPOP_F32 && dtype != KVPOP_BF16) ||
+      (q == nullptr) != (q_out == nullptr) || (q && (n_q_heads < 1 || n_q_heads > (1 << 20))) || rot_dim < 0 ||
+      rot_dim > pool->head_dim || rot_dim % 16 != 0 || (rot_dim > 0 && (!cos_dev || !sin_dev || max_pos < 1)) ||
+      (interleaved != 0 && interleaved != 1))
+    return KVPOP_ERR_INVALID_ARG;
+  // every (block of tokens, head) has a number below 2^31
+  const long long units = (long long)batch->n_tokens / paged::BLK + 2ll * batch->n_seq;
+  if (units * (2ll * pool->n_kv_heads + (q ? n_q_heads : 0)) > INT32_MAX - 1024) return KVPOP_ERR_INVALID_ARG;
+  if (batch->n_seq == 0 || batch->n_tokens == 0) return KVPOP_OK;
+  if (!batch->table_dev || !batch->lens_dev || !k->data_dev || !v->data_dev || (q && !q->data_dev))
+    return KVPOP_ERR_INVALID_ARG;
+  const int esz = dtype == KVPOP_BF16 ? 2 : 4;
+  if (!paged_aligned(pool, batch) || !rows_aligned(k, esz) || !rows_aligned(v, esz) ||
+      (q && (!rows_aligned(q, esz) || !aligned16(q_out))) ||
+      (rot_dim > 0 && (!aligned16(cos_dev) || !aligned16(sin_dev))))
+    return KVPOP_ERR_ALIGN;
+  return from_cuda(NOTE(launch_paged_append(
+      paged_pool(pool), paged_batch(batch), q ? q->data_dev : nullptr, q ? q->token_stride : 0,
+      q ? q->head_stride : 0, n_q_heads, k->data_dev, k->token_stride, k->head_stride, v->data_dev,
+      v->token_stride, v->head_stride, dtype, cos_dev, sin_dev, rot_dim, max_pos, interleaved, q_out,
+      standalone_err(), stream)));
+}
+
+size_t kvpop_paged_workspace_bytes(void) {
+  const int sms = device_sms();
+  return sms > 0 ? paged_attend_workspace(sms) : 0;
+}
+
+kvpop_status kvpop_paged_attend(const kvpop_paged_pool* pool, const kvpop_paged_batch* batch,
+                                const kvpop_rows* q, int32_t n_q_heads, void* out, kvpop_dtype out_dtype,
+                                float* lse, void* workspace, size_t workspace_bytes, cudaStream_t stream) {
+  if (!paged_pool_ok(pool) || !paged_batch_ok(batch) || !q || (out_dtype != KVPOP_F32 && out_dtype != KVPOP_BF16) ||
+      n_q_heads < 1 || n_q_heads % pool->n_kv_heads != 0 || n_q_heads > (1 << 20))
+    return KVPOP_ERR_INVALID_ARG;
+  if (batch->n_seq == 0 || batch->n_tokens == 0) return KVPOP_OK;
+  if (!batch->table_dev || !batch->lens_dev || !q->data_dev || !out || !workspace) return KVPOP_ERR_INVALID_ARG;
+  if (!paged_aligned(pool, batch) || !rows_aligned(q, 2) || !aligned16(out) || !aligned4(lse) ||
+      (reinterpret_cast<uintptr_t>(workspace) & 255u))
+    return KVPOP_ERR_ALIGN;
+  const int sms = device_sms();
+  if (sms <= 0) return KVPOP_ERR_CUDA;
+  if (workspace_bytes < paged_attend_workspace(sms)) return KVPOP_ERR_INVALID_ARG;
+  return from_cuda(NOTE(launch_paged_attend(paged_pool(pool), paged_batch(batch), q->data_dev, q->token_stride,
+                                            q->head_stride, n_q_heads, out, out_dtype == KVPOP_F32, lse, workspace,
+                                            sms, standalone_err(), stream)));
 }
 
 kvpop_status kvpop_decode_ingest(kvpop_cache* c, const void* q, const void* k, const void* v,

@@ -1,0 +1,87 @@
+// Paged 8-bit key/value cache: what its kernels share.
+//
+// A page holds `page` consecutive positions of one sequence for every KV head, keys and values
+// apart: [n_pages][H][page][d] e4m3 bytes.  A block is 16 consecutive positions; each (block, KV
+// head) has one scale for its keys and one for its values, [n_pages][H][page / 16] fp32, always a
+// power of two 2^e with e in [-96, 100].  e4m3 has the same relative precision at every scale, so
+// a power of two costs nothing against amax / 448, and products by scales are exact.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "kvpop_internal.cuh"
+
+namespace kvpop {
+namespace paged {
+
+constexpr int BLK = 16;                // positions that share a scale
+constexpr int E_MIN = -96;             // smallest scale exponent
+constexpr float VALUE_LIMIT = 3.2451855e32f;   // 2^108: from here on a value is stored as NaN
+enum : int {
+  ERR_PAGE = 41,                       // a page number outside the pool, or a position past the table
+  ERR_BATCH = 42,                      // token offsets that are not ascending, or more than max_new tokens
+  ERR_ROTATION = 43,                   // a position past the rotation table
+};
+
+struct Batch {                         // kvpop_paged_batch
+  const int32_t* table;                // [n_seq] rows of max_pages page numbers, table_stride apart
+  const int32_t* lens;                 // [n_seq] tokens held before the new ones, -1: idle
+  const int32_t* starts;               // [n_seq + 1] first new token of each sequence, or null: one each
+  long long table_stride;
+  int max_pages, n_seq, n_tokens, max_new;
+};
+
+struct Pool {                          // kvpop_paged_pool
+  unsigned char *k, *v;
+  float *ks, *vs;
+  int n_pages, H, d, page, page_shift;
+};
+
+__device__ __forceinline__ void report(int32_t* err, int code) {
+  if (err) atomicCAS(err, 0, code);
+}
+
+// New tokens of a sequence: first, first + n are rows of the batch's token tensors whatever
+// `starts` holds.
+struct SeqTokens {
+  int first, n, len;
+};
+__device__ __forceinline__ SeqTokens seq_tokens(const Batch& b, int s, int32_t* err) {
+  SeqTokens t;
+  t.len = b.lens[s];
+  if (b.starts == nullptr) {
+    t.first = s;
+    t.n = 1;
+  } else {
+    const int a = b.starts[s], e = b.starts[s + 1];
+    t.first = min(max(a, 0), b.n_tokens);
+    t.n = max(min(e, b.n_tokens) - t.first, 0);
+    if (a < 0 || e < a || e > b.n_tokens) report(err, ERR_BATCH);
+  }
+  return t;
+}
+
+// Page of a sequence's position `pos` (pos / page below max_pages); -1, recorded, if it is none.
+__device__ __forceinline__ int page_of(const Batch& b, const Pool& p, int s, int pos, int32_t* err) {
+  const int id = b.table[(long long)s * b.table_stride + (pos >> p.page_shift)];
+  if ((unsigned)id < (unsigned)p.n_pages) return id;
+  report(err, ERR_PAGE);
+  return -1;
+}
+
+}  // namespace paged
+
+cudaError_t launch_paged_append(const paged::Pool& pool, const paged::Batch& b, const void* q, long long q_ts,
+                                long long q_hs, int HQ, const void* k, long long k_ts, long long k_hs,
+                                const void* v, long long v_ts, long long v_hs, int dtype, const float* cos_,
+                                const float* sin_, int rot, int max_pos, int interleaved, void* q_out,
+                                int32_t* err, cudaStream_t stream);
+
+// Workspace of the attention on the current device: bytes, of which the first
+// paged_attend_counter_bytes have to be zero before the first call and are zero after every call.
+size_t paged_attend_workspace(int sms);
+cudaError_t launch_paged_attend(const paged::Pool& pool, const paged::Batch& b, const void* q, long long q_ts,
+                                long long q_hs, int HQ, void* out, int out_f32, float* lse, void* workspace,
+                                int sms, int32_t* err, cudaStream_t stream);
+
+}  // namespace kvpop

@@ -43,6 +43,22 @@ class kvpop_scorer(ctypes.Structure):
                 ("log_gamma", c_void_p), ("input_kind", c_int32), ("activation", c_int32)]
 
 
+class kvpop_paged_pool(ctypes.Structure):
+    _fields_ = [("k_pages_dev", c_void_p), ("v_pages_dev", c_void_p), ("k_scale_dev", c_void_p),
+                ("v_scale_dev", c_void_p), ("n_pages", c_int32), ("n_kv_heads", c_int32),
+                ("head_dim", c_int32), ("page", c_int32)]
+
+
+class kvpop_paged_batch(ctypes.Structure):
+    _fields_ = [("table_dev", c_void_p), ("lens_dev", c_void_p), ("starts_dev", c_void_p),
+                ("table_stride", ctypes.c_int64), ("max_pages", c_int32), ("n_seq", c_int32),
+                ("n_tokens", c_int32), ("max_new", c_int32)]
+
+
+class kvpop_rows(ctypes.Structure):
+    _fields_ = [("data_dev", c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
 ACTIVATIONS = {"gelu": 0, "silu": 1, "identity": 2}
 
 
@@ -94,6 +110,10 @@ _SIGS = {
     "kvpop_project_qkv_settled": (ctypes.c_int, [_P, _P, _P, _P, c_int32, c_int32, c_int32, c_int32, _P,
                                                  _P, _P, _P]),
     "kvpop_project_out_settled": (ctypes.c_int, [_P, _P, _P, c_int32, c_int32, c_int32, _P, _P]),
+    "kvpop_paged_append": (ctypes.c_int, [_P, _P, _P, c_int32, _P, _P, ctypes.c_int, _P, _P, c_int32, c_int32,
+                                          c_int32, _P, _P]),
+    "kvpop_paged_workspace_bytes": (c_size_t, []),
+    "kvpop_paged_attend": (ctypes.c_int, [_P, _P, _P, c_int32, _P, ctypes.c_int, _P, _P, c_size_t, _P]),
     "kvpop_standalone_status": (ctypes.c_int, [_P]),
     "kvpop_last_error": (ctypes.c_char_p, []),
     "kvpop_debug_fail_alloc_after": (None, [c_int32]),

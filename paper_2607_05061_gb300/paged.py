@@ -1,0 +1,242 @@
+"""Paged 8-bit key/value cache: layers that keep every token, beside the compressed ones.
+
+``PagedCache`` is one attention layer's pages (e4m3 bytes with a power-of-two scale for each
+block of 16 tokens and KV head) and the two calls on them, ``append`` (rotation and write) and
+``attend``; both run in ``libkvpop.so`` and this module only checks and passes arguments.
+``PageTable`` hands pages out to the sequences of a batch on the host; the layers of a model
+share one table and one ``lens``, and each has its own pages.
+
+One decode step of a batch::
+
+    table.grow(new=1)                                   # pages for the coming tokens
+    for layer, cache in ...:
+        q = cache.append(table.dev, table.lens, q, k, v, cos, sin)
+        o, _ = cache.attend(table.dev, table.lens, q)
+    table.advance(new=1)                                # once, after the last layer
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import List, Optional, Sequence
+
+import torch
+
+from .kvpop import (KVPOP_BF16, KVPOP_F32, _ck, _ptr, _stream, kvpop_paged_append, kvpop_paged_attend,
+                    kvpop_paged_batch, kvpop_paged_pool, kvpop_paged_workspace_bytes, kvpop_rows)
+
+BLOCK = 16               # tokens that share a scale
+_F8 = torch.float8_e4m3fn
+_CODES = {torch.float32: KVPOP_F32, torch.bfloat16: KVPOP_BF16}
+
+
+def _want(what, name, t, dtype, shape):
+    """Refuses a tensor that a call would read or write past its end or as another type."""
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{what}: {name} is {t.dtype} {tuple(t.shape)} (strides {tuple(t.stride())}), not "
+                         f"contiguous {dtype} {tuple(shape)}")
+
+
+class PagedCache:
+    """One layer's pages.  ``k_pages, v_pages [n_pages][H][page][d]`` (float8_e4m3fn) and
+    ``k_scale, v_scale [n_pages][H][page / 16]`` (fp32) stay the caller's; ``PagedCache.empty``
+    makes them.  ``workspace``: another cache's, to share (calls on both are then serialised)."""
+
+    def __init__(self, k_pages, v_pages, k_scale, v_scale, workspace: Optional[torch.Tensor] = None):
+        n, H, page, d = k_pages.shape
+        for name, t in (("k_pages", k_pages), ("v_pages", v_pages)):
+            _want("PagedCache", name, t, _F8, (n, H, page, d))
+        for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+            _want("PagedCache", name, t, torch.float32, (n, H, page // BLOCK))
+        if d not in (64, 128) or page < BLOCK or page > 1024 or page & (page - 1):
+            raise ValueError(f"PagedCache: head size {d} (64 or 128), page {page} (a power of two, 16 to 1024)")
+        self.device = k_pages.device
+        for name, t in (("v_pages", v_pages), ("k_scale", k_scale), ("v_scale", v_scale)):
+            if t.device != self.device:
+                raise ValueError(f"PagedCache: {name} is on {t.device}, k_pages on {self.device}")
+        self.k_pages, self.v_pages, self.k_scale, self.v_scale = k_pages, v_pages, k_scale, v_scale
+        self.H, self.page, self.d = H, page, d
+        self._pool = kvpop_paged_pool(_ptr(k_pages), _ptr(v_pages), _ptr(k_scale), _ptr(v_scale), n, H, d, page)
+        if workspace is None and self.device.type == "cuda":
+            with torch.cuda.device(self.device):
+                workspace = torch.zeros(int(kvpop_paged_workspace_bytes()), dtype=torch.uint8, device=self.device)
+                torch.cuda.current_stream().synchronize()      # zero for whatever stream comes first
+        self.workspace = workspace
+
+    @classmethod
+    def empty(cls, n_pages: int, n_kv_heads: int, head_dim: int, page: int = 64, device="cuda",
+              workspace: Optional[torch.Tensor] = None) -> "PagedCache":
+        pages = [torch.zeros((n_pages, n_kv_heads, page, head_dim), dtype=torch.uint8, device=device).view(_F8)
+                 for _ in range(2)]
+        scales = [torch.ones((n_pages, n_kv_heads, page // BLOCK), device=device) for _ in range(2)]
+        return cls(*pages, *scales, workspace=workspace)
+
+    # ------------------------------------------------------------------ arguments
+    def _here(self, what, **tensors):
+        for name, t in tensors.items():
+            if t is not None and t.device != self.device:
+                raise ValueError(f"{what}: {name} is on {t.device}, the cache on {self.device}")
+        if self.device.type != "cuda" or self.device.index != torch.cuda.current_device():
+            raise ValueError(f"{what}: the cache is on {self.device}, which is not the current CUDA device")
+
+    def _batch(self, what, table, lens, starts, n_tokens, max_new):
+        n = lens.shape[0] if lens.dim() == 1 else -1
+        _want(what, "lens", lens, torch.int32, (n,))
+        if table.dtype != torch.int32 or table.dim() != 2 or table.shape[0] != n or table.shape[1] < 1 or \
+                table.stride(1) != 1 or (n > 1 and table.stride(0) < table.shape[1]):
+            raise ValueError(f"{what}: table is {table.dtype} {tuple(table.shape)} (strides {tuple(table.stride())}), "
+                             f"not {torch.int32} ({n}, pages) with neighbouring entries")
+        if starts is not None:
+            _want(what, "starts", starts, torch.int32, (n + 1,))
+        elif n_tokens != n:
+            raise ValueError(f"{what}: {n_tokens} tokens of {n} sequences need starts")
+        if max_new is None:
+            max_new = 1 if starts is None else max(n_tokens, 1)
+        stride = max(table.stride(0), table.shape[1])
+        return kvpop_paged_batch(_ptr(table), _ptr(lens), _ptr(starts), stride, table.shape[1], n, n_tokens,
+                                 max(int(max_new), 1))
+
+    def _rows(self, what, name, t, dtype, n_tokens, heads):
+        if t.dtype != dtype or t.dim() != 3 or t.shape[0] != n_tokens or t.shape[2] != self.d or \
+                (heads is not None and t.shape[1] != heads) or t.shape[1] < 1 or t.stride(2) != 1 or \
+                t.stride(0) < 0 or t.stride(1) < 0:
+            raise ValueError(f"{what}: {name} is {t.dtype} {tuple(t.shape)} (strides {tuple(t.stride())}), not {dtype} "
+                             f"({n_tokens}, {heads or 'heads'}, {self.d}) with contiguous rows")
+        return kvpop_rows(_ptr(t), t.stride(0), t.stride(1))
+
+    # ------------------------------------------------------------------ calls
+    def append(self, table, lens, q, k, v, cos=None, sin=None, starts=None, max_new: Optional[int] = None,
+               interleaved: bool = False, q_out=None, stream=None):
+        """Rotates the new tokens' ``q [tokens][heads][d]`` and ``k [tokens][H][d]`` by the rows of
+        ``cos, sin [positions][rot / 2]`` (none: no rotation) and writes k and ``v`` to the cache
+        (q, k and v of one type, bf16 or fp32, any token and head strides of 16 bytes).  ``table
+        [n][pages]`` int32, ``lens [n]`` int32 tokens held before (-1: idle), ``starts [n + 1]``
+        int32 first token of each sequence (none: one each).  Returns the rotated queries, bf16."""
+        what = "PagedCache.append"
+        n_tokens = k.shape[0]
+        if k.dtype not in _CODES:
+            raise ValueError(f"{what}: k is {k.dtype}, not bf16 or fp32")
+        kr = self._rows(what, "k", k, k.dtype, n_tokens, self.H)
+        vr = self._rows(what, "v", v, k.dtype, n_tokens, self.H)
+        qr, heads = None, 0
+        if q is not None:
+            qr, heads = self._rows(what, "q", q, k.dtype, n_tokens, None), q.shape[1]
+            if q_out is None:
+                q_out = torch.empty((n_tokens, heads, self.d), dtype=torch.bfloat16, device=k.device)
+            _want(what, "q_out", q_out, torch.bfloat16, (n_tokens, heads, self.d))
+        elif q_out is not None:
+            raise ValueError(f"{what}: q_out without q")
+        rot = positions = 0
+        if (cos is None) != (sin is None):
+            raise ValueError(f"{what}: cos and sin come together")
+        if cos is not None:
+            positions, rot = cos.shape[0], 2 * cos.shape[1]
+            if positions < 1 or rot < 16 or rot > self.d or rot % 16:
+                raise ValueError(f"{what}: cos is {tuple(cos.shape)}: 2 * {rot // 2} values of {self.d} cannot be "
+                                 "rotated (a multiple of 16 can)")
+            _want(what, "cos", cos, torch.float32, (positions, rot // 2))
+            _want(what, "sin", sin, torch.float32, (positions, rot // 2))
+        batch = self._batch(what, table, lens, starts, n_tokens, max_new)
+        self._here(what, table=table, lens=lens, starts=starts, q=q, k=k, v=v, cos=cos, sin=sin, q_out=q_out)
+        _ck(kvpop_paged_append(ctypes.byref(self._pool), ctypes.byref(batch),
+                               None if qr is None else ctypes.byref(qr), heads, ctypes.byref(kr), ctypes.byref(vr),
+                               _CODES[k.dtype], _ptr(cos), _ptr(sin), rot, positions, int(bool(interleaved)),
+                               _ptr(q_out), _stream(stream)), "kvpop_paged_append")
+        return q_out
+
+    def attend(self, table, lens, q, starts=None, max_new: Optional[int] = None, out=None, lse=None,
+               out_dtype=torch.float32, want_lse: bool = False, stream=None):
+        """Attention of the new tokens' ``q [tokens][H * G][d]`` (bf16, rotated) over positions
+        0 .. lens + i of their sequences; arguments as ``append``, with which the tokens' own keys
+        came.  Returns (out fp32 or bf16 ``[tokens][H * G][d]``, natural-log normalisers
+        ``[tokens][H * G]`` or None)."""
+        what = "PagedCache.attend"
+        n_tokens = q.shape[0]
+        qr = self._rows(what, "q", q, torch.bfloat16, n_tokens, None)
+        heads = q.shape[1]
+        if heads % self.H:
+            raise ValueError(f"{what}: {heads} query heads over {self.H} KV heads")
+        if out is None:
+            out = torch.empty((n_tokens, heads, self.d), dtype=out_dtype, device=q.device)
+        if out.dtype not in _CODES:
+            raise ValueError(f"{what}: out is {out.dtype}, not fp32 or bf16")
+        _want(what, "out", out, out.dtype, (n_tokens, heads, self.d))
+        if lse is None and want_lse:
+            lse = torch.empty((n_tokens, heads), dtype=torch.float32, device=q.device)
+        if lse is not None:
+            _want(what, "lse", lse, torch.float32, (n_tokens, heads))
+        batch = self._batch(what, table, lens, starts, n_tokens, max_new)
+        self._here(what, table=table, lens=lens, starts=starts, q=q, out=out, lse=lse)
+        _ck(kvpop_paged_attend(ctypes.byref(self._pool), ctypes.byref(batch), ctypes.byref(qr), heads, _ptr(out),
+                               _CODES[out.dtype], _ptr(lse), _ptr(self.workspace), self.workspace.numel(),
+                               _stream(stream)), "kvpop_paged_attend")
+        return out, lse
+
+
+class PageTable:
+    """Pages of a batch's sequences, handed out on the host: ``dev [n][max_pages]`` and
+    ``lens [n]`` (int32, on the device) are what the caches take.  A place of the batch is idle
+    (length -1) until ``open``."""
+
+    def __init__(self, n_seq: int, max_pages: int, n_pages: int, page: int = 64, device="cuda"):
+        self.page, self.max_pages = page, max_pages
+        self.held: List[int] = [-1] * n_seq
+        self.pages: List[List[int]] = [[] for _ in range(n_seq)]
+        self.free: List[int] = list(range(n_pages - 1, -1, -1))
+        self.dev = torch.full((n_seq, max_pages), -1, dtype=torch.int32, device=device)
+        self.lens = torch.full((n_seq,), -1, dtype=torch.int32, device=device)
+
+    def _new(self, new) -> List[int]:
+        n = len(self.held)
+        counts = [int(new)] * n if isinstance(new, int) else [int(x) for x in new]
+        if len(counts) != n or min(counts, default=0) < 0:
+            raise ValueError(f"PageTable: {len(counts)} token counts for {n} places, none below 0")
+        return [c if h >= 0 else 0 for c, h in zip(counts, self.held)]
+
+    def open(self, s: int):
+        """A new sequence at place s."""
+        self.close(s)
+        self.held[s] = 0
+        self.lens[s] = 0
+
+    def close(self, s: int):
+        """Gives place s's pages back and leaves it idle."""
+        self.free.extend(reversed(self.pages[s]))
+        self.pages[s] = []
+        self.held[s] = -1
+        self.lens[s] = -1
+        self.dev[s] = -1
+
+    def grow(self, new):
+        """Pages for ``new`` more tokens of every sequence (a number, or one for each place); none
+        are handed out when they do not suffice (MemoryError)."""
+        counts = self._new(new)
+        need = [max(0, -(-(max(h, 0) + c) // self.page) - len(p)) for h, c, p in zip(self.held, counts, self.pages)]
+        if any(len(p) + k > self.max_pages for p, k in zip(self.pages, need)):
+            raise MemoryError(f"PageTable: a sequence needs more than {self.max_pages} pages")
+        if sum(need) > len(self.free):
+            raise MemoryError(f"PageTable: {sum(need)} pages wanted, {len(self.free)} free")
+        where, ids = [], []
+        for s, k in enumerate(need):
+            for _ in range(k):
+                where.append((s, len(self.pages[s])))
+                ids.append(self.free.pop())
+                self.pages[s].append(ids[-1])
+        if ids:
+            at = torch.tensor(where, dtype=torch.int64, device=self.dev.device)
+            self.dev[at[:, 0], at[:, 1]] = torch.tensor(ids, dtype=torch.int32, device=self.dev.device)
+
+    def advance(self, new):
+        """The new tokens are in every layer's cache."""
+        counts = self._new(new)
+        self.held = [h + c if h >= 0 else h for h, c in zip(self.held, counts)]
+        if len(set(counts)) == 1 and min(self.held) >= 0:
+            self.lens += counts[0]
+        else:
+            self.lens += torch.tensor(counts, dtype=torch.int32, device=self.lens.device)
+
+    def starts(self, new: Sequence[int]) -> torch.Tensor:
+        """First token of every place, for the calls' ``starts``."""
+        at = [0]
+        for c in self._new(new):
+            at.append(at[-1] + c)
+        return torch.tensor(at, dtype=torch.int32, device=self.dev.device)
