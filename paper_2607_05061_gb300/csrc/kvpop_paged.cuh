@@ -69,6 +69,20 @@ __device__ __forceinline__ int page_of(const Batch& b, const Pool& p, int s, int
   return -1;
 }
 
+// Positions a sequence's tokens see at most, as far as its row of the table reaches.
+__device__ __forceinline__ int context(const Batch& b, const Pool& p, const SeqTokens& t, int32_t* err) {
+  const long long all = t.len < 0 ? 0 : (long long)t.len + t.n;
+  const long long cap = min((long long)b.max_pages << p.page_shift, (long long)(INT32_MAX - 1024));
+  if (all > cap) report(err, ERR_PAGE);
+  return (int)min(all, cap);
+}
+
+// Whether a sequence's rows go to the tcgen05 kernel, where one is launched.
+constexpr int LONG_ROWS = 64;
+__device__ __forceinline__ bool long_rows(const SeqTokens& t, int G) {
+  return t.len >= 0 && (long long)t.n * G > LONG_ROWS;
+}
+
 }  // namespace paged
 
 cudaError_t launch_paged_append(const paged::Pool& pool, const paged::Batch& b, const void* q, long long q_ts,
@@ -83,5 +97,11 @@ size_t paged_attend_workspace(int sms);
 cudaError_t launch_paged_attend(const paged::Pool& pool, const paged::Batch& b, const void* q, long long q_ts,
                                 long long q_hs, int HQ, void* out, int out_f32, float* lse, void* workspace,
                                 int sms, int32_t* err, cudaStream_t stream);
+
+// The same for sequences with long_rows, where paged_prompt_fits.
+bool paged_prompt_fits(const paged::Pool& pool, const paged::Batch& b, int HQ);
+cudaError_t launch_paged_prompt(const paged::Pool& pool, const paged::Batch& b, const void* q, long long q_ts,
+                                long long q_hs, int HQ, void* out, int out_f32, float* lse, int32_t* err,
+                                cudaStream_t stream);
 
 }  // namespace kvpop

@@ -50,6 +50,7 @@ struct AttendArgs {
   int32_t* err;
   float c;                             // log2(e) / sqrt(d)
   int G, out_f32;
+  int skip_long;                       // the tcgen05 kernel takes sequences with long_rows
 };
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
@@ -103,10 +104,8 @@ __device__ __forceinline__ SeqUnits seq_units(const AttendArgs& a, int s) {
   u.len = t.len;
   u.n = t.n;
   u.groups = (int)(((long long)t.n * a.G + ROWS - 1) / ROWS);
-  const long long all = t.len < 0 ? 0 : (long long)t.len + t.n;
-  const long long cap = min((long long)a.b.max_pages << a.pool.page_shift, (long long)(INT32_MAX - BLK));
-  if (all > cap) report(a.err, ERR_PAGE);
-  u.ctx = (int)min(all, cap);
+  if (a.skip_long && long_rows(t, a.G)) u.groups = 0;
+  u.ctx = u.groups > 0 ? context(a.b, a.pool, t, a.err) : 0;
   u.tiles = max((u.ctx + BLK - 1) / BLK, 1);
   return u;
 }
@@ -310,22 +309,31 @@ __global__ void __launch_bounds__(AT_THREADS, NT == 1 ? AT_CTAS : 1) paged_atten
         const int ebits = (int)(__float_as_uint(vs) >> 23);
         const float ev = (float)(ebits - 127), vinv = __uint_as_float((uint32_t)(254 - ebits) << 23);
         const bool edge = t * BLK + BLK - 1 > lim_lo;      // some row does not see the whole block
+        // exponents from the row's base, in one rounding: as long as there is none (-inf) every
+        // logit is too large
+        float y[NT][4];
+        auto exponents = [&](float off, bool based) {
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              y[j][e] = fmaf(sc[j][e], rc[j][e & 1] * ksc, based ? ev + (off - m[j][e & 1]) : ev);
+              if (edge && t * BLK + g + 8 * (e >> 1) > lim[j][e & 1]) y[j][e] = -INFINITY;
+            }
+        };
+        exponents(AT_OFF, true);
         bool up = false;
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float y = fmaf(sc[j][e], rc[j][e & 1] * ksc, ev);
-            if (edge && t * BLK + g + 8 * (e >> 1) > lim[j][e & 1]) y = -INFINITY;
-            sc[j][e] = y;
-            up |= y > m[j][e & 1] + AT_STEP;
-          }
+          for (int e = 0; e < 4; ++e) up |= y[j][e] > AT_OFF + AT_STEP;
         if (__any_sync(0xffffffffu, up)) {
+          exponents(0.f, false);
 #pragma unroll
           for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              float mx = fmaxf(sc[j][e], sc[j][e + 2]);
+              float mx = fmaxf(y[j][e], y[j][e + 2]);
 #pragma unroll
               for (int x = 4; x < 32; x <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
               mx = fmaxf(mx, m[j][e]);
@@ -338,24 +346,22 @@ __global__ void __launch_bounds__(AT_THREADS, NT == 1 ? AT_CTAS : 1) paged_atten
                 o[j][k][e + 2] *= al;
               }
             }
+          exponents(AT_OFF, true);
         }
         uint32_t ph[NT][2], pl[NT][2];
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float b = m[j][e] == -INFINITY ? 0.f : AT_OFF - m[j][e];
-            sc[j][e] = ex2(sc[j][e] + b);
-            sc[j][e + 2] = ex2(sc[j][e + 2] + b);
-            l[j][e] = fmaf(sc[j][e] + sc[j][e + 2], vinv, l[j][e]);
-          }
+          for (int e = 0; e < 4; ++e) y[j][e] = ex2(y[j][e]);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) l[j][e] = fmaf(y[j][e] + y[j][e + 2], vinv, l[j][e]);
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const uint32_t hi = pack_f16(sc[j][2 * e], sc[j][2 * e + 1]);
+            const uint32_t hi = pack_f16(y[j][2 * e], y[j][2 * e + 1]);
             ph[j][e] = movm(hi);
             if (SPLIT) {
               const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-              pl[j][e] = movm(pack_f16(sc[j][2 * e] - b.x, sc[j][2 * e + 1] - b.y));
+              pl[j][e] = movm(pack_f16(y[j][2 * e] - b.x, y[j][2 * e + 1] - b.y));
             }
           }
         }
@@ -375,7 +381,7 @@ __global__ void __launch_bounds__(AT_THREADS, NT == 1 ? AT_CTAS : 1) paged_atten
             }
           }
         }
-        uint32_t nan_at[4][VW];                            // 0x80 in the bytes that are NaN
+        uint32_t nan_at[4][VW];                            // 0xff in the bytes that are NaN
         if (edge && __any_sync(0xffffffffu, bad != 0)) {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
@@ -563,7 +569,13 @@ cudaError_t launch_paged_attend(const Pool& pool, const Batch& b, const void* q,
   a.err = err;
   a.c = (float)(1.4426950408889634 / sqrt((double)pool.d));
   a.G = HQ / pool.H;
-  const long long rows = (long long)a.G * (b.starts ? b.max_new : 1);
+  long long rows = (long long)a.G * (b.starts ? b.max_new : 1);
+  if (rows > LONG_ROWS && b.starts && paged_prompt_fits(pool, b, HQ)) {
+    a.skip_long = 1;
+    rows = LONG_ROWS;
+    const cudaError_t e = launch_paged_prompt(pool, b, q, q_ts, q_hs, HQ, out, out_f32, lse, err, stream);
+    if (e != cudaSuccess) return e;
+  }
   return pool.d == 128 ? launch_d<128>(a, sms, rows, stream) : launch_d<64>(a, sms, rows, stream);
 }
 

@@ -255,7 +255,7 @@ def check_attend(got, lse, want, out_dtype):
     live = np.isfinite(wl)
     gl = lse.double().cpu().numpy()
     assert np.array_equal(np.isfinite(gl), live) and (gl[~live] == -math.inf).all()
-    assert (np.abs(gl - wl)[live] <= (2 * eps + 2.0 ** -22 * np.abs(wl))[live]).all()
+    assert (np.abs(gl[live] - wl[live]) <= (2 * eps + 2.0 ** -22 * np.abs(wl))[live]).all()
 
 
 ATTEND = [
@@ -274,6 +274,12 @@ ATTEND = [
     (64, 1, 4, 16, [0], [8]),
     (128, 1, 4, 128, [5, 200], [40, 19]),           # longer than a row group
     (64, 2, 2, 64, [0, 3, 90], [150, 1, 33]),
+    (128, 1, 4, 64, [0], [17]),                     # one row more than a short sequence has
+    (128, 2, 4, 64, [130, 0, 700], [64, 65, 129]),  # 256 rows, one token more, and a third tile
+    (128, 1, 7, 16, [3, 511], [37, 80]),            # tiles that cut a token's heads
+    (64, 1, 1, 128, [250], [600]),
+    (128, 1, 8, 32, [1200], [33]),                  # more blocks than the ring holds
+    (64, 3, 4, 16, [0, 5, 20, 7], [40, 2, 0, 90]),  # short and long ones in one call
 ]
 
 
@@ -320,13 +326,14 @@ def test_attend_long_rows_over_many_parts(dev, out_dtype):
 
 def test_idle_places_and_sequences_without_tokens(dev):
     d, H, G, page = 128, 2, 4, 16
-    held, new = [-1, 20, -1, 5, 0], [3, 0, 1, 2, 1]
-    cache = make_cache(dev, 12, H, d, page, seed=9)
-    table, lens, starts = tables(held, new, page, 12, dev)
-    q = (torch.randn((7, H * G, d)) * 0.02).bfloat16().to(dev)
-    out, lse = cache.attend(table, lens, q, starts=starts, want_lse=True)
-    check_attend(out, lse, attend_reference(cache, table, held, new, q, page), torch.float32)
-    assert (out[:4] == 0).all() and (lse[:4] == -math.inf).all() and status()[0] == 0
+    cache = make_cache(dev, 16, H, d, page, seed=9)
+    for held, new, most in (([-1, 20, -1, 5, 0], [3, 0, 1, 2, 1], 3), ([-1, 20, -1, 5, 0], [30, 0, 1, 40, 1], 40)):
+        table, lens, starts = tables(held, new, page, 16, dev)
+        q = (torch.randn((sum(new), H * G, d)) * 0.02).bfloat16().to(dev)
+        out, lse = cache.attend(table, lens, q, starts=starts, max_new=most, want_lse=True)
+        check_attend(out, lse, attend_reference(cache, table, held, new, q, page), torch.float32)
+        n = new[0] + 1
+        assert (out[:n] == 0).all() and (lse[:n] == -math.inf).all() and status()[0] == 0
 
 
 def test_scales_far_apart(dev):
@@ -335,10 +342,11 @@ def test_scales_far_apart(dev):
     cache = make_cache(dev, 6, H, d, page, seed=10)
     cache.v_scale.copy_(torch.tensor([2.0 ** e for e in (-20, 20, 0, -40, 7, 3)], device=dev).view(6, 1, 1))
     cache.k_scale.copy_(torch.tensor([2.0 ** e for e in (-10, -3, -8, -4, -20, -90)], device=dev).view(6, 1, 1))
-    table, lens, _ = tables(held, [1], page, 6, dev)
-    q = (torch.randn((1, G, d), generator=torch.Generator().manual_seed(2)) * 0.05).bfloat16().to(dev)
-    out, lse = cache.attend(table, lens, q, want_lse=True)
-    check_attend(out, lse, attend_reference(cache, table, held, [1], q, page), torch.float32)
+    for held, new in (([95], [1]), ([63], [33])):
+        table, lens, starts = tables(held, new, page, 6, dev)
+        q = (torch.randn((new[0], G, d), generator=torch.Generator().manual_seed(2)) * 0.05).bfloat16().to(dev)
+        out, lse = cache.attend(table, lens, q, starts=starts, max_new=new[0], want_lse=True)
+        check_attend(out, lse, attend_reference(cache, table, held, new, q, page), torch.float32)
 
 
 @pytest.mark.parametrize("size", [2.0 ** -100, 2.0 ** -30, 2.0 ** 30])
@@ -350,6 +358,32 @@ def test_queries_of_any_size(dev, size):
     q = (torch.randn((1, G, d), generator=torch.Generator().manual_seed(2)) * size).bfloat16().to(dev)
     out, lse = cache.attend(table, lens, q, want_lse=True)
     check_attend(out, lse, attend_reference(cache, table, held, [1], q, page), torch.float32)
+
+
+@pytest.mark.parametrize("out_dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("new", [1, 6, 50])
+def test_logits_that_rise_and_fall_along_the_keys(dev, new, out_dtype):
+    """The running base moves often: key scales grow block by block, then shrink."""
+    d, H, G, page, held = 128, 1, 4, 32, [700]
+    cache = make_cache(dev, 24, H, d, page, seed=16)
+    table, lens, starts = tables(held, [new], page, 24, dev)
+    n = -(-(held[0] + new) // page)
+    for i in range(n):
+        cache.k_scale[int(table[0, i])] = 2.0 ** (-6 + min(i, n - 1 - i) * 0.25 // 1)
+    q = (torch.randn((new, G, d), generator=torch.Generator().manual_seed(2)) * 0.05).bfloat16().to(dev)
+    out, lse = cache.attend(table, lens, q, starts=starts, max_new=new, out_dtype=out_dtype, want_lse=True)
+    check_attend(out, lse, attend_reference(cache, table, held, [new], q, page), out_dtype)
+
+
+def test_outputs_do_not_rest_on_max_new(dev):
+    d, H, G, page, held, new = 128, 2, 4, 64, [40, 9], [30, 2]
+    cache = make_cache(dev, 8, H, d, page, seed=17)
+    table, lens, starts = tables(held, new, page, 8, dev)
+    q = (torch.randn((32, H * G, d)) * 0.02).bfloat16().to(dev)
+    want = attend_reference(cache, table, held, new, q, page)
+    for most in (1, 2, 4, 8, 30, 10 ** 9, None):
+        out, lse = cache.attend(table, lens, q, starts=starts, max_new=most, want_lse=True)
+        check_attend(out, lse, want, torch.float32)
 
 
 @pytest.mark.parametrize("out_dtype", [torch.float32, torch.bfloat16])
