@@ -21,6 +21,7 @@ enum : int {
   ERR_PAGE = 41,                       // a page number outside the pool, or a position past the table
   ERR_BATCH = 42,                      // token offsets that are not ascending, or more than max_new tokens
   ERR_ROTATION = 43,                   // a position past the rotation table
+  ERR_WAIT = 44,                       // a wait for a copy, a product or a row ran out
 };
 
 struct Batch {                         // kvpop_paged_batch

@@ -7,36 +7,62 @@
 // Bound by the cache's bytes (2 d + 1/2 per position and KV head).  A warp takes one block of 16
 // positions at a time, S^T = K Q^T and O^T += V^T P^T as m16n8k16 with the positions (then the
 // values) as the 16-row operand and NT groups of 8 query rows as the 8-column one, so that each
-// byte is read and converted once for all query heads.  Lanes load whole rows straight into
-// registers: the order of the contraction index is free, so a lane takes 16 neighbouring bytes of
-// a row, which become its operand words by e4m3 -> f16 conversion alone; for V the bytes of two
-// positions are interleaved first.  f16 holds every e4m3 value, and q, scaled by a power of two
-// per row, to 2^-39 of the row's largest value, so the products are exact.
+// byte is read and converted once for all query heads.  Each warp has its own ring of blocks in
+// shared memory, which its lanes fill by 16-byte cp.async (swizzled so that the reads below touch
+// every bank once) and read alone: no warp waits for another, and the ring runs on across the ends
+// of units while the warps join their rows.  (TMA was slower here: a copy takes about 140 clocks
+// of its engine whatever its size, and a page of 16 positions makes 2 KB pieces; 64 sequences of
+// 8192 tokens 226 us with 8 KB boxes, 277 with 2 KB ones.)  The order of the contraction index is
+// free, so a lane takes neighbouring bytes of a row, which become its operand words by
+// e4m3 -> f16 conversion alone; for V the bytes of two positions are interleaved first.  f16 holds
+// every e4m3 value, and q, scaled by a power of two per row, to 2^-39 of the row's largest value,
+// so the products are exact.
 //
 // The scales cost next to nothing: ek multiplies the logits, and ev joins the exponent,
 //   p_t = 2^(x_t log2 e + ev - M + 7),  O = sum p_t code_t,  l = sum p_t 2^-ev,  y = O / l,
 // where M, the running base of a row, moves when a term exceeds it by 2^8.  p_t lies in [0, 2^15]:
 // rounded to f16 it has 11 bits, enough for a bf16 result (SPLIT false); for an fp32 result it is
-// the sum of two f16 values, 22 bits, and the second product is taken too (SPLIT).
+// the sum of two f16 values, 22 bits, and the second product is taken too (SPLIT).  The tensor
+// cores cut their fp32 sums off instead of rounding them, which adds up along a row (2.1e-6 of the
+// result over 512 blocks): with SPLIT a block's product is formed from zero and added by a rounded
+// fp32 sum (5e-7).
 //
-// The blocks of all (sequence, KV head, row group) units form one list that is cut evenly over a
-// grid of resident CTAs; a CTA's 8 warps take its blocks in turn and join their rows in warp
-// order.  A unit that lies in several CTAs' parts is joined, in the order of the parts, by the CTA
-// that arrives last (no CTA waits).
+// The blocks of all (sequence, KV head, row group) units form one list that is cut evenly over the
+// SMs; a CTA's warps take its blocks in turn and join their rows in warp order.  A unit that lies in several CTAs' parts is
+// joined, in the order of the parts, by the CTA that arrives last (no CTA waits).
 #include <algorithm>
 
 #include "kvpop_mma.cuh"
 #include "kvpop_paged.cuh"
+#include "kvpop_ptx.cuh"
 
 namespace kvpop {
 namespace {
 
 using namespace paged;
 
-constexpr int AT_WARPS = 8, AT_THREADS = 32 * AT_WARPS;
-constexpr int AT_CTAS = 2;             // resident per SM
+constexpr int AT_LEAST = 12;           // blocks of a part, unless there are fewer
 constexpr int AT_MAX_ROWS = 32;        // query rows of a unit at most
 constexpr float AT_OFF = 7.f, AT_STEP = 8.f;
+
+// The rings: a block's 16 rows of K, then of V.  The 16-byte chunk c of row r lies at chunk
+// c ^ (r mod 8) of its 128 bytes (d = 128), or c ^ (r / 2 mod 4) of its 64 (d = 64).
+template <int D, int W>
+struct Ring {
+  static constexpr int BLOCK = 2 * BLK * D, ST = (W == 12 ? 3 : 5) * (128 / D);
+  static constexpr int OFF_ACC = W * ST * BLOCK;                       // a warp's 8 rows: 8 (d + 4) floats
+  static constexpr int OFF_Q = OFF_ACC + W * 8 * (D + 4) * 4;          // 4 groups of query operands
+  static constexpr int BYTES = OFF_Q + 4 * (D / 16) * 256;
+  static __device__ __forceinline__ int chunk_at(int r, int c) {
+    return r * D + ((c ^ (D == 128 ? r & 7 : (r >> 1) & 3)) << 4);
+  }
+  // a lane's i-th 16 bytes of K: bytes D/4 t + 16 i .. of row r
+  static __device__ __forceinline__ int k_at(int r, int t, int i) { return chunk_at(r, D == 128 ? 2 * t + i : t); }
+  // a lane's bytes of V: bytes D/8 g .. of row r
+  static __device__ __forceinline__ int v_at(int r, int g) {
+    return D == 128 ? chunk_at(r, g) : chunk_at(r, g >> 1) + 8 * (g & 1);
+  }
+};
 
 struct AttendArgs {
   Pool pool;
@@ -73,28 +99,16 @@ __device__ __forceinline__ uint32_t movm(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-__device__ __forceinline__ uint4 ldg16(const unsigned char* p) {
-  uint4 v;
-  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-               : "l"(p));
-  return v;
-}
-__device__ __forceinline__ uint2 ldg8(const unsigned char* p) {
-  uint2 v;
-  asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
-  return v;
-}
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&v);
 }
 
-// Units of a sequence: H x row groups, each of `tiles` blocks (one at least, so that a row that
+// Units of a sequence: H x row groups, each of `blocks` blocks (one at least, so that a row that
 // sees nothing is written too).
 struct SeqUnits {
-  int first, n, len, ctx, groups, tiles;
-  __device__ long long work(int H) const { return (long long)H * groups * tiles; }
+  int first, n, len, ctx, groups, blocks;
+  __device__ long long work(int H) const { return (long long)H * groups * blocks; }
 };
 template <int ROWS>
 __device__ __forceinline__ SeqUnits seq_units(const AttendArgs& a, int s) {
@@ -106,7 +120,7 @@ __device__ __forceinline__ SeqUnits seq_units(const AttendArgs& a, int s) {
   u.groups = (int)(((long long)t.n * a.G + ROWS - 1) / ROWS);
   if (a.skip_long && long_rows(t, a.G)) u.groups = 0;
   u.ctx = u.groups > 0 ? context(a.b, a.pool, t, a.err) : 0;
-  u.tiles = max((u.ctx + BLK - 1) / BLK, 1);
+  u.blocks = max((u.ctx + BLK - 1) / BLK, 1);
   return u;
 }
 
@@ -125,19 +139,27 @@ __device__ __forceinline__ void write_out(const AttendArgs& a, int first, int h,
   if (cc == 0 && a.lse) a.lse[row] = l == 0.f ? -INFINITY : (m - AT_OFF + log2f(l)) * 0.69314718055994530942f;
 }
 
-template <int D, int NT, bool SPLIT>
-__global__ void __launch_bounds__(AT_THREADS, NT == 1 ? AT_CTAS : 1) paged_attend_kernel(AttendArgs a) {
+template <int D, int NT, int W, bool SPLIT>
+__global__ void __launch_bounds__(32 * W, 1) paged_attend_kernel(AttendArgs a) {
+  using R = Ring<D, W>;
   constexpr int ROWS = 8 * NT, KW = D / 16, VW = D / 32;   // words a lane holds of a K / V row
   constexpr int RS = 8 * (D + 4);                          // a warp's 8 rows in shared memory
-  __shared__ float accS[AT_WARPS * RS];
-  __shared__ float mS[AT_WARPS][ROWS], lS[AT_WARPS][ROWS];
-  __shared__ long long scanS[AT_THREADS / 32 + 1];
-  __shared__ int lastS;
+  constexpr bool QS = NT == 4;                             // query operands in shared memory: no registers left
+  extern __shared__ __align__(128) unsigned char sma[];
+  float* accS = reinterpret_cast<float*>(sma + R::OFF_ACC);
+  uint2* qS = reinterpret_cast<uint2*>(sma + R::OFF_Q);
+  __shared__ float mS[W][ROWS], lS[W][ROWS];
+  __shared__ float scaleS[W][R::ST][2];
+  __shared__ long long scanS[W];
+  __shared__ long long b0S;
+  __shared__ int s0S, lastS;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
   const int H = a.pool.H, G = a.G;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   // ---- this CTA's part of the list: [w0, w1), and the sequence that w0 lies in
-  const int per = (a.b.n_seq + AT_THREADS - 1) / AT_THREADS, sA = min(tid * per, a.b.n_seq);
+  const int per = (a.b.n_seq + 32 * W - 1) / (32 * W), sA = min(tid * per, a.b.n_seq);
   const int sB = min(sA + per, a.b.n_seq);
   long long mine = 0;
   for (int s = sA; s < sB; ++s) mine += seq_units<ROWS>(a, s).work(H);
@@ -150,13 +172,12 @@ __global__ void __launch_bounds__(AT_THREADS, NT == 1 ? AT_CTAS : 1) paged_atten
   if (lane == 31) scanS[warp] = pre;
   __syncthreads();
   long long total = 0;
-  for (int w = 0; w < AT_WARPS; ++w) {
+  for (int w = 0; w < W; ++w) {
     if (w < warp) pre += scanS[w];
     total += scanS[w];
   }
-  __syncthreads();
-  // parts of at least one block a warp
-  const long long grid = max(min((long long)gridDim.x, total / AT_WARPS), 1ll);
+  if (total == 0) return;
+  const long long grid = max(min((long long)gridDim.x, total / AT_LEAST), 1ll);
   auto part_start = [&](long long c) { return c * total / grid; };
   auto part_of = [&](long long w) {                        // the part that block w lies in
     long long c = w * grid / total;
@@ -164,11 +185,8 @@ __global__ void __launch_bounds__(AT_THREADS, NT == 1 ? AT_CTAS : 1) paged_atten
     while (part_start(c) > w) --c;
     return c;
   };
-  if (blockIdx.x >= grid || total == 0) return;
+  if (blockIdx.x >= grid) return;
   const long long w0 = part_start(blockIdx.x), w1 = part_start(blockIdx.x + 1);
-  if (w0 >= w1) return;
-  __shared__ int s0S;
-  __shared__ long long b0S;
   if (pre - mine <= w0 && w0 < pre) {
     long long base = pre - mine;
     int s = sA;
@@ -181,20 +199,91 @@ __global__ void __launch_bounds__(AT_THREADS, NT == 1 ? AT_CTAS : 1) paged_atten
     b0S = base;
   }
   __syncthreads();
-  int s = s0S;
-  long long base = b0S;                                    // list position of sequence s
-  SeqUnits u = seq_units<ROWS>(a, s);
 
-  for (long long w = w0; w < w1;) {
-    while (w >= base + u.work(H)) {                        // (sequences without tokens have no blocks)
-      base += u.work(H);
-      u = seq_units<ROWS>(a, ++s);
+  // Place in the list: the unit that a position lies in, found by walking on from an earlier one.
+  struct Walk {
+    SeqUnits u;
+    long long base, start;                                 // list positions of the sequence and the unit
+    int s, h, row0, rows, lim_hi;
+  };
+  auto seek = [&](Walk& x, long long w) {
+    while (w >= x.base + x.u.work(H)) {                    // (sequences without tokens have no blocks)
+      x.base += x.u.work(H);
+      x.u = seq_units<ROWS>(a, ++x.s);
     }
-    const int unit = (int)((w - base) / u.tiles), h = unit % H, grp = unit / H;
-    const long long ustart = base + (long long)unit * u.tiles;
-    const int ta = (int)(w - ustart), tb = (int)min((long long)u.tiles, w1 - ustart);
+    const int unit = (int)((w - x.base) / x.u.blocks);
+    x.h = unit % H;
+    x.start = x.base + (long long)unit * x.u.blocks;
+    x.row0 = unit / H * ROWS;
+    x.rows = min(ROWS, x.u.n * G - x.row0);
+    x.lim_hi = min(x.u.len + (x.row0 + x.rows - 1) / G, x.u.ctx - 1);   // its rows see at most 0 .. lim_hi
+  };
+  Walk at;
+  at.s = s0S;
+  at.base = b0S;
+  at.u = seq_units<ROWS>(a, at.s);
+  seek(at, w0);
+
+  // ---- the warp's ring: blocks w0 + warp, w0 + warp + W, ...
+  const uint32_t ring = smem_u32(sma) + warp * (R::ST * R::BLOCK);
+  const int count = (int)max((w1 - w0 - warp + W - 1) / W, 0ll);       // the warp's blocks
+  // a lane copies the 16 bytes at 512 i + 16 lane of a block's K and of its V
+  constexpr int RPI = 512 / D;
+  const int r0 = lane / (D / 16), c0 = lane % (D / 16), put0 = R::chunk_at(r0, c0), put1 = R::chunk_at(r0 + RPI, c0);
+  Walk ahead = at;
+  int asked = 0, slot = 0;                                 // blocks asked for; the next one's slot,
+  int nt = (int)(w0 - at.start) + warp, left = (int)min((long long)at.u.blocks, w1 - at.start);   // place, the unit's end,
+  const int32_t* row = a.b.table + (long long)ahead.s * a.b.table_stride;
+  int id = -1;                                             // and page
+  auto look = [&] {
+    if (asked >= count) return;
+    if (nt >= left) {
+      const long long w = w0 + warp + (long long)asked * W;
+      seek(ahead, w);
+      nt = (int)(w - ahead.start);
+      left = (int)min((long long)ahead.u.blocks, w1 - ahead.start);
+      row = a.b.table + (long long)ahead.s * a.b.table_stride;
+    }
+    if (nt * BLK <= ahead.lim_hi) id = __ldg(row + (nt * BLK >> a.pool.page_shift));
+  };
+  auto ask = [&] {
+    if (asked < count) {
+      const int pos = nt * BLK;
+      float* sc = &scaleS[warp][slot][0];
+      if (pos <= ahead.lim_hi && (unsigned)id < (unsigned)a.pool.n_pages) {
+        const long long rows0 = ((long long)id * H + ahead.h) * a.pool.page + (pos & (a.pool.page - 1));
+        const unsigned char *kp = a.pool.k + rows0 * D + 16 * lane, *vp = a.pool.v + rows0 * D + 16 * lane;
+        const uint32_t dst = ring + slot * R::BLOCK;
+#pragma unroll
+        for (int i = 0; i < BLK / RPI; ++i) {
+          const uint32_t at = dst + (i & 1 ? put1 : put0) + 512 * (i & ~1);
+          cp_async16(at, kp + 512 * i, 16);
+          cp_async16(at + BLK * D, vp + 512 * i, 16);
+        }
+        if (lane < 2) cp_async4(smem_u32(sc + lane), (lane ? a.pool.vs : a.pool.ks) + rows0 / BLK);
+      } else if (lane == 0) {                              // no row sees the block, or a bad page
+        if (pos <= ahead.lim_hi) report(a.err, ERR_PAGE);
+        sc[1] = -1.f;
+      }
+      nt += W;
+      ++asked;
+      slot = slot + 1 == R::ST ? 0 : slot + 1;
+      look();
+    }
+    cp_commit();
+  };
+  look();
+#pragma unroll 1
+  for (int i = 0; i < R::ST; ++i) ask();
+
+  int next = warp, done = 0, stage = 0;                    // the warp's next block of the CTA's; blocks so far
+  for (long long w = w0; w < w1;) {
+    seek(at, w);
+    const SeqUnits& u = at.u;
+    const int h = at.h, row0 = at.row0, rows = at.rows, lim_hi = at.lim_hi;
+    const long long ustart = at.start;
+    const int ta = (int)(w - ustart), tb = (int)min((long long)u.blocks, w1 - ustart);
     w = ustart + tb;
-    const int row0 = grp * ROWS, rows = min(ROWS, u.n * G - row0);
 
     // ---- query rows, each scaled by a power of two, and what that makes of the logits
     uint32_t qf[NT][KW][2];
@@ -204,19 +293,17 @@ __global__ void __launch_bounds__(AT_THREADS, NT == 1 ? AT_CTAS : 1) paged_atten
     for (int j = 0; j < NT; ++j) {
       const int r = row0 + 8 * j + g;
       const bool ok = 8 * j + g < rows;
-      const bf16* qp = a.q + (long long)(u.first + (ok ? r / G : 0)) * a.q_ts + (long long)(h * G + (ok ? r % G : 0)) * a.q_hs;
-      uint32_t raw[KW][2];
+      const bf16* qp = a.q + (long long)(u.first + (ok ? r / G : 0)) * a.q_ts +
+                       (long long)(h * G + (ok ? r % G : 0)) * a.q_hs + 4 * KW * t4;
       uint32_t top = 0;
 #pragma unroll
-      for (int k = 0; k < KW; k += 4)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const uint4 v = ok ? *reinterpret_cast<const uint4*>(qp + 16 * k + 16 * t4 + 8 * e) : make_uint4(0, 0, 0, 0);
-          raw[k + 2 * e][0] = v.x; raw[k + 2 * e][1] = v.y;
-          raw[k + 2 * e + 1][0] = v.z; raw[k + 2 * e + 1][1] = v.w;
-          top = max(top, max(max(v.x & 0x7fffu, v.x >> 16 & 0x7fffu), max(v.y & 0x7fffu, v.y >> 16 & 0x7fffu)));
-          top = max(top, max(max(v.z & 0x7fffu, v.z >> 16 & 0x7fffu), max(v.w & 0x7fffu, v.w >> 16 & 0x7fffu)));
-        }
+      for (int k = 0; k < KW; k += 2) {
+        const uint4 v = ok ? *reinterpret_cast<const uint4*>(qp + 4 * k) : make_uint4(0, 0, 0, 0);
+        qf[j][k][0] = v.x; qf[j][k][1] = v.y;
+        qf[j][k + 1][0] = v.z; qf[j][k + 1][1] = v.w;
+        top = max(top, max(max(v.x & 0x7fffu, v.x >> 16 & 0x7fffu), max(v.y & 0x7fffu, v.y >> 16 & 0x7fffu)));
+        top = max(top, max(max(v.z & 0x7fffu, v.z >> 16 & 0x7fffu), max(v.w & 0x7fffu, v.w >> 16 & 0x7fffu)));
+      }
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
       // 2^up brings the largest value into [2^14, 2^15)
@@ -225,8 +312,13 @@ __global__ void __launch_bounds__(AT_THREADS, NT == 1 ? AT_CTAS : 1) paged_atten
 #pragma unroll
       for (int k = 0; k < KW; ++k)
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-          qf[j][k][e] = pack_f16(__uint_as_float(raw[k][e] << 16) * f, __uint_as_float(raw[k][e] & 0xffff0000u) * f);
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t x = qf[j][k][e];
+          qf[j][k][e] = pack_f16(__uint_as_float(x << 16) * f, __uint_as_float(x & 0xffff0000u) * f);
+        }
+      if (QS && warp == j)
+#pragma unroll
+        for (int k = 0; k < KW; ++k) qS[(j * KW + k) * 32 + lane] = make_uint2(qf[j][k][0], qf[j][k][1]);
       const float down = a.c * __uint_as_float((uint32_t)(127 - up) << 23);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
@@ -235,8 +327,8 @@ __global__ void __launch_bounds__(AT_THREADS, NT == 1 ? AT_CTAS : 1) paged_atten
         lim[j][e] = min(u.len + rr / G, u.ctx - 1);
       }
     }
+    if (QS) __syncthreads();
     const int lim_lo = min(u.len + row0 / G, u.ctx - 1);   // the unit's rows see at least 0 .. lim_lo
-    const int lim_hi = min(u.len + (row0 + rows - 1) / G, u.ctx - 1);   // and at most 0 .. lim_hi
 
     float o[NT][KW][4], m[NT][2], l[NT][2];
 #pragma unroll
@@ -250,62 +342,53 @@ __global__ void __launch_bounds__(AT_THREADS, NT == 1 ? AT_CTAS : 1) paged_atten
     }
 
     // ---- the stream
-    auto page = [&](int t) { return t * BLK <= lim_hi ? page_of(a.b, a.pool, s, t * BLK, a.err) : -1; };
-    auto block_at = [&](int id, int t) {                   // row of the pools, in blocks
-      return ((long long)max(id, 0) * H + h) * (a.pool.page / BLK) + (t & (a.pool.page / BLK - 1));
-    };
-    uint32_t kr[2][KW], vr[4][VW];
-    float ks, vs;
-    auto load_k = [&](long long blk) {
-      const unsigned char* p = a.pool.k + (blk * BLK + g) * D + 16 * t4;
+    const int done0 = done;
+    done += tb - ta;
+    for (; next < done; next += W) {
+      const int t = ta + next - done0;                     // the block's place in the unit
+      cp_wait<R::ST - 1>();
+      __syncwarp();
+      const float ks = scaleS[warp][stage][0], vs = scaleS[warp][stage][1];
+      const unsigned char* kp = sma + (warp * R::ST + stage) * R::BLOCK;
+      if (vs >= 0.f) {                                     // (warp-uniform)
+        float sc[NT][4], sd[NT][4];
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[j][e] = sd[j][e] = 0.f;
 #pragma unroll
         for (int k = 0; k < KW; k += 4) {
-          const uint4 v = ldg16(p + e * 8 * D + 16 * k);
-          kr[e][k] = v.x; kr[e][k + 1] = v.y; kr[e][k + 2] = v.z; kr[e][k + 3] = v.w;
+          const uint4 ka = *reinterpret_cast<const uint4*>(kp + R::k_at(g, t4, k >> 2));
+          const uint4 kb = *reinterpret_cast<const uint4*>(kp + R::k_at(g + 8, t4, k >> 2));
+          const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t a0, a1, a2, a3;
+            cvt4(wa[i], a0, a2);
+            cvt4(wb[i], a1, a3);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+              const uint2 b = QS ? qS[(j * KW + k + i) * 32 + lane] : make_uint2(qf[j][k + i][0], qf[j][k + i][1]);
+              mma_f16(i & 1 ? sd[j] : sc[j], a0, a1, a2, a3, b.x, b.y);
+            }
+          }
         }
-      ks = a.pool.ks[blk];
-    };
-    auto load_v = [&](long long blk) {
-      const unsigned char* p = a.pool.v + (blk * BLK + 2 * t4) * D + 4 * VW * g;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const unsigned char* pe = p + ((e & 1) + 8 * (e >> 1)) * D;
-        if constexpr (VW == 4) {
-          const uint4 v = ldg16(pe);
-          vr[e][0] = v.x; vr[e][1] = v.y; vr[e][2] = v.z; vr[e][3] = v.w;
-        } else {
-          const uint2 v = ldg8(pe);
-          vr[e][0] = v.x; vr[e][1] = v.y;
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[j][e] += sd[j][e];
+        uint32_t vr[4][VW];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const unsigned char* q = kp + BLK * D + R::v_at(2 * t4 + (e & 1) + 8 * (e >> 1), g);
+          if constexpr (VW == 4) {
+            const uint4 v = *reinterpret_cast<const uint4*>(q);
+            vr[e][0] = v.x; vr[e][1] = v.y; vr[e][2] = v.z; vr[e][3] = v.w;
+          } else {
+            const uint2 v = *reinterpret_cast<const uint2*>(q);
+            vr[e][0] = v.x; vr[e][1] = v.y;
+          }
         }
-      }
-      vs = a.pool.vs[blk];
-    };
-    int t = ta + warp;
-    int id = t < tb ? page(t) : -1, id_next = t + AT_WARPS < tb ? page(t + AT_WARPS) : -1;
-    if (t < tb && id >= 0) {
-      load_k(block_at(id, t));
-      load_v(block_at(id, t));
-    }
-    for (; t < tb; t += AT_WARPS) {
-      const int tn = t + AT_WARPS;
-      const bool next = tn < tb && id_next >= 0;
-      const long long bn = block_at(id_next, tn);
-      if (id >= 0) {                                       // (warp-uniform; otherwise no row sees the block)
-        float sc[NT][4];
-#pragma unroll
-        for (int j = 0; j < NT; ++j) sc[j][0] = sc[j][1] = sc[j][2] = sc[j][3] = 0.f;
-#pragma unroll
-        for (int k = 0; k < KW; ++k) {
-          uint32_t a0, a1, a2, a3;
-          cvt4(kr[0][k], a0, a2);
-          cvt4(kr[1][k], a1, a3);
-#pragma unroll
-          for (int j = 0; j < NT; ++j) mma_f16(sc[j], a0, a1, a2, a3, qf[j][k][0], qf[j][k][1]);
-        }
-        const float ksc = ks;
-        if (next) load_k(bn);
         const int ebits = (int)(__float_as_uint(vs) >> 23);
         const float ev = (float)(ebits - 127), vinv = __uint_as_float((uint32_t)(254 - ebits) << 23);
         const bool edge = t * BLK + BLK - 1 > lim_lo;      // some row does not see the whole block
@@ -317,7 +400,7 @@ __global__ void __launch_bounds__(AT_THREADS, NT == 1 ? AT_CTAS : 1) paged_atten
           for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              y[j][e] = fmaf(sc[j][e], rc[j][e & 1] * ksc, based ? ev + (off - m[j][e & 1]) : ev);
+              y[j][e] = fmaf(sc[j][e], rc[j][e & 1] * ks, based ? ev + (off - m[j][e & 1]) : ev);
               if (edge && t * BLK + g + 8 * (e >> 1) > lim[j][e & 1]) y[j][e] = -INFINITY;
             }
         };
@@ -424,17 +507,21 @@ __global__ void __launch_bounds__(AT_THREADS, NT == 1 ? AT_CTAS : 1) paged_atten
             cvt4(__byte_perm(vr[2][k], vr[3][k], e ? 0x7362 : 0x5140), a2, a3);
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-              mma_f16(o[j][2 * k + e], a0, a1, a2, a3, ph[j][0], ph[j][1]);
-              if (SPLIT) mma_f16(o[j][2 * k + e], a0, a1, a2, a3, pl[j][0], pl[j][1]);
+              if (SPLIT) {
+                float z[4] = {0.f, 0.f, 0.f, 0.f};
+                mma_f16(z, a0, a1, a2, a3, pl[j][0], pl[j][1]);
+                mma_f16(z, a0, a1, a2, a3, ph[j][0], ph[j][1]);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) o[j][2 * k + e][x] += z[x];
+              } else {
+                mma_f16(o[j][2 * k + e], a0, a1, a2, a3, ph[j][0], ph[j][1]);
+              }
             }
           }
-        if (next) load_v(bn);
-      } else if (next) {
-        load_k(bn);
-        load_v(bn);
       }
-      id = id_next;
-      id_next = tn + AT_WARPS < tb ? page(tn + AT_WARPS) : -1;
+      __syncwarp();                                        // every lane has read the block
+      ask();
+      stage = stage + 1 == R::ST ? 0 : stage + 1;
     }
 
     // ---- the warps' rows join, 8 at a time
@@ -449,9 +536,9 @@ __global__ void __launch_bounds__(AT_THREADS, NT == 1 ? AT_CTAS : 1) paged_atten
           lS[warp][8 * j + 2 * t4 + e] = l[j][e];
         }
       }
-    const bool whole = ta == 0 && tb == u.tiles;
-    const long long c0 = whole ? 0 : part_of(ustart), c1 = whole ? 0 : part_of(ustart + u.tiles - 1);
-    float* mypart = a.part + ((long long)blockIdx.x * 2 + (blockIdx.x == c0 ? 1 : 0)) * ROWS * (D + 2);
+    const bool whole = ta == 0 && tb == u.blocks;
+    const long long p0 = whole ? 0 : part_of(ustart), p1 = whole ? 0 : part_of(ustart + u.blocks - 1);
+    float* mypart = a.part + ((long long)blockIdx.x * 2 + (blockIdx.x == p0 ? 1 : 0)) * ROWS * (D + 2);
 #pragma unroll 1
     for (int j = 0; j < NT; ++j) {
       __syncthreads();
@@ -463,7 +550,7 @@ __global__ void __launch_bounds__(AT_THREADS, NT == 1 ? AT_CTAS : 1) paged_atten
             const int col = 8 * j + 2 * t4 + e;
             float mt = mS[0][col];
 #pragma unroll
-            for (int x = 1; x < AT_WARPS; ++x) mt = fmaxf(mt, mS[x][col]);
+            for (int x = 1; x < W; ++x) mt = fmaxf(mt, mS[x][col]);
             const float f = m[jj][e] == -INFINITY ? 0.f : ex2(m[jj][e] - mt);
             float* p = accS + warp * RS + (2 * t4 + e) * (D + 4) + 2 * KW * g;
 #pragma unroll
@@ -472,15 +559,15 @@ __global__ void __launch_bounds__(AT_THREADS, NT == 1 ? AT_CTAS : 1) paged_atten
           }
         }
       __syncthreads();
-      for (int i = tid; i < 8 * (D / 4); i += AT_THREADS) {
+      for (int i = tid; i < 8 * (D / 4); i += 32 * W) {
         const int r = i / (D / 4), cc = i % (D / 4), col = 8 * j + r;
         if (col >= rows) continue;
         float mt = mS[0][col], lt = 0.f;
 #pragma unroll
-        for (int x = 1; x < AT_WARPS; ++x) mt = fmaxf(mt, mS[x][col]);
+        for (int x = 1; x < W; ++x) mt = fmaxf(mt, mS[x][col]);
         float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int x = 0; x < AT_WARPS; ++x) {
+        for (int x = 0; x < W; ++x) {
           const float4 z = *reinterpret_cast<const float4*>(accS + x * RS + r * (D + 4) + 4 * cc);
           y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
           lt += lS[x][col] * (mS[x][col] == -INFINITY ? 0.f : ex2(mS[x][col] - mt));
@@ -498,58 +585,73 @@ __global__ void __launch_bounds__(AT_THREADS, NT == 1 ? AT_CTAS : 1) paged_atten
     if (!whole) {
       __threadfence();
       __syncthreads();
-      if (tid == 0) lastS = atomicAdd(a.count + c0, 1) == (int)(c1 - c0);
+      if (tid == 0) lastS = atomicAdd(a.count + p0, 1) == (int)(p1 - p0);
       __syncthreads();
       if (lastS) {
         __threadfence();
-        for (int i = tid; i < rows * (D / 4); i += AT_THREADS) {
+        for (int i = tid; i < rows * (D / 4); i += 32 * W) {
           const int col = i / (D / 4), cc = i % (D / 4);
           float mt = -INFINITY, lt = 0.f;
           float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-          for (long long c = c0; c <= c1; ++c) {
-            const float* p = a.part + ((c * 2 + (c == c0 ? 1 : 0)) * ROWS + col) * (D + 2);
+          const float* first = a.part + ((p0 * 2 + 1) * ROWS + col) * (D + 2);
+          const long long step = 2 * ROWS * (D + 2);       // a part behind the first has slot 0
+          auto part = [&](long long c) { return first + (c - p0) * step - (c > p0 ? ROWS * (D + 2) : 0); };
+#pragma unroll 8
+          for (long long c = p0; c <= p1; ++c) mt = fmaxf(mt, __ldcg(part(c) + D));
+#pragma unroll 4
+          for (long long c = p0; c <= p1; ++c) {
+            const float* p = part(c);
             const float2 ml = __ldcg(reinterpret_cast<const float2*>(p + D));
             const float2 ya = __ldcg(reinterpret_cast<const float2*>(p + 4 * cc));
             const float2 yb = __ldcg(reinterpret_cast<const float2*>(p + 4 * cc + 2));
-            const float mn = fmaxf(mt, ml.x);
-            // (a NaN in a part without a base stays one)
-            const float fo = mt == -INFINITY ? 0.f : ex2(mt - mn);
-            const float fn = ml.x == -INFINITY ? 0.f : ex2(ml.x - mn);
-            y.x = y.x * fo + ya.x * fn;
-            y.y = y.y * fo + ya.y * fn;
-            y.z = y.z * fo + yb.x * fn;
-            y.w = y.w * fo + yb.y * fn;
-            lt = lt * fo + ml.y * fn;
-            mt = mn;
+            const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - mt);   // (a NaN stays one)
+            y.x = fmaf(ya.x, f, y.x);
+            y.y = fmaf(ya.y, f, y.y);
+            y.z = fmaf(yb.x, f, y.z);
+            y.w = fmaf(yb.y, f, y.w);
+            lt = fmaf(ml.y, f, lt);
           }
           write_out<D>(a, u.first, h, row0 + col, cc, y, mt, lt);
         }
-        if (tid == 0) a.count[c0] = 0;
+        if (tid == 0) a.count[p0] = 0;
       }
     }
     __syncthreads();                                       // shared memory is free for the next unit
   }
 }
 
-template <int D, int NT>
+template <int D, int NT, int W, bool SPLIT>
 cudaError_t launch(const AttendArgs& a, int grid, cudaStream_t stream) {
-  if (a.out_f32) paged_attend_kernel<D, NT, true><<<grid, AT_THREADS, 0, stream>>>(a);
-  else paged_attend_kernel<D, NT, false><<<grid, AT_THREADS, 0, stream>>>(a);
-  return cudaGetLastError();
+  using R = Ring<D, W>;
+  auto k = paged_attend_kernel<D, NT, W, SPLIT>;
+  const cudaError_t e = raise_smem_limit(k, R::BYTES);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3(32 * W);
+  cfg.dynamicSmemBytes = R::BYTES;
+  cfg.stream = stream;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, k, a);
 }
 template <int D>
 cudaError_t launch_d(const AttendArgs& a, int sms, long long rows, cudaStream_t stream) {
-  if (rows <= 8) return launch<D, 1>(a, AT_CTAS * sms, stream);
-  if (rows <= 16) return launch<D, 2>(a, sms, stream);
-  return launch<D, 4>(a, sms, stream);
+  // (as many warps as the registers allow: 12 of 168, or 8 of 255)
+  if (rows <= 8) return a.out_f32 ? launch<D, 1, 12, true>(a, sms, stream) : launch<D, 1, 12, false>(a, sms, stream);
+  if (rows <= 16) return a.out_f32 ? launch<D, 2, 8, true>(a, sms, stream) : launch<D, 2, 8, false>(a, sms, stream);
+  return a.out_f32 ? launch<D, 4, 8, true>(a, sms, stream) : launch<D, 4, 8, false>(a, sms, stream);
 }
 
-size_t counter_bytes(int sms) { return ((size_t)AT_CTAS * sms * 4 + 255) / 256 * 256; }
+size_t counter_bytes(int sms) { return ((size_t)sms * 4 + 255) / 256 * 256; }
 
 }  // namespace
 
 size_t paged_attend_workspace(int sms) {
-  return counter_bytes(sms) + (size_t)AT_CTAS * sms * 2 * AT_MAX_ROWS * (128 + 2) * 4;
+  return counter_bytes(sms) + (size_t)sms * 2 * AT_MAX_ROWS * (128 + 2) * 4;
 }
 
 cudaError_t launch_paged_attend(const Pool& pool, const Batch& b, const void* q, long long q_ts, long long q_hs,

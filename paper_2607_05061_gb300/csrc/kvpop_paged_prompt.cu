@@ -31,7 +31,6 @@ constexpr int PP_THREADS = 32 * (PP_MMA_WARP + 1 + PP_CONV);
 constexpr int PP_RING = 5;
 constexpr int PP_TMEM = 512;                             // O_h: 128 h; S_h: 256 + 128 h
 constexpr float PP_OFF = 7.f, PP_STEP = 8.f;
-enum : int { PPERR_WAIT = 44 };
 // barriers
 constexpr int PB_FULL = 0;                               // [ring] converters -> MMA
 constexpr int PB_EMPTY = PB_FULL + PP_RING;              // [ring] MMA -> converters
@@ -208,7 +207,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     load(0, a.pool.k);
     for (int i = 0; i < 2 * nblk && ok; ++i) {
       const int j = i >> 1, st = i % PP_RING;
-      if (i >= PP_RING && !(ok = uniform(mbar_wait(bar(PB_EMPTY + st), (i / PP_RING - 1) & 1, a.err, PPERR_WAIT)))) break;
+      if (i >= PP_RING && !(ok = uniform(mbar_wait(bar(PB_EMPTY + st), (i / PP_RING - 1) & 1, a.err, ERR_WAIT)))) break;
       if ((i & 1) && (j + 1) * PP_KEYS - 1 > lim_lo) {
         // Values that some row does not see: a NaN must not reach the rows before it, where its
         // weight is 0.  Its column is set at the end, for the rows that see it.
@@ -253,7 +252,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     const uint64_t qd0 = kmajor_desc(sb, PP_HALF, 0), kd0 = kmajor_desc(sb + L::OFF_RING, PP_KEYS, 0);
     const uint64_t vd0 = mnmajor_desc(sb + L::OFF_RING, PP_KEYS, 0);
     auto wait = [&](int b, int parity) {
-      ok = ok && mbar_wait(bar(b), parity, a.err, PPERR_WAIT);
+      ok = ok && mbar_wait(bar(b), parity, a.err, ERR_WAIT);
       ok = uniform(ok);
       if (ok) fence_after();
     };
@@ -320,7 +319,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     };
     float scale = scale_of(0);
     for (int j = 0; j < nblk; ++j) {
-      if (!(ok = uniform(mbar_wait(bar(PB_S + hf), j & 1, a.err, PPERR_WAIT)))) break;
+      if (!(ok = uniform(mbar_wait(bar(PB_S + hf), j & 1, a.err, ERR_WAIT)))) break;
       fence_after();
       const float now = scale;
       scale = scale_of(j + 1);
@@ -352,7 +351,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
       const float al = m == -INFINITY ? 0.f : ex2(m - mn);
       if (j > 0 && __any_sync(0xffffffffu, move)) {
         // PV_{j-1} has to be in O before O changes
-        if (!(ok = uniform(mbar_wait(bar(PB_O + hf), (j - 1) & 1, a.err, PPERR_WAIT)))) break;
+        if (!(ok = uniform(mbar_wait(bar(PB_O + hf), (j - 1) & 1, a.err, ERR_WAIT)))) break;
         fence_after();
         const float f = move ? al : 1.f;
 #pragma unroll
@@ -413,7 +412,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
         }
       }
     }
-    if (ok) ok = uniform(mbar_wait(bar(PB_O + hf), (nblk - 1) & 1, a.err, PPERR_WAIT));
+    if (ok) ok = uniform(mbar_wait(bar(PB_O + hf), (nblk - 1) & 1, a.err, ERR_WAIT));
   }
   fence_before();
   __syncthreads();                                       // every product is done; shared memory is free
