@@ -41,7 +41,7 @@ namespace {
 
 using namespace paged;
 
-constexpr int AT_LEAST = 12;           // blocks of a part, unless there are fewer
+constexpr int AT_SHORT = 48;           // blocks of a unit that one CTA takes whole
 constexpr int AT_MAX_ROWS = 32;        // query rows of a unit at most
 constexpr float AT_OFF = 7.f, AT_STEP = 8.f;
 
@@ -75,7 +75,9 @@ struct AttendArgs {
   int* count;                          // [grid], zero between calls
   int32_t* err;
   float c;                             // log2(e) / sqrt(d)
+  float inv_g;                         // 1 / G
   int G, out_f32;
+  int one;                             // row groups of a single token
   int skip_long;                       // the tcgen05 kernel takes sequences with long_rows
 };
 
@@ -86,6 +88,15 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1,
       " {%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// the same from zero
+__device__ __forceinline__ void mma_f16_0(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                          uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9},"
+      " {%10, %10, %10, %10};"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 // four e4m3 bytes -> two words of two f16
 __device__ __forceinline__ void cvt4(uint32_t w, uint32_t& lo, uint32_t& hi) {
@@ -117,19 +128,55 @@ __device__ __forceinline__ SeqUnits seq_units(const AttendArgs& a, int s) {
   u.first = t.first;
   u.len = t.len;
   u.n = t.n;
-  u.groups = (int)(((long long)t.n * a.G + ROWS - 1) / ROWS);
+  u.groups = t.n > 1 ? (int)(((long long)t.n * a.G + ROWS - 1) / ROWS) : t.n * a.one;
   if (a.skip_long && long_rows(t, a.G)) u.groups = 0;
   u.ctx = u.groups > 0 ? context(a.b, a.pool, t, a.err) : 0;
   u.blocks = max((u.ctx + BLK - 1) / BLK, 1);
   return u;
 }
+__device__ __forceinline__ long long div_pos(long long a, long long b) {   // a, b >= 0
+  return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
+// A unit of the list.
+struct Unit {
+  SeqUnits u;
+  long long base, start;               // list positions of its sequence and of itself
+  int s, h, row0, rows;                // sequence, KV head, rows of the sequence
+  int tok0, rem0;                      // row0 = tok0 G + rem0
+  int lim_hi;                          // its rows see at most 0 .. lim_hi
+  __device__ __forceinline__ long long end() const { return start + u.blocks; }
+};
+// The unit that list position w lies in, from an earlier one (or from a sequence and its base).
+template <int ROWS>
+__device__ __forceinline__ void seek(const AttendArgs& a, Unit& x, long long w) {
+  while (w >= x.base + x.u.work(a.pool.H)) {               // (sequences without tokens have no blocks)
+    x.base += x.u.work(a.pool.H);
+    x.u = seq_units<ROWS>(a, ++x.s);
+  }
+  const int unit = (int)div_pos(w - x.base, x.u.blocks), grp = unit / a.pool.H;
+  x.h = unit - grp * a.pool.H;
+  x.start = x.base + (long long)unit * x.u.blocks;
+  x.row0 = grp * ROWS;
+  x.rows = min(ROWS, x.u.n * a.G - x.row0);
+  x.tok0 = x.row0 / a.G;
+  x.rem0 = x.row0 - x.tok0 * a.G;
+  x.lim_hi = min(x.u.len + (x.row0 + x.rows - 1) / a.G, x.u.ctx - 1);
+}
+// Token and head of the unit's row i, without an integer division (i < 32, G up to 2^20: the
+// quotient is at most 32, and its distance from the next whole number at least 1 / (2 G)).
+__device__ __forceinline__ void token_of(const AttendArgs& a, const Unit& x, int i, int& tok, int& head) {
+  const int r = x.rem0 + i, q = a.G >= 64 ? (r >= a.G) : (int)(((float)r + 0.5f) * a.inv_g);
+  tok = x.tok0 + q;
+  head = r - q * a.G;
+}
 
 // Four values of a finished row, and its normaliser.  A row that saw nothing: zeros and -inf.
 template <int D>
-__device__ __forceinline__ void write_out(const AttendArgs& a, int first, int h, int r, int cc, float4 y, float m,
+__device__ __forceinline__ void write_out(const AttendArgs& a, const Unit& x, int i, int cc, float4 y, float m,
                                           float l) {
-  const int i = r / a.G;
-  const long long row = (long long)(first + i) * a.pool.H * a.G + h * a.G + (r - i * a.G);
+  int tok, head;
+  token_of(a, x, i, tok, head);
+  const long long row = ((long long)(x.u.first + tok) * a.pool.H + x.h) * a.G + head;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   y.x *= inv; y.y *= inv; y.z *= inv; y.w *= inv;
   if (a.out_f32)
@@ -150,17 +197,16 @@ __global__ void __launch_bounds__(32 * W, 1) paged_attend_kernel(AttendArgs a) {
   uint2* qS = reinterpret_cast<uint2*>(sma + R::OFF_Q);
   __shared__ float mS[W][ROWS], lS[W][ROWS];
   __shared__ float scaleS[W][R::ST][2];
-  __shared__ long long scanS[W];
-  __shared__ long long b0S;
-  __shared__ int s0S, lastS;
+  __shared__ long long scanS[W], foundS[2];
+  __shared__ int foundsS[2], lastS;
+  __shared__ Unit unitS[2], aheadS[W];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
-  const int H = a.pool.H, G = a.G;
+  const int H = a.pool.H;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-  // ---- this CTA's part of the list: [w0, w1), and the sequence that w0 lies in
-  const int per = (a.b.n_seq + 32 * W - 1) / (32 * W), sA = min(tid * per, a.b.n_seq);
-  const int sB = min(sA + per, a.b.n_seq);
+  // ---- the list, and this CTA's part [w0, w1) of it
+  const int per = (a.b.n_seq + 32 * W - 1) / (32 * W), sA = min(tid * per, a.b.n_seq), sB = min(sA + per, a.b.n_seq);
   long long mine = 0;
   for (int s = sA; s < sB; ++s) mine += seq_units<ROWS>(a, s).work(H);
   long long pre = mine;
@@ -172,57 +218,51 @@ __global__ void __launch_bounds__(32 * W, 1) paged_attend_kernel(AttendArgs a) {
   if (lane == 31) scanS[warp] = pre;
   __syncthreads();
   long long total = 0;
+#pragma unroll
   for (int w = 0; w < W; ++w) {
     if (w < warp) pre += scanS[w];
     total += scanS[w];
   }
   if (total == 0) return;
-  const long long grid = max(min((long long)gridDim.x, total / AT_LEAST), 1ll);
-  auto part_start = [&](long long c) { return c * total / grid; };
-  auto part_of = [&](long long w) {                        // the part that block w lies in
-    long long c = w * grid / total;
-    while (c + 1 < grid && part_start(c + 1) <= w) ++c;
-    while (part_start(c) > w) --c;
-    return c;
-  };
-  if (blockIdx.x >= grid) return;
-  const long long w0 = part_start(blockIdx.x), w1 = part_start(blockIdx.x + 1);
-  if (pre - mine <= w0 && w0 < pre) {
-    long long base = pre - mine;
-    int s = sA;
-    for (; s < sB; ++s) {
-      const long long k = seq_units<ROWS>(a, s).work(H);
-      if (w0 < base + k) break;
-      base += k;
+  const long long share = max(div_pos(total + gridDim.x - 1, gridDim.x), (long long)W);   // a block a warp at least
+  long long w0 = share * blockIdx.x, w1 = min(w0 + share, total);
+  if (w0 >= total) return;
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {                            // the sequences of its first and its last block
+    const long long w = e ? w1 - 1 : w0;
+    if (pre - mine <= w && w < pre) {
+      long long base = pre - mine;
+      int s = sA;
+      for (; s + 1 < sB; ++s) {
+        const long long k = seq_units<ROWS>(a, s).work(H);
+        if (w < base + k) break;
+        base += k;
+      }
+      foundsS[e] = s;
+      foundS[e] = base;
     }
-    s0S = s;
-    b0S = base;
   }
   __syncthreads();
-
-  // Place in the list: the unit that a position lies in, found by walking on from an earlier one.
-  struct Walk {
-    SeqUnits u;
-    long long base, start;                                 // list positions of the sequence and the unit
-    int s, h, row0, rows, lim_hi;
-  };
-  auto seek = [&](Walk& x, long long w) {
-    while (w >= x.base + x.u.work(H)) {                    // (sequences without tokens have no blocks)
-      x.base += x.u.work(H);
-      x.u = seq_units<ROWS>(a, ++x.s);
+  Unit x;
+  x.s = foundsS[1];
+  x.base = foundS[1];
+  x.u = seq_units<ROWS>(a, x.s);
+  seek<ROWS>(a, x, w1 - 1);
+  // a short unit is not cut: it belongs to the part that it begins in
+  if (x.u.blocks <= AT_SHORT) w1 = x.end();
+  if (x.start > w0) {
+    if (foundsS[0] != x.s) {
+      x.s = foundsS[0];
+      x.base = foundS[0];
+      x.u = seq_units<ROWS>(a, x.s);
     }
-    const int unit = (int)((w - x.base) / x.u.blocks);
-    x.h = unit % H;
-    x.start = x.base + (long long)unit * x.u.blocks;
-    x.row0 = unit / H * ROWS;
-    x.rows = min(ROWS, x.u.n * G - x.row0);
-    x.lim_hi = min(x.u.len + (x.row0 + x.rows - 1) / G, x.u.ctx - 1);   // its rows see at most 0 .. lim_hi
-  };
-  Walk at;
-  at.s = s0S;
-  at.base = b0S;
-  at.u = seq_units<ROWS>(a, at.s);
-  seek(at, w0);
+    seek<ROWS>(a, x, w0);
+  }
+  if (x.u.blocks <= AT_SHORT && x.start < w0) w0 = x.end();
+  if (w0 >= w1) return;
+  seek<ROWS>(a, x, w0);
+  if (tid < W) aheadS[tid] = x;
+  if (tid == 0) unitS[0] = x;
 
   // ---- the warp's ring: blocks w0 + warp, w0 + warp + W, ...
   const uint32_t ring = smem_u32(sma) + warp * (R::ST * R::BLOCK);
@@ -230,28 +270,34 @@ __global__ void __launch_bounds__(32 * W, 1) paged_attend_kernel(AttendArgs a) {
   // a lane copies the 16 bytes at 512 i + 16 lane of a block's K and of its V
   constexpr int RPI = 512 / D;
   const int r0 = lane / (D / 16), c0 = lane % (D / 16), put0 = R::chunk_at(r0, c0), put1 = R::chunk_at(r0 + RPI, c0);
-  Walk ahead = at;
   int asked = 0, slot = 0;                                 // blocks asked for; the next one's slot,
-  int nt = (int)(w0 - at.start) + warp, left = (int)min((long long)at.u.blocks, w1 - at.start);   // place, the unit's end,
-  const int32_t* row = a.b.table + (long long)ahead.s * a.b.table_stride;
-  int id = -1;                                             // and page
+  int nt = (int)(w0 - x.start) + warp, stop = (int)min((long long)x.u.blocks, w1 - x.start);   // place, its unit's end,
+  int nh = x.h, seen = x.lim_hi, id = -1;                  // head, last position that is seen, and page
+  const int32_t* row = a.b.table + (long long)x.s * a.b.table_stride;
+  __syncthreads();
   auto look = [&] {
     if (asked >= count) return;
-    if (nt >= left) {
+    if (nt >= stop) {
       const long long w = w0 + warp + (long long)asked * W;
-      seek(ahead, w);
-      nt = (int)(w - ahead.start);
-      left = (int)min((long long)ahead.u.blocks, w1 - ahead.start);
-      row = a.b.table + (long long)ahead.s * a.b.table_stride;
+      Unit y = aheadS[warp];
+      seek<ROWS>(a, y, w);
+      __syncwarp();
+      if (lane == 0) aheadS[warp] = y;
+      __syncwarp();
+      nt = (int)(w - y.start);
+      stop = (int)min((long long)y.u.blocks, w1 - y.start);
+      nh = y.h;
+      seen = y.lim_hi;
+      row = a.b.table + (long long)y.s * a.b.table_stride;
     }
-    if (nt * BLK <= ahead.lim_hi) id = __ldg(row + (nt * BLK >> a.pool.page_shift));
+    if (nt * BLK <= seen) id = __ldg(row + (nt * BLK >> a.pool.page_shift));
   };
   auto ask = [&] {
     if (asked < count) {
       const int pos = nt * BLK;
       float* sc = &scaleS[warp][slot][0];
-      if (pos <= ahead.lim_hi && (unsigned)id < (unsigned)a.pool.n_pages) {
-        const long long rows0 = ((long long)id * H + ahead.h) * a.pool.page + (pos & (a.pool.page - 1));
+      if (pos <= seen && (unsigned)id < (unsigned)a.pool.n_pages) {
+        const long long rows0 = ((long long)id * H + nh) * a.pool.page + (pos & (a.pool.page - 1));
         const unsigned char *kp = a.pool.k + rows0 * D + 16 * lane, *vp = a.pool.v + rows0 * D + 16 * lane;
         const uint32_t dst = ring + slot * R::BLOCK;
 #pragma unroll
@@ -262,7 +308,7 @@ __global__ void __launch_bounds__(32 * W, 1) paged_attend_kernel(AttendArgs a) {
         }
         if (lane < 2) cp_async4(smem_u32(sc + lane), (lane ? a.pool.vs : a.pool.ks) + rows0 / BLK);
       } else if (lane == 0) {                              // no row sees the block, or a bad page
-        if (pos <= ahead.lim_hi) report(a.err, ERR_PAGE);
+        if (pos <= seen) report(a.err, ERR_PAGE);
         sc[1] = -1.f;
       }
       nt += W;
@@ -276,14 +322,14 @@ __global__ void __launch_bounds__(32 * W, 1) paged_attend_kernel(AttendArgs a) {
 #pragma unroll 1
   for (int i = 0; i < R::ST; ++i) ask();
 
-  int next = warp, done = 0, stage = 0;                    // the warp's next block of the CTA's; blocks so far
-  for (long long w = w0; w < w1;) {
-    seek(at, w);
-    const SeqUnits& u = at.u;
-    const int h = at.h, row0 = at.row0, rows = at.rows, lim_hi = at.lim_hi;
-    const long long ustart = at.start;
-    const int ta = (int)(w - ustart), tb = (int)min((long long)u.blocks, w1 - ustart);
-    w = ustart + tb;
+  int next = warp, done = 0, stage = 0, turn = 0;          // the warp's next block of the CTA's; blocks so far
+  for (long long w = w0; w < w1; turn ^= 1) {
+    x = unitS[turn];
+    seek<ROWS>(a, x, w);
+    if (tid == 0) unitS[turn ^ 1] = x;                     // (read again behind the next barrier)
+    const int ta = (int)(w - x.start), tb = (int)min((long long)x.u.blocks, w1 - x.start);
+    const int lim_lo = min(x.u.len + x.tok0, x.u.ctx - 1), lim_hi = x.lim_hi;   // all rows see 0 .. lim_lo
+    w = x.start + tb;
 
     // ---- query rows, each scaled by a power of two, and what that makes of the logits
     uint32_t qf[NT][KW][2];
@@ -291,10 +337,10 @@ __global__ void __launch_bounds__(32 * W, 1) paged_attend_kernel(AttendArgs a) {
     int lim[NT][2];                                        // last position a row sees
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-      const int r = row0 + 8 * j + g;
-      const bool ok = 8 * j + g < rows;
-      const bf16* qp = a.q + (long long)(u.first + (ok ? r / G : 0)) * a.q_ts +
-                       (long long)(h * G + (ok ? r % G : 0)) * a.q_hs + 4 * KW * t4;
+      const bool ok = 8 * j + g < x.rows;
+      int tok, head;
+      token_of(a, x, ok ? 8 * j + g : 0, tok, head);
+      const bf16* qp = a.q + (long long)(x.u.first + tok) * a.q_ts + (long long)(x.h * a.G + head) * a.q_hs + 4 * KW * t4;
       uint32_t top = 0;
 #pragma unroll
       for (int k = 0; k < KW; k += 2) {
@@ -313,8 +359,8 @@ __global__ void __launch_bounds__(32 * W, 1) paged_attend_kernel(AttendArgs a) {
       for (int k = 0; k < KW; ++k)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const uint32_t x = qf[j][k][e];
-          qf[j][k][e] = pack_f16(__uint_as_float(x << 16) * f, __uint_as_float(x & 0xffff0000u) * f);
+          const uint32_t v = qf[j][k][e];
+          qf[j][k][e] = pack_f16(__uint_as_float(v << 16) * f, __uint_as_float(v & 0xffff0000u) * f);
         }
       if (QS && warp == j)
 #pragma unroll
@@ -323,12 +369,11 @@ __global__ void __launch_bounds__(32 * W, 1) paged_attend_kernel(AttendArgs a) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         rc[j][e] = __shfl_sync(0xffffffffu, down, (2 * t4 + e) * 4);
-        const int rr = min(row0 + 8 * j + 2 * t4 + e, row0 + rows - 1);
-        lim[j][e] = min(u.len + rr / G, u.ctx - 1);
+        token_of(a, x, min(8 * j + 2 * t4 + e, x.rows - 1), tok, head);
+        lim[j][e] = min(x.u.len + tok, x.u.ctx - 1);
       }
     }
     if (QS) __syncthreads();
-    const int lim_lo = min(u.len + row0 / G, u.ctx - 1);   // the unit's rows see at least 0 .. lim_lo
 
     float o[NT][KW][4], m[NT][2], l[NT][2];
 #pragma unroll
@@ -351,11 +396,7 @@ __global__ void __launch_bounds__(32 * W, 1) paged_attend_kernel(AttendArgs a) {
       const float ks = scaleS[warp][stage][0], vs = scaleS[warp][stage][1];
       const unsigned char* kp = sma + (warp * R::ST + stage) * R::BLOCK;
       if (vs >= 0.f) {                                     // (warp-uniform)
-        float sc[NT][4], sd[NT][4];
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sc[j][e] = sd[j][e] = 0.f;
+        float sc[NT][4], sd[NT][4];                        // (two sums, even and odd words)
 #pragma unroll
         for (int k = 0; k < KW; k += 4) {
           const uint4 ka = *reinterpret_cast<const uint4*>(kp + R::k_at(g, t4, k >> 2));
@@ -369,7 +410,8 @@ __global__ void __launch_bounds__(32 * W, 1) paged_attend_kernel(AttendArgs a) {
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
               const uint2 b = QS ? qS[(j * KW + k + i) * 32 + lane] : make_uint2(qf[j][k + i][0], qf[j][k + i][1]);
-              mma_f16(i & 1 ? sd[j] : sc[j], a0, a1, a2, a3, b.x, b.y);
+              if (k + i < 2) mma_f16_0(i & 1 ? sd[j] : sc[j], a0, a1, a2, a3, b.x, b.y);
+              else mma_f16(i & 1 ? sd[j] : sc[j], a0, a1, a2, a3, b.x, b.y);
             }
           }
         }
@@ -478,10 +520,10 @@ __global__ void __launch_bounds__(32 * W, 1) paged_attend_kernel(AttendArgs a) {
               vr[e][k] &= ~mask;
             }
           // rows that do see such a value get it: NaN in that column
+#pragma unroll 1
+          for (int y = 0; y < 4; ++y)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
+            for (int e = 0; e < 4; ++e) {
               const int pos = t * BLK + 2 * y + (e & 1) + 8 * (e >> 1);
 #pragma unroll
               for (int k = 0; k < VW; ++k) {
@@ -508,11 +550,12 @@ __global__ void __launch_bounds__(32 * W, 1) paged_attend_kernel(AttendArgs a) {
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
               if (SPLIT) {
-                float z[4] = {0.f, 0.f, 0.f, 0.f};
-                mma_f16(z, a0, a1, a2, a3, pl[j][0], pl[j][1]);
+                float z[4];
+                mma_f16_0(z, a0, a1, a2, a3, pl[j][0], pl[j][1]);
                 mma_f16(z, a0, a1, a2, a3, ph[j][0], ph[j][1]);
-#pragma unroll
-                for (int x = 0; x < 4; ++x) o[j][2 * k + e][x] += z[x];
+                float (&y)[4] = o[j][2 * k + e];
+                f2_unpack(f2_add(f2_pack(y[0], y[1]), f2_pack(z[0], z[1])), y[0], y[1]);
+                f2_unpack(f2_add(f2_pack(y[2], y[3]), f2_pack(z[2], z[3])), y[2], y[3]);
               } else {
                 mma_f16(o[j][2 * k + e], a0, a1, a2, a3, ph[j][0], ph[j][1]);
               }
@@ -530,93 +573,92 @@ __global__ void __launch_bounds__(32 * W, 1) paged_attend_kernel(AttendArgs a) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
 #pragma unroll
-        for (int x = 4; x < 32; x <<= 1) l[j][e] += __shfl_xor_sync(0xffffffffu, l[j][e], x);
+        for (int z = 4; z < 32; z <<= 1) l[j][e] += __shfl_xor_sync(0xffffffffu, l[j][e], z);
         if (g == 0) {
           mS[warp][8 * j + 2 * t4 + e] = m[j][e];
           lS[warp][8 * j + 2 * t4 + e] = l[j][e];
         }
       }
-    const bool whole = ta == 0 && tb == u.blocks;
-    const long long p0 = whole ? 0 : part_of(ustart), p1 = whole ? 0 : part_of(ustart + u.blocks - 1);
-    float* mypart = a.part + ((long long)blockIdx.x * 2 + (blockIdx.x == p0 ? 1 : 0)) * ROWS * (D + 2);
 #pragma unroll 1
     for (int j = 0; j < NT; ++j) {
-      __syncthreads();
 #pragma unroll
       for (int jj = 0; jj < NT; ++jj)
         if (jj == j) {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const int col = 8 * j + 2 * t4 + e;
-            float mt = mS[0][col];
-#pragma unroll
-            for (int x = 1; x < W; ++x) mt = fmaxf(mt, mS[x][col]);
-            const float f = m[jj][e] == -INFINITY ? 0.f : ex2(m[jj][e] - mt);
             float* p = accS + warp * RS + (2 * t4 + e) * (D + 4) + 2 * KW * g;
 #pragma unroll
             for (int k = 0; k < KW; ++k)
-              *reinterpret_cast<float2*>(p + 2 * k) = make_float2(o[jj][k][e] * f, o[jj][k][e + 2] * f);
+              *reinterpret_cast<float2*>(p + 2 * k) = make_float2(o[jj][k][e], o[jj][k][e + 2]);
           }
         }
       __syncthreads();
+      const Unit& y = unitS[turn ^ 1];
+      const bool whole = ta == 0 && tb == y.u.blocks;
+      const long long p0 = whole ? 0 : div_pos(y.start, share);   // the part that the unit begins in
+      float* mypart = a.part + ((long long)blockIdx.x * 2 + (blockIdx.x == p0 ? 1 : 0)) * ROWS * (D + 2);
       for (int i = tid; i < 8 * (D / 4); i += 32 * W) {
         const int r = i / (D / 4), cc = i % (D / 4), col = 8 * j + r;
-        if (col >= rows) continue;
-        float mt = mS[0][col], lt = 0.f;
+        if (col >= y.rows) continue;
+        float mw[W], mt = -INFINITY, lt = 0.f;
 #pragma unroll
-        for (int x = 1; x < W; ++x) mt = fmaxf(mt, mS[x][col]);
-        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int z = 0; z < W; ++z) mt = fmaxf(mt, mw[z] = mS[z][col]);
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int x = 0; x < W; ++x) {
-          const float4 z = *reinterpret_cast<const float4*>(accS + x * RS + r * (D + 4) + 4 * cc);
-          y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
-          lt += lS[x][col] * (mS[x][col] == -INFINITY ? 0.f : ex2(mS[x][col] - mt));
+        for (int z = 0; z < W; ++z) {
+          const float4 b = *reinterpret_cast<const float4*>(accS + z * RS + r * (D + 4) + 4 * cc);
+          const float f = mw[z] == -INFINITY ? 0.f : ex2(mw[z] - mt);   // (a NaN stays one)
+          v.x = fmaf(b.x, f, v.x);
+          v.y = fmaf(b.y, f, v.y);
+          v.z = fmaf(b.z, f, v.z);
+          v.w = fmaf(b.w, f, v.w);
+          lt = fmaf(lS[z][col], f, lt);
         }
         if (whole) {
-          write_out<D>(a, u.first, h, row0 + col, cc, y, mt, lt);
+          write_out<D>(a, y, col, cc, v, mt, lt);
         } else {
           float* p = mypart + (long long)col * (D + 2);
-          __stcg(reinterpret_cast<float2*>(p + 4 * cc), make_float2(y.x, y.y));
-          __stcg(reinterpret_cast<float2*>(p + 4 * cc + 2), make_float2(y.z, y.w));
+          __stcg(reinterpret_cast<float2*>(p + 4 * cc), make_float2(v.x, v.y));
+          __stcg(reinterpret_cast<float2*>(p + 4 * cc + 2), make_float2(v.z, v.w));
           if (cc == 0) __stcg(reinterpret_cast<float2*>(p + D), make_float2(mt, lt));
         }
       }
-    }
-    if (!whole) {
-      __threadfence();
-      __syncthreads();
-      if (tid == 0) lastS = atomicAdd(a.count + p0, 1) == (int)(p1 - p0);
-      __syncthreads();
-      if (lastS) {
+      if (!whole && j == NT - 1) {
+        const long long p1 = div_pos(y.start + y.u.blocks - 1, share);
         __threadfence();
-        for (int i = tid; i < rows * (D / 4); i += 32 * W) {
-          const int col = i / (D / 4), cc = i % (D / 4);
-          float mt = -INFINITY, lt = 0.f;
-          float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-          const float* first = a.part + ((p0 * 2 + 1) * ROWS + col) * (D + 2);
-          const long long step = 2 * ROWS * (D + 2);       // a part behind the first has slot 0
-          auto part = [&](long long c) { return first + (c - p0) * step - (c > p0 ? ROWS * (D + 2) : 0); };
-#pragma unroll 8
-          for (long long c = p0; c <= p1; ++c) mt = fmaxf(mt, __ldcg(part(c) + D));
+        __syncthreads();
+        if (tid == 0) lastS = atomicAdd(a.count + p0, 1) == (int)(p1 - p0);
+        __syncthreads();
+        if (lastS) {
+          __threadfence();
+          for (int i = tid; i < y.rows * (D / 4); i += 32 * W) {
+            const int col = i / (D / 4), cc = i % (D / 4);
+            const float* first = a.part + ((p0 * 2 + 1) * ROWS + col) * (D + 2);
+            const long long step = 2 * ROWS * (D + 2);     // a part behind the first has slot 0
+            float mt = -INFINITY, lt = 0.f;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-          for (long long c = p0; c <= p1; ++c) {
-            const float* p = part(c);
-            const float2 ml = __ldcg(reinterpret_cast<const float2*>(p + D));
-            const float2 ya = __ldcg(reinterpret_cast<const float2*>(p + 4 * cc));
-            const float2 yb = __ldcg(reinterpret_cast<const float2*>(p + 4 * cc + 2));
-            const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - mt);   // (a NaN stays one)
-            y.x = fmaf(ya.x, f, y.x);
-            y.y = fmaf(ya.y, f, y.y);
-            y.z = fmaf(yb.x, f, y.z);
-            y.w = fmaf(yb.y, f, y.w);
-            lt = fmaf(ml.y, f, lt);
+            for (int c = 0; c <= (int)(p1 - p0); ++c) {
+              const float* p = first + c * step - (c > 0 ? ROWS * (D + 2) : 0);
+              const float2 ml = __ldcg(reinterpret_cast<const float2*>(p + D));
+              const float2 va = __ldcg(reinterpret_cast<const float2*>(p + 4 * cc));
+              const float2 vb = __ldcg(reinterpret_cast<const float2*>(p + 4 * cc + 2));
+              const float mn = fmaxf(mt, ml.x);
+              const float fo = mt == -INFINITY ? 0.f : ex2(mt - mn), fn = ml.x == -INFINITY ? 0.f : ex2(ml.x - mn);
+              v.x = fmaf(v.x, fo, va.x * fn);
+              v.y = fmaf(v.y, fo, va.y * fn);
+              v.z = fmaf(v.z, fo, vb.x * fn);
+              v.w = fmaf(v.w, fo, vb.y * fn);
+              lt = fmaf(lt, fo, ml.y * fn);
+              mt = mn;
+            }
+            write_out<D>(a, y, col, cc, v, mt, lt);
           }
-          write_out<D>(a, u.first, h, row0 + col, cc, y, mt, lt);
+          if (tid == 0) a.count[p0] = 0;
         }
-        if (tid == 0) a.count[p0] = 0;
       }
+      __syncthreads();                                     // shared memory is free for the next rows
     }
-    __syncthreads();                                       // shared memory is free for the next unit
   }
 }
 
@@ -639,8 +681,9 @@ cudaError_t launch(const AttendArgs& a, int grid, cudaStream_t stream) {
   return cudaLaunchKernelEx(&cfg, k, a);
 }
 template <int D>
-cudaError_t launch_d(const AttendArgs& a, int sms, long long rows, cudaStream_t stream) {
+cudaError_t launch_d(AttendArgs& a, int sms, long long rows, cudaStream_t stream) {
   // (as many warps as the registers allow: 12 of 168, or 8 of 255)
+  a.one = (a.G + (rows <= 8 ? 8 : rows <= 16 ? 16 : 32) - 1) / (rows <= 8 ? 8 : rows <= 16 ? 16 : 32);
   if (rows <= 8) return a.out_f32 ? launch<D, 1, 12, true>(a, sms, stream) : launch<D, 1, 12, false>(a, sms, stream);
   if (rows <= 16) return a.out_f32 ? launch<D, 2, 8, true>(a, sms, stream) : launch<D, 2, 8, false>(a, sms, stream);
   return a.out_f32 ? launch<D, 4, 8, true>(a, sms, stream) : launch<D, 4, 8, false>(a, sms, stream);
@@ -671,6 +714,7 @@ cudaError_t launch_paged_attend(const Pool& pool, const Batch& b, const void* q,
   a.err = err;
   a.c = (float)(1.4426950408889634 / sqrt((double)pool.d));
   a.G = HQ / pool.H;
+  a.inv_g = 1.f / (float)a.G;
   long long rows = (long long)a.G * (b.starts ? b.max_new : 1);
   if (rows > LONG_ROWS && b.starts && paged_prompt_fits(pool, b, HQ)) {
     a.skip_long = 1;
