@@ -22,7 +22,7 @@ namespace {
 
 using namespace paged;
 
-constexpr int AP_WARPS = 8;
+constexpr int AP_WARPS = 4, AP_QH = 2;
 
 struct AppendArgs {
   Pool pool;
@@ -35,50 +35,91 @@ struct AppendArgs {
   int tasks, HQ, rot, max_pos, interleaved;
 };
 
-__device__ __forceinline__ void load8(const bf16* p, float (&x)[8]) {
-  const uint4 w = *reinterpret_cast<const uint4*>(p);
-  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(u[i] << 16);
-    x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-  }
-}
-__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
-  const float4 a = reinterpret_cast<const float4*>(p)[0], c = reinterpret_cast<const float4*>(p)[1];
-  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-  x[4] = c.x; x[5] = c.y; x[6] = c.z; x[7] = c.w;
-}
-
-// Values 8 c .. 8 c + 7 of a row, rotated by position pos.
+// 8 values as they lie in memory
 template <typename T>
-__device__ __forceinline__ void load_rotated(const AppendArgs& a, const T* row, int c, int pos, float (&x)[8]) {
-  load8(row + 8 * c, x);
-  if (8 * c >= a.rot) return;
+struct Raw;
+template <>
+struct Raw<bf16> {
+  uint4 w;
+  __device__ __forceinline__ void load(const bf16* p) { w = __ldg(reinterpret_cast<const uint4*>(p)); }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(u[i] << 16);
+      x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    }
+  }
+};
+template <>
+struct Raw<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = __ldg(reinterpret_cast<const float4*>(p));
+    b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+  }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  }
+};
+
+// What a lane's 8 values of a row are: their place, their pairs' (the same where it holds both),
+// and where its cosines and sines lie in a row of the tables.
+struct Lane {
+  int own, other, angle;
+  bool turned, low;
+};
+__device__ __forceinline__ Lane lane_of(const AppendArgs& a, int c, bool rotate) {
   const int half = a.rot >> 1;
-  const long long at = (long long)pos * half;
+  Lane n;
+  n.own = 8 * c;
+  n.turned = rotate && 8 * c < a.rot;
+  n.low = 8 * c < half;
+  n.other = !n.turned || a.interleaved ? 8 * c : n.low ? 8 * c + half : 8 * c - half;
+  n.angle = a.interleaved ? 4 * c : n.low ? 8 * c : 8 * c - half;
+  return n;
+}
+// Cosines and sines of 8 pairs (of 4 when interleaved); the sines of the pairs' first values are
+// negated, so that u cos + w sin is the rotation of either.
+struct Turn {
+  float cs[8] = {}, sn[8] = {};
+};
+__device__ __forceinline__ Turn turn_of(const AppendArgs& a, const Lane& n, const float* cosR, const float* sinR) {
+  Turn t;
+  if (!n.turned) return t;
+  Raw<float> cs, sn;
   if (a.interleaved) {
-    const float4 co = *reinterpret_cast<const float4*>(a.cosT + at + 4 * c);
-    const float4 si = *reinterpret_cast<const float4*>(a.sinT + at + 4 * c);
-    const float cs[4] = {co.x, co.y, co.z, co.w}, sn[4] = {si.x, si.y, si.z, si.w};
+    cs.a = cs.b = __ldg(reinterpret_cast<const float4*>(cosR));
+    sn.a = sn.b = __ldg(reinterpret_cast<const float4*>(sinR));
+  } else {
+    cs.load(cosR);
+    sn.load(sinR);
+  }
+  cs.get(t.cs);
+  sn.get(t.sn);
+  if (n.low && !a.interleaved)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t.sn[i] = -t.sn[i];
+  return t;
+}
+template <typename T>
+__device__ __forceinline__ void rotated(const AppendArgs& a, const Lane& n, const Turn& t, const Raw<T>& own,
+                                        const Raw<T>& other, float (&x)[8]) {
+  own.get(x);
+  if (!n.turned) return;
+  if (a.interleaved) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float u = x[2 * i], w = x[2 * i + 1];
-      x[2 * i] = __fsub_rn(__fmul_rn(u, cs[i]), __fmul_rn(w, sn[i]));
-      x[2 * i + 1] = __fadd_rn(__fmul_rn(w, cs[i]), __fmul_rn(u, sn[i]));
+      x[2 * i] = __fsub_rn(__fmul_rn(u, t.cs[i]), __fmul_rn(w, t.sn[i]));
+      x[2 * i + 1] = __fadd_rn(__fmul_rn(w, t.cs[i]), __fmul_rn(u, t.sn[i]));
     }
   } else {
-    const bool low = 8 * c < half;
-    const int j = low ? 8 * c : 8 * c - half;
-    float y[8], cs[8], sn[8];
-    load8(row + (low ? 8 * c + half : j), y);
-    load8(a.cosT + at + j, cs);
-    load8(a.sinT + at + j, sn);
+    float y[8];
+    other.get(y);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float u = __fmul_rn(x[i], cs[i]), w = __fmul_rn(y[i], sn[i]);
-      x[i] = low ? __fsub_rn(u, w) : __fadd_rn(u, w);
-    }
+    for (int i = 0; i < 8; ++i) x[i] = __fadd_rn(__fmul_rn(x[i], t.cs[i]), __fmul_rn(y[i], t.sn[i]));
   }
 }
 
@@ -94,18 +135,17 @@ __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
   return r;
 }
-// Codes of 8 values under the scale 2^e (inv = 2^-e); all finite ones are at most 448 * 2^e.
-__device__ __forceinline__ uint2 codes8(const float (&x)[8], float inv) {
-  uint32_t h[4];
+// Codes of 8 values under the scale 2^e (inv = 2^-e); all finite ones are at most 448 * 2^e, unless
+// `special`: then those that no scale holds become NaN (a NaN does by itself).
+__device__ __forceinline__ uint2 codes8(const float (&x)[8], float inv, bool special) {
+  float y[8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float y[2];
+  for (int i = 0; i < 8; ++i) y[i] = x[i] * inv;
+  if (special)
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
-      y[k] = fabsf(x[2 * i + k]) < VALUE_LIMIT ? x[2 * i + k] * inv : __uint_as_float(0x7fffffffu);
-    h[i] = e4m3x2(y[0], y[1]);
-  }
-  return make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
+    for (int i = 0; i < 8; ++i)
+      if (!(fabsf(x[i]) < VALUE_LIMIT)) y[i] = __uint_as_float(0x7fffffffu);
+  return make_uint2(e4m3x2(y[0], y[1]) | e4m3x2(y[2], y[3]) << 16, e4m3x2(y[4], y[5]) | e4m3x2(y[6], y[7]) << 16);
 }
 // Codes multiplied by f (a power of two) and rounded again; NaN stays NaN.
 __device__ __forceinline__ uint32_t rescale2(uint32_t two, float f) {
@@ -121,10 +161,11 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t w, float f) {
 // ONE: one token a sequence.  D / 8 lanes per row; a warp takes one (block, head) of up to 16 rows,
 // or, with ONE, 32 / (D / 8) of them with one row each.
 template <typename T, int D, bool ONE>
-__global__ void __launch_bounds__(32 * AP_WARPS) paged_append_kernel(AppendArgs a) {
-  constexpr int LPR = D / 8, RPI = 32 / LPR, IT = ONE ? 1 : BLK / RPI;
+__global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendArgs a) {
+  constexpr int LPR = D / 8, RPI = 32 / LPR, IT = ONE ? 1 : BLK / RPI, QH = ONE ? 1 : AP_QH;
   const int lane = threadIdx.x & 31, c = lane % LPR, sub = lane / LPR;
-  const int slots = 2 * a.pool.H + a.HQ;
+  // a slot: a head of K or of V, or QH heads of q, which share their positions' cosines and sines
+  const int slots = 2 * a.pool.H + (a.HQ + QH - 1) / QH;
   const int warp = blockIdx.x * AP_WARPS + (threadIdx.x >> 5);
   int task = ONE ? warp * RPI + sub : warp;
   const bool live = task < a.tasks;                 // (a whole row's lanes agree; all stay for the shuffles)
@@ -164,21 +205,37 @@ __global__ void __launch_bounds__(32 * AP_WARPS) paged_append_kernel(AppendArgs 
   if (!ONE && !some) return;                        // warp-uniform
 
   if (slot >= 2 * a.pool.H) {                       // ------------------------------ queries
-    const int h = slot - 2 * a.pool.H;
-#pragma unroll
+    const int h0 = (slot - 2 * a.pool.H) * QH;
+    const Lane n = lane_of(a, c, true);
+    int pos = ONE ? p0 : p0 + sub;
+    const long long tok = t.first + (pos - t.len);
+    const T* from = static_cast<const T*>(a.q) + tok * a.q_ts + h0 * a.q_hs;
+    const float *cosR = a.cosT + (long long)pos * (a.rot >> 1) + n.angle, *sinR = a.sinT + (cosR - a.cosT);
+    bf16* to = a.q_out + (tok * a.HQ + h0) * D + n.own;
+#pragma unroll 1
     for (int it = 0; it < IT; ++it) {
-      const int pos = ONE ? p0 : p0 + it * RPI + sub;
       if (pos < end) {
-        const long long tok = t.first + (pos - t.len);
-        float x[8];
-        load_rotated(a, static_cast<const T*>(a.q) + tok * a.q_ts + h * a.q_hs, c, pos, x);
-        uint4 o;
-        o.x = pack_bf16(x[0], x[1]);
-        o.y = pack_bf16(x[2], x[3]);
-        o.z = pack_bf16(x[4], x[5]);
-        o.w = pack_bf16(x[6], x[7]);
-        *reinterpret_cast<uint4*>(a.q_out + (tok * a.HQ + h) * D + 8 * c) = o;
+        const Turn turn = turn_of(a, n, cosR, sinR);
+        Raw<T> own[QH], other[QH];
+#pragma unroll
+        for (int e = 0; e < QH; ++e) {
+          const T* row = from + (h0 + e < a.HQ ? e * a.q_hs : 0);
+          own[e].load(row + n.own);
+          other[e].load(row + n.other);
+        }
+#pragma unroll
+        for (int e = 0; e < QH; ++e) {
+          float x[8];
+          rotated(a, n, turn, own[e], other[e], x);
+          const uint4 o = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+          if (h0 + e < a.HQ) *reinterpret_cast<uint4*>(to + e * D) = o;
+        }
       }
+      pos += RPI;
+      from += RPI * a.q_ts;
+      cosR += RPI * (a.rot >> 1);
+      sinR += RPI * (a.rot >> 1);
+      to += (long long)RPI * a.HQ * D;
     }
     if (!ONE) return;
   }
@@ -195,23 +252,38 @@ __global__ void __launch_bounds__(32 * AP_WARPS) paged_append_kernel(AppendArgs 
   // one lane reads the block's scale and writes it
   const int lead = ONE ? lane - c : 0;
   float was = lane == lead && id >= 0 && head > 0 ? *scale : 0.f;
-  float x[IT][8], amax = 0.f;
+  const Lane n = lane_of(a, c, !is_v);
+  // The rows are read twice, for the largest value and for the codes: kept between, they would
+  // take the registers of half the warps, whose loads are what the first pass waits for.
+  const int pos0 = ONE ? p0 : p0 + sub;
+  const T* const from = src + (t.first + (pos0 - t.len)) * ts;
+  const long long angle0 = (long long)pos0 * (a.rot >> 1) + n.angle;
+  auto read = [&](int it, float (&x)[8]) {
+    const T* row = from + it * RPI * ts;
+    const long long at = angle0 + it * RPI * (a.rot >> 1);
+    Raw<T> own, other;
+    own.load(row + n.own);
+    other.load(row + n.other);
+    rotated(a, n, turn_of(a, n, a.cosT + at, a.sinT + at), own, other, x);
+  };
+  auto largest = [&](float limit) {
+    float m = 0.f;
+    if (id >= 0)
+#pragma unroll 2
+      for (int it = 0; it < IT; ++it)
+        if (pos0 + it * RPI < end) {
+          float x[8];
+          read(it, x);
 #pragma unroll
-  for (int it = 0; it < IT; ++it) {
-    const int pos = ONE ? p0 : p0 + it * RPI + sub;
-    if (id >= 0 && pos < end) {
-      const T* row = src + (t.first + (pos - t.len)) * ts;
-      if (is_v) load8(row + 8 * c, x[it]);
-      else load_rotated(a, row, c, pos, x[it]);
+          for (int i = 0; i < 8; ++i) m = fmaxf(m, limit > 0.f && !(fabsf(x[i]) < limit) ? 0.f : fabsf(x[i]));
+        }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float y = fabsf(x[it][i]);
-        amax = fmaxf(amax, y < VALUE_LIMIT ? y : 0.f);
-      }
-    }
-  }
-#pragma unroll
-  for (int o = ONE ? LPR / 2 : 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+    for (int o = ONE ? LPR / 2 : 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    return m;
+  };
+  float amax = largest(0.f);                        // (a NaN is no maximum)
+  const bool special = !(amax < VALUE_LIMIT);       // values that no scale holds: not counted
+  if (__any_sync(0xffffffffu, special)) amax = largest(VALUE_LIMIT);
   was = __shfl_sync(0xffffffffu, was, lead);
   if (id < 0) return;
   unsigned char* rows = (is_v ? a.pool.v : a.pool.k) + (at + (row0 - head)) * D;
@@ -231,18 +303,21 @@ __global__ void __launch_bounds__(32 * AP_WARPS) paged_append_kernel(AppendArgs 
     }
   }
   const float inv = 1.f / sc;                       // exact: sc is a power of two
-#pragma unroll
-  for (int it = 0; it < IT; ++it) {
-    const int pos = ONE ? p0 : p0 + it * RPI + sub;
-    if (pos < end) *reinterpret_cast<uint2*>(rows + (head + (pos - p0)) * D + 8 * c) = codes8(x[it], inv);
-  }
+  unsigned char* to = rows + (head + (pos0 - p0)) * D + n.own;
+#pragma unroll 2
+  for (int it = 0; it < IT; ++it)
+    if (pos0 + it * RPI < end) {
+      float x[8];
+      read(it, x);
+      *reinterpret_cast<uint2*>(to + it * RPI * D) = codes8(x, inv, special);
+    }
   if (lane == lead) *scale = sc;
 }
 
 template <typename T, int D>
 cudaError_t launch(AppendArgs& a, cudaStream_t stream) {
   const bool one = a.b.starts == nullptr;
-  const long long tasks = (2 * a.pool.H + a.HQ) * (one ? (long long)a.b.n_seq : a.b.n_tokens / BLK + 2ll * a.b.n_seq);
+  const long long tasks = (2 * a.pool.H + (one ? a.HQ : (a.HQ + AP_QH - 1) / AP_QH)) * (one ? (long long)a.b.n_seq : a.b.n_tokens / BLK + 2ll * a.b.n_seq);
   if (tasks > INT32_MAX - 32 * AP_WARPS) return cudaErrorInvalidValue;   // (refused before)
   a.tasks = (int)tasks;
   const int per_block = AP_WARPS * (one ? 32 / (D / 8) : 1), grid = (a.tasks + per_block - 1) / per_block;

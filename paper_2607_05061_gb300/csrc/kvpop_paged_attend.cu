@@ -41,7 +41,11 @@ namespace {
 
 using namespace paged;
 
+// What the two ends of a unit cost, in blocks (us at 0, 16, 32, 64: 40 ragged sequences of up to
+// 20000 tokens 82, 71, 66, 67; 128 of 200 to 1500 70, 53, 51, 53; 64 of 8192 170, 169, 170, 172).
+constexpr int AT_ENDS = 32;
 constexpr int AT_SHORT = 48;           // blocks of a unit that one CTA takes whole
+constexpr int AT_CTAS = 2;             // resident per SM: one streams while the other joins its rows
 constexpr int AT_MAX_ROWS = 32;        // query rows of a unit at most
 constexpr float AT_OFF = 7.f, AT_STEP = 8.f;
 
@@ -49,7 +53,7 @@ constexpr float AT_OFF = 7.f, AT_STEP = 8.f;
 // c ^ (r mod 8) of its 128 bytes (d = 128), or c ^ (r / 2 mod 4) of its 64 (d = 64).
 template <int D, int W>
 struct Ring {
-  static constexpr int BLOCK = 2 * BLK * D, ST = (W == 12 ? 3 : 5) * (128 / D);
+  static constexpr int BLOCK = 2 * BLK * D, ST = (W == 6 ? 3 : 5) * (128 / D);
   static constexpr int OFF_ACC = W * ST * BLOCK;                       // a warp's 8 rows: 8 (d + 4) floats
   static constexpr int OFF_Q = OFF_ACC + W * 8 * (D + 4) * 4;          // 4 groups of query operands
   static constexpr int BYTES = OFF_Q + 4 * (D / 16) * 256;
@@ -116,10 +120,12 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
 }
 
 // Units of a sequence: H x row groups, each of `blocks` blocks (one at least, so that a row that
-// sees nothing is written too).
+// sees nothing is written too).  In the list a unit takes span() places: what its beginning and end
+// cost a CTA, in blocks, comes on top, and the places behind its blocks are empty.
 struct SeqUnits {
   int first, n, len, ctx, groups, blocks;
-  __device__ long long work(int H) const { return (long long)H * groups * blocks; }
+  __device__ int span() const { return blocks + AT_ENDS; }
+  __device__ long long work(int H) const { return (long long)H * groups * span(); }
 };
 template <int ROWS>
 __device__ __forceinline__ SeqUnits seq_units(const AttendArgs& a, int s) {
@@ -144,7 +150,7 @@ struct Unit {
   int s, h, row0, rows;                // sequence, KV head, rows of the sequence
   int tok0, rem0;                      // row0 = tok0 G + rem0
   int lim_hi;                          // its rows see at most 0 .. lim_hi
-  __device__ __forceinline__ long long end() const { return start + u.blocks; }
+  __device__ __forceinline__ long long end() const { return start + u.span(); }
 };
 // The unit that list position w lies in, from an earlier one (or from a sequence and its base).
 template <int ROWS>
@@ -153,9 +159,9 @@ __device__ __forceinline__ void seek(const AttendArgs& a, Unit& x, long long w) 
     x.base += x.u.work(a.pool.H);
     x.u = seq_units<ROWS>(a, ++x.s);
   }
-  const int unit = (int)div_pos(w - x.base, x.u.blocks), grp = unit / a.pool.H;
+  const int unit = (int)div_pos(w - x.base, x.u.span()), grp = unit / a.pool.H;
   x.h = unit - grp * a.pool.H;
-  x.start = x.base + (long long)unit * x.u.blocks;
+  x.start = x.base + (long long)unit * x.u.span();
   x.row0 = grp * ROWS;
   x.rows = min(ROWS, x.u.n * a.G - x.row0);
   x.tok0 = x.row0 / a.G;
@@ -187,7 +193,7 @@ __device__ __forceinline__ void write_out(const AttendArgs& a, const Unit& x, in
 }
 
 template <int D, int NT, int W, bool SPLIT>
-__global__ void __launch_bounds__(32 * W, 1) paged_attend_kernel(AttendArgs a) {
+__global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArgs a) {
   using R = Ring<D, W>;
   constexpr int ROWS = 8 * NT, KW = D / 16, VW = D / 32;   // words a lane holds of a K / V row
   constexpr int RS = 8 * (D + 4);                          // a warp's 8 rows in shared memory
@@ -258,42 +264,40 @@ __global__ void __launch_bounds__(32 * W, 1) paged_attend_kernel(AttendArgs a) {
     }
     seek<ROWS>(a, x, w0);
   }
-  if (x.u.blocks <= AT_SHORT && x.start < w0) w0 = x.end();
+  if (x.start < w0 && (x.u.blocks <= AT_SHORT || w0 >= x.start + x.u.blocks)) w0 = x.end();
   if (w0 >= w1) return;
   seek<ROWS>(a, x, w0);
   if (tid < W) aheadS[tid] = x;
   if (tid == 0) unitS[0] = x;
 
-  // ---- the warp's ring: blocks w0 + warp, w0 + warp + W, ...
+  // ---- the warp's ring: every W-th block of the part
   const uint32_t ring = smem_u32(sma) + warp * (R::ST * R::BLOCK);
-  const int count = (int)max((w1 - w0 - warp + W - 1) / W, 0ll);       // the warp's blocks
   // a lane copies the 16 bytes at 512 i + 16 lane of a block's K and of its V
   constexpr int RPI = 512 / D;
   const int r0 = lane / (D / 16), c0 = lane % (D / 16), put0 = R::chunk_at(r0, c0), put1 = R::chunk_at(r0 + RPI, c0);
-  int asked = 0, slot = 0;                                 // blocks asked for; the next one's slot,
-  int nt = (int)(w0 - x.start) + warp, stop = (int)min((long long)x.u.blocks, w1 - x.start);   // place, its unit's end,
+  bool more = true;                                        // the next block to ask for: its slot,
+  int slot = 0, nt = (int)(w0 - x.start) + warp, stop = (int)min((long long)x.u.blocks, w1 - x.start);   // place, its unit's end,
   int nh = x.h, seen = x.lim_hi, id = -1;                  // head, last position that is seen, and page
   const int32_t* row = a.b.table + (long long)x.s * a.b.table_stride;
   __syncthreads();
   auto look = [&] {
-    if (asked >= count) return;
-    if (nt >= stop) {
-      const long long w = w0 + warp + (long long)asked * W;
+    while (more && nt >= stop) {
       Unit y = aheadS[warp];
-      seek<ROWS>(a, y, w);
+      if (!(more = y.end() < w1)) break;
+      seek<ROWS>(a, y, y.end());
       __syncwarp();
       if (lane == 0) aheadS[warp] = y;
       __syncwarp();
-      nt = (int)(w - y.start);
+      nt -= stop;
       stop = (int)min((long long)y.u.blocks, w1 - y.start);
       nh = y.h;
       seen = y.lim_hi;
       row = a.b.table + (long long)y.s * a.b.table_stride;
     }
-    if (nt * BLK <= seen) id = __ldg(row + (nt * BLK >> a.pool.page_shift));
+    if (more && nt * BLK <= seen) id = __ldg(row + (nt * BLK >> a.pool.page_shift));
   };
   auto ask = [&] {
-    if (asked < count) {
+    if (more) {
       const int pos = nt * BLK;
       float* sc = &scaleS[warp][slot][0];
       if (pos <= seen && (unsigned)id < (unsigned)a.pool.n_pages) {
@@ -312,7 +316,6 @@ __global__ void __launch_bounds__(32 * W, 1) paged_attend_kernel(AttendArgs a) {
         sc[1] = -1.f;
       }
       nt += W;
-      ++asked;
       slot = slot + 1 == R::ST ? 0 : slot + 1;
       look();
     }
@@ -323,13 +326,13 @@ __global__ void __launch_bounds__(32 * W, 1) paged_attend_kernel(AttendArgs a) {
   for (int i = 0; i < R::ST; ++i) ask();
 
   int next = warp, done = 0, stage = 0, turn = 0;          // the warp's next block of the CTA's; blocks so far
-  for (long long w = w0; w < w1; turn ^= 1) {
+  for (long long w = w0; w < w1; turn ^= 1) {              // (never begins behind a unit's blocks)
     x = unitS[turn];
     seek<ROWS>(a, x, w);
     if (tid == 0) unitS[turn ^ 1] = x;                     // (read again behind the next barrier)
     const int ta = (int)(w - x.start), tb = (int)min((long long)x.u.blocks, w1 - x.start);
     const int lim_lo = min(x.u.len + x.tok0, x.u.ctx - 1), lim_hi = x.lim_hi;   // all rows see 0 .. lim_lo
-    w = x.start + tb;
+    w = x.end();
 
     // ---- query rows, each scaled by a power of two, and what that makes of the logits
     uint32_t qf[NT][KW][2];
@@ -682,19 +685,20 @@ cudaError_t launch(const AttendArgs& a, int grid, cudaStream_t stream) {
 }
 template <int D>
 cudaError_t launch_d(AttendArgs& a, int sms, long long rows, cudaStream_t stream) {
-  // (as many warps as the registers allow: 12 of 168, or 8 of 255)
   a.one = (a.G + (rows <= 8 ? 8 : rows <= 16 ? 16 : 32) - 1) / (rows <= 8 ? 8 : rows <= 16 ? 16 : 32);
-  if (rows <= 8) return a.out_f32 ? launch<D, 1, 12, true>(a, sms, stream) : launch<D, 1, 12, false>(a, sms, stream);
-  if (rows <= 16) return a.out_f32 ? launch<D, 2, 8, true>(a, sms, stream) : launch<D, 2, 8, false>(a, sms, stream);
-  return a.out_f32 ? launch<D, 4, 8, true>(a, sms, stream) : launch<D, 4, 8, false>(a, sms, stream);
+  // (as many warps as the registers allow: 2 x 6 of 168, or 2 x 4 of 255)
+  const int grid = AT_CTAS * sms;
+  if (rows <= 8) return a.out_f32 ? launch<D, 1, 6, true>(a, grid, stream) : launch<D, 1, 6, false>(a, grid, stream);
+  if (rows <= 16) return a.out_f32 ? launch<D, 2, 4, true>(a, grid, stream) : launch<D, 2, 4, false>(a, grid, stream);
+  return a.out_f32 ? launch<D, 4, 4, true>(a, grid, stream) : launch<D, 4, 4, false>(a, grid, stream);
 }
 
-size_t counter_bytes(int sms) { return ((size_t)sms * 4 + 255) / 256 * 256; }
+size_t counter_bytes(int sms) { return ((size_t)AT_CTAS * sms * 4 + 255) / 256 * 256; }
 
 }  // namespace
 
 size_t paged_attend_workspace(int sms) {
-  return counter_bytes(sms) + (size_t)sms * 2 * AT_MAX_ROWS * (128 + 2) * 4;
+  return counter_bytes(sms) + (size_t)AT_CTAS * sms * 2 * AT_MAX_ROWS * (128 + 2) * 4;
 }
 
 cudaError_t launch_paged_attend(const Pool& pool, const Batch& b, const void* q, long long q_ts, long long q_hs,
