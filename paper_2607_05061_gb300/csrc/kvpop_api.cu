@@ -1,5 +1,6 @@
 // Host side of the C ABI declared in include/kvpop.h: argument checks, device
 // memory, kernel launches.  No call throws or aborts; every failure is a status.
+#include <atomic>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -844,14 +845,36 @@ static paged::Batch paged_batch(const kvpop_paged_batch* b) {
   c.max_new = b->max_new;
   return c;
 }
-static int device_sms() {
-  int dev = 0, sms = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+// What every call needs of the current device, asked for once per device: its SMs (0 on failure)
+// and its error word of the cache-free calls.
+struct PagedDevice {
+  int sms = 0;
+  int32_t* err = nullptr;
+};
+static PagedDevice paged_device() {
+  static std::atomic<int> known_sms[64];
+  static std::atomic<int32_t*> known_err[64];
+  PagedDevice d;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) {
     cudaGetLastError();
-    return 0;
+    return d;
   }
-  return sms;
+  if (dev < 64 && (d.sms = known_sms[dev].load(std::memory_order_acquire)) > 0) {
+    d.err = known_err[dev].load(std::memory_order_relaxed);
+    return d;
+  }
+  d.sms = 0;
+  d.err = standalone_err();
+  if (!d.err || cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+    cudaGetLastError();
+    return PagedDevice{};
+  }
+  if (dev < 64) {
+    known_err[dev].store(d.err, std::memory_order_relaxed);
+    known_sms[dev].store(d.sms, std::memory_order_release);
+  }
+  return d;
 }
 
 kvpop_status kvpop_paged_append(const kvpop_paged_pool* pool, const kvpop_paged_batch* batch,
@@ -875,15 +898,17 @@ kvpop_status kvpop_paged_append(const kvpop_paged_pool* pool, const kvpop_paged_
       (q && (!rows_aligned(q, esz) || !aligned16(q_out))) ||
       (rot_dim > 0 && (!aligned16(cos_dev) || !aligned16(sin_dev))))
     return KVPOP_ERR_ALIGN;
+  const PagedDevice dev = paged_device();
+  if (dev.sms <= 0) return KVPOP_ERR_CUDA;
   return from_cuda(NOTE(launch_paged_append(
       paged_pool(pool), paged_batch(batch), q ? q->data_dev : nullptr, q ? q->token_stride : 0,
       q ? q->head_stride : 0, n_q_heads, k->data_dev, k->token_stride, k->head_stride, v->data_dev,
       v->token_stride, v->head_stride, dtype, cos_dev, sin_dev, rot_dim, max_pos, interleaved, q_out,
-      standalone_err(), stream)));
+      dev.err, stream)));
 }
 
 size_t kvpop_paged_workspace_bytes(void) {
-  const int sms = device_sms();
+  const int sms = paged_device().sms;
   return sms > 0 ? paged_attend_workspace(sms) : 0;
 }
 
@@ -898,12 +923,12 @@ kvpop_status kvpop_paged_attend(const kvpop_paged_pool* pool, const kvpop_paged_
   if (!paged_aligned(pool, batch) || !rows_aligned(q, 2) || !aligned16(out) || !aligned4(lse) ||
       (reinterpret_cast<uintptr_t>(workspace) & 255u))
     return KVPOP_ERR_ALIGN;
-  const int sms = device_sms();
-  if (sms <= 0) return KVPOP_ERR_CUDA;
-  if (workspace_bytes < paged_attend_workspace(sms)) return KVPOP_ERR_INVALID_ARG;
+  const PagedDevice dev = paged_device();
+  if (dev.sms <= 0) return KVPOP_ERR_CUDA;
+  if (workspace_bytes < paged_attend_workspace(dev.sms)) return KVPOP_ERR_INVALID_ARG;
   return from_cuda(NOTE(launch_paged_attend(paged_pool(pool), paged_batch(batch), q->data_dev, q->token_stride,
                                             q->head_stride, n_q_heads, out, out_dtype == KVPOP_F32, lse, workspace,
-                                            sms, standalone_err(), stream)));
+                                            dev.sms, dev.err, stream)));
 }
 
 kvpop_status kvpop_decode_ingest(kvpop_cache* c, const void* q, const void* k, const void* v,

@@ -9,6 +9,8 @@
 
 #include <cuda_fp16.h>
 
+#include <atomic>
+
 #include "kvpop_internal.cuh"
 
 namespace kvpop {
@@ -82,6 +84,20 @@ __device__ __forceinline__ int context(const Batch& b, const Pool& p, const SeqT
 constexpr int LONG_ROWS = 64;
 __device__ __forceinline__ bool long_rows(const SeqTokens& t, int G) {
   return t.len >= 0 && (long long)t.n * G > LONG_ROWS;
+}
+
+// raise_smem_limit once per device (`done`: one bit each, of one kernel): it takes longer on the
+// host than a launch.
+template <typename K>
+inline cudaError_t raise_smem_limit_once(std::atomic<unsigned long long>& done, K* func, size_t need) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
+  if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
+  e = raise_smem_limit(func, need);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+  return e;
 }
 
 }  // namespace paged

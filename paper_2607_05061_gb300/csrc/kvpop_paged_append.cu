@@ -35,13 +35,24 @@ struct AppendArgs {
   int tasks, HQ, rot, max_pos, interleaved;
 };
 
+// Loads that no store of this kernel can change.  (As volatile assembly they stay behind
+// griddepcontrol.wait, and in the order in which they are written.)
+__device__ __forceinline__ uint4 ld16(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ float4 ld16f(const float* p) {
+  const uint4 v = ld16(p);
+  return make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
+}
 // 8 values as they lie in memory
 template <typename T>
 struct Raw;
 template <>
 struct Raw<bf16> {
   uint4 w;
-  __device__ __forceinline__ void load(const bf16* p) { w = __ldg(reinterpret_cast<const uint4*>(p)); }
+  __device__ __forceinline__ void load(const bf16* p) { w = ld16(p); }
   __device__ __forceinline__ void get(float (&x)[8]) const {
     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -55,8 +66,8 @@ template <>
 struct Raw<float> {
   float4 a, b;
   __device__ __forceinline__ void load(const float* p) {
-    a = __ldg(reinterpret_cast<const float4*>(p));
-    b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+    a = ld16f(p);
+    b = ld16f(p + 4);
   }
   __device__ __forceinline__ void get(float (&x)[8]) const {
     x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
@@ -90,8 +101,8 @@ __device__ __forceinline__ Turn turn_of(const AppendArgs& a, const Lane& n, cons
   if (!n.turned) return t;
   Raw<float> cs, sn;
   if (a.interleaved) {
-    cs.a = cs.b = __ldg(reinterpret_cast<const float4*>(cosR));
-    sn.a = sn.b = __ldg(reinterpret_cast<const float4*>(sinR));
+    cs.a = cs.b = ld16f(cosR);
+    sn.a = sn.b = ld16f(sinR);
   } else {
     cs.load(cosR);
     sn.load(sinR);
@@ -164,6 +175,8 @@ template <typename T, int D, bool ONE>
 __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendArgs a) {
   constexpr int LPR = D / 8, RPI = 32 / LPR, IT = ONE ? 1 : BLK / RPI, QH = ONE ? 1 : AP_QH;
   const int lane = threadIdx.x & 31, c = lane % LPR, sub = lane / LPR;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   // a slot: a head of K or of V, or QH heads of q, which share their positions' cosines and sines
   const int slots = 2 * a.pool.H + (a.HQ + QH - 1) / QH;
   const int warp = blockIdx.x * AP_WARPS + (threadIdx.x >> 5);
@@ -321,9 +334,17 @@ cudaError_t launch(AppendArgs& a, cudaStream_t stream) {
   if (tasks > INT32_MAX - 32 * AP_WARPS) return cudaErrorInvalidValue;   // (refused before)
   a.tasks = (int)tasks;
   const int per_block = AP_WARPS * (one ? 32 / (D / 8) : 1), grid = (a.tasks + per_block - 1) / per_block;
-  if (one) paged_append_kernel<T, D, true><<<(unsigned)grid, 32 * AP_WARPS, 0, stream>>>(a);
-  else paged_append_kernel<T, D, false><<<(unsigned)grid, 32 * AP_WARPS, 0, stream>>>(a);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3(32 * AP_WARPS);
+  cfg.stream = stream;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return one ? cudaLaunchKernelEx(&cfg, paged_append_kernel<T, D, true>, a)
+             : cudaLaunchKernelEx(&cfg, paged_append_kernel<T, D, false>, a);
 }
 
 }  // namespace

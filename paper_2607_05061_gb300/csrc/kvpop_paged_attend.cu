@@ -294,7 +294,7 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
       seen = y.lim_hi;
       row = a.b.table + (long long)y.s * a.b.table_stride;
     }
-    if (more && nt * BLK <= seen) id = __ldg(row + (nt * BLK >> a.pool.page_shift));
+    if (more && nt * BLK <= seen) id = row[nt * BLK >> a.pool.page_shift];
   };
   auto ask = [&] {
     if (more) {
@@ -669,7 +669,8 @@ template <int D, int NT, int W, bool SPLIT>
 cudaError_t launch(const AttendArgs& a, int grid, cudaStream_t stream) {
   using R = Ring<D, W>;
   auto k = paged_attend_kernel<D, NT, W, SPLIT>;
-  const cudaError_t e = raise_smem_limit(k, R::BYTES);
+  static std::atomic<unsigned long long> raised{0};
+  const cudaError_t e = raise_smem_limit_once(raised, k, R::BYTES);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid);

@@ -477,7 +477,8 @@ template <int D, bool SPLIT>
 cudaError_t launch(const PromptArgs& a, long long places, cudaStream_t stream) {
   auto k = paged_prompt_kernel<D, SPLIT>;
   const size_t smem = PL<D>::BYTES;
-  const cudaError_t e = raise_smem_limit(k, smem);
+  static std::atomic<unsigned long long> raised{0};
+  const cudaError_t e = raise_smem_limit_once(raised, k, smem);
   if (e != cudaSuccess) return e;
   k<<<(unsigned)(places * a.pool.H), PP_THREADS, smem, stream>>>(a);
   return cudaGetLastError();

@@ -17,21 +17,28 @@ One decode step of a batch::
 from __future__ import annotations
 
 import ctypes
+import struct
 from typing import List, Optional, Sequence
 
 import torch
 
-from .kvpop import (KVPOP_BF16, KVPOP_F32, _ck, _ptr, _stream, kvpop_paged_append, kvpop_paged_attend,
-                    kvpop_paged_batch, kvpop_paged_pool, kvpop_paged_workspace_bytes, kvpop_rows)
+from .kvpop import (KVPOP_BF16, KVPOP_F32, _ck, _ptr, _raw_stream, _stream, kvpop_paged_append,
+                    kvpop_paged_attend, kvpop_paged_batch, kvpop_paged_pool, kvpop_paged_workspace_bytes, kvpop_rows)
 
 BLOCK = 16               # tokens that share a scale
 _F8 = torch.float8_e4m3fn
 _CODES = {torch.float32: KVPOP_F32, torch.bfloat16: KVPOP_BF16}
+# the C structs kvpop_paged_batch and kvpop_rows as bytes: a call of a few tokens takes less time on
+# the GPU than filling ctypes structures takes on the host
+_batch_bytes, _rows_bytes = struct.Struct("PPPqiiii").pack, struct.Struct("Pqq").pack
+assert struct.calcsize("PPPqiiii") == ctypes.sizeof(kvpop_paged_batch) and \
+    struct.calcsize("Pqq") == ctypes.sizeof(kvpop_rows)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _want(what, name, t, dtype, shape):
     """Refuses a tensor that a call would read or write past its end or as another type."""
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{what}: {name} is {t.dtype} {tuple(t.shape)} (strides {tuple(t.stride())}), not "
                          f"contiguous {dtype} {tuple(shape)}")
 
@@ -61,6 +68,9 @@ class PagedCache:
                 workspace = torch.zeros(int(kvpop_paged_workspace_bytes()), dtype=torch.uint8, device=self.device)
                 torch.cuda.current_stream().synchronize()      # zero for whatever stream comes first
         self.workspace = workspace
+        self._index = k_pages.get_device()
+        self._pool_ptr = ctypes.addressof(self._pool)
+        self._work = (0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
 
     @classmethod
     def empty(cls, n_pages: int, n_kv_heads: int, head_dim: int, page: int = 64, device="cuda",
@@ -71,37 +81,42 @@ class PagedCache:
         return cls(*pages, *scales, workspace=workspace)
 
     # ------------------------------------------------------------------ arguments
-    def _here(self, what, **tensors):
-        for name, t in tensors.items():
-            if t is not None and t.device != self.device:
-                raise ValueError(f"{what}: {name} is on {t.device}, the cache on {self.device}")
-        if self.device.type != "cuda" or self.device.index != torch.cuda.current_device():
+    def _here(self, what, stream, *tensors):
+        """The stream's handle, once every tensor is on the cache's device and that is the current one."""
+        at = self._index
+        for t in tensors:
+            if t is not None and t.get_device() != at:
+                raise ValueError(f"{what}: a tensor is on {t.device}, the cache on {self.device}")
+        if at < 0 or _current_device() != at:
             raise ValueError(f"{what}: the cache is on {self.device}, which is not the current CUDA device")
+        return _raw_stream(at) if stream is None and _raw_stream is not None else _stream(stream)
 
-    def _batch(self, what, table, lens, starts, n_tokens, max_new):
-        n = lens.shape[0] if lens.dim() == 1 else -1
+    @staticmethod
+    def _batch(what, table, lens, starts, n_tokens, max_new):
+        shape = table.shape
+        n, stride = shape[0], table.stride()
+        if table.dtype is not torch.int32 or len(shape) != 2 or shape[1] < 1 or stride[1] != 1 or \
+                (n > 1 and stride[0] < shape[1]):
+            raise ValueError(f"{what}: table is {table.dtype} {tuple(shape)} (strides {tuple(stride)}), "
+                             f"not {torch.int32} (sequences, pages) with neighbouring entries")
         _want(what, "lens", lens, torch.int32, (n,))
-        if table.dtype != torch.int32 or table.dim() != 2 or table.shape[0] != n or table.shape[1] < 1 or \
-                table.stride(1) != 1 or (n > 1 and table.stride(0) < table.shape[1]):
-            raise ValueError(f"{what}: table is {table.dtype} {tuple(table.shape)} (strides {tuple(table.stride())}), "
-                             f"not {torch.int32} ({n}, pages) with neighbouring entries")
-        if starts is not None:
+        if starts is None:
+            if n_tokens != n:
+                raise ValueError(f"{what}: {n_tokens} tokens of {n} sequences need starts")
+            first, most = 0, 1
+        else:
             _want(what, "starts", starts, torch.int32, (n + 1,))
-        elif n_tokens != n:
-            raise ValueError(f"{what}: {n_tokens} tokens of {n} sequences need starts")
-        if max_new is None:
-            max_new = 1 if starts is None else max(n_tokens, 1)
-        stride = max(table.stride(0), table.shape[1])
-        return kvpop_paged_batch(_ptr(table), _ptr(lens), _ptr(starts), stride, table.shape[1], n, n_tokens,
-                                 max(int(max_new), 1))
+            first, most = starts.data_ptr(), max(n_tokens if max_new is None else min(max_new, 0x7fffffff), 1)
+        return _batch_bytes(table.data_ptr(), lens.data_ptr(), first, max(stride[0], shape[1]), shape[1], n, n_tokens,
+                            most)
 
     def _rows(self, what, name, t, dtype, n_tokens, heads):
-        if t.dtype != dtype or t.dim() != 3 or t.shape[0] != n_tokens or t.shape[2] != self.d or \
-                (heads is not None and t.shape[1] != heads) or t.shape[1] < 1 or t.stride(2) != 1 or \
-                t.stride(0) < 0 or t.stride(1) < 0:
-            raise ValueError(f"{what}: {name} is {t.dtype} {tuple(t.shape)} (strides {tuple(t.stride())}), not {dtype} "
+        shape, stride = t.shape, t.stride()
+        if t.dtype is not dtype or len(shape) != 3 or shape[0] != n_tokens or shape[2] != self.d or \
+                (shape[1] < 1 if heads is None else shape[1] != heads) or stride[2] != 1 or stride[0] < 0 or stride[1] < 0:
+            raise ValueError(f"{what}: {name} is {t.dtype} {tuple(shape)} (strides {tuple(stride)}), not {dtype} "
                              f"({n_tokens}, {heads or 'heads'}, {self.d}) with contiguous rows")
-        return kvpop_rows(_ptr(t), t.stride(0), t.stride(1))
+        return _rows_bytes(t.data_ptr(), stride[0], stride[1])
 
     # ------------------------------------------------------------------ calls
     def append(self, table, lens, q, k, v, cos=None, sin=None, starts=None, max_new: Optional[int] = None,
@@ -111,36 +126,39 @@ class PagedCache:
         (q, k and v of one type, bf16 or fp32, any token and head strides of 16 bytes).  ``table
         [n][pages]`` int32, ``lens [n]`` int32 tokens held before (-1: idle), ``starts [n + 1]``
         int32 first token of each sequence (none: one each).  Returns the rotated queries, bf16."""
-        what = "PagedCache.append"
-        n_tokens = k.shape[0]
-        if k.dtype not in _CODES:
-            raise ValueError(f"{what}: k is {k.dtype}, not bf16 or fp32")
-        kr = self._rows(what, "k", k, k.dtype, n_tokens, self.H)
-        vr = self._rows(what, "v", v, k.dtype, n_tokens, self.H)
-        qr, heads = None, 0
+        what, dtype, n_tokens = "PagedCache.append", k.dtype, k.shape[0]
+        code = _CODES.get(dtype)
+        if code is None:
+            raise ValueError(f"{what}: k is {dtype}, not bf16 or fp32")
+        kr = self._rows(what, "k", k, dtype, n_tokens, self.H)
+        vr = self._rows(what, "v", v, dtype, n_tokens, self.H)
+        qr, heads, to = None, 0, None
         if q is not None:
-            qr, heads = self._rows(what, "q", q, k.dtype, n_tokens, None), q.shape[1]
+            qr, heads = self._rows(what, "q", q, dtype, n_tokens, None), q.shape[1]
             if q_out is None:
                 q_out = torch.empty((n_tokens, heads, self.d), dtype=torch.bfloat16, device=k.device)
             _want(what, "q_out", q_out, torch.bfloat16, (n_tokens, heads, self.d))
+            to = q_out.data_ptr()
         elif q_out is not None:
             raise ValueError(f"{what}: q_out without q")
         rot = positions = 0
-        if (cos is None) != (sin is None):
-            raise ValueError(f"{what}: cos and sin come together")
-        if cos is not None:
+        cos_ptr = sin_ptr = None
+        if cos is not None and sin is not None:
             positions, rot = cos.shape[0], 2 * cos.shape[1]
             if positions < 1 or rot < 16 or rot > self.d or rot % 16:
                 raise ValueError(f"{what}: cos is {tuple(cos.shape)}: 2 * {rot // 2} values of {self.d} cannot be "
                                  "rotated (a multiple of 16 can)")
             _want(what, "cos", cos, torch.float32, (positions, rot // 2))
             _want(what, "sin", sin, torch.float32, (positions, rot // 2))
+            cos_ptr, sin_ptr = cos.data_ptr(), sin.data_ptr()
+        elif cos is not None or sin is not None:
+            raise ValueError(f"{what}: cos and sin come together")
         batch = self._batch(what, table, lens, starts, n_tokens, max_new)
-        self._here(what, table=table, lens=lens, starts=starts, q=q, k=k, v=v, cos=cos, sin=sin, q_out=q_out)
-        _ck(kvpop_paged_append(ctypes.byref(self._pool), ctypes.byref(batch),
-                               None if qr is None else ctypes.byref(qr), heads, ctypes.byref(kr), ctypes.byref(vr),
-                               _CODES[k.dtype], _ptr(cos), _ptr(sin), rot, positions, int(bool(interleaved)),
-                               _ptr(q_out), _stream(stream)), "kvpop_paged_append")
+        at = self._here(what, stream, table, lens, starts, q, k, v, cos, sin, q_out)
+        status = kvpop_paged_append(self._pool_ptr, batch, qr, heads, kr, vr, code, cos_ptr, sin_ptr, rot, positions,
+                                    1 if interleaved else 0, to, at)
+        if status != 0:
+            _ck(status, "kvpop_paged_append")
         return q_out
 
     def attend(self, table, lens, q, starts=None, max_new: Optional[int] = None, out=None, lse=None,
@@ -150,14 +168,14 @@ class PagedCache:
         came.  Returns (out fp32 or bf16 ``[tokens][H * G][d]``, natural-log normalisers
         ``[tokens][H * G]`` or None)."""
         what = "PagedCache.attend"
-        n_tokens = q.shape[0]
+        n_tokens, heads = q.shape[0], q.shape[1]
         qr = self._rows(what, "q", q, torch.bfloat16, n_tokens, None)
-        heads = q.shape[1]
         if heads % self.H:
             raise ValueError(f"{what}: {heads} query heads over {self.H} KV heads")
         if out is None:
             out = torch.empty((n_tokens, heads, self.d), dtype=out_dtype, device=q.device)
-        if out.dtype not in _CODES:
+        code = _CODES.get(out.dtype)
+        if code is None:
             raise ValueError(f"{what}: out is {out.dtype}, not fp32 or bf16")
         _want(what, "out", out, out.dtype, (n_tokens, heads, self.d))
         if lse is None and want_lse:
@@ -165,10 +183,11 @@ class PagedCache:
         if lse is not None:
             _want(what, "lse", lse, torch.float32, (n_tokens, heads))
         batch = self._batch(what, table, lens, starts, n_tokens, max_new)
-        self._here(what, table=table, lens=lens, starts=starts, q=q, out=out, lse=lse)
-        _ck(kvpop_paged_attend(ctypes.byref(self._pool), ctypes.byref(batch), ctypes.byref(qr), heads, _ptr(out),
-                               _CODES[out.dtype], _ptr(lse), _ptr(self.workspace), self.workspace.numel(),
-                               _stream(stream)), "kvpop_paged_attend")
+        at = self._here(what, stream, table, lens, starts, q, out, lse)
+        status = kvpop_paged_attend(self._pool_ptr, batch, qr, heads, out.data_ptr(), code,
+                                    None if lse is None else lse.data_ptr(), *self._work, at)
+        if status != 0:
+            _ck(status, "kvpop_paged_attend")
         return out, lse
 
 
