@@ -26,8 +26,11 @@ using namespace paged;
 using namespace tc05;
 
 constexpr int PP_HALF = 128, PP_ROWS = 2 * PP_HALF, PP_KEYS = 128;
-constexpr int PP_MMA_WARP = 8, PP_CONV = 4;              // warps 0-7: softmax, 8: MMA, 9-12: converters
-constexpr int PP_THREADS = 32 * (PP_MMA_WARP + 1 + PP_CONV);
+constexpr int PP_MMA_WARP = 8, PP_CONV_WARP = 12, PP_CONV = 4;   // warps 0-7: softmax, 8: MMA, 12-15: converters
+constexpr int PP_THREADS = 32 * (PP_CONV_WARP + PP_CONV);
+// Registers of a thread: at launch, and of the softmax, MMA and converter warpgroups.
+constexpr int PP_REGS = 128, PP_REGS_ROW = 200, PP_REGS_MMA = 56, PP_REGS_CONV = 56;
+static_assert(PP_THREADS * PP_REGS <= 65536 && 2 * PP_REGS_ROW + PP_REGS_MMA + PP_REGS_CONV <= 4 * PP_REGS, "");
 constexpr int PP_RING = 5;
 constexpr int PP_TMEM = 512;                             // O_h: 128 h; S_h: 256 + 128 h
 constexpr float PP_OFF = 7.f, PP_STEP = 8.f;
@@ -56,8 +59,9 @@ template <int D>
 struct PL {
   static constexpr int QB = PP_HALF * D * 2, KB = PP_KEYS * D * 2;
   static constexpr int OFF_RING = 2 * QB, OFF_BAR = OFF_RING + PP_RING * KB;
-  static constexpr int OFF_TMEM = OFF_BAR + 8 * PB_N, OFF_NAN = OFF_TMEM + 8;
-  static constexpr int BYTES = OFF_NAN + 4 * PP_NANW;
+  static constexpr int OFF_TMEM = OFF_BAR + 8 * PB_N, OFF_NAN = (OFF_TMEM + 4 + 15) / 16 * 16;
+  static constexpr int OFF_SCALE = OFF_NAN + 4 * PP_NANW;  // [8 warps][2][24] key scales, value exponents, 2^-those
+  static constexpr int BYTES = OFF_SCALE + 8 * 2 * 24 * 4;
   static constexpr int OUT_WARP = 32 * D * 4;            // a warp's finished rows, in the ring
   static_assert(8 * OUT_WARP <= OFF_BAR, "");
 };
@@ -90,6 +94,20 @@ __device__ __forceinline__ bool has_nan(uint32_t w) {   // an e4m3 NaN (0x7f, 0x
 __device__ __forceinline__ uint32_t drop_nan(uint32_t w) {
   const uint32_t x = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
   return w & ~((x >> 7) * 255u);
+}
+
+// Registers of a thread from here on, for a whole warpgroup.
+template <int N, bool MORE>
+__device__ __forceinline__ void set_registers() {
+  if (MORE) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+  else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+
+// (volatile: read where it is used, not kept in registers that a row of logits needs)
+__device__ __forceinline__ float2 lds2(uint32_t p) {
+  float2 v;
+  asm volatile("ld.volatile.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(p));
+  return v;
 }
 
 template <int D, bool SPLIT>
@@ -183,10 +201,11 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
   float m = -INFINITY, l = 0.f;
   bool ok = true;
 
-  if (warp > PP_MMA_WARP) {
+  if (warp >= PP_CONV_WARP) {
     // ---------------------------------------------------------------- converters
+    set_registers<PP_REGS_CONV, false>();
     constexpr int LPR = D / 16, RPI = 32 / LPR, IT = 32 / RPI;   // lanes of a row, rows at a time
-    const int cw = warp - PP_MMA_WARP - 1, c = lane % LPR, sub = lane / LPR;
+    const int cw = warp - PP_CONV_WARP, c = lane % LPR, sub = lane / LPR;
     uint4 w[IT];
     int id[2];
     auto lookup = [&](int j) {
@@ -235,17 +254,19 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
         *reinterpret_cast<uint4*>(tile + tile_off(row, 2 * c + first, PP_KEYS)) = first ? q : p;
         *reinterpret_cast<uint4*>(tile + tile_off(row, 2 * c + 1 - first, PP_KEYS)) = first ? p : q;
       }
+      fence_async_smem();                                // (it would wait for loads before it)
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(PB_FULL + st));
       if (i & 1) {
         load(j + 1, a.pool.k);                           // (pages looked up below, one item ago)
       } else {
         load(j, a.pool.v);
         lookup(j + 1);
       }
-      fence_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(PB_FULL + st));
     }
-  } else if (warp == PP_MMA_WARP) {
+  } else if (warp >= PP_MMA_WARP) {
+    set_registers<PP_REGS_MMA, false>();
+    if (warp == PP_MMA_WARP) {
     // ---------------------------------------------------------------- MMA issue
     const uint32_t idS = idesc_f16(128, PP_KEYS, 0), idO = idesc_f16(128, D, 1);
     const bool lead = elect_one();
@@ -300,51 +321,62 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
         if (j + 1 < nblk) issue_s(hf, j + 1);
       }
     }
+    }
   } else {
     // ---------------------------------------------------------------- softmax rows
+    set_registers<PP_REGS_ROW, true>();
     const int hf = warp >> 2;
     const uint32_t trow = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tO = tmem + trow + hf * 128, tS = tmem + trow + 256 + hf * 128;
-    // lanes 0-7: key scales of a block's 8 groups of 16 positions, 8-15: value exponents (-inf
-    // where there is nothing to see)
+    // lanes 0-7: key scales of a block's 8 groups of 16 positions; 8-15: value exponents, -inf where
+    // there is nothing to see; 16-23: 2^-those, 0
     auto scale_of = [&](int j) {
       float x = 0.f;
-      if (lane < 16) {
+      if (lane < 24) {
         const int pos = j * PP_KEYS + (lane & 7) * 16, id = j < nblk ? page16(pos) : -1;
         const long long at = (((long long)max(id, 0) * H + h) * a.pool.page + (pos & (a.pool.page - 1))) / BLK;
-        if (lane < 8) x = id >= 0 ? a.pool.ks[at] : 0.f;
-        else x = id >= 0 ? (float)((int)(__float_as_uint(a.pool.vs[at]) >> 23) - 127) : -INFINITY;
+        if (lane < 8) {
+          x = id >= 0 ? a.pool.ks[at] : 0.f;
+        } else {
+          const uint32_t e = __float_as_uint(a.pool.vs[at]) >> 23;
+          if (lane < 16) x = id >= 0 ? (float)((int)e - 127) : -INFINITY;
+          else x = id >= 0 ? __uint_as_float((254u - e) << 23) : 0.f;
+        }
       }
       return x;
     };
+    const uint32_t scaleS = sb + L::OFF_SCALE + warp * 192;
     float scale = scale_of(0);
     for (int j = 0; j < nblk; ++j) {
+      const uint32_t sc = scaleS + (j & 1) * 96;
+      if (lane < 24) asm volatile("st.shared.f32 [%0], %1;" ::"r"(sc + 4 * lane), "f"(scale) : "memory");
+      scale = scale_of(j + 1);
       if (!(ok = uniform(mbar_wait(bar(PB_S + hf), j & 1, a.err, ERR_WAIT)))) break;
       fence_after();
-      const float now = scale;
-      scale = scale_of(j + 1);
       const bool edge = (j + 1) * PP_KEYS - 1 > lim_lo;
       const int see = lim - j * PP_KEYS;                 // last column the row sees
+      float v[128];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tmem_ld32(tS + 32 * c, *reinterpret_cast<float(*)[32]>(v + 32 * c));
+      tmem_wait_ld();
+      if (edge) {
+#pragma unroll
+        for (int i = 0; i < 128; ++i)
+          if (i > see) v[i] = -INFINITY;
+      }
       float top = -INFINITY;
+      float2 ks2, ev2, vi2;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        float v[32];
-        tmem_ld32(tS + 32 * c, v);
-        tmem_wait_ld();
-        if (edge) {
-#pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if (32 * c + i > see) v[i] = -INFINITY;
+      for (int e = 0; e < 8; ++e) {
+        const float* x = v + 16 * e;
+        if (!(e & 1)) {
+          ks2 = lds2(sc + 4 * e);
+          ev2 = lds2(sc + 4 * (8 + e));
         }
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float* x = v + 16 * e;
-          const float m0 = fmax3(x[0], x[1], x[2]), m1 = fmax3(x[3], x[4], x[5]), m2 = fmax3(x[6], x[7], x[8]);
-          const float m3 = fmax3(x[9], x[10], x[11]), m4 = fmax3(x[12], x[13], x[14]);
-          const float bm = fmaxf(fmax3(m0, m1, m2), fmax3(m3, m4, x[15]));
-          const float ks = __shfl_sync(0xffffffffu, now, 2 * c + e), ev = __shfl_sync(0xffffffffu, now, 8 + 2 * c + e);
-          top = fmaxf(top, fmaf(bm, rc * ks, ev));
-        }
+        const float m0 = fmax3(x[0], x[1], x[2]), m1 = fmax3(x[3], x[4], x[5]), m2 = fmax3(x[6], x[7], x[8]);
+        const float m3 = fmax3(x[9], x[10], x[11]), m4 = fmax3(x[12], x[13], x[14]);
+        const float bm = fmaxf(fmax3(m0, m1, m2), fmax3(m3, m4, x[15]));
+        top = fmaxf(top, fmaf(bm, rc * (e & 1 ? ks2.y : ks2.x), e & 1 ? ev2.y : ev2.x));
       }
       const bool move = top > m + PP_STEP;
       const float mn = move ? top : m;
@@ -370,37 +402,37 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
       const float base = m == -INFINITY ? 0.f : PP_OFF - m;
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        float v[32], hi[16], lo_[16];
-        tmem_ld32(tS + 32 * c, v);
-        tmem_wait_ld();
+        float hi[16], lo_[16];
+        ks2 = lds2(sc + 8 * c);
+        ev2 = lds2(sc + 32 + 8 * c);
+        vi2 = lds2(sc + 64 + 8 * c);
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float ks = __shfl_sync(0xffffffffu, now, 2 * c + e), ev = __shfl_sync(0xffffffffu, now, 8 + 2 * c + e);
-          const float cc = rc * ks, add = ev + base;
-          const float vinv = ev == -INFINITY ? 0.f : __uint_as_float((uint32_t)(127 - (int)ev) << 23);
+        for (int e = 2 * c; e < 2 * c + 2; ++e) {
+          const float cc = rc * (e & 1 ? ks2.y : ks2.x), add = (e & 1 ? ev2.y : ev2.x) + base;
           const uint64_t c2 = f2_pack(cc, cc), a2 = f2_pack(add, add);
           uint64_t s0 = 0ull, s1 = 0ull;
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
+            const int at = 16 * e + 2 * i, k = 8 * (e & 1) + i;
             float x0, x1;
-            f2_unpack(f2_fma(f2_pack(v[16 * e + 2 * i], v[16 * e + 2 * i + 1]), c2, a2), x0, x1);
-            if (edge) {
-              if (32 * c + 16 * e + 2 * i > see) x0 = -INFINITY;
-              if (32 * c + 16 * e + 2 * i + 1 > see) x1 = -INFINITY;
+            f2_unpack(f2_fma(f2_pack(v[at], v[at + 1]), c2, a2), x0, x1);
+            if (edge) {                                  // (-inf times a factor that is 0 is no -inf)
+              if (at > see) x0 = -INFINITY;
+              if (at + 1 > see) x1 = -INFINITY;
             }
             x0 = ex2(x0);
             x1 = ex2(x1);
             const uint32_t w = pack_h2(x0, x1);
-            hi[8 * e + i] = __uint_as_float(w);
+            hi[k] = __uint_as_float(w);
             if (SPLIT) {
               const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&w));
-              lo_[8 * e + i] = __uint_as_float(pack_h2(x0 - b.x, x1 - b.y));
+              lo_[k] = __uint_as_float(pack_h2(x0 - b.x, x1 - b.y));
             }
             if (i & 1) s1 = f2_add(s1, f2_pack(x0, x1)); else s0 = f2_add(s0, f2_pack(x0, x1));
           }
           float x0, x1;
           f2_unpack(f2_add(s0, s1), x0, x1);
-          l = fmaf(x0 + x1, vinv, l);
+          l = fmaf(x0 + x1, e & 1 ? vi2.y : vi2.x, l);
         }
         tmem_st16(tS + 32 * c, hi);
         if (SPLIT) tmem_st16(tS + 32 * c + 16, lo_);
