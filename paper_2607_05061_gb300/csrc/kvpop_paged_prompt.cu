@@ -4,16 +4,21 @@
 // the value scales in the exponent, p = 2^(x log2 e + ev - M + 7) as one f16 (bf16 results) or
 // the sum of two (fp32 results, SPLIT).  A CTA owns 256 consecutive rows (token, query head) of
 // one (sequence, KV head), as two halves of 128 rows, and streams the positions they see in blocks
-// of 128, the same bytes for both halves.  Roles:
-//  * 4 converter warps bring the bytes of a block's keys, then of its values, into registers while
-//    the ones before are used, and write them as f16 into a ring of 5 128B-swizzled tiles.
-//  * 1 MMA warp: S = Q K^T (M 128, N 128, K d) per half, and O += P V (N d, K 128) with P in
-//    tensor memory and the values read MN-major from their rows.
-//  * 2 x 4 softmax warps, a thread per row: the row's maximum, then its probabilities, written
-//    over the logits 32 columns at a time and handed over in two parts, so that the product with
-//    the first half of the block runs while the second is formed.
-// Tensor memory: O (2 x d columns) and S (2 x 128) leave no second S buffer at d = 128, so the two
-// halves alternate: one's logits and products run beside the other's exponentials.
+// of 64, the same bytes for both halves.  Roles:
+//  * 3 converter warps bring the bytes of keys and values into registers, a tile each, and write
+//    them as f16 into a ring of 10 128B-swizzled tiles (a block's keys, then its values), with the
+//    scales beside them.
+//  * 1 MMA warp: S = Q K^T (M 128, N 64, K d) per half, and O += P V (N d, K 64) with P in tensor
+//    memory and the values read MN-major from their rows.
+//  * 2 x 4 softmax warps, a thread per row: logits into registers, which frees S for the next
+//    block, the row's maximum, probabilities to tensor memory.
+// A half may be a block ahead of the other one, so what it signals once a block and without having
+// to wait for an answer in between (P there, product done) has a barrier each for even and odd
+// blocks: an mbarrier's parity tells a phase from the next one only.
+// Tensor memory: O (2 x 128 columns), S (2 x 64) and two buffers of P (4 x 32; with SPLIT one, of
+// 64).  P has a place of its own so that the logits of the next block are formed while this one's
+// exponentials are: with P over the logits (blocks of 128, the next logits behind the product) a
+// half's rows and its products took turns, and both halves fell into step.
 #include "kvpop_mma.cuh"
 #include "kvpop_paged.cuh"
 #include "kvpop_ptx.cuh"
@@ -25,22 +30,20 @@ namespace {
 using namespace paged;
 using namespace tc05;
 
-constexpr int PP_HALF = 128, PP_ROWS = 2 * PP_HALF, PP_KEYS = 128;
-constexpr int PP_MMA_WARP = 8, PP_CONV_WARP = 12, PP_CONV = 4;   // warps 0-7: softmax, 8: MMA, 12-15: converters
+constexpr int PP_HALF = 128, PP_ROWS = 2 * PP_HALF, PP_KEYS = 64;
+constexpr int PP_MMA_WARP = 8, PP_CONV_WARP = 9, PP_CONV = 3;    // warps 0-7: softmax, 8: MMA, 9-11: converters
 constexpr int PP_THREADS = 32 * (PP_CONV_WARP + PP_CONV);
-// Registers of a thread: at launch, and of the softmax, MMA and converter warpgroups.
-constexpr int PP_REGS = 128, PP_REGS_ROW = 200, PP_REGS_MMA = 56, PP_REGS_CONV = 56;
-static_assert(PP_THREADS * PP_REGS <= 65536 && 2 * PP_REGS_ROW + PP_REGS_MMA + PP_REGS_CONV <= 4 * PP_REGS, "");
-constexpr int PP_RING = 5;
-constexpr int PP_TMEM = 512;                             // O_h: 128 h; S_h: 256 + 128 h
+constexpr int PP_RING = 10, PP_SCALES = 16;          // tiles; blocks whose scales are held
+constexpr int PP_TMEM = 512;                             // O_h: 128 h; S_h: 256 + 64 h; P_h: 384 + 64 h
 constexpr float PP_OFF = 7.f, PP_STEP = 8.f;
 // barriers
 constexpr int PB_FULL = 0;                               // [ring] converters -> MMA
 constexpr int PB_EMPTY = PB_FULL + PP_RING;              // [ring] MMA -> converters
-constexpr int PB_S = PB_EMPTY + PP_RING;                 // [2] MMA -> softmax
-constexpr int PB_P = PB_S + 2;                           // [2][2] softmax -> MMA, two parts
-constexpr int PB_O = PB_P + 4;                           // [2] MMA -> softmax
-constexpr int PB_N = PB_O + 2;
+constexpr int PB_S = PB_EMPTY + PP_RING;                 // [2] MMA -> softmax: logits there
+constexpr int PB_READ = PB_S + 2;                        // [2] softmax -> MMA: logits read
+constexpr int PB_P = PB_READ + 2;                        // [2][2] softmax -> MMA: probabilities of even, odd blocks there
+constexpr int PB_O = PB_P + 4;                           // [2][2] MMA -> softmax: products of even, odd blocks done
+constexpr int PB_N = PB_O + 4;
 constexpr int PP_NANW = (PP_ROWS + 2 * PP_KEYS) / 32;    // words of the map of NaN values
 
 struct PromptArgs {
@@ -60,8 +63,8 @@ struct PL {
   static constexpr int QB = PP_HALF * D * 2, KB = PP_KEYS * D * 2;
   static constexpr int OFF_RING = 2 * QB, OFF_BAR = OFF_RING + PP_RING * KB;
   static constexpr int OFF_TMEM = OFF_BAR + 8 * PB_N, OFF_NAN = (OFF_TMEM + 4 + 15) / 16 * 16;
-  static constexpr int OFF_SCALE = OFF_NAN + 4 * PP_NANW;  // [8 warps][2][24] key scales, value exponents, 2^-those
-  static constexpr int BYTES = OFF_SCALE + 8 * 2 * 24 * 4;
+  static constexpr int OFF_SCALE = OFF_NAN + 4 * PP_NANW;   // [16 blocks] 4 key scales, 4 value exponents, 4 2^-those
+  static constexpr int BYTES = OFF_SCALE + PP_SCALES * 48;
   static constexpr int OUT_WARP = 32 * D * 4;            // a warp's finished rows, in the ring
   static_assert(8 * OUT_WARP <= OFF_BAR, "");
 };
@@ -73,6 +76,12 @@ __device__ __forceinline__ uint32_t idesc_f16(int M, int N, int b_mn_major) {
 __device__ __forceinline__ uint32_t pack_h2(float lo, float hi) {
   __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&v);
+}
+// (read once: no place in L1)
+__device__ __forceinline__ void ld16(uint4& v, const unsigned char* p) {
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(p));
 }
 // 16 e4m3 bytes -> 16 f16
 __device__ __forceinline__ void cvt16(const uint4& w, uint4& a, uint4& b) {
@@ -94,20 +103,6 @@ __device__ __forceinline__ bool has_nan(uint32_t w) {   // an e4m3 NaN (0x7f, 0x
 __device__ __forceinline__ uint32_t drop_nan(uint32_t w) {
   const uint32_t x = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
   return w & ~((x >> 7) * 255u);
-}
-
-// Registers of a thread from here on, for a whole warpgroup.
-template <int N, bool MORE>
-__device__ __forceinline__ void set_registers() {
-  if (MORE) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
-  else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
-}
-
-// (volatile: read where it is used, not kept in registers that a row of logits needs)
-__device__ __forceinline__ float2 lds2(uint32_t p) {
-  float2 v;
-  asm volatile("ld.volatile.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(p));
-  return v;
 }
 
 template <int D, bool SPLIT>
@@ -143,14 +138,16 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
 
   if (tid == 0) {
     for (int i = 0; i < PP_RING; ++i) {
-      mbar_init(bar(PB_FULL + i), PP_CONV);
+      mbar_init(bar(PB_FULL + i), 1);
       mbar_init(bar(PB_EMPTY + i), 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar(PB_S + i), 1);
-      mbar_init(bar(PB_O + i), 1);
+      mbar_init(bar(PB_READ + i), 4);
       mbar_init(bar(PB_P + 2 * i), 4);
       mbar_init(bar(PB_P + 2 * i + 1), 4);
+      mbar_init(bar(PB_O + 2 * i), 1);
+      mbar_init(bar(PB_O + 2 * i + 1), 1);
     }
     mbar_fence_init();
   }
@@ -195,7 +192,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
   __syncthreads();
   fence_after();
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smp + L::OFF_TMEM);
-  // page of a block of 16 positions, -1 where the rows see none of it
+  // page of a position, -1 where the rows do not see it
   auto page16 = [&](int pos) { return pos <= lim_hi ? page_of(a.b, a.pool, s, pos, a.err) : -1; };
   auto uniform = [](bool x) { return __all_sync(0xffffffffu, x); };
   float m = -INFINITY, l = 0.f;
@@ -203,70 +200,84 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
 
   if (warp >= PP_CONV_WARP) {
     // ---------------------------------------------------------------- converters
-    set_registers<PP_REGS_CONV, false>();
-    constexpr int LPR = D / 16, RPI = 32 / LPR, IT = 32 / RPI;   // lanes of a row, rows at a time
-    const int cw = warp - PP_CONV_WARP, c = lane % LPR, sub = lane / LPR;
+    // Tile i (keys of block i / 2, or its values) is warp i mod 3's.  Its bytes and scales are asked
+    // for right behind the fence of the warp's tile before: that fence waits for every load that is
+    // on its way, and this one comes when they are there.
+    constexpr int LPR = D / 16, RPI = 32 / LPR, IT = PP_KEYS / RPI, PER = PP_KEYS / BLK;   // lanes of a row, rows at a time
+    const int c = lane % LPR, sub = lane / LPR, tiles = 2 * nblk;
+    const int32_t* const trow = a.b.table + (long long)s * a.b.table_stride;
     uint4 w[IT];
-    int id[2];
-    auto lookup = [&](int j) {
+    float scale = 0.f;                                   // lanes 0-3: of the groups' keys, 4-7: of their values
+    // Every load is unconditional, from a row that is there: a choice between its value and another
+    // would wait for it.  What is not to be seen is cleared when it is used.
+    auto group_pos = [&](int i) { return (i >> 1) * PP_KEYS + (lane & (PER - 1)) * BLK; };
+    auto look = [&](int i) { return trow[min(group_pos(i), lim_hi) >> a.pool.page_shift]; };   // page of group lane mod 4
+    auto is_page = [&](int id) { return (unsigned)id < (unsigned)a.pool.n_pages; };
+    auto load = [&](int i, int id) {
+      const unsigned char* pages = i & 1 ? a.pool.v : a.pool.k;
+      const long long head = ((long long)(is_page(id) ? id : 0) * H + h) * a.pool.page;
 #pragma unroll
-      for (int e = 0; e < 2; ++e) id[e] = j < nblk ? page16(j * PP_KEYS + cw * 32 + 16 * e) : -1;
-    };
-    auto load = [&](int j, const unsigned char* pages) {
-#pragma unroll
-      for (int i = 0; i < IT; ++i) {
-        const int row = i * RPI + sub, pos = j * PP_KEYS + cw * 32 + row, pg = id[(i * RPI) >> 4];
-        w[i] = make_uint4(0, 0, 0, 0);
-        if (pg >= 0 && pos <= lim_hi)
-          w[i] = __ldg(reinterpret_cast<const uint4*>(
-              pages + (((long long)pg * H + h) * a.pool.page + (pos & (a.pool.page - 1))) * D + 16 * c));
+      for (int x = 0; x < IT; ++x) {
+        const long long base = __shfl_sync(0xffffffffu, head, x * RPI / BLK);
+        const int pos = (i >> 1) * PP_KEYS + x * RPI + sub;
+        ld16(w[x], pages + (base + (pos & (a.pool.page - 1))) * D + 16 * c);
       }
+      scale = (lane & PER ? a.pool.vs : a.pool.ks)[(head + (group_pos(i) & (a.pool.page - 1))) / BLK];
     };
-    lookup(0);
-    load(0, a.pool.k);
-    for (int i = 0; i < 2 * nblk && ok; ++i) {
-      const int j = i >> 1, st = i % PP_RING;
-      if (i >= PP_RING && !(ok = uniform(mbar_wait(bar(PB_EMPTY + st), (i / PP_RING - 1) & 1, a.err, ERR_WAIT)))) break;
-      if ((i & 1) && (j + 1) * PP_KEYS - 1 > lim_lo) {
+    int i = warp - PP_CONV_WARP, id = look(i), id_next;
+    load(i, id);
+    id_next = look(i + PP_CONV);
+#pragma unroll 1
+    for (; i < tiles; i += PP_CONV) {
+      const int st = i % PP_RING, pos0 = (i >> 1) * PP_KEYS;
+      if (i >= PP_RING && !uniform(mbar_wait(bar(PB_EMPTY + st), (i / PP_RING - 1) & 1, a.err, ERR_WAIT))) break;
+      const bool seen = group_pos(i) <= lim_hi, in = seen && is_page(id);
+      if (seen && !in) report(a.err, ERR_PAGE);
+      if (!in) scale = 0.f;                              // (nothing to see)
+      if (!uniform(in && pos0 + PP_KEYS - 1 <= lim_hi)) {
+#pragma unroll
+        for (int x = 0; x < IT; ++x) {
+          const bool ok_ = __shfl_sync(0xffffffffu, (int)in, x * RPI / BLK) && pos0 + x * RPI + sub <= lim_hi;
+          if (!ok_) w[x] = make_uint4(0, 0, 0, 0);
+        }
+      }
+      if (!(i & 1) && lane < 2 * PER) {                  // both scales with the keys, which the logits wait for
+        float* to = reinterpret_cast<float*>(smp + L::OFF_SCALE) + (i >> 1) % PP_SCALES * 12 + lane;
+        const uint32_t e = __float_as_uint(scale) >> 23;
+        to[0] = lane < PER ? scale : scale > 0.f ? (float)((int)e - 127) : -INFINITY;
+        if (lane >= PER) to[PER] = scale > 0.f ? __uint_as_float((254u - e) << 23) : 0.f;
+      }
+      if ((i & 1) && pos0 + PP_KEYS - 1 > lim_lo) {
         // Values that some row does not see: a NaN must not reach the rows before it, where its
         // weight is 0.  Its column is set at the end, for the rows that see it.
 #pragma unroll
-        for (int x = 0; x < IT; ++x) {
-          const bool bad = has_nan(w[x].x) || has_nan(w[x].y) || has_nan(w[x].z) || has_nan(w[x].w);
-          if (bad) {
-            const int pos = j * PP_KEYS + cw * 32 + x * RPI + sub;
-            if (pos >= nan0) {
-              atomicOr(nanS + ((pos - nan0) >> 5), 1u << ((pos - nan0) & 31));
-              w[x] = make_uint4(drop_nan(w[x].x), drop_nan(w[x].y), drop_nan(w[x].z), drop_nan(w[x].w));
-            }
+        for (int x = 0; x < IT; ++x)
+          if (has_nan(w[x].x) || has_nan(w[x].y) || has_nan(w[x].z) || has_nan(w[x].w)) {
+            const int at = pos0 + x * RPI + sub - nan0;
+            atomicOr(nanS + (at >> 5), 1u << (at & 31));
+            w[x] = make_uint4(drop_nan(w[x].x), drop_nan(w[x].y), drop_nan(w[x].z), drop_nan(w[x].w));
           }
-        }
       }
       unsigned char* tile = smp + L::OFF_RING + st * L::KB;
 #pragma unroll
       for (int x = 0; x < IT; ++x) {
         uint4 p, q;
         cvt16(w[x], p, q);
-        const int row = cw * 32 + x * RPI + sub;
+        const int row = x * RPI + sub;
         // (d = 128: lanes of the upper 64 values store their second chunk first, so that the 8
         // lanes of a row touch all banks)
         const int first = D == 128 ? c >> 2 : 0;
         *reinterpret_cast<uint4*>(tile + tile_off(row, 2 * c + first, PP_KEYS)) = first ? q : p;
         *reinterpret_cast<uint4*>(tile + tile_off(row, 2 * c + 1 - first, PP_KEYS)) = first ? p : q;
       }
-      fence_async_smem();                                // (it would wait for loads before it)
+      fence_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(PB_FULL + st));
-      if (i & 1) {
-        load(j + 1, a.pool.k);                           // (pages looked up below, one item ago)
-      } else {
-        load(j, a.pool.v);
-        lookup(j + 1);
-      }
+      id = id_next;
+      load(i + PP_CONV, id);
+      id_next = look(i + 2 * PP_CONV);
     }
-  } else if (warp >= PP_MMA_WARP) {
-    set_registers<PP_REGS_MMA, false>();
-    if (warp == PP_MMA_WARP) {
+  } else if (warp == PP_MMA_WARP) {
     // ---------------------------------------------------------------- MMA issue
     const uint32_t idS = idesc_f16(128, PP_KEYS, 0), idO = idesc_f16(128, D, 1);
     const bool lead = elect_one();
@@ -284,7 +295,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
         const uint64_t kd = desc_at(kd0, st * L::KB), qd = desc_at(qd0, hf * L::QB);
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks)
-          mma_bf16(tmem + 256 + hf * 128, kmajor_step(qd, PP_HALF, ks), kmajor_step(kd, PP_KEYS, ks), idS, ks > 0);
+          mma_bf16(tmem + 256 + hf * 64, kmajor_step(qd, PP_HALF, ks), kmajor_step(kd, PP_KEYS, ks), idS, ks > 0);
         commit(bar(PB_S + hf));
         if (hf == 1) commit(bar(PB_EMPTY + st));
       }
@@ -295,120 +306,101 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     for (int j = 0; j < nblk && ok; ++j) {
       const int st = (2 * j + 1) % PP_RING;
       const uint64_t vd = desc_at(vd0, st * L::KB);
-#pragma unroll 1
-      for (int hf = 0; hf < 2 && ok; ++hf) {
-        if (hf == 0) wait(PB_FULL + st, ((2 * j + 1) / PP_RING) & 1);
-        const uint32_t tP = tmem + 256 + hf * 128, dO = tmem + hf * 128;
+      if (j + 1 < nblk)
 #pragma unroll
-        for (int part = 0; part < 2; ++part) {
-          wait(PB_P + 2 * hf + part, j & 1);
-          if (ok && lead) {
-#pragma unroll
-            for (int k = 4 * part; k < 4 * part + 4; ++k) {
-              const uint32_t ta = tP + 32 * (k >> 1) + 8 * (k & 1);
-              const uint64_t vk = desc_at(vd, k * 16 * 128);
-              mma_bf16_ts(dO, ta, vk, idO, j > 0 || k > 0);
-              if (SPLIT) mma_bf16_ts(dO, ta + 16, vk, idO, 1);
-            }
-          }
-          __syncwarp();
+        for (int hf = 0; hf < 2; ++hf) {
+          wait(PB_READ + hf, j & 1);
+          issue_s(hf, j + 1);
         }
+      wait(PB_FULL + st, ((2 * j + 1) / PP_RING) & 1);
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        wait(PB_P + 2 * hf + (j & 1), j >> 1 & 1);
         if (ok && lead) {
-          commit(bar(PB_O + hf));
+          const uint32_t tP = tmem + 384 + hf * 64 + (SPLIT ? 0 : (j & 1) * 32), dO = tmem + hf * 128;
+#pragma unroll
+          for (int k = 0; k < PP_KEYS / 16; ++k) {
+            const uint64_t vk = desc_at(vd, k * 16 * 128);
+            mma_bf16_ts(dO, tP + 8 * k, vk, idO, j > 0 || k > 0);
+            if (SPLIT) mma_bf16_ts(dO, tP + 32 + 8 * k, vk, idO, 1);
+          }
+          commit(bar(PB_O + 2 * hf + (j & 1)));
           if (hf == 1) commit(bar(PB_EMPTY + st));
         }
         __syncwarp();
-        if (j + 1 < nblk) issue_s(hf, j + 1);
       }
-    }
     }
   } else {
     // ---------------------------------------------------------------- softmax rows
-    set_registers<PP_REGS_ROW, true>();
     const int hf = warp >> 2;
     const uint32_t trow = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t tO = tmem + trow + hf * 128, tS = tmem + trow + 256 + hf * 128;
-    // lanes 0-7: key scales of a block's 8 groups of 16 positions; 8-15: value exponents, -inf where
-    // there is nothing to see; 16-23: 2^-those, 0
-    auto scale_of = [&](int j) {
-      float x = 0.f;
-      if (lane < 24) {
-        const int pos = j * PP_KEYS + (lane & 7) * 16, id = j < nblk ? page16(pos) : -1;
-        const long long at = (((long long)max(id, 0) * H + h) * a.pool.page + (pos & (a.pool.page - 1))) / BLK;
-        if (lane < 8) {
-          x = id >= 0 ? a.pool.ks[at] : 0.f;
-        } else {
-          const uint32_t e = __float_as_uint(a.pool.vs[at]) >> 23;
-          if (lane < 16) x = id >= 0 ? (float)((int)e - 127) : -INFINITY;
-          else x = id >= 0 ? __uint_as_float((254u - e) << 23) : 0.f;
-        }
-      }
-      return x;
+    const uint32_t tO = tmem + trow + hf * 128, tS = tmem + trow + 256 + hf * 64, tP = tmem + trow + 384 + hf * 64;
+    auto done = [&](int j) {                             // the product with block j is in O
+      return uniform(mbar_wait(bar(PB_O + 2 * hf + (j & 1)), (j >> 1) & 1, a.err, ERR_WAIT));
     };
-    const uint32_t scaleS = sb + L::OFF_SCALE + warp * 192;
-    float scale = scale_of(0);
     for (int j = 0; j < nblk; ++j) {
-      const uint32_t sc = scaleS + (j & 1) * 96;
-      if (lane < 24) asm volatile("st.shared.f32 [%0], %1;" ::"r"(sc + 4 * lane), "f"(scale) : "memory");
-      scale = scale_of(j + 1);
       if (!(ok = uniform(mbar_wait(bar(PB_S + hf), j & 1, a.err, ERR_WAIT)))) break;
       fence_after();
+      float v[64];
+      tmem_ld32(tS, *reinterpret_cast<float(*)[32]>(v));
+      tmem_ld32(tS + 32, *reinterpret_cast<float(*)[32]>(v + 32));
+      const float4* sc = reinterpret_cast<const float4*>(smp + L::OFF_SCALE + j % PP_SCALES * 48);
+      const float4 ks4 = sc[0], ev4 = sc[1], vi4 = sc[2];
+      const float ks[4] = {ks4.x, ks4.y, ks4.z, ks4.w}, ev[4] = {ev4.x, ev4.y, ev4.z, ev4.w};
+      const float vi[4] = {vi4.x, vi4.y, vi4.z, vi4.w};
+      tmem_wait_ld();
+      fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(PB_READ + hf));
       const bool edge = (j + 1) * PP_KEYS - 1 > lim_lo;
       const int see = lim - j * PP_KEYS;                 // last column the row sees
-      float v[128];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) tmem_ld32(tS + 32 * c, *reinterpret_cast<float(*)[32]>(v + 32 * c));
-      tmem_wait_ld();
       if (edge) {
 #pragma unroll
-        for (int i = 0; i < 128; ++i)
+        for (int i = 0; i < 64; ++i)
           if (i > see) v[i] = -INFINITY;
       }
       float top = -INFINITY;
-      float2 ks2, ev2, vi2;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < 4; ++e) {
         const float* x = v + 16 * e;
-        if (!(e & 1)) {
-          ks2 = lds2(sc + 4 * e);
-          ev2 = lds2(sc + 4 * (8 + e));
-        }
         const float m0 = fmax3(x[0], x[1], x[2]), m1 = fmax3(x[3], x[4], x[5]), m2 = fmax3(x[6], x[7], x[8]);
         const float m3 = fmax3(x[9], x[10], x[11]), m4 = fmax3(x[12], x[13], x[14]);
         const float bm = fmaxf(fmax3(m0, m1, m2), fmax3(m3, m4, x[15]));
-        top = fmaxf(top, fmaf(bm, rc * (e & 1 ? ks2.y : ks2.x), e & 1 ? ev2.y : ev2.x));
+        top = fmaxf(top, fmaf(bm, rc * ks[e], ev[e]));
       }
       const bool move = top > m + PP_STEP;
-      const float mn = move ? top : m;
-      const float al = m == -INFINITY ? 0.f : ex2(m - mn);
-      if (j > 0 && __any_sync(0xffffffffu, move)) {
-        // PV_{j-1} has to be in O before O changes
-        if (!(ok = uniform(mbar_wait(bar(PB_O + hf), (j - 1) & 1, a.err, ERR_WAIT)))) break;
-        fence_after();
-        const float f = move ? al : 1.f;
+      if (__any_sync(0xffffffffu, move)) {
+        const float mn = move ? top : m, f = m == -INFINITY ? 0.f : ex2(m - mn);   // (1 where it stays)
+        if (j > 0) {
+          if (!(ok = done(j - 1))) break;                // before O changes
+          fence_after();
+          const float g = move ? f : 1.f;
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
-          float o[32];
-          tmem_ld32(tO + c * 32, o);
-          tmem_wait_ld();
+          for (int c = 0; c < D / 32; ++c) {
+            float o[32];
+            tmem_ld32(tO + c * 32, o);
+            tmem_wait_ld();
 #pragma unroll
-          for (int i = 0; i < 32; ++i) o[i] *= f;
-          tmem_st32(tO + c * 32, o);
+            for (int i = 0; i < 32; ++i) o[i] *= g;
+            tmem_st32(tO + c * 32, o);
+          }
+          tmem_wait_st();
         }
-        tmem_wait_st();
+        if (move) l *= f;
+        m = mn;
       }
-      if (move) l *= al;
-      m = mn;
       const float base = m == -INFINITY ? 0.f : PP_OFF - m;
+      // the buffer that P goes to is free once its last product is done
+      if (SPLIT ? j > 0 : j > 1) {
+        if (!(ok = done(SPLIT ? j - 1 : j - 2))) break;
+        fence_after();
+      }
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
+      for (int c = 0; c < 2; ++c) {
         float hi[16], lo_[16];
-        ks2 = lds2(sc + 8 * c);
-        ev2 = lds2(sc + 32 + 8 * c);
-        vi2 = lds2(sc + 64 + 8 * c);
 #pragma unroll
         for (int e = 2 * c; e < 2 * c + 2; ++e) {
-          const float cc = rc * (e & 1 ? ks2.y : ks2.x), add = (e & 1 ? ev2.y : ev2.x) + base;
+          const float cc = rc * ks[e], add = ev[e] + base;
           const uint64_t c2 = f2_pack(cc, cc), a2 = f2_pack(add, add);
           uint64_t s0 = 0ull, s1 = 0ull;
 #pragma unroll
@@ -416,7 +408,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
             const int at = 16 * e + 2 * i, k = 8 * (e & 1) + i;
             float x0, x1;
             f2_unpack(f2_fma(f2_pack(v[at], v[at + 1]), c2, a2), x0, x1);
-            if (edge) {                                  // (-inf times a factor that is 0 is no -inf)
+            if (edge) {                                  // (here: -inf times a factor that is 0 is no -inf)
               if (at > see) x0 = -INFINITY;
               if (at + 1 > see) x1 = -INFINITY;
             }
@@ -432,19 +424,18 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
           }
           float x0, x1;
           f2_unpack(f2_add(s0, s1), x0, x1);
-          l = fmaf(x0 + x1, e & 1 ? vi2.y : vi2.x, l);
+          l = fmaf(x0 + x1, vi[e], l);
         }
-        tmem_st16(tS + 32 * c, hi);
-        if (SPLIT) tmem_st16(tS + 32 * c + 16, lo_);
-        if (c & 1) {
-          tmem_wait_st();
-          fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar(PB_P + 2 * hf + (c >> 1)));
-        }
+        const uint32_t to = tP + (SPLIT ? 0 : (j & 1) * 32) + 16 * c;
+        tmem_st16(to, hi);
+        if (SPLIT) tmem_st16(to + 32, lo_);
       }
+      tmem_wait_st();
+      fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(PB_P + 2 * hf + (j & 1)));
     }
-    if (ok) ok = uniform(mbar_wait(bar(PB_O + hf), (nblk - 1) & 1, a.err, ERR_WAIT));
+    if (ok) ok = done(nblk - 1);
   }
   fence_before();
   __syncthreads();                                       // every product is done; shared memory is free
