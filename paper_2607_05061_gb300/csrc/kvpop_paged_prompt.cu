@@ -10,15 +10,15 @@
 //    scales beside them.
 //  * 1 MMA warp: S = Q K^T (M 128, N 64, K d) per half, and O += P V (N d, K 64) with P in tensor
 //    memory and the values read MN-major from their rows.
-//  * 2 x 4 softmax warps, a thread per row: logits into registers, which frees S for the next
-//    block, the row's maximum, probabilities to tensor memory.
-// A half may be a block ahead of the other one, so what it signals once a block and without having
-// to wait for an answer in between (P there, product done) has a barrier each for even and odd
-// blocks: an mbarrier's parity tells a phase from the next one only.
-// Tensor memory: O (2 x 128 columns), S (2 x 64) and two buffers of P (4 x 32; with SPLIT one, of
-// 64).  P has a place of its own so that the logits of the next block are formed while this one's
-// exponentials are: with P over the logits (blocks of 128, the next logits behind the product) a
-// half's rows and its products took turns, and both halves fell into step.
+//  * 2 x 4 softmax warps, a thread per row: logits into registers, the row's maximum,
+//    probabilities over the logits.
+// Tensor memory: O (2 x 128 columns) and two buffers of logits (4 x 64), P in the place of its
+// logits.  The logits of block j + 2 follow the product with block j into its buffer in the order
+// the MMAs are issued, and those of block j + 1 are there when a row is done with block j, so a
+// block costs a softmax warp one wait and one signal.  Measured before that: blocks of 128 in one
+// buffer, where a half's rows and its products took turns, 672 us (a prompt of 8192 tokens, 32
+// query and 8 KV heads); blocks of 64 with P in a place of its own, two waits and two signals a
+// block, 622.
 #include "kvpop_mma.cuh"
 #include "kvpop_paged.cuh"
 #include "kvpop_ptx.cuh"
@@ -34,16 +34,15 @@ constexpr int PP_HALF = 128, PP_ROWS = 2 * PP_HALF, PP_KEYS = 64;
 constexpr int PP_MMA_WARP = 8, PP_CONV_WARP = 9, PP_CONV = 3;    // warps 0-7: softmax, 8: MMA, 9-11: converters
 constexpr int PP_THREADS = 32 * (PP_CONV_WARP + PP_CONV);
 constexpr int PP_RING = 10, PP_SCALES = 16;          // tiles; blocks whose scales are held
-constexpr int PP_TMEM = 512;                             // O_h: 128 h; S_h: 256 + 64 h; P_h: 384 + 64 h
+constexpr int PP_TMEM = 512;                             // O_h: 128 h; S_h,b: 256 + 128 h + 64 b
 constexpr float PP_OFF = 7.f, PP_STEP = 8.f;
 // barriers
 constexpr int PB_FULL = 0;                               // [ring] converters -> MMA
 constexpr int PB_EMPTY = PB_FULL + PP_RING;              // [ring] MMA -> converters
-constexpr int PB_S = PB_EMPTY + PP_RING;                 // [2] MMA -> softmax: logits there
-constexpr int PB_READ = PB_S + 2;                        // [2] softmax -> MMA: logits read
-constexpr int PB_P = PB_READ + 2;                        // [2][2] softmax -> MMA: probabilities of even, odd blocks there
-constexpr int PB_O = PB_P + 4;                           // [2][2] MMA -> softmax: products of even, odd blocks done
-constexpr int PB_N = PB_O + 4;
+constexpr int PB_S = PB_EMPTY + PP_RING;                 // [2][2] MMA -> softmax: logits of even, odd blocks there
+constexpr int PB_P = PB_S + 4;                           // [2][2] softmax -> MMA: their probabilities there
+constexpr int PB_O = PB_P + 4;                           // [2] MMA -> softmax: a product done
+constexpr int PB_N = PB_O + 2;
 constexpr int PP_NANW = (PP_ROWS + 2 * PP_KEYS) / 32;    // words of the map of NaN values
 
 struct PromptArgs {
@@ -141,14 +140,12 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
       mbar_init(bar(PB_FULL + i), 1);
       mbar_init(bar(PB_EMPTY + i), 1);
     }
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 4; ++i) {
       mbar_init(bar(PB_S + i), 1);
-      mbar_init(bar(PB_READ + i), 4);
-      mbar_init(bar(PB_P + 2 * i), 4);
-      mbar_init(bar(PB_P + 2 * i + 1), 4);
-      mbar_init(bar(PB_O + 2 * i), 1);
-      mbar_init(bar(PB_O + 2 * i + 1), 1);
+      mbar_init(bar(PB_P + i), 4);
     }
+    mbar_init(bar(PB_O + 0), 1);
+    mbar_init(bar(PB_O + 1), 1);
     mbar_fence_init();
   }
   if (tid < PP_NANW) nanS[tid] = 0;
@@ -194,7 +191,10 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smp + L::OFF_TMEM);
   // page of a position, -1 where the rows do not see it
   auto page16 = [&](int pos) { return pos <= lim_hi ? page_of(a.b, a.pool, s, pos, a.err) : -1; };
-  auto uniform = [](bool x) { return __all_sync(0xffffffffu, x); };
+  auto wait = [&](int b, int parity) {                   // the whole warp; false: gave up
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar(b), parity))) return true;
+    return (bool)__all_sync(0xffffffffu, mbar_wait(bar(b), parity, a.err, ERR_WAIT));
+  };
   float m = -INFINITY, l = 0.f;
   bool ok = true;
 
@@ -230,11 +230,11 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
 #pragma unroll 1
     for (; i < tiles; i += PP_CONV) {
       const int st = i % PP_RING, pos0 = (i >> 1) * PP_KEYS;
-      if (i >= PP_RING && !uniform(mbar_wait(bar(PB_EMPTY + st), (i / PP_RING - 1) & 1, a.err, ERR_WAIT))) break;
+      if (i >= PP_RING && !wait(PB_EMPTY + st, (i / PP_RING - 1) & 1)) break;
       const bool seen = group_pos(i) <= lim_hi, in = seen && is_page(id);
       if (seen && !in) report(a.err, ERR_PAGE);
       if (!in) scale = 0.f;                              // (nothing to see)
-      if (!uniform(in && pos0 + PP_KEYS - 1 <= lim_hi)) {
+      if (!__all_sync(0xffffffffu, in && pos0 + PP_KEYS - 1 <= lim_hi)) {
 #pragma unroll
         for (int x = 0; x < IT; ++x) {
           const bool ok_ = __shfl_sync(0xffffffffu, (int)in, x * RPI / BLK) && pos0 + x * RPI + sub <= lim_hi;
@@ -283,64 +283,59 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     const bool lead = elect_one();
     const uint64_t qd0 = kmajor_desc(sb, PP_HALF, 0), kd0 = kmajor_desc(sb + L::OFF_RING, PP_KEYS, 0);
     const uint64_t vd0 = mnmajor_desc(sb + L::OFF_RING, PP_KEYS, 0);
-    auto wait = [&](int b, int parity) {
-      ok = ok && mbar_wait(bar(b), parity, a.err, ERR_WAIT);
-      ok = uniform(ok);
-      if (ok) fence_after();
-    };
     auto issue_s = [&](int hf, int j) {                  // logits of half hf against block j
       const int st = 2 * j % PP_RING;
-      if (hf == 0) wait(PB_FULL + st, (2 * j / PP_RING) & 1);
-      if (ok && lead) {
+      if (hf == 0) {
+        if (!(ok = ok && wait(PB_FULL + st, (2 * j / PP_RING) & 1))) return;
+        fence_after();
+      }
+      if (lead) {
         const uint64_t kd = desc_at(kd0, st * L::KB), qd = desc_at(qd0, hf * L::QB);
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks)
-          mma_bf16(tmem + 256 + hf * 64, kmajor_step(qd, PP_HALF, ks), kmajor_step(kd, PP_KEYS, ks), idS, ks > 0);
-        commit(bar(PB_S + hf));
+          mma_bf16(tmem + 256 + hf * 128 + (j & 1) * 64, kmajor_step(qd, PP_HALF, ks), kmajor_step(kd, PP_KEYS, ks), idS,
+                   ks > 0);
+        commit(bar(PB_S + 2 * hf + (j & 1)));
         if (hf == 1) commit(bar(PB_EMPTY + st));
       }
       __syncwarp();
     };
-    issue_s(0, 0);
-    issue_s(1, 0);
+    for (int j = 0; j < min(nblk, 2) && ok; ++j) {
+      issue_s(0, j);
+      if (ok) issue_s(1, j);
+    }
     for (int j = 0; j < nblk && ok; ++j) {
       const int st = (2 * j + 1) % PP_RING;
       const uint64_t vd = desc_at(vd0, st * L::KB);
-      if (j + 1 < nblk)
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          wait(PB_READ + hf, j & 1);
-          issue_s(hf, j + 1);
-        }
-      wait(PB_FULL + st, ((2 * j + 1) / PP_RING) & 1);
+      if (!(ok = wait(PB_FULL + st, ((2 * j + 1) / PP_RING) & 1))) break;
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
-        wait(PB_P + 2 * hf + (j & 1), j >> 1 & 1);
-        if (ok && lead) {
-          const uint32_t tP = tmem + 384 + hf * 64 + (SPLIT ? 0 : (j & 1) * 32), dO = tmem + hf * 128;
+        if (!(ok = ok && wait(PB_P + 2 * hf + (j & 1), j >> 1 & 1))) break;
+        fence_after();
+        if (lead) {
+          const uint32_t tP = tmem + 256 + hf * 128 + (j & 1) * 64, dO = tmem + hf * 128;
 #pragma unroll
           for (int k = 0; k < PP_KEYS / 16; ++k) {
             const uint64_t vk = desc_at(vd, k * 16 * 128);
             mma_bf16_ts(dO, tP + 8 * k, vk, idO, j > 0 || k > 0);
             if (SPLIT) mma_bf16_ts(dO, tP + 32 + 8 * k, vk, idO, 1);
           }
-          commit(bar(PB_O + 2 * hf + (j & 1)));
+          commit(bar(PB_O + hf));
           if (hf == 1) commit(bar(PB_EMPTY + st));
         }
         __syncwarp();
+        if (j + 2 < nblk) issue_s(hf, j + 2);
       }
     }
   } else {
     // ---------------------------------------------------------------- softmax rows
     const int hf = warp >> 2;
     const uint32_t trow = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t tO = tmem + trow + hf * 128, tS = tmem + trow + 256 + hf * 64, tP = tmem + trow + 384 + hf * 64;
-    auto done = [&](int j) {                             // the product with block j is in O
-      return uniform(mbar_wait(bar(PB_O + 2 * hf + (j & 1)), (j >> 1) & 1, a.err, ERR_WAIT));
-    };
+    const uint32_t tO = tmem + trow + hf * 128;
     for (int j = 0; j < nblk; ++j) {
-      if (!(ok = uniform(mbar_wait(bar(PB_S + hf), j & 1, a.err, ERR_WAIT)))) break;
+      if (!(ok = wait(PB_S + 2 * hf + (j & 1), j >> 1 & 1))) break;
       fence_after();
+      const uint32_t tS = tmem + trow + 256 + hf * 128 + (j & 1) * 64;
       float v[64];
       tmem_ld32(tS, *reinterpret_cast<float(*)[32]>(v));
       tmem_ld32(tS + 32, *reinterpret_cast<float(*)[32]>(v + 32));
@@ -349,9 +344,6 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
       const float ks[4] = {ks4.x, ks4.y, ks4.z, ks4.w}, ev[4] = {ev4.x, ev4.y, ev4.z, ev4.w};
       const float vi[4] = {vi4.x, vi4.y, vi4.z, vi4.w};
       tmem_wait_ld();
-      fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(PB_READ + hf));
       const bool edge = (j + 1) * PP_KEYS - 1 > lim_lo;
       const int see = lim - j * PP_KEYS;                 // last column the row sees
       if (edge) {
@@ -372,7 +364,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
       if (__any_sync(0xffffffffu, move)) {
         const float mn = move ? top : m, f = m == -INFINITY ? 0.f : ex2(m - mn);   // (1 where it stays)
         if (j > 0) {
-          if (!(ok = done(j - 1))) break;                // before O changes
+          if (!(ok = wait(PB_O + hf, (j - 1) & 1))) break;   // the product before has to be in O
           fence_after();
           const float g = move ? f : 1.f;
 #pragma unroll
@@ -390,11 +382,6 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
         m = mn;
       }
       const float base = m == -INFINITY ? 0.f : PP_OFF - m;
-      // the buffer that P goes to is free once its last product is done
-      if (SPLIT ? j > 0 : j > 1) {
-        if (!(ok = done(SPLIT ? j - 1 : j - 2))) break;
-        fence_after();
-      }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         float hi[16], lo_[16];
@@ -426,16 +413,15 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
           f2_unpack(f2_add(s0, s1), x0, x1);
           l = fmaf(x0 + x1, vi[e], l);
         }
-        const uint32_t to = tP + (SPLIT ? 0 : (j & 1) * 32) + 16 * c;
-        tmem_st16(to, hi);
-        if (SPLIT) tmem_st16(to + 32, lo_);
+        tmem_st16(tS + 16 * c, hi);
+        if (SPLIT) tmem_st16(tS + 32 + 16 * c, lo_);
       }
       tmem_wait_st();
       fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(PB_P + 2 * hf + (j & 1)));
     }
-    if (ok) ok = done(nblk - 1);
+    if (ok) ok = wait(PB_O + hf, (nblk - 1) & 1);
   }
   fence_before();
   __syncthreads();                                       // every product is done; shared memory is free
