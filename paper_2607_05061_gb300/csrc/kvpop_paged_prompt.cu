@@ -204,7 +204,10 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     // for right behind the fence of the warp's tile before: that fence waits for every load that is
     // on its way, and this one comes when they are there.
     constexpr int LPR = D / 16, RPI = 32 / LPR, IT = PP_KEYS / RPI, PER = PP_KEYS / BLK;   // lanes of a row, rows at a time
-    const int c = lane % LPR, sub = lane / LPR, tiles = 2 * nblk;
+    // (d = 128: 8 neighbouring lanes hold half of two neighbouring rows, so that their stores, even
+    // chunks and then odd ones, touch every bank)
+    const int c = D == 128 ? (lane & 3) + (lane >> 1 & 4) : lane % LPR;
+    const int sub = D == 128 ? (lane >> 2 & 1) + 2 * (lane >> 4) : lane / LPR, tiles = 2 * nblk;
     const int32_t* const trow = a.b.table + (long long)s * a.b.table_stride;
     uint4 w[IT];
     float scale = 0.f;                                   // lanes 0-3: of the groups' keys, 4-7: of their values
@@ -264,11 +267,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
         uint4 p, q;
         cvt16(w[x], p, q);
         const int row = x * RPI + sub;
-        // (d = 128: lanes of the upper 64 values store their second chunk first, so that the 8
-        // lanes of a row touch all banks)
-        const int first = D == 128 ? c >> 2 : 0;
-        *reinterpret_cast<uint4*>(tile + tile_off(row, 2 * c + first, PP_KEYS)) = first ? q : p;
-        *reinterpret_cast<uint4*>(tile + tile_off(row, 2 * c + 1 - first, PP_KEYS)) = first ? p : q;
+        *reinterpret_cast<uint4*>(tile + tile_off(row, 2 * c, PP_KEYS)) = p;
+        *reinterpret_cast<uint4*>(tile + tile_off(row, 2 * c + 1, PP_KEYS)) = q;
       }
       fence_async_smem();
       __syncwarp();
