@@ -115,10 +115,13 @@ cudaError_t launch_paged_attend(const paged::Pool& pool, const paged::Batch& b, 
                                 long long q_hs, int HQ, void* out, int out_f32, float* lse, void* workspace,
                                 int sms, int32_t* err, cudaStream_t stream);
 
-// The same for sequences with long_rows, where paged_prompt_fits.
+// The same for sequences with long_rows, where paged_prompt_fits.  Its share of the workspace:
+// counters (zero between calls) and partial results.
 bool paged_prompt_fits(const paged::Pool& pool, const paged::Batch& b, int HQ);
+size_t paged_prompt_counters(int sms);
+size_t paged_prompt_parts(int sms);
 cudaError_t launch_paged_prompt(const paged::Pool& pool, const paged::Batch& b, const void* q, long long q_ts,
-                                long long q_hs, int HQ, void* out, int out_f32, float* lse, int32_t* err,
-                                cudaStream_t stream);
+                                long long q_hs, int HQ, void* out, int out_f32, float* lse, void* counters,
+                                void* parts, int sms, int32_t* err, cudaStream_t stream);
 
 }  // namespace kvpop

@@ -159,8 +159,10 @@ __device__ __forceinline__ void seek(const AttendArgs& a, Unit& x, long long w) 
     x.base += x.u.work(a.pool.H);
     x.u = seq_units<ROWS>(a, ++x.s);
   }
-  const int unit = (int)div_pos(w - x.base, x.u.span()), grp = unit / a.pool.H;
-  x.h = unit - grp * a.pool.H;
+  // (a head's row groups are neighbours: the later ones find its blocks in L2)
+  const int unit = (int)div_pos(w - x.base, x.u.span());
+  x.h = unit / x.u.groups;
+  const int grp = unit - x.h * x.u.groups;
   x.start = x.base + (long long)unit * x.u.span();
   x.row0 = grp * ROWS;
   x.rows = min(ROWS, x.u.n * a.G - x.row0);
@@ -197,7 +199,7 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
   using R = Ring<D, W>;
   constexpr int ROWS = 8 * NT, KW = D / 16, VW = D / 32;   // words a lane holds of a K / V row
   constexpr int RS = 8 * (D + 4);                          // a warp's 8 rows in shared memory
-  constexpr bool QS = NT == 4;                             // query operands in shared memory: no registers left
+  constexpr bool QS = NT >= 2;                             // query operands in shared memory: no registers left
   extern __shared__ __align__(128) unsigned char sma[];
   float* accS = reinterpret_cast<float*>(sma + R::OFF_ACC);
   uint2* qS = reinterpret_cast<uint2*>(sma + R::OFF_Q);
@@ -208,7 +210,10 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
   __shared__ Unit unitS[2], aheadS[W];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
   const int H = a.pool.H;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  // Behind the kernel of the long sequences, which started when all that came before it was done,
+  // nothing is to be waited for but that this one does not end first.
+  auto wait_before = [] { asm volatile("griddepcontrol.wait;" ::: "memory"); };
+  if (!a.skip_long) wait_before();
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   // ---- the list, and this CTA's part [w0, w1) of it
@@ -229,10 +234,16 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
     if (w < warp) pre += scanS[w];
     total += scanS[w];
   }
-  if (total == 0) return;
+  if (total == 0) {
+    if (a.skip_long) wait_before();
+    return;
+  }
   const long long share = max(div_pos(total + gridDim.x - 1, gridDim.x), (long long)W);   // a block a warp at least
   long long w0 = share * blockIdx.x, w1 = min(w0 + share, total);
-  if (w0 >= total) return;
+  if (w0 >= total) {
+    if (a.skip_long) wait_before();
+    return;
+  }
 #pragma unroll
   for (int e = 0; e < 2; ++e) {                            // the sequences of its first and its last block
     const long long w = e ? w1 - 1 : w0;
@@ -265,7 +276,10 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
     seek<ROWS>(a, x, w0);
   }
   if (x.start < w0 && (x.u.blocks <= AT_SHORT || w0 >= x.start + x.u.blocks)) w0 = x.end();
-  if (w0 >= w1) return;
+  if (w0 >= w1) {
+    if (a.skip_long) wait_before();
+    return;
+  }
   seek<ROWS>(a, x, w0);
   if (tid < W) aheadS[tid] = x;
   if (tid == 0) unitS[0] = x;
@@ -663,6 +677,7 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
       __syncthreads();                                     // shared memory is free for the next rows
     }
   }
+  if (a.skip_long) wait_before();
 }
 
 template <int D, int NT, int W, bool SPLIT>
@@ -686,20 +701,28 @@ cudaError_t launch(const AttendArgs& a, int grid, cudaStream_t stream) {
 }
 template <int D>
 cudaError_t launch_d(AttendArgs& a, int sms, long long rows, cudaStream_t stream) {
-  a.one = (a.G + (rows <= 8 ? 8 : rows <= 16 ? 16 : 32) - 1) / (rows <= 8 ? 8 : rows <= 16 ? 16 : 32);
-  // (as many warps as the registers allow: 2 x 6 of 168, or 2 x 4 of 255)
   const int grid = AT_CTAS * sms;
-  if (rows <= 8) return a.out_f32 ? launch<D, 1, 6, true>(a, grid, stream) : launch<D, 1, 6, false>(a, grid, stream);
-  if (rows <= 16) return a.out_f32 ? launch<D, 2, 4, true>(a, grid, stream) : launch<D, 2, 4, false>(a, grid, stream);
-  return a.out_f32 ? launch<D, 4, 4, true>(a, grid, stream) : launch<D, 4, 4, false>(a, grid, stream);
+  // Groups of 8 rows a warp takes at once, and its registers (2 CTAs of 6 warps of 168, or of 4 of
+  // 255).  With fp32 results, whose second product and sums need registers too, more than one group
+  // pays from 4 on: 16 sequences of up to 6 tokens and 4 heads (24 rows, 900 to 9000 keys) 71 us in
+  // three units of a group, 78 in two of two, 104 in one of four; bf16 65, 56 and 66, and 16 tokens
+  // (64 rows) 182, 126 and 112.
+  // (Beside long sequences the others have mostly one token.)
+  const int nt = a.skip_long ? (a.G <= 8 ? 1 : 2) : a.out_f32 ? (rows <= 24 ? 1 : 2) : rows <= 8 ? 1 : rows <= 32 ? 2 : 4;
+  a.one = (a.G + 8 * nt - 1) / (8 * nt);
+  if (nt == 1) return a.out_f32 ? launch<D, 1, 6, true>(a, grid, stream) : launch<D, 1, 6, false>(a, grid, stream);
+  if (nt == 2) return a.out_f32 ? launch<D, 2, 6, true>(a, grid, stream) : launch<D, 2, 6, false>(a, grid, stream);
+  return launch<D, 4, 4, false>(a, grid, stream);
 }
 
 size_t counter_bytes(int sms) { return ((size_t)AT_CTAS * sms * 4 + 255) / 256 * 256; }
 
 }  // namespace
 
+static size_t part_bytes(int sms) { return (size_t)AT_CTAS * sms * 2 * AT_MAX_ROWS * (128 + 2) * 4; }
+// [counters here][there] [partial results here][there]
 size_t paged_attend_workspace(int sms) {
-  return counter_bytes(sms) + (size_t)AT_CTAS * sms * 2 * AT_MAX_ROWS * (128 + 2) * 4;
+  return counter_bytes(sms) + paged_prompt_counters(sms) + part_bytes(sms) + paged_prompt_parts(sms);
 }
 
 cudaError_t launch_paged_attend(const Pool& pool, const Batch& b, const void* q, long long q_ts, long long q_hs,
@@ -715,7 +738,9 @@ cudaError_t launch_paged_attend(const Pool& pool, const Batch& b, const void* q,
   a.out_f32 = out_f32;
   a.lse = lse;
   a.count = static_cast<int*>(workspace);
-  a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + counter_bytes(sms));
+  char* const counters = static_cast<char*>(workspace) + counter_bytes(sms);
+  char* const parts = counters + paged_prompt_counters(sms);
+  a.part = reinterpret_cast<float*>(parts);
   a.err = err;
   a.c = (float)(1.4426950408889634 / sqrt((double)pool.d));
   a.G = HQ / pool.H;
@@ -724,7 +749,8 @@ cudaError_t launch_paged_attend(const Pool& pool, const Batch& b, const void* q,
   if (rows > LONG_ROWS && b.starts && paged_prompt_fits(pool, b, HQ)) {
     a.skip_long = 1;
     rows = LONG_ROWS;
-    const cudaError_t e = launch_paged_prompt(pool, b, q, q_ts, q_hs, HQ, out, out_f32, lse, err, stream);
+    const cudaError_t e = launch_paged_prompt(pool, b, q, q_ts, q_hs, HQ, out, out_f32, lse, counters,
+                                              parts + part_bytes(sms), sms, err, stream);
     if (e != cudaSuccess) return e;
   }
   return pool.d == 128 ? launch_d<128>(a, sms, rows, stream) : launch_d<64>(a, sms, rows, stream);

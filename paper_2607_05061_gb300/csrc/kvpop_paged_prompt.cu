@@ -35,6 +35,7 @@ constexpr int PP_MMA_WARP = 8, PP_CONV_WARP = 9, PP_CONV = 3;    // warps 0-7: s
 constexpr int PP_THREADS = 32 * (PP_CONV_WARP + PP_CONV);
 constexpr int PP_RING = 10, PP_SCALES = 16;          // tiles; blocks whose scales are held
 constexpr int PP_TMEM = 512;                             // O_h: 128 h; S_h,b: 256 + 128 h + 64 b
+constexpr int PP_PARTS = 8, PP_LEAST = 8;                // parts of a tile at most; blocks of a part at least
 constexpr float PP_OFF = 7.f, PP_STEP = 8.f;
 // barriers
 constexpr int PB_FULL = 0;                               // [ring] converters -> MMA
@@ -53,6 +54,9 @@ struct PromptArgs {
   void* out;
   float* lse;
   int32_t* err;
+  float* part;                                           // [slots][256][d] sums of parts
+  float2* part_ml;                                       // [slots][256] their bases and normalisers
+  int* count;                                            // [slots] parts there, zero between calls
   float c;                                               // log2(e) / sqrt(d)
   int G, out_f32;
 };
@@ -63,7 +67,8 @@ struct PL {
   static constexpr int OFF_RING = 2 * QB, OFF_BAR = OFF_RING + PP_RING * KB;
   static constexpr int OFF_TMEM = OFF_BAR + 8 * PB_N, OFF_NAN = (OFF_TMEM + 4 + 15) / 16 * 16;
   static constexpr int OFF_SCALE = OFF_NAN + 4 * PP_NANW;   // [16 blocks] 4 key scales, 4 value exponents, 4 2^-those
-  static constexpr int BYTES = OFF_SCALE + PP_SCALES * 48;
+  static constexpr int OFF_KEEP = OFF_SCALE + PP_SCALES * 48;   // what only the end needs
+  static constexpr int BYTES = OFF_KEEP + 32;
   static constexpr int OUT_WARP = 32 * D * 4;            // a warp's finished rows, in the ring
   static_assert(8 * OUT_WARP <= OFF_BAR, "");
 };
@@ -111,11 +116,14 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
   const uint32_t sb = smem_u32(smp);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int H = a.pool.H, G = a.G;
+  // the sequences with few rows may come into the SMs that are done with this
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   auto bar = [&](int i) { return sb + L::OFF_BAR + 8u * (uint32_t)i; };
   uint32_t* nanS = reinterpret_cast<uint32_t*>(smp + L::OFF_NAN);
 
   // ---- the tile: sequence s owns the places from starts[s] G / 256 + s on, which leaves one for
-  // each of its tiles.  Later tokens see more, and go first.
+  // each of its tiles.  Later tokens see more, and go first.  The positions of a long tile are cut
+  // into up to gridDim.y parts.
   const unsigned order = gridDim.x - 1 - blockIdx.x;
   const int place = (int)(order / (unsigned)H), h = (int)(order % (unsigned)H);
   auto first_place = [&](int s) { return (long long)a.b.starts[s] * G / PP_ROWS + s; };
@@ -132,7 +140,10 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
   const int ctx = context(a.b, a.pool, t, a.err);
   const int lim_lo = min(t.len + row0 / G, ctx - 1);     // every row sees 0 .. lim_lo
   const int lim_hi = min(t.len + (row0 + rows - 1) / G, ctx - 1);   // none sees past lim_hi
-  const int nblk = lim_hi / PP_KEYS + 1;
+  const int blocks = lim_hi / PP_KEYS + 1, cut = max(min((int)gridDim.y, blocks / PP_LEAST), 1), part = blockIdx.y;
+  if (part >= cut) return;
+  const int blk0 = (int)((long long)blocks * part / cut), nblk = (int)((long long)blocks * (part + 1) / cut) - blk0;
+  const int key0 = blk0 * PP_KEYS;                       // first position of the part
   const int nan0 = (lim_lo + 1) / PP_KEYS * PP_KEYS;     // first position of the NaN map
 
   if (tid == 0) {
@@ -149,6 +160,17 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     mbar_fence_init();
   }
   if (tid < PP_NANW) nanS[tid] = 0;
+  // The end reads these from here: in registers they would be spilled around the roles' loops.
+  volatile int* keep = reinterpret_cast<volatile int*>(smp + L::OFF_KEEP);
+  if (tid == 0) {
+    keep[0] = t.first;
+    keep[1] = row0;
+    keep[2] = rows;
+    keep[3] = cut;
+    keep[4] = place;
+    keep[5] = h;
+    keep[6] = nan0;
+  }
   if (warp == PP_MMA_WARP) tmem_alloc(sb + L::OFF_TMEM, PP_TMEM);
 
   // ---- query rows as f16, each scaled by a power of two (a softmax thread has its row)
@@ -213,7 +235,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     float scale = 0.f;                                   // lanes 0-3: of the groups' keys, 4-7: of their values
     // Every load is unconditional, from a row that is there: a choice between its value and another
     // would wait for it.  What is not to be seen is cleared when it is used.
-    auto group_pos = [&](int i) { return (i >> 1) * PP_KEYS + (lane & (PER - 1)) * BLK; };
+    auto group_pos = [&](int i) { return key0 + (i >> 1) * PP_KEYS + (lane & (PER - 1)) * BLK; };
     auto look = [&](int i) { return trow[min(group_pos(i), lim_hi) >> a.pool.page_shift]; };   // page of group lane mod 4
     auto is_page = [&](int id) { return (unsigned)id < (unsigned)a.pool.n_pages; };
     auto load = [&](int i, int id) {
@@ -222,7 +244,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
 #pragma unroll
       for (int x = 0; x < IT; ++x) {
         const long long base = __shfl_sync(0xffffffffu, head, x * RPI / BLK);
-        const int pos = (i >> 1) * PP_KEYS + x * RPI + sub;
+        const int pos = key0 + (i >> 1) * PP_KEYS + x * RPI + sub;
         ld16(w[x], pages + (base + (pos & (a.pool.page - 1))) * D + 16 * c);
       }
       scale = (lane & PER ? a.pool.vs : a.pool.ks)[(head + (group_pos(i) & (a.pool.page - 1))) / BLK];
@@ -232,7 +254,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     id_next = look(i + PP_CONV);
 #pragma unroll 1
     for (; i < tiles; i += PP_CONV) {
-      const int st = i % PP_RING, pos0 = (i >> 1) * PP_KEYS;
+      const int st = i % PP_RING, pos0 = key0 + (i >> 1) * PP_KEYS;
       if (i >= PP_RING && !wait(PB_EMPTY + st, (i / PP_RING - 1) & 1)) break;
       const bool seen = group_pos(i) <= lim_hi, in = seen && is_page(id);
       if (seen && !in) report(a.err, ERR_PAGE);
@@ -344,8 +366,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
       const float ks[4] = {ks4.x, ks4.y, ks4.z, ks4.w}, ev[4] = {ev4.x, ev4.y, ev4.z, ev4.w};
       const float vi[4] = {vi4.x, vi4.y, vi4.z, vi4.w};
       tmem_wait_ld();
-      const bool edge = (j + 1) * PP_KEYS - 1 > lim_lo;
-      const int see = lim - j * PP_KEYS;                 // last column the row sees
+      const bool edge = key0 + (j + 1) * PP_KEYS - 1 > lim_lo;
+      const int see = lim - key0 - j * PP_KEYS;                 // last column the row sees
       if (edge) {
 #pragma unroll
         for (int i = 0; i < 64; ++i)
@@ -427,12 +449,25 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
   __syncthreads();                                       // every product is done; shared memory is free
   fence_after();
 
+  const int first = keep[0], row0_ = keep[1], rows_ = keep[2], cut_ = keep[3], h_ = keep[5], nan0_ = keep[6];
+  const long long HQ = (long long)H * G, pair = (long long)keep[4] * H + h_, slot = pair * gridDim.y + blockIdx.y;
+  auto row_of = [&](int r) {                             // of the outputs
+    const int tok = r / G;
+    return (first + tok) * HQ + h_ * G + (r - tok * G);
+  };
+  auto write = [&](int r, int cc, const float4& v) {     // four values of row r
+    const long long row = row_of(r);
+    if (a.out_f32)
+      reinterpret_cast<float4*>(a.out)[row * (D / 4) + cc] = v;
+    else
+      reinterpret_cast<uint2*>(a.out)[row * (D / 4) + cc] = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+  };
   if (warp < PP_MMA_WARP && ok) {
     const uint32_t tO = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (warp >> 2) * 128;
     uint32_t any = 0;
     for (int i = 0; i < PP_NANW; ++i) any |= nanS[i];
     unsigned char* stage = smp + warp * L::OUT_WARP;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float inv = cut_ > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;   // (a part's rows stay as they are)
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {
       float o[32];
@@ -444,9 +479,9 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
       if (any) {                                         // NaN values that this row sees
         for (int w = 0; w < PP_NANW; ++w)
           for (uint32_t bits = nanS[w]; bits; bits &= bits - 1) {
-            const int pos = nan0 + 32 * w + __ffs(bits) - 1, id = page16(pos);
+            const int pos = nan0_ + 32 * w + __ffs(bits) - 1, id = page16(pos);
             if (pos > lim || id < 0) continue;
-            const unsigned char* p = a.pool.v + (((long long)id * H + h) * a.pool.page + (pos & (a.pool.page - 1))) * D + 32 * c;
+            const unsigned char* p = a.pool.v + (((long long)id * H + h_) * a.pool.page + (pos & (a.pool.page - 1))) * D + 32 * c;
 #pragma unroll
             for (int i = 0; i < 32; ++i)
               if ((p[i] & 0x7f) == 0x7f) o[i] = __uint_as_float(0x7fffffffu);
@@ -457,50 +492,91 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
         *reinterpret_cast<float4*>(stage + lane * (4 * D) + (((c * 8 + i) ^ (lane & 7)) << 4)) =
             make_float4(o[4 * i] * inv, o[4 * i + 1] * inv, o[4 * i + 2] * inv, o[4 * i + 3] * inv);
     }
-    const long long HQ = (long long)H * G;
-    if (lim >= 0 && a.lse) {
-      const int r = row0 + tid, tok = r / G;
-      a.lse[(t.first + tok) * HQ + h * G + (r - tok * G)] =
+    if (cut_ > 1) {
+      __stcg(a.part_ml + slot * PP_ROWS + tid, make_float2(m, l));
+    } else if (lim >= 0 && a.lse) {
+      a.lse[row_of(row0_ + tid)] =
           l == 0.f ? -INFINITY : (m - PP_OFF + log2f(l)) * 0.69314718055994530942f;
     }
     __syncwarp();
     constexpr int LPR = D / 4, RPI = 32 / LPR;           // whole rows leave, D / 4 lanes each
     for (int i = 0; i < 32; i += RPI) {
-      const int rw = i + lane / LPR, cc = lane % LPR, r = row0 + warp * 32 + rw;
-      if (warp * 32 + rw >= rows) break;
+      const int rw = i + lane / LPR, cc = lane % LPR, r = row0_ + warp * 32 + rw;
+      if (warp * 32 + rw >= rows_) break;
       const float4 v = *reinterpret_cast<const float4*>(stage + rw * (4 * D) + ((cc ^ (rw & 7)) << 4));
-      const int tok = r / G;
-      const long long row = (t.first + tok) * HQ + h * G + (r - tok * G);
-      if (a.out_f32)
-        reinterpret_cast<float4*>(a.out)[row * (D / 4) + cc] = v;
-      else
-        reinterpret_cast<uint2*>(a.out)[row * (D / 4) + cc] = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+      if (cut_ > 1) __stcg(reinterpret_cast<float4*>(a.part) + (slot * PP_ROWS + warp * 32 + rw) * (D / 4) + cc, v);
+      else write(r, cc, v);
     }
   }
   fence_before();
+  if (cut_ > 1) __threadfence();
   __syncthreads();
   if (warp == PP_MMA_WARP) tmem_dealloc(tmem, PP_TMEM);
+  if (cut_ > 1) {
+    // the part that comes last joins them, in their order (a part whose waits ran out comes too)
+    int* const count = a.count + pair;
+    volatile int* last = reinterpret_cast<volatile int*>(smp + L::OFF_TMEM);
+    __syncthreads();
+    if (tid == 0) *last = atomicAdd(count, 1) == cut_ - 1;
+    __syncthreads();
+    if (*last) {
+      __threadfence();
+      const long long slot0 = pair * gridDim.y;
+      for (int i = tid; i < rows_ * (D / 4); i += PP_THREADS) {
+        const int rw = i / (D / 4), cc = i % (D / 4);
+        float mt = -INFINITY, lt = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int c = 0; c < cut_; ++c) {
+          const float2 ml = __ldcg(a.part_ml + (slot0 + c) * PP_ROWS + rw);
+          const float4 b = __ldcg(reinterpret_cast<const float4*>(a.part) + ((slot0 + c) * PP_ROWS + rw) * (D / 4) + cc);
+          const float mn = fmaxf(mt, ml.x);
+          // (a NaN in a part without a base stays one)
+          const float fo = mt == -INFINITY ? 0.f : ex2(mt - mn), fn = ml.x == -INFINITY ? 0.f : ex2(ml.x - mn);
+          v.x = fmaf(v.x, fo, b.x * fn);
+          v.y = fmaf(v.y, fo, b.y * fn);
+          v.z = fmaf(v.z, fo, b.z * fn);
+          v.w = fmaf(v.w, fo, b.w * fn);
+          lt = fmaf(lt, fo, ml.y * fn);
+          mt = mn;
+        }
+        const float inv = lt == 0.f ? 0.f : 1.f / lt;
+        write(row0_ + rw, cc, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+        if (cc == 0 && a.lse) {
+          a.lse[row_of(row0_ + rw)] =
+              lt == 0.f ? -INFINITY : (mt - PP_OFF + log2f(lt)) * 0.69314718055994530942f;
+        }
+      }
+      if (tid == 0) *count = 0;
+    }
+  }
 }
 
 template <int D, bool SPLIT>
-cudaError_t launch(const PromptArgs& a, long long places, cudaStream_t stream) {
+cudaError_t launch(const PromptArgs& a, dim3 grid, cudaStream_t stream) {
   auto k = paged_prompt_kernel<D, SPLIT>;
   const size_t smem = PL<D>::BYTES;
   static std::atomic<unsigned long long> raised{0};
   const cudaError_t e = raise_smem_limit_once(raised, k, smem);
   if (e != cudaSuccess) return e;
-  k<<<(unsigned)(places * a.pool.H), PP_THREADS, smem, stream>>>(a);
+  k<<<grid, PP_THREADS, smem, stream>>>(a);
   return cudaGetLastError();
 }
+
+// Places for parts of tiles: 3 an SM (60 MB at d = 128).
+long long slots_of(int sms) { return 3ll * sms; }
 
 }  // namespace
 
 bool paged_prompt_fits(const Pool& pool, const Batch& b, int HQ) {
   return ((long long)b.n_tokens * (HQ / pool.H) / PP_ROWS + b.n_seq) * pool.H <= INT32_MAX;
 }
+size_t paged_prompt_counters(int sms) { return ((size_t)slots_of(sms) * 4 + 255) / 256 * 256; }
+size_t paged_prompt_parts(int sms) { return (size_t)slots_of(sms) * PP_ROWS * (128 + 2) * 4; }
 
 cudaError_t launch_paged_prompt(const Pool& pool, const Batch& b, const void* q, long long q_ts, long long q_hs,
-                                int HQ, void* out, int out_f32, float* lse, int32_t* err, cudaStream_t stream) {
+                                int HQ, void* out, int out_f32, float* lse, void* counters, void* parts, int sms,
+                                int32_t* err, cudaStream_t stream) {
   PromptArgs a{};
   a.pool = pool;
   a.b = b;
@@ -513,9 +589,15 @@ cudaError_t launch_paged_prompt(const Pool& pool, const Batch& b, const void* q,
   a.err = err;
   a.c = (float)(1.4426950408889634 / sqrt((double)pool.d));
   a.G = HQ / pool.H;
-  const long long places = (long long)b.n_tokens * a.G / PP_ROWS + b.n_seq;
-  if (pool.d == 128) return out_f32 ? launch<128, true>(a, places, stream) : launch<128, false>(a, places, stream);
-  return out_f32 ? launch<64, true>(a, places, stream) : launch<64, false>(a, places, stream);
+  a.count = static_cast<int*>(counters);
+  a.part = static_cast<float*>(parts);
+  a.part_ml = reinterpret_cast<float2*>(a.part + slots_of(sms) * PP_ROWS * pool.d);
+  // Tiles are cut where there may be too few of them for the SMs; the most there can be counts, as
+  // the lengths are not known here.
+  const long long most = ((long long)b.n_tokens * a.G / PP_ROWS + b.n_seq) * pool.H, cuts = slots_of(sms) / most;
+  const dim3 grid((unsigned)most, (unsigned)(cuts < 1 ? 1 : cuts < PP_PARTS ? cuts : PP_PARTS));
+  if (pool.d == 128) return out_f32 ? launch<128, true>(a, grid, stream) : launch<128, false>(a, grid, stream);
+  return out_f32 ? launch<64, true>(a, grid, stream) : launch<64, false>(a, grid, stream);
 }
 
 }  // namespace kvpop
