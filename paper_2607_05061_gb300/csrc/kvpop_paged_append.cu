@@ -16,6 +16,7 @@
 // scale and codes have one writer; with one token a sequence, D / 8 lanes take it.
 #include "kvpop_paged.cuh"
 #include "kvpop_mma.cuh"
+#include "kvpop_ptx.cuh"
 
 namespace kvpop {
 namespace {
@@ -169,6 +170,19 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t w, float f) {
   return rescale2(w & 0xffffu, f) | rescale2(w >> 16, f) << 16;
 }
 
+// Sends every RPI-th of a lane's `rows` rows to L2, for up to NH heads: the loads that follow, a few
+// rows at a time, then wait for L2 only.
+template <typename T, int IT, int RPI, int NH>
+__device__ __forceinline__ void ahead(const T* p, long long ts, long long hs, int heads, int rows, int c) {
+  constexpr int PER = 128 / (8 * (int)sizeof(T));   // lanes that share a line
+  if (c % PER) return;
+#pragma unroll
+  for (int it = 0; it < IT; ++it)
+#pragma unroll
+    for (int e = 0; e < NH; ++e)
+      if (it * RPI < rows && e < heads) prefetch_l2_line(p + it * RPI * ts + e * hs);
+}
+
 // ONE: one token a sequence.  D / 8 lanes per row; a warp takes one (block, head) of up to 16 rows,
 // or, with ONE, 32 / (D / 8) of them with one row each.
 template <typename T, int D, bool ONE>
@@ -225,6 +239,7 @@ __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendAr
     const T* from = static_cast<const T*>(a.q) + tok * a.q_ts + h0 * a.q_hs;
     const float *cosR = a.cosT + (long long)pos * (a.rot >> 1) + n.angle, *sinR = a.sinT + (cosR - a.cosT);
     bf16* to = a.q_out + (tok * a.HQ + h0) * D + n.own;
+    if (!ONE) ahead<T, IT, RPI, QH>(from + n.own, a.q_ts, a.q_hs, min(a.HQ - h0, QH), end - pos, c);
 #pragma unroll 1
     for (int it = 0; it < IT; ++it) {
       if (pos < end) {
@@ -271,6 +286,7 @@ __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendAr
   const int pos0 = ONE ? p0 : p0 + sub;
   const T* const from = src + (t.first + (pos0 - t.len)) * ts;
   const long long angle0 = (long long)pos0 * (a.rot >> 1) + n.angle;
+  if (!ONE && id >= 0) ahead<T, IT, RPI, 1>(from + n.own, ts, 0, 1, end - pos0, c);
   auto read = [&](int it, float (&x)[8]) {
     const T* row = from + it * RPI * ts;
     const long long at = angle0 + it * RPI * (a.rot >> 1);
