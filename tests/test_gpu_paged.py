@@ -324,6 +324,30 @@ def test_attend_long_rows_over_many_parts(dev, out_dtype):
     check_attend(out, lse, attend_reference(cache, table, held, [1] * 5, q, page), out_dtype)
 
 
+@pytest.mark.parametrize("out_dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("d", [64, 128])
+def test_long_tiles_cut_into_parts(dev, d, out_dtype):
+    """Few tiles over many positions: each tile's positions are cut, one sequence's last part holds
+    nothing that its first rows see, and short sequences run beside them."""
+    held, new, H, G, page = [4000, 1500, 0, 90, -1], [40, 130, 300, 1, 2], 1, 4, 64
+    cache = make_cache(dev, 110, H, d, page, seed=18)
+    table, lens, starts = tables(held, new, page, 110, dev, seed=19)
+    hide_rest(cache, table, held, new, page)
+    cache.v_pages.view(torch.uint8)[int(table[0, 4010 // page]), 0, 4010 % page, 11] = 127    # token 10's
+    q = (torch.randn((sum(new), H * G, d), generator=torch.Generator().manual_seed(8)) * 0.02).bfloat16().to(dev)
+    want = attend_reference(cache, table, held, new, q, page)
+    y, bad = want[0], np.isnan(want[0])
+    assert not bad[:10].any() and bad[10:40, :, 11].all() and bad.sum() == 30 * G
+    for _ in range(2):
+        out, lse = cache.attend(table, lens, q, starts=starts, max_new=300, out_dtype=out_dtype, want_lse=True)
+        got = out.double().cpu().numpy()
+        assert np.array_equal(np.isnan(got), bad)
+        clean = torch.from_numpy(np.where(bad, 0, got))
+        top = np.where(np.isnan(want[3]), np.nanmax(want[3]), want[3])
+        check_attend(clean, lse, (np.where(bad, 0, y), want[1], want[2], top), out_dtype)
+    assert status()[0] == 0
+
+
 def test_idle_places_and_sequences_without_tokens(dev):
     d, H, G, page = 128, 2, 4, 16
     cache = make_cache(dev, 16, H, d, page, seed=9)
