@@ -19,6 +19,8 @@
 // buffer, where a half's rows and its products took turns, 672 us (a prompt of 8192 tokens, 32
 // query and 8 KV heads); blocks of 64 with P in a place of its own, two waits and two signals a
 // block, 622.
+#include <type_traits>
+
 #include "kvpop_mma.cuh"
 #include "kvpop_paged.cuh"
 #include "kvpop_ptx.cuh"
@@ -54,12 +56,19 @@ struct PromptArgs {
   void* out;
   float* lse;
   int32_t* err;
-  float* part;                                           // [slots][256][d] sums of parts
+  float* part;                                           // [slots][d / 8][256][8] sums of parts
   float2* part_ml;                                       // [slots][256] their bases and normalisers
   int* count;                                            // [slots] parts there, zero between calls
   float c;                                               // log2(e) / sqrt(d)
-  int G, out_f32;
+  int G, out_f32, sms;
 };
+
+// 32 bytes, 32-byte aligned
+__device__ __forceinline__ void st32(void* p, const float* v) {
+  asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]),
+               "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+               : "memory");
+}
 
 template <int D>
 struct PL {
@@ -69,8 +78,7 @@ struct PL {
   static constexpr int OFF_SCALE = OFF_NAN + 4 * PP_NANW;   // [16 blocks] 4 key scales, 4 value exponents, 4 2^-those
   static constexpr int OFF_KEEP = OFF_SCALE + PP_SCALES * 48;   // what only the end needs
   static constexpr int BYTES = OFF_KEEP + 32;
-  static constexpr int OUT_WARP = 32 * D * 4;            // a warp's finished rows, in the ring
-  static_assert(8 * OUT_WARP <= OFF_BAR, "");
+  static_assert(PP_PARTS * PP_ROWS * 4 <= OFF_BAR, "");  // factors of the parts, where queries and ring were
 };
 
 // f16 A and B, fp32 D, M x N, optional MN-major B
@@ -109,6 +117,22 @@ __device__ __forceinline__ uint32_t drop_nan(uint32_t w) {
   return w & ~((x >> 7) * 255u);
 }
 
+// Blocks of a part at most, by all lanes of a warp.  A tile costs what ENDS blocks do besides its own, and
+// its parts, if it is cut, JOIN blocks each (one SM reads 64 KB (d = 64) of a part in about a us).
+// Where every part has an SM of its own, the longest is what the call takes; else they fill the
+// SMs in turn, and half of the longest is left at the end.
+template <int D>
+__device__ __forceinline__ int share_of(int tiles, int most, float all, int sms, int parts, int lane) {
+  constexpr float ENDS = D == 128 ? 6.f : 12.f, JOIN = D == 128 ? 3.f : 5.f;
+  const int c = min(lane + 1, parts), b = (most - 1) / c + 1;
+  const float n = c == 1 ? (float)tiles : fmaxf(__fdividef(all, (float)b) + 0.5f * (float)tiles, (float)tiles);
+  const float one = ENDS + (c > 1 ? JOIN * (float)c : 0.f), each = __frcp_rn((float)sms);
+  float cost = n <= (float)sms ? one + (float)b : (all + n * one) * each + 0.5f * ((float)b + one);
+  if (c > 1 && b < PP_LEAST) cost = 3e38f;
+  const unsigned key = __reduce_min_sync(0xffffffffu, (__float_as_uint(cost) & ~31u) | (unsigned)(c - 1));
+  return __shfl_sync(0xffffffffu, b, key & 31u);
+}
+
 template <int D, bool SPLIT>
 __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs a) {
   using L = PL<D>;
@@ -122,17 +146,54 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
   uint32_t* nanS = reinterpret_cast<uint32_t*>(smp + L::OFF_NAN);
 
   // ---- the tile: sequence s owns the places from starts[s] G / 256 + s on, which leaves one for
-  // each of its tiles.  Later tokens see more, and go first.  The positions of a long tile are cut
-  // into up to gridDim.y parts.
+  // each of its tiles.  Later tokens see more, and go first.
   const unsigned order = gridDim.x - 1 - blockIdx.x;
   const int place = (int)(order / (unsigned)H), h = (int)(order % (unsigned)H);
   auto first_place = [&](int s) { return (long long)a.b.starts[s] * G / PP_ROWS + s; };
-  int lo = 0, hi = a.b.n_seq - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (first_place(mid) <= place) lo = mid; else hi = mid - 1;
+  struct Plan {
+    int s, tiles[PP_THREADS / 32], most[PP_THREADS / 32];
+    float blocks[PP_THREADS / 32];
+  };
+  Plan& plan = *reinterpret_cast<Plan*>(smp);
+  int tiles = 0, most = 0;                               // of all sequences; blocks of the longest, of all
+  float all_blocks = 0.f;
+  for (int i = tid; i < a.b.n_seq; i += PP_THREADS) {
+    if (first_place(i) <= place && (i + 1 == a.b.n_seq || place < first_place(i + 1))) plan.s = i;
+    const SeqTokens t = seq_tokens(a.b, i, a.err);
+    if (gridDim.y > 1 && long_rows(t, G)) {
+      const long long end = min((long long)t.len + t.n, (long long)a.b.max_pages << a.pool.page_shift);
+      const int k = (int)(((long long)t.n * G + PP_ROWS - 1) / PP_ROWS) * H, b = (int)(end / PP_KEYS) + 1;
+      tiles += k;
+      most = max(most, b);
+      all_blocks += (float)k * (float)((min((long long)t.len, end) / PP_KEYS + 1 + b) >> 1);
+    }
   }
-  const int s = lo;
+  if (gridDim.y > 1) {
+    tiles = __reduce_add_sync(0xffffffffu, tiles);
+    most = __reduce_max_sync(0xffffffffu, most);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) all_blocks += __shfl_xor_sync(0xffffffffu, all_blocks, o);
+    if (lane == 0) {
+      plan.tiles[warp] = tiles;
+      plan.most[warp] = most;
+      plan.blocks[warp] = all_blocks;
+    }
+  }
+  __syncthreads();
+  const int s = plan.s;                                  // (offsets that do not ascend: any, or none)
+  if ((unsigned)s >= (unsigned)a.b.n_seq) return;
+  int share = INT32_MAX;                                 // blocks of a part at most
+  if (gridDim.y > 1) {
+    tiles = most = 0;
+    all_blocks = 0.f;
+#pragma unroll
+    for (int w = 0; w < PP_THREADS / 32; ++w) {
+      tiles += plan.tiles[w];
+      most = max(most, plan.most[w]);
+      all_blocks += plan.blocks[w];
+    }
+    share = max(share_of<D>(tiles, most, all_blocks, a.sms, (int)gridDim.y, lane), 1);
+  }
   const SeqTokens t = seq_tokens(a.b, s, a.err);
   const long long row0l = (place - first_place(s)) * PP_ROWS, all_rows = (long long)t.n * G;
   if (!long_rows(t, G) || row0l < 0 || row0l >= all_rows) return;
@@ -140,7 +201,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
   const int ctx = context(a.b, a.pool, t, a.err);
   const int lim_lo = min(t.len + row0 / G, ctx - 1);     // every row sees 0 .. lim_lo
   const int lim_hi = min(t.len + (row0 + rows - 1) / G, ctx - 1);   // none sees past lim_hi
-  const int blocks = lim_hi / PP_KEYS + 1, cut = max(min((int)gridDim.y, blocks / PP_LEAST), 1), part = blockIdx.y;
+  const int blocks = lim_hi / PP_KEYS + 1, part = blockIdx.y;
+  const int cut = min((blocks - 1) / share + 1, (int)gridDim.y);
   if (part >= cut) return;
   const int blk0 = (int)((long long)blocks * part / cut), nblk = (int)((long long)blocks * (part + 1) / cut) - blk0;
   const int key0 = blk0 * PP_KEYS;                       // first position of the part
@@ -172,45 +234,53 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     keep[6] = nan0;
   }
   if (warp == PP_MMA_WARP) tmem_alloc(sb + L::OFF_TMEM, PP_TMEM);
-
-  // ---- query rows as f16, each scaled by a power of two (a softmax thread has its row)
-  float rc = 0.f;
-  int lim = -1;
-  if (warp < PP_MMA_WARP) {
-    const int r = row0 + tid;
-    const bool ok = tid < rows;
-    const int tok = ok ? r / G : 0;
-    if (ok) lim = min(t.len + tok, ctx - 1);
-    const uint4* qp = reinterpret_cast<const uint4*>(a.q + (long long)(t.first + tok) * a.q_ts +
-                                                     (long long)(h * G + (ok ? r - tok * G : 0)) * a.q_hs);
-    uint4 v[D / 8];
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < D / 8; ++i) {
-      v[i] = ok ? qp[i] : make_uint4(0, 0, 0, 0);
-      const uint32_t u[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-#pragma unroll
-      for (int k = 0; k < 4; ++k) top = max(top, max(u[k] & 0x7fffu, u[k] >> 16 & 0x7fffu));
-    }
-    const int up = max(min(14 - ((int)(top >> 7) - 127), 110), -113);   // the largest to [2^14, 2^15)
-    const float f = __uint_as_float((uint32_t)(up + 127) << 23);
-    rc = a.c * __uint_as_float((uint32_t)(127 - up) << 23);
-#pragma unroll
-    for (int i = 0; i < D / 8; ++i) {
-      const uint32_t u[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-      uint32_t o[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        o[k] = pack_h2(__uint_as_float(u[k] << 16) * f, __uint_as_float(u[k] & 0xffff0000u) * f);
-      *reinterpret_cast<uint4*>(smp + (tid >> 7) * L::QB + tile_off(tid & 127, i, PP_HALF)) =
-          make_uint4(o[0], o[1], o[2], o[3]);
-    }
-    fence_async_smem();
-  }
   fence_before();
   __syncthreads();
   fence_after();
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smp + L::OFF_TMEM);
+
+  // ---- query rows as f16, each scaled by a power of two.  A warp reads whole rows, 16 bytes a
+  // lane; rc and lim are those of the row that the thread owns in the softmax.
+  float rc = 0.f;
+  int lim = -1;
+  if (warp < PP_MMA_WARP) {
+    constexpr int LPR = D / 8, RPI = 32 / LPR, IT = 32 / RPI;   // lanes of a row, rows at a time
+    const int r = row0 + min(tid, rows - 1), tok = r / G;
+    const long long off = (t.first + tok) * a.q_ts + (long long)(h * G + (r - tok * G)) * a.q_hs;
+    const int c = lane % LPR, sub = lane / LPR;
+    if (tid < rows) lim = min(t.len + tok, ctx - 1);
+    uint4 v[IT];
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+      const long long o = __shfl_sync(0xffffffffu, off, i * RPI + sub);
+      v[i] = *reinterpret_cast<const uint4*>(a.q + o + 8 * c);
+    }
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+      const uint32_t u[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+      uint32_t top = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) top = max(top, max(u[k] & 0x7fffu, u[k] >> 16 & 0x7fffu));
+#pragma unroll
+      for (int k = 1; k < LPR; k <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, k));
+      const int up = max(min(14 - ((int)(top >> 7) - 127), 110), -113);   // the largest to [2^14, 2^15)
+      const int its = __shfl_sync(0xffffffffu, up, lane % RPI * LPR);
+      if (lane / RPI == i) mine = its;
+      const float f = __uint_as_float((uint32_t)(up + 127) << 23);
+      uint32_t o[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        o[k] = pack_h2(__uint_as_float(u[k] << 16) * f, __uint_as_float(u[k] & 0xffff0000u) * f);
+      const int row = warp * 32 + i * RPI + sub;         // (rows that are none: the last one again)
+      *reinterpret_cast<uint4*>(smp + (row >> 7) * L::QB + tile_off(row & 127, c, PP_HALF)) =
+          make_uint4(o[0], o[1], o[2], o[3]);
+    }
+    rc = a.c * __uint_as_float((uint32_t)(127 - mine) << 23);
+    fence_async_smem();
+    // (only the products wait for them: the converters are on their way)
+    asm volatile("bar.arrive 1, %0;" ::"n"(32 * PP_MMA_WARP + 32) : "memory");
+  }
   // page of a position, -1 where the rows do not see it
   auto page16 = [&](int pos) { return pos <= lim_hi ? page_of(a.b, a.pool, s, pos, a.err) : -1; };
   auto wait = [&](int b, int parity) {                   // the whole warp; false: gave up
@@ -303,6 +373,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     // ---------------------------------------------------------------- MMA issue
     const uint32_t idS = idesc_f16(128, PP_KEYS, 0), idO = idesc_f16(128, D, 1);
     const bool lead = elect_one();
+    asm volatile("bar.sync 1, %0;" ::"n"(32 * PP_MMA_WARP + 32) : "memory");
     const uint64_t qd0 = kmajor_desc(sb, PP_HALF, 0), kd0 = kmajor_desc(sb + L::OFF_RING, PP_KEYS, 0);
     const uint64_t vd0 = mnmajor_desc(sb + L::OFF_RING, PP_KEYS, 0);
     auto issue_s = [&](int hf, int j) {                  // logits of half hf against block j
@@ -354,8 +425,9 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     const int hf = warp >> 2;
     const uint32_t trow = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tO = tmem + trow + hf * 128;
-    for (int j = 0; j < nblk; ++j) {
-      if (!(ok = wait(PB_S + 2 * hf + (j & 1), j >> 1 & 1))) break;
+    auto block = [&](int j, auto at_edge) {
+      constexpr bool edge = decltype(at_edge)::value;
+      if (!wait(PB_S + 2 * hf + (j & 1), j >> 1 & 1)) return false;
       fence_after();
       const uint32_t tS = tmem + trow + 256 + hf * 128 + (j & 1) * 64;
       float v[64];
@@ -366,7 +438,6 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
       const float ks[4] = {ks4.x, ks4.y, ks4.z, ks4.w}, ev[4] = {ev4.x, ev4.y, ev4.z, ev4.w};
       const float vi[4] = {vi4.x, vi4.y, vi4.z, vi4.w};
       tmem_wait_ld();
-      const bool edge = key0 + (j + 1) * PP_KEYS - 1 > lim_lo;
       const int see = lim - key0 - j * PP_KEYS;                 // last column the row sees
       if (edge) {
 #pragma unroll
@@ -386,7 +457,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
       if (__any_sync(0xffffffffu, move)) {
         const float mn = move ? top : m, f = m == -INFINITY ? 0.f : ex2(m - mn);   // (1 where it stays)
         if (j > 0) {
-          if (!(ok = wait(PB_O + hf, (j - 1) & 1))) break;   // the product before has to be in O
+          if (!wait(PB_O + hf, (j - 1) & 1)) return false;   // the product before has to be in O
           fence_after();
           const float g = move ? f : 1.f;
 #pragma unroll
@@ -442,7 +513,15 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
       fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(PB_P + 2 * hf + (j & 1)));
-    }
+      return true;
+    };
+    // the blocks that every row sees whole, and the others
+    const int whole = min(max((lim_lo + 1 - key0) / PP_KEYS, 0), nblk);
+    int j = 0;
+#pragma unroll 1
+    for (; j < whole && ok; ++j) ok = block(j, std::false_type{});
+#pragma unroll 1
+    for (; j < nblk && ok; ++j) ok = block(j, std::true_type{});
     if (ok) ok = wait(PB_O + hf, (nblk - 1) & 1);
   }
   fence_before();
@@ -455,19 +534,27 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     const int tok = r / G;
     return (first + tok) * HQ + h_ * G + (r - tok * G);
   };
-  auto write = [&](int r, int cc, const float4& v) {     // four values of row r
-    const long long row = row_of(r);
-    if (a.out_f32)
-      reinterpret_cast<float4*>(a.out)[row * (D / 4) + cc] = v;
-    else
-      reinterpret_cast<uint2*>(a.out)[row * (D / 4) + cc] = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+  const bool wide = (reinterpret_cast<uintptr_t>(a.out) & 31) == 0;
+  auto write = [&](long long row, int c, const float* v) {   // 8 values of a row of the output
+    if (a.out_f32) {
+      float* to = reinterpret_cast<float*>(a.out) + row * D + 8 * c;
+      if (wide) {
+        st32(to, v);
+      } else {
+        reinterpret_cast<float4*>(to)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4*>(to)[1] = make_float4(v[4], v[5], v[6], v[7]);
+      }
+    } else {
+      reinterpret_cast<uint4*>(a.out)[row * (D / 8) + c] =
+          make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+    }
   };
-  if (warp < PP_MMA_WARP && ok) {
+  if (warp < PP_MMA_WARP && ok) {                        // a thread writes its row, 32 bytes at a time
     const uint32_t tO = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (warp >> 2) * 128;
     uint32_t any = 0;
     for (int i = 0; i < PP_NANW; ++i) any |= nanS[i];
-    unsigned char* stage = smp + warp * L::OUT_WARP;
     const float inv = cut_ > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;   // (a part's rows stay as they are)
+    const long long row = row_of(row0_ + min(tid, rows_ - 1));
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {
       float o[32];
@@ -487,25 +574,35 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
               if ((p[i] & 0x7f) == 0x7f) o[i] = __uint_as_float(0x7fffffffu);
           }
       }
+      if (tid < rows_) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        *reinterpret_cast<float4*>(stage + lane * (4 * D) + (((c * 8 + i) ^ (lane & 7)) << 4)) =
-            make_float4(o[4 * i] * inv, o[4 * i + 1] * inv, o[4 * i + 2] * inv, o[4 * i + 3] * inv);
+        for (int i = 0; i < 32; ++i) o[i] *= inv;
+        if (cut_ > 1) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) st32(a.part + ((slot * (D / 8) + 4 * c + i) * PP_ROWS + tid) * 8, o + 8 * i);
+        } else if (a.out_f32) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) write(row, 4 * c + i, o + 8 * i);
+        } else {
+          uint32_t* to = reinterpret_cast<uint32_t*>(a.out) + (row * D + 32 * c) / 2;
+          uint32_t w[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) w[i] = pack_bf16(o[2 * i], o[2 * i + 1]);
+          if (wide) {
+            st32(to, reinterpret_cast<const float*>(w));
+            st32(to + 8, reinterpret_cast<const float*>(w + 8));
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              reinterpret_cast<uint4*>(to)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+          }
+        }
+      }
     }
     if (cut_ > 1) {
       __stcg(a.part_ml + slot * PP_ROWS + tid, make_float2(m, l));
     } else if (lim >= 0 && a.lse) {
-      a.lse[row_of(row0_ + tid)] =
-          l == 0.f ? -INFINITY : (m - PP_OFF + log2f(l)) * 0.69314718055994530942f;
-    }
-    __syncwarp();
-    constexpr int LPR = D / 4, RPI = 32 / LPR;           // whole rows leave, D / 4 lanes each
-    for (int i = 0; i < 32; i += RPI) {
-      const int rw = i + lane / LPR, cc = lane % LPR, r = row0_ + warp * 32 + rw;
-      if (warp * 32 + rw >= rows_) break;
-      const float4 v = *reinterpret_cast<const float4*>(stage + rw * (4 * D) + ((cc ^ (rw & 7)) << 4));
-      if (cut_ > 1) __stcg(reinterpret_cast<float4*>(a.part) + (slot * PP_ROWS + warp * 32 + rw) * (D / 4) + cc, v);
-      else write(r, cc, v);
+      a.lse[row] = l == 0.f ? -INFINITY : (m - PP_OFF + log2f(l)) * 0.69314718055994530942f;
     }
   }
   fence_before();
@@ -521,30 +618,65 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     __syncthreads();
     if (*last) {
       __threadfence();
+      // a row's factors of the parts, and its normaliser
       const long long slot0 = pair * gridDim.y;
-      for (int i = tid; i < rows_ * (D / 4); i += PP_THREADS) {
-        const int rw = i / (D / 4), cc = i % (D / 4);
+      float* const fS = reinterpret_cast<float*>(smp);   // [parts][rows]
+      for (int rw = tid; rw < rows_; rw += PP_THREADS) {
+        float2 ml[PP_PARTS];
+#pragma unroll
+        for (int c = 0; c < PP_PARTS; ++c)
+          if (c < cut_) ml[c] = __ldcg(a.part_ml + (slot0 + c) * PP_ROWS + rw);
         float mt = -INFINITY, lt = 0.f;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int c = 0; c < cut_; ++c) {
-          const float2 ml = __ldcg(a.part_ml + (slot0 + c) * PP_ROWS + rw);
-          const float4 b = __ldcg(reinterpret_cast<const float4*>(a.part) + ((slot0 + c) * PP_ROWS + rw) * (D / 4) + cc);
-          const float mn = fmaxf(mt, ml.x);
-          // (a NaN in a part without a base stays one)
-          const float fo = mt == -INFINITY ? 0.f : ex2(mt - mn), fn = ml.x == -INFINITY ? 0.f : ex2(ml.x - mn);
-          v.x = fmaf(v.x, fo, b.x * fn);
-          v.y = fmaf(v.y, fo, b.y * fn);
-          v.z = fmaf(v.z, fo, b.z * fn);
-          v.w = fmaf(v.w, fo, b.w * fn);
-          lt = fmaf(lt, fo, ml.y * fn);
-          mt = mn;
-        }
+#pragma unroll
+        for (int c = 0; c < PP_PARTS; ++c)
+          if (c < cut_) mt = fmaxf(mt, ml[c].x);
+#pragma unroll
+        for (int c = 0; c < PP_PARTS; ++c)
+          if (c < cut_) {
+            const float f = ml[c].x == -INFINITY ? 0.f : ex2(ml[c].x - mt);   // (times a NaN: a NaN)
+            lt = fmaf(ml[c].y, f, lt);
+            fS[c * PP_ROWS + rw] = f;
+          }
         const float inv = lt == 0.f ? 0.f : 1.f / lt;
-        write(row0_ + rw, cc, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
-        if (cc == 0 && a.lse) {
+        for (int c = 0; c < cut_; ++c) fS[c * PP_ROWS + rw] *= inv;
+        if (a.lse)
           a.lse[row_of(row0_ + rw)] =
               lt == 0.f ? -INFINITY : (mt - PP_OFF + log2f(lt)) * 0.69314718055994530942f;
+      }
+      __syncthreads();
+      constexpr int ITEMS = PP_ROWS * (D / 8);           // of 8 values, two a thread at once
+      for (int i = tid; i < ITEMS; i += 2 * PP_THREADS) {
+        float v[2][8] = {};
+        for (int c0 = 0; c0 < cut_; c0 += 4) {
+          float4 b[2][4][2];
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              if (c0 + c >= cut_) break;
+              const int at = min(i + u * PP_THREADS, ITEMS - 1), part = c0 + c;
+              const float4* p = reinterpret_cast<const float4*>(
+                  a.part + (((slot0 + part) * (D / 8) + at / PP_ROWS) * PP_ROWS + min(at % PP_ROWS, rows_ - 1)) * 8);
+              b[u][c][0] = __ldcg(p);
+              b[u][c][1] = __ldcg(p + 1);
+            }
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+              if (c0 + c < cut_) {
+                const int rw = min(min(i + u * PP_THREADS, ITEMS - 1) % PP_ROWS, rows_ - 1);
+                const float f = fS[(c0 + c) * PP_ROWS + rw];
+                const float4 x = b[u][c][0], y = b[u][c][1];
+                float (&z)[8] = v[u];
+                z[0] = fmaf(x.x, f, z[0]); z[1] = fmaf(x.y, f, z[1]); z[2] = fmaf(x.z, f, z[2]); z[3] = fmaf(x.w, f, z[3]);
+                z[4] = fmaf(y.x, f, z[4]); z[5] = fmaf(y.y, f, z[5]); z[6] = fmaf(y.z, f, z[6]); z[7] = fmaf(y.w, f, z[7]);
+              }
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int at = i + u * PP_THREADS;
+          if (at < ITEMS && at % PP_ROWS < rows_) write(row_of(row0_ + at % PP_ROWS), at / PP_ROWS, v[u]);
         }
       }
       if (tid == 0) *count = 0;
@@ -589,6 +721,7 @@ cudaError_t launch_paged_prompt(const Pool& pool, const Batch& b, const void* q,
   a.err = err;
   a.c = (float)(1.4426950408889634 / sqrt((double)pool.d));
   a.G = HQ / pool.H;
+  a.sms = sms;
   a.count = static_cast<int*>(counters);
   a.part = static_cast<float*>(parts);
   a.part_ml = reinterpret_cast<float2*>(a.part + slots_of(sms) * PP_ROWS * pool.d);
