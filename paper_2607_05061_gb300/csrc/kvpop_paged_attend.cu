@@ -31,6 +31,7 @@
 // SMs; a CTA's warps take its blocks in turn and join their rows in warp order.  A unit that lies in several CTAs' parts is
 // joined, in the order of the parts, by the CTA that arrives last (no CTA waits).
 #include <algorithm>
+#include <type_traits>
 
 #include "kvpop_mma.cuh"
 #include "kvpop_paged.cuh"
@@ -406,7 +407,8 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
     // ---- the stream
     const int done0 = done;
     done += tb - ta;
-    for (; next < done; next += W) {
+    auto block = [&](auto at_edge) {
+      constexpr bool edge = decltype(at_edge)::value;      // some row does not see the whole block
       const int t = ta + next - done0;                     // the block's place in the unit
       cp_wait<R::ST - 1>();
       __syncwarp();
@@ -448,9 +450,21 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
             vr[e][0] = v.x; vr[e][1] = v.y;
           }
         }
+        uint32_t va[VW][2][4];                             // the values as operands
+        auto values = [&] {
+#pragma unroll
+          for (int k = 0; k < VW; ++k)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              // bytes 2 e, 2 e + 1 of word k of the four positions: values 2 (2 k + e) and the next
+              cvt4(__byte_perm(vr[0][k], vr[1][k], e ? 0x7362 : 0x5140), va[k][e][0], va[k][e][1]);
+              cvt4(__byte_perm(vr[2][k], vr[3][k], e ? 0x7362 : 0x5140), va[k][e][2], va[k][e][3]);
+            }
+        };
+        constexpr bool EARLY = W == 6 && !edge;            // while the logits are on their way, where registers allow
+        if (EARLY) values();
         const int ebits = (int)(__float_as_uint(vs) >> 23);
         const float ev = (float)(ebits - 127), vinv = __uint_as_float((uint32_t)(254 - ebits) << 23);
-        const bool edge = t * BLK + BLK - 1 > lim_lo;      // some row does not see the whole block
         // exponents from the row's base, in one rounding: as long as there is none (-inf) every
         // logit is too large
         float y[NT][4];
@@ -556,14 +570,12 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
               }
             }
         }
+        if (!EARLY) values();
 #pragma unroll
         for (int k = 0; k < VW; ++k)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            // bytes 2 e, 2 e + 1 of word k of the four positions: values 2 (2 k + e) and the next
-            uint32_t a0, a1, a2, a3;
-            cvt4(__byte_perm(vr[0][k], vr[1][k], e ? 0x7362 : 0x5140), a0, a1);
-            cvt4(__byte_perm(vr[2][k], vr[3][k], e ? 0x7362 : 0x5140), a2, a3);
+            const uint32_t a0 = va[k][e][0], a1 = va[k][e][1], a2 = va[k][e][2], a3 = va[k][e][3];
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
               if (SPLIT) {
@@ -582,7 +594,13 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
       __syncwarp();                                        // every lane has read the block
       ask();
       stage = stage + 1 == R::ST ? 0 : stage + 1;
-    }
+      next += W;
+    };
+    const int whole = min(done, done0 + (lim_lo + 1) / BLK - ta);   // blocks before this every row sees whole
+#pragma unroll 1
+    while (next < whole) block(std::false_type{});
+#pragma unroll 1
+    while (next < done) block(std::true_type{});
 
     // ---- the warps' rows join, 8 at a time
 #pragma unroll
@@ -700,19 +718,25 @@ cudaError_t launch(const AttendArgs& a, int grid, cudaStream_t stream) {
   return cudaLaunchKernelEx(&cfg, k, a);
 }
 template <int D>
-cudaError_t launch_d(AttendArgs& a, int sms, long long rows, cudaStream_t stream) {
+cudaError_t launch_d(AttendArgs& a, int sms, cudaStream_t stream) {
   const int grid = AT_CTAS * sms;
   // Groups of 8 rows a warp takes at once, and its registers (2 CTAs of 6 warps of 168, or of 4 of
-  // 255).  With fp32 results, whose second product and sums need registers too, more than one group
-  // pays from 4 on: 16 sequences of up to 6 tokens and 4 heads (24 rows, 900 to 9000 keys) 71 us in
-  // three units of a group, 78 in two of two, 104 in one of four; bf16 65, 56 and 66, and 16 tokens
-  // (64 rows) 182, 126 and 112.
-  // (Beside long sequences the others have mostly one token.)
-  const int nt = a.skip_long ? (a.G <= 8 ? 1 : 2) : a.out_f32 ? (rows <= 24 ? 1 : 2) : rows <= 8 ? 1 : rows <= 32 ? 2 : 4;
+  // 255), by the rows that a sequence has on average.  One group streams at the rate of HBM and reads
+  // a cache once for each; more read it less often, and compute longer.  16 sequences of 10000
+  // positions and 4 heads, us for 16 / 24 / 32 / 64 rows: fp32 results, groups of 1 (6 warps) 103,
+  // 155, 200, 383; of 2 (4 warps) 80, 140, 141, 262; (6 warps) 93, 161, 162, 303; of 3 118, 122, 213,
+  // 308; of 4 169, 173, 177, -.  bf16: 1 101, 155, 199, 382; 2 (6 warps) 67, 109, 111, 206; (4 warps)
+  // 70, 117, 119, 220; 3 80, 85, 143, 204; 4 96, 100, 104, 179.  Lengths of 8 to 24 rows, 900 to 9000
+  // positions: fp32 68, 64, 74, 77, 104; bf16 61, 53, 56, 56, 65.
+  const long long rows = !a.b.starts || a.skip_long ? a.G : ((long long)a.b.n_tokens * a.G + a.b.n_seq - 1) / a.b.n_seq;
+  const int nt = rows <= 8 ? 1 : a.out_f32 ? (rows > 20 && rows <= 24 ? 3 : 2)
+                 : rows <= 18 ? 2 : rows <= 24 || (rows > 32 && rows <= 48) ? 3 : 4;
   a.one = (a.G + 8 * nt - 1) / (8 * nt);
-  if (nt == 1) return a.out_f32 ? launch<D, 1, 6, true>(a, grid, stream) : launch<D, 1, 6, false>(a, grid, stream);
-  if (nt == 2) return a.out_f32 ? launch<D, 2, 6, true>(a, grid, stream) : launch<D, 2, 6, false>(a, grid, stream);
-  return launch<D, 4, 4, false>(a, grid, stream);
+  if (a.out_f32)
+    return nt == 1 ? launch<D, 1, 6, true>(a, grid, stream) : nt == 2 ? launch<D, 2, 4, true>(a, grid, stream)
+                                                            : launch<D, 3, 4, true>(a, grid, stream);
+  return nt == 1 ? launch<D, 1, 6, false>(a, grid, stream) : nt == 2 ? launch<D, 2, 6, false>(a, grid, stream)
+         : nt == 3 ? launch<D, 3, 4, false>(a, grid, stream) : launch<D, 4, 4, false>(a, grid, stream);
 }
 
 size_t counter_bytes(int sms) { return ((size_t)AT_CTAS * sms * 4 + 255) / 256 * 256; }
@@ -745,15 +769,13 @@ cudaError_t launch_paged_attend(const Pool& pool, const Batch& b, const void* q,
   a.c = (float)(1.4426950408889634 / sqrt((double)pool.d));
   a.G = HQ / pool.H;
   a.inv_g = 1.f / (float)a.G;
-  long long rows = (long long)a.G * (b.starts ? b.max_new : 1);
-  if (rows > LONG_ROWS && b.starts && paged_prompt_fits(pool, b, HQ)) {
+  if (b.starts && (long long)a.G * b.max_new > LONG_ROWS && paged_prompt_fits(pool, b, HQ)) {
     a.skip_long = 1;
-    rows = LONG_ROWS;
     const cudaError_t e = launch_paged_prompt(pool, b, q, q_ts, q_hs, HQ, out, out_f32, lse, counters,
                                               parts + part_bytes(sms), sms, err, stream);
     if (e != cudaSuccess) return e;
   }
-  return pool.d == 128 ? launch_d<128>(a, sms, rows, stream) : launch_d<64>(a, sms, rows, stream);
+  return pool.d == 128 ? launch_d<128>(a, sms, stream) : launch_d<64>(a, sms, stream);
 }
 
 }  // namespace kvpop
