@@ -211,10 +211,13 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
   __shared__ Unit unitS[2], aheadS[W];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
   const int H = a.pool.H;
-  // Behind the kernel of the long sequences, which started when all that came before it was done,
-  // nothing is to be waited for but that this one does not end first.
-  auto wait_before = [] { asm volatile("griddepcontrol.wait;" ::: "memory"); };
-  if (!a.skip_long) wait_before();
+  // Behind the kernel of the long sequences, which lets this one start when all that came before is
+  // done, nothing is to be waited for but that this one does not end first: its last CTA sees to that,
+  // the others leave their places to those that have not begun.
+  if (!a.skip_long) asm volatile("griddepcontrol.wait;" ::: "memory");
+  auto leave = [&] {
+    if (a.skip_long && blockIdx.x == gridDim.x - 1) asm volatile("griddepcontrol.wait;" ::: "memory");
+  };
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   // ---- the list, and this CTA's part [w0, w1) of it
@@ -236,13 +239,13 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
     total += scanS[w];
   }
   if (total == 0) {
-    if (a.skip_long) wait_before();
+    leave();
     return;
   }
   const long long share = max(div_pos(total + gridDim.x - 1, gridDim.x), (long long)W);   // a block a warp at least
   long long w0 = share * blockIdx.x, w1 = min(w0 + share, total);
   if (w0 >= total) {
-    if (a.skip_long) wait_before();
+    leave();
     return;
   }
 #pragma unroll
@@ -278,7 +281,7 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
   }
   if (x.start < w0 && (x.u.blocks <= AT_SHORT || w0 >= x.start + x.u.blocks)) w0 = x.end();
   if (w0 >= w1) {
-    if (a.skip_long) wait_before();
+    leave();
     return;
   }
   seek<ROWS>(a, x, w0);
@@ -695,7 +698,7 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
       __syncthreads();                                     // shared memory is free for the next rows
     }
   }
-  if (a.skip_long) wait_before();
+  leave();
 }
 
 template <int D, int NT, int W, bool SPLIT>

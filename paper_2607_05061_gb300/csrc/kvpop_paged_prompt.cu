@@ -117,13 +117,12 @@ __device__ __forceinline__ uint32_t drop_nan(uint32_t w) {
   return w & ~((x >> 7) * 255u);
 }
 
-// Blocks of a part at most, by all lanes of a warp.  A tile costs what ENDS blocks do besides its own, and
-// its parts, if it is cut, JOIN blocks each (one SM reads 64 KB (d = 64) of a part in about a us).
-// Where every part has an SM of its own, the longest is what the call takes; else they fill the
-// SMs in turn, and half of the longest is left at the end.
-template <int D>
+// Blocks of a part at most, by all lanes of a warp.  A tile costs what ENDS blocks do besides its
+// own (5 to 7 us; a block takes 0.7 us at d = 64, 1.0 at 128), and its parts, if it is cut, JOIN
+// blocks each: one SM reads them all.  Where every part has an SM of its own, the longest is what
+// the call takes; else they fill the SMs in turn, and half of the longest is left at the end.
 __device__ __forceinline__ int share_of(int tiles, int most, float all, int sms, int parts, int lane) {
-  constexpr float ENDS = D == 128 ? 6.f : 12.f, JOIN = D == 128 ? 3.f : 5.f;
+  constexpr float ENDS = 7.f, JOIN = 3.f;
   const int c = min(lane + 1, parts), b = (most - 1) / c + 1;
   const float n = c == 1 ? (float)tiles : fmaxf(__fdividef(all, (float)b) + 0.5f * (float)tiles, (float)tiles);
   const float one = ENDS + (c > 1 ? JOIN * (float)c : 0.f), each = __frcp_rn((float)sms);
@@ -140,7 +139,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
   const uint32_t sb = smem_u32(smp);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int H = a.pool.H, G = a.G;
-  // the sequences with few rows may come into the SMs that are done with this
+  // What came before is done; the sequences with few rows may come into the SMs that are done with this.
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   auto bar = [&](int i) { return sb + L::OFF_BAR + 8u * (uint32_t)i; };
   uint32_t* nanS = reinterpret_cast<uint32_t*>(smp + L::OFF_NAN);
@@ -150,49 +150,37 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
   const unsigned order = gridDim.x - 1 - blockIdx.x;
   const int place = (int)(order / (unsigned)H), h = (int)(order % (unsigned)H);
   auto first_place = [&](int s) { return (long long)a.b.starts[s] * G / PP_ROWS + s; };
-  struct Plan {
-    int s, tiles[PP_THREADS / 32], most[PP_THREADS / 32];
-    float blocks[PP_THREADS / 32];
-  };
-  Plan& plan = *reinterpret_cast<Plan*>(smp);
-  int tiles = 0, most = 0;                               // of all sequences; blocks of the longest, of all
+  int s = -1, tiles = 0, most = 0;                       // tiles of all sequences, blocks of the longest
   float all_blocks = 0.f;
-  for (int i = tid; i < a.b.n_seq; i += PP_THREADS) {
-    if (first_place(i) <= place && (i + 1 == a.b.n_seq || place < first_place(i + 1))) plan.s = i;
-    const SeqTokens t = seq_tokens(a.b, i, a.err);
-    if (gridDim.y > 1 && long_rows(t, G)) {
-      const long long end = min((long long)t.len + t.n, (long long)a.b.max_pages << a.pool.page_shift);
-      const int k = (int)(((long long)t.n * G + PP_ROWS - 1) / PP_ROWS) * H, b = (int)(end / PP_KEYS) + 1;
-      tiles += k;
-      most = max(most, b);
-      all_blocks += (float)k * (float)((min((long long)t.len, end) / PP_KEYS + 1 + b) >> 1);
+  for (int i0 = 0; i0 < a.b.n_seq; i0 += 32) {           // (each warp for itself)
+    const int i = i0 + lane;
+    const bool in = i < a.b.n_seq;
+    const bool has = in && first_place(i) <= place && (i + 1 == a.b.n_seq || place < first_place(i + 1));
+    const unsigned who = __ballot_sync(0xffffffffu, has);
+    if (who) s = i0 + __ffs(who) - 1;
+    if (gridDim.y > 1) {
+      if (in) {
+        const SeqTokens t = seq_tokens(a.b, i, a.err);
+        if (long_rows(t, G)) {
+          const long long end = min((long long)t.len + t.n, (long long)a.b.max_pages << a.pool.page_shift);
+          const int k = (int)(((long long)t.n * G + PP_ROWS - 1) / PP_ROWS) * H, b = (int)(end / PP_KEYS) + 1;
+          tiles += k;
+          most = max(most, b);
+          all_blocks += (float)k * (float)((min((long long)t.len, end) / PP_KEYS + 1 + b) >> 1);
+        }
+      }
+    } else if (who) {
+      break;
     }
   }
+  if (s < 0) return;                                     // (offsets that do not ascend)
+  int share = INT32_MAX;                                 // blocks of a part at most
   if (gridDim.y > 1) {
     tiles = __reduce_add_sync(0xffffffffu, tiles);
     most = __reduce_max_sync(0xffffffffu, most);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) all_blocks += __shfl_xor_sync(0xffffffffu, all_blocks, o);
-    if (lane == 0) {
-      plan.tiles[warp] = tiles;
-      plan.most[warp] = most;
-      plan.blocks[warp] = all_blocks;
-    }
-  }
-  __syncthreads();
-  const int s = plan.s;                                  // (offsets that do not ascend: any, or none)
-  if ((unsigned)s >= (unsigned)a.b.n_seq) return;
-  int share = INT32_MAX;                                 // blocks of a part at most
-  if (gridDim.y > 1) {
-    tiles = most = 0;
-    all_blocks = 0.f;
-#pragma unroll
-    for (int w = 0; w < PP_THREADS / 32; ++w) {
-      tiles += plan.tiles[w];
-      most = max(most, plan.most[w]);
-      all_blocks += plan.blocks[w];
-    }
-    share = max(share_of<D>(tiles, most, all_blocks, a.sms, (int)gridDim.y, lane), 1);
+    share = max(share_of(tiles, most, all_blocks, a.sms, (int)gridDim.y, lane), 1);
   }
   const SeqTokens t = seq_tokens(a.b, s, a.err);
   const long long row0l = (place - first_place(s)) * PP_ROWS, all_rows = (long long)t.n * G;
@@ -259,9 +247,9 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
       const uint32_t u[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-      uint32_t top = 0;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) top = max(top, max(u[k] & 0x7fffu, u[k] >> 16 & 0x7fffu));
+      uint32_t top = __vmaxu2(__vmaxu2(u[0] & 0x7fff7fffu, u[1] & 0x7fff7fffu),
+                              __vmaxu2(u[2] & 0x7fff7fffu, u[3] & 0x7fff7fffu));
+      top = max(top >> 16, top & 0xffffu);
 #pragma unroll
       for (int k = 1; k < LPR; k <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, k));
       const int up = max(min(14 - ((int)(top >> 7) - 127), 110), -113);   // the largest to [2^14, 2^15)
@@ -691,8 +679,17 @@ cudaError_t launch(const PromptArgs& a, dim3 grid, cudaStream_t stream) {
   static std::atomic<unsigned long long> raised{0};
   const cudaError_t e = raise_smem_limit_once(raised, k, smem);
   if (e != cudaSuccess) return e;
-  k<<<grid, PP_THREADS, smem, stream>>>(a);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(PP_THREADS);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, k, a);
 }
 
 // Places for parts of tiles: 3 an SM (60 MB at d = 128).
