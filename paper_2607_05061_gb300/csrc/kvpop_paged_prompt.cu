@@ -35,7 +35,7 @@ using namespace tc05;
 constexpr int PP_HALF = 128, PP_ROWS = 2 * PP_HALF, PP_KEYS = 64;
 constexpr int PP_MMA_WARP = 8, PP_CONV_WARP = 9, PP_CONV = 3;    // warps 0-7: softmax, 8: MMA, 9-11: converters
 constexpr int PP_THREADS = 32 * (PP_CONV_WARP + PP_CONV);
-constexpr int PP_RING = 10, PP_SCALES = 16;          // tiles; blocks whose scales are held
+constexpr int PP_RING = 10, PP_SCALES = 16;              // tiles at most; blocks whose scales are held
 constexpr int PP_TMEM = 512;                             // O_h: 128 h; S_h,b: 256 + 128 h + 64 b
 constexpr int PP_PARTS = 8, PP_LEAST = 8;                // parts of a tile at most; blocks of a part at least
 constexpr float PP_OFF = 7.f, PP_STEP = 8.f;
@@ -45,7 +45,8 @@ constexpr int PB_EMPTY = PB_FULL + PP_RING;              // [ring] MMA -> conver
 constexpr int PB_S = PB_EMPTY + PP_RING;                 // [2][2] MMA -> softmax: logits of even, odd blocks there
 constexpr int PB_P = PB_S + 4;                           // [2][2] softmax -> MMA: their probabilities there
 constexpr int PB_O = PB_P + 4;                           // [2] MMA -> softmax: a product done
-constexpr int PB_N = PB_O + 2;
+constexpr int PB_RAW = PB_O + 2;                         // [converters][2] bytes there
+constexpr int PB_N = PB_RAW + 2 * PP_CONV;
 constexpr int PP_NANW = (PP_ROWS + 2 * PP_KEYS) / 32;    // words of the map of NaN values
 
 struct PromptArgs {
@@ -73,7 +74,8 @@ __device__ __forceinline__ void st32(void* p, const float* v) {
 template <int D>
 struct PL {
   static constexpr int QB = PP_HALF * D * 2, KB = PP_KEYS * D * 2;
-  static constexpr int OFF_RING = 2 * QB, OFF_BAR = OFF_RING + PP_RING * KB;
+  static constexpr int RING = D == 128 ? 7 : PP_RING, RAW = PP_KEYS * D;   // tiles of f16; bytes of a tile of codes
+  static constexpr int OFF_RING = 2 * QB, OFF_RAW = OFF_RING + RING * KB, OFF_BAR = OFF_RAW + 2 * PP_CONV * RAW;
   static constexpr int OFF_TMEM = OFF_BAR + 8 * PB_N, OFF_NAN = (OFF_TMEM + 4 + 15) / 16 * 16;
   static constexpr int OFF_SCALE = OFF_NAN + 4 * PP_NANW;   // [16 blocks] 4 key scales, 4 value exponents, 4 2^-those
   static constexpr int OFF_KEEP = OFF_SCALE + PP_SCALES * 48;   // what only the end needs
@@ -88,12 +90,6 @@ __device__ __forceinline__ uint32_t idesc_f16(int M, int N, int b_mn_major) {
 __device__ __forceinline__ uint32_t pack_h2(float lo, float hi) {
   __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&v);
-}
-// (read once: no place in L1)
-__device__ __forceinline__ void ld16(uint4& v, const unsigned char* p) {
-  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-               : "l"(p));
 }
 // 16 e4m3 bytes -> 16 f16
 __device__ __forceinline__ void cvt16(const uint4& w, uint4& a, uint4& b) {
@@ -135,6 +131,7 @@ __device__ __forceinline__ int share_of(int tiles, int most, float all, int sms,
 template <int D, bool SPLIT>
 __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs a) {
   using L = PL<D>;
+  constexpr int RING = L::RING;
   extern __shared__ __align__(1024) unsigned char smp[];
   const uint32_t sb = smem_u32(smp);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -197,7 +194,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
   const int nan0 = (lim_lo + 1) / PP_KEYS * PP_KEYS;     // first position of the NaN map
 
   if (tid == 0) {
-    for (int i = 0; i < PP_RING; ++i) {
+    for (int i = 0; i < RING; ++i) {
       mbar_init(bar(PB_FULL + i), 1);
       mbar_init(bar(PB_EMPTY + i), 1);
     }
@@ -205,6 +202,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
       mbar_init(bar(PB_S + i), 1);
       mbar_init(bar(PB_P + i), 4);
     }
+    for (int i = 0; i < 2 * PP_CONV; ++i) mbar_init(bar(PB_RAW + i), 1);
     mbar_init(bar(PB_O + 0), 1);
     mbar_init(bar(PB_O + 1), 1);
     mbar_fence_init();
@@ -280,40 +278,55 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
 
   if (warp >= PP_CONV_WARP) {
     // ---------------------------------------------------------------- converters
-    // Tile i (keys of block i / 2, or its values) is warp i mod 3's.  Its bytes and scales are asked
-    // for right behind the fence of the warp's tile before: that fence waits for every load that is
-    // on its way, and this one comes when they are there.
+    // Tile i (keys of block i / 2, or its values) is warp i mod 3's.  Its bytes are asked for two of
+    // the warp's tiles ahead, as bulk copies, which the fence of a tile does not wait for.
     constexpr int LPR = D / 16, RPI = 32 / LPR, IT = PP_KEYS / RPI, PER = PP_KEYS / BLK;   // lanes of a row, rows at a time
     // (d = 128: 8 neighbouring lanes hold half of two neighbouring rows, so that their stores, even
     // chunks and then odd ones, touch every bank)
     const int c = D == 128 ? (lane & 3) + (lane >> 1 & 4) : lane % LPR;
     const int sub = D == 128 ? (lane >> 2 & 1) + 2 * (lane >> 4) : lane / LPR, tiles = 2 * nblk;
     const int32_t* const trow = a.b.table + (long long)s * a.b.table_stride;
-    uint4 w[IT];
-    float scale = 0.f;                                   // lanes 0-3: of the groups' keys, 4-7: of their values
-    // Every load is unconditional, from a row that is there: a choice between its value and another
-    // would wait for it.  What is not to be seen is cleared when it is used.
+    const int cw = warp - PP_CONV_WARP, per_copy = min(a.pool.page, PP_KEYS);
     auto group_pos = [&](int i) { return key0 + (i >> 1) * PP_KEYS + (lane & (PER - 1)) * BLK; };
     auto look = [&](int i) { return trow[min(group_pos(i), lim_hi) >> a.pool.page_shift]; };   // page of group lane mod 4
     auto is_page = [&](int id) { return (unsigned)id < (unsigned)a.pool.n_pages; };
-    auto load = [&](int i, int id) {
-      const unsigned char* pages = i & 1 ? a.pool.v : a.pool.k;
-      const long long head = ((long long)(is_page(id) ? id : 0) * H + h) * a.pool.page;
-#pragma unroll
-      for (int x = 0; x < IT; ++x) {
-        const long long base = __shfl_sync(0xffffffffu, head, x * RPI / BLK);
-        const int pos = key0 + (i >> 1) * PP_KEYS + x * RPI + sub;
-        ld16(w[x], pages + (base + (pos & (a.pool.page - 1))) * D + 16 * c);
-      }
-      scale = (lane & PER ? a.pool.vs : a.pool.ks)[(head + (group_pos(i) & (a.pool.page - 1))) / BLK];
+    auto head_of = [&](int id) { return ((long long)(is_page(id) ? id : 0) * H + h) * a.pool.page; };
+    // the warp's n-th tile into its buffer n mod 2: whole groups, as far as they are in one page
+    auto fetch = [&](int n, int id) {
+      const int i = cw + n * PP_CONV, pos = group_pos(i);
+      const bool go = lane < PER && (lane * BLK & (per_copy - 1)) == 0 && pos <= lim_hi && is_page(id);
+      const uint32_t to = bar(PB_RAW + 2 * cw + (n & 1));
+      const int copies = __popc(__ballot_sync(0xffffffffu, go));
+      if (lane == 0) mbar_arrive_expect_tx(to, copies * per_copy * D);
+      __syncwarp();
+      if (go)
+        bulk_g2s(sb + L::OFF_RAW + (2 * cw + (n & 1)) * L::RAW + lane * BLK * D,
+                 (i & 1 ? a.pool.v : a.pool.k) + (head_of(id) + (pos & (a.pool.page - 1))) * D, per_copy * D, to);
     };
-    int i = warp - PP_CONV_WARP, id = look(i), id_next;
-    load(i, id);
-    id_next = look(i + PP_CONV);
+    // lanes 0-3: the scales of the groups' keys, 4-7: of their values
+    auto scale_of = [&](int i, int id) {
+      return (lane & PER ? a.pool.vs : a.pool.ks)[(head_of(id) + (group_pos(i) & (a.pool.page - 1))) / BLK];
+    };
+    const int mine = (tiles - cw + PP_CONV - 1) / PP_CONV;   // tiles of the warp
+    int id = look(cw), id1 = look(cw + PP_CONV), id2 = look(cw + 2 * PP_CONV), asked = min(mine, 2), had = 0;
+    float scale = scale_of(cw, id);
+    if (mine > 0) fetch(0, id);
+    if (mine > 1) fetch(1, id1);
 #pragma unroll 1
-    for (; i < tiles; i += PP_CONV) {
-      const int st = i % PP_RING, pos0 = key0 + (i >> 1) * PP_KEYS;
-      if (i >= PP_RING && !wait(PB_EMPTY + st, (i / PP_RING - 1) & 1)) break;
+    for (int n = 0; n < mine; ++n) {
+      const int i = cw + n * PP_CONV, st = i % RING, pos0 = key0 + (i >> 1) * PP_KEYS;
+      if (!wait(PB_RAW + 2 * cw + (n & 1), n >> 1 & 1)) break;
+      had = n + 1;
+      uint4 w[IT];
+      const unsigned char* raw = smp + L::OFF_RAW + (2 * cw + (n & 1)) * L::RAW + sub * D + 16 * c;
+#pragma unroll
+      for (int x = 0; x < IT; ++x) w[x] = *reinterpret_cast<const uint4*>(raw + x * RPI * D);
+      __syncwarp();                                      // every lane has its bytes
+      if (n + 2 < mine) {
+        fetch(n + 2, id2);
+        asked = n + 3;
+      }
+      if (i >= RING && !wait(PB_EMPTY + st, (i / RING - 1) & 1)) break;
       const bool seen = group_pos(i) <= lim_hi, in = seen && is_page(id);
       if (seen && !in) report(a.err, ERR_PAGE);
       if (!in) scale = 0.f;                              // (nothing to see)
@@ -353,10 +366,13 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
       fence_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(PB_FULL + st));
-      id = id_next;
-      load(i + PP_CONV, id);
-      id_next = look(i + 2 * PP_CONV);
+      // (here: the fence above waits for every load that is on its way)
+      id = id1;
+      id1 = id2;
+      id2 = look(i + 3 * PP_CONV);
+      scale = scale_of(i + PP_CONV, id);
     }
+    for (; had < asked; ++had) wait(PB_RAW + 2 * cw + (had & 1), had >> 1 & 1);   // (gave up: no copy is left behind)
   } else if (warp == PP_MMA_WARP) {
     // ---------------------------------------------------------------- MMA issue
     const uint32_t idS = idesc_f16(128, PP_KEYS, 0), idO = idesc_f16(128, D, 1);
@@ -365,9 +381,9 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     const uint64_t qd0 = kmajor_desc(sb, PP_HALF, 0), kd0 = kmajor_desc(sb + L::OFF_RING, PP_KEYS, 0);
     const uint64_t vd0 = mnmajor_desc(sb + L::OFF_RING, PP_KEYS, 0);
     auto issue_s = [&](int hf, int j) {                  // logits of half hf against block j
-      const int st = 2 * j % PP_RING;
+      const int st = 2 * j % RING;
       if (hf == 0) {
-        if (!(ok = ok && wait(PB_FULL + st, (2 * j / PP_RING) & 1))) return;
+        if (!(ok = ok && wait(PB_FULL + st, (2 * j / RING) & 1))) return;
         fence_after();
       }
       if (lead) {
@@ -386,9 +402,9 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
       if (ok) issue_s(1, j);
     }
     for (int j = 0; j < nblk && ok; ++j) {
-      const int st = (2 * j + 1) % PP_RING;
+      const int st = (2 * j + 1) % RING;
       const uint64_t vd = desc_at(vd0, st * L::KB);
-      if (!(ok = wait(PB_FULL + st, ((2 * j + 1) / PP_RING) & 1))) break;
+      if (!(ok = wait(PB_FULL + st, ((2 * j + 1) / RING) & 1))) break;
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
         if (!(ok = ok && wait(PB_P + 2 * hf + (j & 1), j >> 1 & 1))) break;
