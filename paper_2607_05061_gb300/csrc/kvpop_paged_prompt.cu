@@ -36,7 +36,7 @@ constexpr int PP_HALF = 128, PP_ROWS = 2 * PP_HALF, PP_KEYS = 64;
 constexpr int PP_MMA_WARP = 8, PP_CONV_WARP = 9, PP_CONV = 3;    // warps 0-7: softmax, 8: MMA, 9-11: converters
 constexpr int PP_THREADS = 32 * (PP_CONV_WARP + PP_CONV);
 constexpr int PP_RING = 10, PP_SCALES = 16;              // tiles at most; blocks whose scales are held
-constexpr int PP_TMEM = 512;                             // O_h: 128 h; S_h,b: 256 + 128 h + 64 b
+constexpr int PP_TMEM = 512;                             // O_h: 128 h (d = 64: and Q_h, 128 h + 64); S_h,b: 256 + 128 h + 64 b
 constexpr int PP_PARTS = 8, PP_LEAST = 8;                // parts of a tile at most; blocks of a part at least
 constexpr float PP_OFF = 7.f, PP_STEP = 8.f;
 // barriers
@@ -74,6 +74,9 @@ __device__ __forceinline__ void st32(void* p, const float* v) {
 template <int D>
 struct PL {
   static constexpr int QB = PP_HALF * D * 2, KB = PP_KEYS * D * 2;
+  // Queries in tensor memory where there is room (d = 64): from shared memory their 128 rows bound the
+  // products with 64 keys (the 8 of a block 527 clocks, 399 with them there; 8192 tokens 349 us, 329).
+  static constexpr bool Q_TMEM = D == 64;
   static constexpr int RING = D == 128 ? 7 : PP_RING, RAW = PP_KEYS * D;   // tiles of f16; bytes of a tile of codes
   static constexpr int OFF_RING = 2 * QB, OFF_RAW = OFF_RING + RING * KB, OFF_BAR = OFF_RAW + 2 * PP_CONV * RAW;
   static constexpr int OFF_TMEM = OFF_BAR + 8 * PB_N, OFF_NAN = (OFF_TMEM + 4 + 15) / 16 * 16;
@@ -263,7 +266,23 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
           make_uint4(o[0], o[1], o[2], o[3]);
     }
     rc = a.c * __uint_as_float((uint32_t)(127 - mine) << 23);
-    fence_async_smem();
+    if (L::Q_TMEM) {                                     // a thread moves its row on
+      __syncwarp();
+      float q[32];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint4 u = *reinterpret_cast<const uint4*>(smp + (tid >> 7) * L::QB + tile_off(tid & 127, i, PP_HALF));
+        q[4 * i] = __uint_as_float(u.x);
+        q[4 * i + 1] = __uint_as_float(u.y);
+        q[4 * i + 2] = __uint_as_float(u.z);
+        q[4 * i + 3] = __uint_as_float(u.w);
+      }
+      tmem_st32(tmem + ((uint32_t)((warp & 3) * 32) << 16) + (warp >> 2) * 128 + 64, q);
+      tmem_wait_st();
+      fence_before();
+    } else {
+      fence_async_smem();
+    }
     // (only the products wait for them: the converters are on their way)
     asm volatile("bar.arrive 1, %0;" ::"n"(32 * PP_MMA_WARP + 32) : "memory");
   }
@@ -378,6 +397,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     const uint32_t idS = idesc_f16(128, PP_KEYS, 0), idO = idesc_f16(128, D, 1);
     const bool lead = elect_one();
     asm volatile("bar.sync 1, %0;" ::"n"(32 * PP_MMA_WARP + 32) : "memory");
+    fence_after();
     const uint64_t qd0 = kmajor_desc(sb, PP_HALF, 0), kd0 = kmajor_desc(sb + L::OFF_RING, PP_KEYS, 0);
     const uint64_t vd0 = mnmajor_desc(sb + L::OFF_RING, PP_KEYS, 0);
     auto issue_s = [&](int hf, int j) {                  // logits of half hf against block j
@@ -389,9 +409,12 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
       if (lead) {
         const uint64_t kd = desc_at(kd0, st * L::KB), qd = desc_at(qd0, hf * L::QB);
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks)
-          mma_bf16(tmem + 256 + hf * 128 + (j & 1) * 64, kmajor_step(qd, PP_HALF, ks), kmajor_step(kd, PP_KEYS, ks), idS,
-                   ks > 0);
+        for (int ks = 0; ks < D / 16; ++ks) {
+          const uint32_t to = tmem + 256 + hf * 128 + (j & 1) * 64;
+          const uint64_t kk = kmajor_step(kd, PP_KEYS, ks);
+          if (L::Q_TMEM) mma_bf16_ts(to, tmem + hf * 128 + 64 + 8 * ks, kk, idS, ks > 0);
+          else mma_bf16(to, kmajor_step(qd, PP_HALF, ks), kk, idS, ks > 0);
+        }
         commit(bar(PB_S + 2 * hf + (j & 1)));
         if (hf == 1) commit(bar(PB_EMPTY + st));
       }
