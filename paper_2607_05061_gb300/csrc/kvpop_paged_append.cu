@@ -189,6 +189,8 @@ template <typename T, int D, bool ONE>
 __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendArgs a) {
   constexpr int LPR = D / 8, RPI = 32 / LPR, IT = ONE ? 1 : BLK / RPI, QH = ONE ? 1 : AP_QH;
   const int lane = threadIdx.x & 31, c = lane % LPR, sub = lane / LPR;
+  constexpr bool KEEP = !ONE && D == 64;            // rotated rows stay in shared memory: 8 values a lane and turn
+  __shared__ float4 keepS[KEEP ? AP_WARPS : 1][KEEP ? 2 * IT : 1][32];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   // a slot: a head of K or of V, or QH heads of q, which share their positions' cosines and sines
@@ -281,8 +283,11 @@ __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendAr
   const int lead = ONE ? lane - c : 0;
   float was = lane == lead && id >= 0 && head > 0 ? *scale : 0.f;
   const Lane n = lane_of(a, c, !is_v);
-  // The rows are read twice, for the largest value and for the codes: kept between, they would
-  // take the registers of half the warps, whose loads are what the first pass waits for.
+  // The rows are used twice, for the largest value and for the codes.  At d = 64 they stay in 4 KB of
+  // shared memory a warp (4 prompts of 4000 tokens, 8 and 32 heads 42 us, 44 read again); at d = 128
+  // they are read again, from L2: 8 KB a warp cost a quarter of the warps, whose loads are what the
+  // first pass waits for (16384 tokens 98 us, 88 read again; half of the rows kept 88), and registers
+  // more of them (170).
   const int pos0 = ONE ? p0 : p0 + sub;
   const T* const from = src + (t.first + (pos0 - t.len)) * ts;
   const long long angle0 = (long long)pos0 * (a.rot >> 1) + n.angle;
@@ -295,6 +300,15 @@ __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendAr
     other.load(row + n.other);
     rotated(a, n, turn_of(a, n, a.cosT + at, a.sinT + at), own, other, x);
   };
+  auto value = [&](int it, float (&x)[8], bool again) {
+    if (!KEEP || !again) {
+      read(it, x);
+    } else {
+      const float4 u = keepS[threadIdx.x >> 5][2 * it][lane], w = keepS[threadIdx.x >> 5][2 * it + 1][lane];
+      x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
+      x[4] = w.x; x[5] = w.y; x[6] = w.z; x[7] = w.w;
+    }
+  };
   auto largest = [&](float limit) {
     float m = 0.f;
     if (id >= 0)
@@ -302,7 +316,11 @@ __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendAr
       for (int it = 0; it < IT; ++it)
         if (pos0 + it * RPI < end) {
           float x[8];
-          read(it, x);
+          value(it, x, limit > 0.f);
+          if (KEEP && limit == 0.f) {
+            keepS[threadIdx.x >> 5][2 * it][lane] = make_float4(x[0], x[1], x[2], x[3]);
+            keepS[threadIdx.x >> 5][2 * it + 1][lane] = make_float4(x[4], x[5], x[6], x[7]);
+          }
 #pragma unroll
           for (int i = 0; i < 8; ++i) m = fmaxf(m, limit > 0.f && !(fabsf(x[i]) < limit) ? 0.f : fabsf(x[i]));
         }
@@ -337,7 +355,7 @@ __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendAr
   for (int it = 0; it < IT; ++it)
     if (pos0 + it * RPI < end) {
       float x[8];
-      read(it, x);
+      value(it, x, true);
       *reinterpret_cast<uint2*>(to + it * RPI * D) = codes8(x, inv, special);
     }
   if (lane == lead) *scale = sc;
