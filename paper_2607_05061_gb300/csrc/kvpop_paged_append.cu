@@ -12,8 +12,12 @@
 // for an earlier owner does not matter; rows past the new tokens are not touched.
 //
 // Bound by memory: K, V and q are read once, codes and rotated queries written once.  One warp
-// takes one head of K, V or q over the (at most 16) new tokens of one block, so that a block's
-// scale and codes have one writer; with one token a sequence, D / 8 lanes take it.
+// takes one head of K or V, or two of q, over the (at most 16) new tokens of one block, so that a
+// block's scale and codes have one writer; with one token a sequence, D / 8 lanes take a head.  16384
+// tokens of 5 prompts with 32 query and 8 KV heads (bf16) take 88 us, 413 MB at 4.7 TB/s: the warps
+// wait for their loads (less since they send their rows to L2 ahead: 98 before), and the issue slots
+// are half taken by rotations and conversions.  One or four query heads a warp were slower.  64
+// sequences' single tokens take 2.7 us, a launch and three loads in a row.
 #include "kvpop_paged.cuh"
 #include "kvpop_mma.cuh"
 #include "kvpop_ptx.cuh"

@@ -28,8 +28,14 @@
 // fp32 sum (5e-7).
 //
 // The blocks of all (sequence, KV head, row group) units form one list that is cut evenly over the
-// SMs; a CTA's warps take its blocks in turn and join their rows in warp order.  A unit that lies in several CTAs' parts is
-// joined, in the order of the parts, by the CTA that arrives last (no CTA waits).
+// SMs; a CTA's warps take its blocks in turn and join their rows in warp order.  A unit that lies in
+// several CTAs' parts is joined, in the order of the parts, by the CTA that arrives last (no CTA
+// waits).
+//
+// 64 sequences of 8192 positions, 32 query and 8 KV heads: 167 us, 0.95 of the copy rate; one of
+// 131072 54 us (40 by the copy rate: 7 until the stream runs, 7 for the join of 38 parts a head).
+// One CTA of 12 warps an SM took the same for the former and 93 instead of 66 for 40 ragged ones: it
+// streams nothing while its rows join.
 #include <algorithm>
 #include <type_traits>
 
@@ -45,7 +51,10 @@ using namespace paged;
 // What the two ends of a unit cost, in blocks (us at 0, 16, 32, 64: 40 ragged sequences of up to
 // 20000 tokens 82, 71, 66, 67; 128 of 200 to 1500 70, 53, 51, 53; 64 of 8192 170, 169, 170, 172).
 constexpr int AT_ENDS = 32;
-constexpr int AT_SHORT = 48;           // blocks of a unit that one CTA takes whole
+// Blocks of a unit that one CTA takes whole: always, and where there is work for all CTAs.  us with
+// units of up to 0, 24, 48, 96 blocks never cut: 64 sequences of 512 (33 blocks) 25.8, 26.0, 23.1, 23.1;
+// 8 of 700 11.2, 11.2, 13.2, 13.2; one of 332 8.8, 8.5, 8.5, 8.5; 128 of 200 to 1500 52.1, 52.0, 52.6, 55.7.
+constexpr int AT_TINY = 24, AT_SHORT = 48;
 constexpr int AT_CTAS = 2;             // resident per SM: one streams while the other joins its rows
 constexpr int AT_MAX_ROWS = 32;        // query rows of a unit at most
 constexpr float AT_OFF = 7.f, AT_STEP = 8.f;
@@ -160,7 +169,6 @@ __device__ __forceinline__ void seek(const AttendArgs& a, Unit& x, long long w) 
     x.base += x.u.work(a.pool.H);
     x.u = seq_units<ROWS>(a, ++x.s);
   }
-  // (a head's row groups are neighbours: the later ones find its blocks in L2)
   const int unit = (int)div_pos(w - x.base, x.u.span());
   x.h = unit / x.u.groups;
   const int grp = unit - x.h * x.u.groups;
@@ -270,7 +278,8 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
   x.u = seq_units<ROWS>(a, x.s);
   seek<ROWS>(a, x, w1 - 1);
   // a short unit is not cut: it belongs to the part that it begins in
-  if (x.u.blocks <= AT_SHORT) w1 = x.end();
+  auto uncut = [&] { return x.u.blocks <= AT_TINY || (x.u.blocks <= AT_SHORT && x.u.span() <= share); };
+  if (uncut()) w1 = x.end();
   if (x.start > w0) {
     if (foundsS[0] != x.s) {
       x.s = foundsS[0];
@@ -279,7 +288,7 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
     }
     seek<ROWS>(a, x, w0);
   }
-  if (x.start < w0 && (x.u.blocks <= AT_SHORT || w0 >= x.start + x.u.blocks)) w0 = x.end();
+  if (x.start < w0 && (uncut() || w0 >= x.start + x.u.blocks)) w0 = x.end();
   if (w0 >= w1) {
     leave();
     return;

@@ -5,9 +5,9 @@
 // the sum of two (fp32 results, SPLIT).  A CTA owns 256 consecutive rows (token, query head) of
 // one (sequence, KV head), as two halves of 128 rows, and streams the positions they see in blocks
 // of 64, the same bytes for both halves.  Roles:
-//  * 3 converter warps bring the bytes of keys and values into registers, a tile each, and write
-//    them as f16 into a ring of 10 128B-swizzled tiles (a block's keys, then its values), with the
-//    scales beside them.
+//  * 3 converter warps: bulk copies bring the bytes of keys and values into shared memory, two tiles
+//    ahead for each warp, which writes them as f16 into a ring of 7 or 10 128B-swizzled tiles (a
+//    block's keys, then its values), with the scales beside them.
 //  * 1 MMA warp: S = Q K^T (M 128, N 64, K d) per half, and O += P V (N d, K 64) with P in tensor
 //    memory and the values read MN-major from their rows.
 //  * 2 x 4 softmax warps, a thread per row: logits into registers, the row's maximum,
@@ -15,10 +15,21 @@
 // Tensor memory: O (2 x 128 columns) and two buffers of logits (4 x 64), P in the place of its
 // logits.  The logits of block j + 2 follow the product with block j into its buffer in the order
 // the MMAs are issued, and those of block j + 1 are there when a row is done with block j, so a
-// block costs a softmax warp one wait and one signal.  Measured before that: blocks of 128 in one
-// buffer, where a half's rows and its products took turns, 672 us (a prompt of 8192 tokens, 32
-// query and 8 KV heads); blocks of 64 with P in a place of its own, two waits and two signals a
-// block, 622.
+// block costs a softmax warp one wait and one signal.
+//
+// What bounds it, for a block of 64 positions (d = 128, about 1950 clocks; the two products' share of
+// the tensor rate is 1024): the products, which the MMA warp issues for 1630 clocks, 1070 of them for
+// S, whose 128 query rows come from shared memory for every 64 keys (66 clocks a step of 16, 32 by
+// the tensor rate), and the softmax's 1270 clocks a warp, which wait for each other across the
+// halves.  A tile costs 7 to 9 us besides: queries, first products, output.
+// A prompt of 8192 tokens with 32 query and 8 KV heads takes 494 us (bf16 results; 630 with fp32
+// ones), 58% of the bf16 rate; at d = 64 329.  Measured before, in order: blocks of 128 in one
+// buffer, where a half's rows and its products took turns, 672; blocks of 64 with P in a place of its
+// own, two waits and two signals a block, 622; P over its logits 575; queries and results read and
+// written by rows, the converters' first tiles beside them 549; blocks that all rows see whole apart,
+// without the masks' selects, 497.  Not kept: softmax warps that ask for the next logits before the
+// exponentials (642 then) or signal behind the next block's loads (504); register splits between the
+// roles (631); two threads a row (1799); a CTA that takes tile after tile (770: spills).
 #include <type_traits>
 
 #include "kvpop_mma.cuh"

@@ -82,12 +82,14 @@ class PagedCache:
         return cls(*pages, *scales, workspace=workspace)
 
     # ------------------------------------------------------------------ arguments
-    def _here(self, what, stream, *tensors):
-        """The stream's handle, once every tensor is on the cache's device and that is the current one."""
-        at = self._index
+    def _elsewhere(self, what, *tensors):
         for t in tensors:
-            if t is not None and t.get_device() != at:
+            if t is not None and t.get_device() != self._index:
                 raise ValueError(f"{what}: a tensor is on {t.device}, the cache on {self.device}")
+
+    def _on(self, what, stream):
+        """The stream's handle, if the cache's device is the current one."""
+        at = self._index
         if at < 0 or _current_device() != at:
             raise ValueError(f"{what}: the cache is on {self.device}, which is not the current CUDA device")
         return _raw_stream(at) if stream is None and _raw_stream is not None else _stream(stream)
@@ -145,19 +147,28 @@ class PagedCache:
         rot = positions = 0
         cos_ptr = sin_ptr = None
         if cos is not None and sin is not None:
-            positions, rot = cos.shape[0], 2 * cos.shape[1]
+            angles = cos.shape
+            positions, rot = angles[0], 2 * angles[1]
             if positions < 1 or rot < 16 or rot > self.d or rot % 16:
                 raise ValueError(f"{what}: cos is {tuple(cos.shape)}: 2 * {rot // 2} values of {self.d} cannot be "
                                  "rotated (a multiple of 16 can)")
-            _want(what, "cos", cos, torch.float32, (positions, rot // 2))
-            _want(what, "sin", sin, torch.float32, (positions, rot // 2))
+            if cos.dtype is not torch.float32 or sin.dtype is not torch.float32 or sin.shape != angles or \
+                    len(angles) != 2 or not cos.is_contiguous() or not sin.is_contiguous():
+                _want(what, "cos", cos, torch.float32, (positions, rot // 2))
+                _want(what, "sin", sin, torch.float32, (positions, rot // 2))
             cos_ptr, sin_ptr = cos.data_ptr(), sin.data_ptr()
         elif cos is not None or sin is not None:
             raise ValueError(f"{what}: cos and sin come together")
         batch = self._batch(what, table, lens, starts, n_tokens, max_new)
-        at = self._here(what, stream, table, lens, starts, q, k, v, cos, sin, q_out)
+        at = self._index
+        if not (table.get_device() == lens.get_device() == k.get_device() == v.get_device() == at and
+                (q is None or q.get_device() == q_out.get_device() == at) and
+                (cos is None or cos.get_device() == sin.get_device() == at) and
+                (starts is None or starts.get_device() == at)):
+            self._elsewhere(what, table, lens, starts, q, k, v, cos, sin, q_out)
+        on = self._on(what, stream)
         status = kvpop_paged_append(self._pool_ptr, batch, qr, heads, kr, vr, code, cos_ptr, sin_ptr, rot, positions,
-                                    1 if interleaved else 0, to, at)
+                                    1 if interleaved else 0, to, on)
         if status != 0:
             _ck(status, "kvpop_paged_append")
         return q_out
@@ -184,9 +195,13 @@ class PagedCache:
         if lse is not None:
             _want(what, "lse", lse, torch.float32, (n_tokens, heads))
         batch = self._batch(what, table, lens, starts, n_tokens, max_new)
-        at = self._here(what, stream, table, lens, starts, q, out, lse)
+        at = self._index
+        if not (table.get_device() == lens.get_device() == q.get_device() == out.get_device() == at and
+                (starts is None or starts.get_device() == at) and (lse is None or lse.get_device() == at)):
+            self._elsewhere(what, table, lens, starts, q, out, lse)
+        on = self._on(what, stream)
         status = kvpop_paged_attend(self._pool_ptr, batch, qr, heads, out.data_ptr(), code,
-                                    None if lse is None else lse.data_ptr(), *self._work, at)
+                                    None if lse is None else lse.data_ptr(), *self._work, on)
         if status != 0:
             _ck(status, "kvpop_paged_attend")
         return out, lse
