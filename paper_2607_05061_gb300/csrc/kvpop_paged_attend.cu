@@ -57,13 +57,14 @@ constexpr int AT_ENDS = 32;
 constexpr int AT_TINY = 24, AT_SHORT = 48;
 constexpr int AT_CTAS = 2;             // resident per SM: one streams while the other joins its rows
 constexpr int AT_MAX_ROWS = 32;        // query rows of a unit at most
+constexpr int AT_JOIN = 8;            // parts that are joined at once
 constexpr float AT_OFF = 7.f, AT_STEP = 8.f;
 
 // The rings: a block's 16 rows of K, then of V.  The 16-byte chunk c of row r lies at chunk
 // c ^ (r mod 8) of its 128 bytes (d = 128), or c ^ (r / 2 mod 4) of its 64 (d = 64).
 template <int D, int W>
 struct Ring {
-  static constexpr int BLOCK = 2 * BLK * D, ST = (W == 6 ? 3 : 5) * (128 / D);
+  static constexpr int BLOCK = 2 * BLK * D, ST = W == 8 ? 5 : (W == 6 ? 3 : 5) * (128 / D);
   static constexpr int OFF_ACC = W * ST * BLOCK;                       // a warp's 8 rows: 8 (d + 4) floats
   static constexpr int OFF_Q = OFF_ACC + W * 8 * (D + 4) * 4;          // 4 groups of query operands
   static constexpr int BYTES = OFF_Q + 4 * (D / 16) * 256;
@@ -85,7 +86,7 @@ struct AttendArgs {
   long long q_ts, q_hs;
   void* out;
   float* lse;
-  float* part;                         // [grid][2][rows][D + 2]
+  float* part;                         // [grid][2][rows][D + 4]
   int* count;                          // [grid], zero between calls
   int32_t* err;
   float c;                             // log2(e) / sqrt(d)
@@ -162,6 +163,12 @@ struct Unit {
   int lim_hi;                          // its rows see at most 0 .. lim_hi
   __device__ __forceinline__ long long end() const { return start + u.span(); }
 };
+// A unit that lies in several CTAs' parts, the first of them p0.
+struct Cut {
+  Unit x;
+  long long p0;
+  int parts, last;
+};
 // The unit that list position w lies in, from an earlier one (or from a sequence and its base).
 template <int ROWS>
 __device__ __forceinline__ void seek(const AttendArgs& a, Unit& x, long long w) {
@@ -215,7 +222,8 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
   __shared__ float mS[W][ROWS], lS[W][ROWS];
   __shared__ float scaleS[W][R::ST][2];
   __shared__ long long scanS[W], foundS[2];
-  __shared__ int foundsS[2], lastS;
+  __shared__ int foundsS[2];
+  __shared__ Cut cutS[2];
   __shared__ Unit unitS[2], aheadS[W];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
   const int H = a.pool.H;
@@ -352,6 +360,7 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
 #pragma unroll 1
   for (int i = 0; i < R::ST; ++i) ask();
 
+  int cuts = 0, came[2] = {0, 0};                          // units in several parts; parts that came before this one
   int next = warp, done = 0, stage = 0, turn = 0;          // the warp's next block of the CTA's; blocks so far
   for (long long w = w0; w < w1; turn ^= 1) {              // (never begins behind a unit's blocks)
     x = unitS[turn];
@@ -643,7 +652,7 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
       const Unit& y = unitS[turn ^ 1];
       const bool whole = ta == 0 && tb == y.u.blocks;
       const long long p0 = whole ? 0 : div_pos(y.start, share);   // the part that the unit begins in
-      float* mypart = a.part + ((long long)blockIdx.x * 2 + (blockIdx.x == p0 ? 1 : 0)) * ROWS * (D + 2);
+      float* mypart = a.part + ((long long)blockIdx.x * 2 + (blockIdx.x == p0 ? 1 : 0)) * ROWS * (D + 4);
       for (int i = tid; i < 8 * (D / 4); i += 32 * W) {
         const int r = i / (D / 4), cc = i % (D / 4), col = 8 * j + r;
         if (col >= y.rows) continue;
@@ -664,47 +673,76 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
         if (whole) {
           write_out<D>(a, y, col, cc, v, mt, lt);
         } else {
-          float* p = mypart + (long long)col * (D + 2);
-          __stcg(reinterpret_cast<float2*>(p + 4 * cc), make_float2(v.x, v.y));
-          __stcg(reinterpret_cast<float2*>(p + 4 * cc + 2), make_float2(v.z, v.w));
+          float* p = mypart + (long long)col * (D + 4);
+          __stcg(reinterpret_cast<float4*>(p + 4 * cc), v);
           if (cc == 0) __stcg(reinterpret_cast<float2*>(p + D), make_float2(mt, lt));
         }
       }
-      if (!whole && j == NT - 1) {
-        const long long p1 = div_pos(y.start + y.u.blocks - 1, share);
-        __threadfence();
-        __syncthreads();
-        if (tid == 0) lastS = atomicAdd(a.count + p0, 1) == (int)(p1 - p0);
-        __syncthreads();
-        if (lastS) {
-          __threadfence();
-          for (int i = tid; i < y.rows * (D / 4); i += 32 * W) {
-            const int col = i / (D / 4), cc = i % (D / 4);
-            const float* first = a.part + ((p0 * 2 + 1) * ROWS + col) * (D + 2);
-            const long long step = 2 * ROWS * (D + 2);     // a part behind the first has slot 0
-            float mt = -INFINITY, lt = 0.f;
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-            for (int c = 0; c <= (int)(p1 - p0); ++c) {
-              const float* p = first + c * step - (c > 0 ? ROWS * (D + 2) : 0);
-              const float2 ml = __ldcg(reinterpret_cast<const float2*>(p + D));
-              const float2 va = __ldcg(reinterpret_cast<const float2*>(p + 4 * cc));
-              const float2 vb = __ldcg(reinterpret_cast<const float2*>(p + 4 * cc + 2));
-              const float mn = fmaxf(mt, ml.x);
-              const float fo = mt == -INFINITY ? 0.f : ex2(mt - mn), fn = ml.x == -INFINITY ? 0.f : ex2(ml.x - mn);
-              v.x = fmaf(v.x, fo, va.x * fn);
-              v.y = fmaf(v.y, fo, va.y * fn);
-              v.z = fmaf(v.z, fo, vb.x * fn);
-              v.w = fmaf(v.w, fo, vb.y * fn);
-              lt = fmaf(lt, fo, ml.y * fn);
-              mt = mn;
-            }
-            write_out<D>(a, y, col, cc, v, mt, lt);
-          }
-          if (tid == 0) a.count[p0] = 0;
-        }
-      }
       __syncthreads();                                     // shared memory is free for the next rows
+    }
+    if (ta != 0 || tb != unitS[turn ^ 1].u.blocks) {       // (the part's first unit, or its last)
+      if (tid == 0) {
+        Cut& y = cutS[cuts];
+        y.x = unitS[turn ^ 1];
+        y.p0 = div_pos(y.x.start, share);
+        y.parts = (int)(div_pos(y.x.start + y.x.u.blocks - 1, share) - y.p0) + 1;
+        __threadfence();
+        came[0] = came[1];                                 // (not waited for: the value is used at the end)
+        came[1] = atomicAdd(a.count + y.p0, 1);
+      }
+      ++cuts;
+    }
+  }
+  // ---- units in several parts: the CTA that came last joins them, in their order
+  if (cuts > 0) {
+    if (tid == 0) {
+      cutS[cuts - 1].last = came[1] == cutS[cuts - 1].parts - 1;
+      if (cuts > 1) cutS[0].last = came[0] == cutS[0].parts - 1;
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int e = 0; e < cuts; ++e) {
+      const Cut& y = cutS[e];
+      if (!y.last) continue;
+      __threadfence();
+      for (int i = tid; i < y.x.rows * (D / 4); i += 32 * W) {
+        const int col = i / (D / 4), cc = i % (D / 4), parts = y.parts;
+        const float* first = a.part + ((y.p0 * 2 + 1) * ROWS + col) * (D + 4);
+        constexpr long long step = 2 * ROWS * (D + 4);     // a part behind the first has slot 0
+        float mt = -INFINITY, lt = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+        for (int c0 = 0; c0 < parts; c0 += AT_JOIN) {      // (a batch's loads are on their way together)
+          float2 ml[AT_JOIN];
+          float4 b[AT_JOIN];
+#pragma unroll
+          for (int c = 0; c < AT_JOIN; ++c) {              // (past the last part: the last again)
+            const int k = min(c0 + c, parts - 1);
+            const float* p = first + k * step - (k > 0 ? ROWS * (D + 4) : 0);
+            ml[c] = __ldcg(reinterpret_cast<const float2*>(p + D));
+            b[c] = __ldcg(reinterpret_cast<const float4*>(p + 4 * cc));
+          }
+          float mn = mt;
+#pragma unroll
+          for (int c = 0; c < AT_JOIN; ++c) mn = fmaxf(mn, ml[c].x);
+          const float fo = mt == -INFINITY ? 0.f : ex2(mt - mn);
+          v.x *= fo; v.y *= fo; v.z *= fo; v.w *= fo;
+          lt *= fo;
+#pragma unroll
+          for (int c = 0; c < AT_JOIN; ++c)
+            if (c0 + c < parts) {                          // (a NaN in a part without a base stays one)
+              const float fn = ml[c].x == -INFINITY ? 0.f : ex2(ml[c].x - mn);
+              v.x = fmaf(b[c].x, fn, v.x);
+              v.y = fmaf(b[c].y, fn, v.y);
+              v.z = fmaf(b[c].z, fn, v.z);
+              v.w = fmaf(b[c].w, fn, v.w);
+              lt = fmaf(ml[c].y, fn, lt);
+            }
+          mt = mn;
+        }
+        write_out<D>(a, y.x, col, cc, v, mt, lt);
+      }
+      if (tid == 0) a.count[y.p0] = 0;
     }
   }
   leave();
@@ -745,9 +783,9 @@ cudaError_t launch_d(AttendArgs& a, int sms, cudaStream_t stream) {
                  : rows <= 18 ? 2 : rows <= 24 || (rows > 32 && rows <= 48) ? 3 : 4;
   a.one = (a.G + 8 * nt - 1) / (8 * nt);
   if (a.out_f32)
-    return nt == 1 ? launch<D, 1, 6, true>(a, grid, stream) : nt == 2 ? launch<D, 2, 4, true>(a, grid, stream)
+    return nt == 1 ? launch<D, 1, D == 64 ? 8 : 6, true>(a, grid, stream) : nt == 2 ? launch<D, 2, 4, true>(a, grid, stream)
                                                             : launch<D, 3, 4, true>(a, grid, stream);
-  return nt == 1 ? launch<D, 1, 6, false>(a, grid, stream) : nt == 2 ? launch<D, 2, 6, false>(a, grid, stream)
+  return nt == 1 ? launch<D, 1, D == 64 ? 8 : 6, false>(a, grid, stream) : nt == 2 ? launch<D, 2, 6, false>(a, grid, stream)
          : nt == 3 ? launch<D, 3, 4, false>(a, grid, stream) : launch<D, 4, 4, false>(a, grid, stream);
 }
 
@@ -755,7 +793,7 @@ size_t counter_bytes(int sms) { return ((size_t)AT_CTAS * sms * 4 + 255) / 256 *
 
 }  // namespace
 
-static size_t part_bytes(int sms) { return (size_t)AT_CTAS * sms * 2 * AT_MAX_ROWS * (128 + 2) * 4; }
+static size_t part_bytes(int sms) { return (size_t)AT_CTAS * sms * 2 * AT_MAX_ROWS * (128 + 4) * 4; }
 // [counters here][there] [partial results here][there]
 size_t paged_attend_workspace(int sms) {
   return counter_bytes(sms) + paged_prompt_counters(sms) + part_bytes(sms) + paged_prompt_parts(sms);
