@@ -57,7 +57,9 @@ constexpr int AT_ENDS = 32;
 constexpr int AT_TINY = 24, AT_SHORT = 48;
 constexpr int AT_CTAS = 2;             // resident per SM: one streams while the other joins its rows
 constexpr int AT_MAX_ROWS = 32;        // query rows of a unit at most
-constexpr int AT_JOIN = 8;            // parts that are joined at once
+constexpr int AT_JOIN = 8;             // parts that are loaded at once
+// Parts of a unit that one CTA joins; more join in groups first.
+constexpr int AT_FEW = 48, AT_GROUP = 16;
 constexpr float AT_OFF = 7.f, AT_STEP = 8.f;
 
 // The rings: a block's 16 rows of K, then of V.  The 16-byte chunk c of row r lies at chunk
@@ -87,7 +89,7 @@ struct AttendArgs {
   void* out;
   float* lse;
   float* part;                         // [grid][2][rows][D + 4]
-  int* count;                          // [grid], zero between calls
+  int* count;                          // [2][grid] of units and of groups, zero between calls
   int32_t* err;
   float c;                             // log2(e) / sqrt(d)
   float inv_g;                         // 1 / G
@@ -167,7 +169,7 @@ struct Unit {
 struct Cut {
   Unit x;
   long long p0;
-  int parts, last;
+  int parts, first, n, last;           // of all parts, those that join with this CTA's first
 };
 // The unit that list position w lies in, from an earlier one (or from a sequence and its base).
 template <int ROWS>
@@ -222,7 +224,7 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
   __shared__ float mS[W][ROWS], lS[W][ROWS];
   __shared__ float scaleS[W][R::ST][2];
   __shared__ long long scanS[W], foundS[2];
-  __shared__ int foundsS[2];
+  __shared__ int foundsS[2], lastS;
   __shared__ Cut cutS[2];
   __shared__ Unit unitS[2], aheadS[W];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
@@ -686,9 +688,13 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
         y.x = unitS[turn ^ 1];
         y.p0 = div_pos(y.x.start, share);
         y.parts = (int)(div_pos(y.x.start + y.x.u.blocks - 1, share) - y.p0) + 1;
+        // many parts join in groups; a group's counter is that of its last part, which is no other unit's
+        const bool grouped = y.parts > AT_FEW;
+        y.first = grouped ? ((int)(blockIdx.x - y.p0) / AT_GROUP) * AT_GROUP : 0;
+        y.n = grouped ? min(AT_GROUP, y.parts - y.first) : y.parts;
         __threadfence();
         came[0] = came[1];                                 // (not waited for: the value is used at the end)
-        came[1] = atomicAdd(a.count + y.p0, 1);
+        came[1] = atomicAdd(grouped ? a.count + gridDim.x + y.p0 + y.first + y.n - 1 : a.count + y.p0, 1);
       }
       ++cuts;
     }
@@ -696,53 +702,81 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
   // ---- units in several parts: the CTA that came last joins them, in their order
   if (cuts > 0) {
     if (tid == 0) {
-      cutS[cuts - 1].last = came[1] == cutS[cuts - 1].parts - 1;
-      if (cuts > 1) cutS[0].last = came[0] == cutS[0].parts - 1;
+      cutS[cuts - 1].last = came[1] == cutS[cuts - 1].n - 1;
+      if (cuts > 1) cutS[0].last = came[0] == cutS[0].n - 1;
     }
     __syncthreads();
 #pragma unroll 1
     for (int e = 0; e < cuts; ++e) {
       const Cut& y = cutS[e];
       if (!y.last) continue;
-      __threadfence();
-      for (int i = tid; i < y.x.rows * (D / 4); i += 32 * W) {
-        const int col = i / (D / 4), cc = i % (D / 4), parts = y.parts;
-        const float* first = a.part + ((y.p0 * 2 + 1) * ROWS + col) * (D + 4);
-        constexpr long long step = 2 * ROWS * (D + 4);     // a part behind the first has slot 0
-        float mt = -INFINITY, lt = 0.f;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      // the parts begin, begin + stride, ...: all of the unit, those of a group, or the groups' sums,
+      // which lie in the places of their first parts
+      int begin = y.first, stride = 1, n = y.n;
+      bool all = n == y.parts, again;
+      if (tid == 0) (all ? a.count + y.p0 : a.count + gridDim.x + y.p0 + begin + n - 1)[0] = 0;
 #pragma unroll 1
-        for (int c0 = 0; c0 < parts; c0 += AT_JOIN) {      // (a batch's loads are on their way together)
-          float2 ml[AT_JOIN];
-          float4 b[AT_JOIN];
+      do {
+        __threadfence();
+        again = false;
+        const int at_ml = stride == 1 ? D : D + 2;
+        for (int i = tid; i < y.x.rows * (D / 4); i += 32 * W) {
+          const int col = i / (D / 4), cc = i % (D / 4);
+          auto place = [&](int k) { return a.part + (((y.p0 + k) * 2 + (k == 0)) * ROWS + col) * (D + 4); };
+          float mt = -INFINITY, lt = 0.f;
+          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+          for (int c0 = 0; c0 < n; c0 += AT_JOIN) {        // (a batch's loads are on their way together)
+            float2 ml[AT_JOIN];
+            float4 b[AT_JOIN];
 #pragma unroll
-          for (int c = 0; c < AT_JOIN; ++c) {              // (past the last part: the last again)
-            const int k = min(c0 + c, parts - 1);
-            const float* p = first + k * step - (k > 0 ? ROWS * (D + 4) : 0);
-            ml[c] = __ldcg(reinterpret_cast<const float2*>(p + D));
-            b[c] = __ldcg(reinterpret_cast<const float4*>(p + 4 * cc));
-          }
-          float mn = mt;
-#pragma unroll
-          for (int c = 0; c < AT_JOIN; ++c) mn = fmaxf(mn, ml[c].x);
-          const float fo = mt == -INFINITY ? 0.f : ex2(mt - mn);
-          v.x *= fo; v.y *= fo; v.z *= fo; v.w *= fo;
-          lt *= fo;
-#pragma unroll
-          for (int c = 0; c < AT_JOIN; ++c)
-            if (c0 + c < parts) {                          // (a NaN in a part without a base stays one)
-              const float fn = ml[c].x == -INFINITY ? 0.f : ex2(ml[c].x - mn);
-              v.x = fmaf(b[c].x, fn, v.x);
-              v.y = fmaf(b[c].y, fn, v.y);
-              v.z = fmaf(b[c].z, fn, v.z);
-              v.w = fmaf(b[c].w, fn, v.w);
-              lt = fmaf(ml[c].y, fn, lt);
+            for (int c = 0; c < AT_JOIN; ++c) {            // (past the last part: the last again)
+              const float* p = place(begin + min(c0 + c, n - 1) * stride);
+              ml[c] = __ldcg(reinterpret_cast<const float2*>(p + at_ml));
+              b[c] = __ldcg(reinterpret_cast<const float4*>(p + 4 * cc));
             }
-          mt = mn;
+            float mn = mt;
+#pragma unroll
+            for (int c = 0; c < AT_JOIN; ++c) mn = fmaxf(mn, ml[c].x);
+            const float fo = mt == -INFINITY ? 0.f : ex2(mt - mn);
+            v.x *= fo; v.y *= fo; v.z *= fo; v.w *= fo;
+            lt *= fo;
+#pragma unroll
+            for (int c = 0; c < AT_JOIN; ++c)
+              if (c0 + c < n) {                            // (a NaN in a part without a base stays one)
+                const float fn = ml[c].x == -INFINITY ? 0.f : ex2(ml[c].x - mn);
+                v.x = fmaf(b[c].x, fn, v.x);
+                v.y = fmaf(b[c].y, fn, v.y);
+                v.z = fmaf(b[c].z, fn, v.z);
+                v.w = fmaf(b[c].w, fn, v.w);
+                lt = fmaf(ml[c].y, fn, lt);
+              }
+            mt = mn;
+          }
+          if (all) {
+            write_out<D>(a, y.x, col, cc, v, mt, lt);
+          } else {
+            float* p = place(begin);
+            __stcg(reinterpret_cast<float4*>(p + 4 * cc), v);
+            if (cc == 0) __stcg(reinterpret_cast<float2*>(p + D + 2), make_float2(mt, lt));
+          }
         }
-        write_out<D>(a, y.x, col, cc, v, mt, lt);
-      }
-      if (tid == 0) a.count[y.p0] = 0;
+        if (!all) {
+          const int groups = (y.parts - 1) / AT_GROUP + 1;
+          __syncthreads();
+          if (tid == 0) {
+            __threadfence();
+            lastS = atomicAdd(a.count + y.p0, 1) == groups - 1;
+            if (lastS) a.count[y.p0] = 0;
+          }
+          __syncthreads();
+          again = lastS;
+          all = true;
+          begin = 0;
+          stride = AT_GROUP;
+          n = groups;
+        }
+      } while (again);
     }
   }
   leave();
@@ -789,7 +823,7 @@ cudaError_t launch_d(AttendArgs& a, int sms, cudaStream_t stream) {
          : nt == 3 ? launch<D, 3, 4, false>(a, grid, stream) : launch<D, 4, 4, false>(a, grid, stream);
 }
 
-size_t counter_bytes(int sms) { return ((size_t)AT_CTAS * sms * 4 + 255) / 256 * 256; }
+size_t counter_bytes(int sms) { return ((size_t)AT_CTAS * sms * 8 + 255) / 256 * 256; }
 
 }  // namespace
 

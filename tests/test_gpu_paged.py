@@ -348,6 +348,26 @@ def test_long_tiles_cut_into_parts(dev, d, out_dtype):
     assert status()[0] == 0
 
 
+@pytest.mark.parametrize("out_dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("d,G,new", [(128, 4, [1, 1, 1]), (64, 7, [1, 3, 1]), (128, 16, [2, 1, 1])])
+def test_few_heads_over_many_positions(dev, d, G, new, out_dtype):
+    """A KV head's positions lie in the parts of very many CTAs, which join in groups; a second
+    sequence ends inside a part, a third is short."""
+    held, H, page = [9000, 5003, 70], 1, 128
+    cache = make_cache(dev, 120, H, d, page, seed=28)
+    table, lens, starts = tables(held, new, page, 120, dev, seed=29)
+    hide_rest(cache, table, held, new, page)
+    q = (torch.randn((sum(new), H * G, d), generator=torch.Generator().manual_seed(9)) * 0.02).bfloat16().to(dev)
+    want = attend_reference(cache, table, held, new, q, page)
+    first = None
+    for _ in range(3):
+        out, lse = cache.attend(table, lens, q, starts=starts, max_new=3, out_dtype=out_dtype, want_lse=True)
+        check_attend(out, lse, want, out_dtype)
+        first = out.clone() if first is None else first
+        assert torch.equal(out, first)
+    assert status()[0] == 0
+
+
 def test_idle_places_and_sequences_without_tokens(dev):
     d, H, G, page = 128, 2, 4, 16
     cache = make_cache(dev, 16, H, d, page, seed=9)
