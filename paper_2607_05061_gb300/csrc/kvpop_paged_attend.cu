@@ -58,8 +58,11 @@ constexpr int AT_TINY = 24, AT_SHORT = 48;
 constexpr int AT_CTAS = 2;             // resident per SM: one streams while the other joins its rows
 constexpr int AT_MAX_ROWS = 32;        // query rows of a unit at most
 constexpr int AT_JOIN = 8;             // parts that are loaded at once
-// Parts of a unit that one CTA joins; more join in groups first.
-constexpr int AT_FEW = 48, AT_GROUP = 16;
+// Parts of a unit that one CTA joins; more join in groups first, and then the groups.  us without
+// groups, in groups of 8, of 16: one sequence of 131072 and 8 KV heads (38 parts) 55.4, 52.7, 53.9; 4 of
+// 20000 and 2 heads (38) 24.6, 19.9, 21.8; one of 100000 and 1 head (304) 80, 25.3, 23.5.
+constexpr int AT_FEW = 16;
+__device__ __forceinline__ int group_of(int parts) { return parts > 128 ? 16 : 8; }
 constexpr float AT_OFF = 7.f, AT_STEP = 8.f;
 
 // The rings: a block's 16 rows of K, then of V.  The 16-byte chunk c of row r lies at chunk
@@ -690,8 +693,9 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
         y.parts = (int)(div_pos(y.x.start + y.x.u.blocks - 1, share) - y.p0) + 1;
         // many parts join in groups; a group's counter is that of its last part, which is no other unit's
         const bool grouped = y.parts > AT_FEW;
-        y.first = grouped ? ((int)(blockIdx.x - y.p0) / AT_GROUP) * AT_GROUP : 0;
-        y.n = grouped ? min(AT_GROUP, y.parts - y.first) : y.parts;
+        const int group = group_of(y.parts);
+        y.first = grouped ? (int)(blockIdx.x - y.p0) / group * group : 0;
+        y.n = grouped ? min(group, y.parts - y.first) : y.parts;
         __threadfence();
         came[0] = came[1];                                 // (not waited for: the value is used at the end)
         came[1] = atomicAdd(grouped ? a.count + gridDim.x + y.p0 + y.first + y.n - 1 : a.count + y.p0, 1);
@@ -762,7 +766,7 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
           }
         }
         if (!all) {
-          const int groups = (y.parts - 1) / AT_GROUP + 1;
+          const int groups = (y.parts - 1) / group_of(y.parts) + 1;
           __syncthreads();
           if (tid == 0) {
             __threadfence();
@@ -773,7 +777,7 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
           again = lastS;
           all = true;
           begin = 0;
-          stride = AT_GROUP;
+          stride = group_of(y.parts);
           n = groups;
         }
       } while (again);
