@@ -29,11 +29,11 @@
 //
 // The blocks of all (sequence, KV head, row group) units form one list that is cut evenly over the
 // SMs; a CTA's warps take its blocks in turn and join their rows in warp order.  A unit that lies in
-// several CTAs' parts is joined, in the order of the parts, by the CTA that arrives last (no CTA
-// waits).
+// several CTAs' parts is joined, in the order of the parts, by the CTA that arrives last, at its end (no
+// CTA waits); many parts join in groups first.
 //
-// 64 sequences of 8192 positions, 32 query and 8 KV heads: 167 us, 0.95 of the copy rate; one of
-// 131072 54 us (40 by the copy rate: 7 until the stream runs, 7 for the join of 38 parts a head).
+// 64 sequences of 8192 positions, 32 query and 8 KV heads: 168 us, 0.94 of the copy rate; one of
+// 131072 52 us (40 by the copy rate: 7 until the stream runs, 5 for the join of 38 parts a head).
 // One CTA of 12 warps an SM took the same for the former and 93 instead of 66 for 40 ragged ones: it
 // streams nothing while its rows join.
 #include <algorithm>
@@ -808,8 +808,9 @@ cudaError_t launch(const AttendArgs& a, int grid, cudaStream_t stream) {
 template <int D>
 cudaError_t launch_d(AttendArgs& a, int sms, cudaStream_t stream) {
   const int grid = AT_CTAS * sms;
-  // Groups of 8 rows a warp takes at once, and its registers (2 CTAs of 6 warps of 168, or of 4 of
-  // 255), by the rows that a sequence has on average.  One group streams at the rate of HBM and reads
+  // Groups of 8 rows a warp takes at once, and its registers (2 CTAs of 6 warps of 168, of 4 of 255, or,
+  // for one group at d = 64, of 8 of 128: 64 sequences of 8192 102 us, 108 with 6), by the rows that a
+  // sequence has on average.  One group streams at the rate of HBM and reads
   // a cache once for each; more read it less often, and compute longer.  16 sequences of 10000
   // positions and 4 heads, us for 16 / 24 / 32 / 64 rows: fp32 results, groups of 1 (6 warps) 103,
   // 155, 200, 383; of 2 (4 warps) 80, 140, 141, 262; (6 warps) 93, 161, 162, 303; of 3 118, 122, 213,
