@@ -108,8 +108,8 @@ cudaError_t launch_paged_append(const paged::Pool& pool, const paged::Batch& b, 
                                 const float* sin_, int rot, int max_pos, int interleaved, void* q_out,
                                 int32_t* err, cudaStream_t stream);
 
-// Workspace of the attention on the current device: bytes, of which the first
-// paged_attend_counter_bytes have to be zero before the first call and are zero after every call.
+// Bytes of the attention's workspace on a device with that many SMs.  The counters at its start have
+// to be zero before the first call and are zero after every call.
 size_t paged_attend_workspace(int sms);
 cudaError_t launch_paged_attend(const paged::Pool& pool, const paged::Batch& b, const void* q, long long q_ts,
                                 long long q_hs, int HQ, void* out, int out_f32, float* lse, void* workspace,
