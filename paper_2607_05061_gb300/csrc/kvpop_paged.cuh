@@ -12,6 +12,7 @@
 #include <atomic>
 
 #include "kvpop_internal.cuh"
+#include "kvpop_mma.cuh"
 
 namespace kvpop {
 namespace paged {
@@ -84,6 +85,21 @@ __device__ __forceinline__ int context(const Batch& b, const Pool& p, const SeqT
 constexpr int LONG_ROWS = 64;
 __device__ __forceinline__ bool long_rows(const SeqTokens& t, int G) {
   return t.len >= 0 && (long long)t.n * G > LONG_ROWS;
+}
+
+// The attention kernels keep two things of a row's positions, with x_t the logit (times log2 e), 2^ev_t
+// the scale of the position's values and M a base no less than the largest x + ev so far but for 2^8:
+//   w_t = 2^(x_t - M + 2), whose sum is l, and p_t = w_t 2^(ev_t + 5) <= 2^15, the operand of O = sum p_t code_t;
+//   y = O / (32 l),  lse = (M - 2 + log2 l) log 2.
+// The scale is multiplied into p and stays out of w: the weight of a position counts whatever its values
+// are (zeros have the smallest scale, 2^-96).  With 2^E the scale of the values that M came from, l lies
+// between 2^(2 - E) and 2^(10 - E) for each position: with E between -96 and 100 it is a float for 2^21
+// positions, and no weight above 2^-28 of the row's largest falls below 2^-126.
+constexpr float W_OFF = 2.f, P_SCALE = 32.f, BASE_STEP = 8.f;
+// Bases of sums to be joined may lie further apart (up to 196) than one factor reaches, while the weights
+// they stand for are alike: 2^d as two factors.  No base (-inf) gives 0, two of them a factor for zeros.
+__device__ __forceinline__ float2 down2(float d) {
+  return make_float2(ex2(fmaxf(d, -90.f)), ex2(fminf(d + 90.f, 0.f)));
 }
 
 // raise_smem_limit once per device (`done`: one bit each, of one kernel): it takes longer on the

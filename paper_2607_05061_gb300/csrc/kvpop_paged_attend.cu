@@ -18,9 +18,9 @@
 // every e4m3 value, and q, scaled by a power of two per row, to 2^-39 of the row's largest value,
 // so the products are exact.
 //
-// The scales cost next to nothing: ek multiplies the logits, and ev joins the exponent,
-//   p_t = 2^(x_t log2 e + ev - M + 7),  O = sum p_t code_t,  l = sum p_t 2^-ev,  y = O / l,
-// where M, the running base of a row, moves when a term exceeds it by 2^8.  p_t lies in [0, 2^15]:
+// The scales cost little: ek multiplies the logits, and ev the weights,
+//   w_t = 2^(x_t log2 e - M + 2),  p_t = w_t 2^(ev + 5),  O = sum p_t code_t,  l = sum w_t,  y = O / (32 l),
+// where M, the running base of a row, moves when x_t log2 e + ev exceeds it by 8.  p_t lies in [0, 2^15]:
 // rounded to f16 it has 11 bits, enough for a bf16 result (SPLIT false); for an fp32 result it is
 // the sum of two f16 values, 22 bits, and the second product is taken too (SPLIT).  The tensor
 // cores cut their fp32 sums off instead of rounding them, which adds up along a row (2.1e-6 of the
@@ -63,7 +63,6 @@ constexpr int AT_JOIN = 8;             // parts that are loaded at once
 // 20000 and 2 heads (38) 24.6, 19.9, 21.8; one of 100000 and 1 head (304) 80, 25.3, 23.5.
 constexpr int AT_FEW = 16;
 __device__ __forceinline__ int group_of(int parts) { return parts > 128 ? 16 : 8; }
-constexpr float AT_OFF = 7.f, AT_STEP = 8.f;
 
 // The rings: a block's 16 rows of K, then of V.  The 16-byte chunk c of row r lies at chunk
 // c ^ (r mod 8) of its 128 bytes (d = 128), or c ^ (r / 2 mod 4) of its 64 (d = 64).
@@ -206,13 +205,13 @@ __device__ __forceinline__ void write_out(const AttendArgs& a, const Unit& x, in
   int tok, head;
   token_of(a, x, i, tok, head);
   const long long row = ((long long)(x.u.first + tok) * a.pool.H + x.h) * a.G + head;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const float inv = l == 0.f ? 0.f : (1.f / P_SCALE) / l;
   y.x *= inv; y.y *= inv; y.z *= inv; y.w *= inv;
   if (a.out_f32)
     reinterpret_cast<float4*>(a.out)[row * (D / 4) + cc] = y;
   else
     reinterpret_cast<uint2*>(a.out)[row * (D / 4) + cc] = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
-  if (cc == 0 && a.lse) a.lse[row] = l == 0.f ? -INFINITY : (m - AT_OFF + log2f(l)) * 0.69314718055994530942f;
+  if (cc == 0 && a.lse) a.lse[row] = l == 0.f ? -INFINITY : (m - W_OFF + log2f(l)) * 0.69314718055994530942f;
 }
 
 template <int D, int NT, int W, bool SPLIT>
@@ -489,28 +488,27 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
         };
         constexpr bool EARLY = W == 6 && !edge;            // while the logits are on their way, where registers allow
         if (EARLY) values();
-        const int ebits = (int)(__float_as_uint(vs) >> 23);
-        const float ev = (float)(ebits - 127), vinv = __uint_as_float((uint32_t)(254 - ebits) << 23);
+        const float ev = (float)((int)(__float_as_uint(vs) >> 23) - 127);
         // exponents from the row's base, in one rounding: as long as there is none (-inf) every
         // logit is too large
         float y[NT][4];
-        auto exponents = [&](float off, bool based) {
+        auto exponents = [&](bool based) {
 #pragma unroll
           for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              y[j][e] = fmaf(sc[j][e], rc[j][e & 1] * ks, based ? ev + (off - m[j][e & 1]) : ev);
+              y[j][e] = fmaf(sc[j][e], rc[j][e & 1] * ks, based ? W_OFF - m[j][e & 1] : 0.f);
               if (edge && t * BLK + g + 8 * (e >> 1) > lim[j][e & 1]) y[j][e] = -INFINITY;
             }
         };
-        exponents(AT_OFF, true);
+        exponents(true);
         bool up = false;
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) up |= y[j][e] > AT_OFF + AT_STEP;
+          for (int e = 0; e < 4; ++e) up |= y[j][e] > W_OFF + BASE_STEP - ev;
         if (__any_sync(0xffffffffu, up)) {
-          exponents(0.f, false);
+          exponents(false);
 #pragma unroll
           for (int j = 0; j < NT; ++j)
 #pragma unroll
@@ -518,32 +516,37 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
               float mx = fmaxf(y[j][e], y[j][e + 2]);
 #pragma unroll
               for (int x = 4; x < 32; x <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
-              mx = fmaxf(mx, m[j][e]);
-              const float al = m[j][e] == -INFINITY ? 0.f : ex2(m[j][e] - mx);
+              mx = fmaxf(mx + ev, m[j][e]);
+              const float2 f = down2(m[j][e] - mx);
+              const float al = f.x * f.y;
               m[j][e] = mx;
-              l[j][e] *= al;
+              l[j][e] = l[j][e] * f.x * f.y;
 #pragma unroll
               for (int k = 0; k < KW; ++k) {
                 o[j][k][e] *= al;
                 o[j][k][e + 2] *= al;
               }
             }
-          exponents(AT_OFF, true);
+          exponents(true);
         }
+        const float pf = vs * P_SCALE;
+        const uint64_t pf2 = f2_pack(pf, pf);
         uint32_t ph[NT][2], pl[NT][2];
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) y[j][e] = ex2(y[j][e]);
 #pragma unroll
-          for (int e = 0; e < 2; ++e) l[j][e] = fmaf(y[j][e] + y[j][e + 2], vinv, l[j][e]);
+          for (int e = 0; e < 2; ++e) l[j][e] += y[j][e] + y[j][e + 2];
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const uint32_t hi = pack_f16(y[j][2 * e], y[j][2 * e + 1]);
+            float p0, p1;
+            f2_unpack(f2_mul(f2_pack(y[j][2 * e], y[j][2 * e + 1]), pf2), p0, p1);
+            const uint32_t hi = pack_f16(p0, p1);
             ph[j][e] = movm(hi);
             if (SPLIT) {
               const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-              pl[j][e] = movm(pack_f16(y[j][2 * e] - b.x, y[j][2 * e + 1] - b.y));
+              pl[j][e] = movm(pack_f16(p0 - b.x, p1 - b.y));
             }
           }
         }
@@ -668,12 +671,13 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
 #pragma unroll
         for (int z = 0; z < W; ++z) {
           const float4 b = *reinterpret_cast<const float4*>(accS + z * RS + r * (D + 4) + 4 * cc);
-          const float f = mw[z] == -INFINITY ? 0.f : ex2(mw[z] - mt);   // (a NaN stays one)
+          const float2 f2 = down2(mw[z] - mt);
+          const float f = f2.x * f2.y;                     // (a NaN among the sums stays one)
           v.x = fmaf(b.x, f, v.x);
           v.y = fmaf(b.y, f, v.y);
           v.z = fmaf(b.z, f, v.z);
           v.w = fmaf(b.w, f, v.w);
-          lt = fmaf(lS[z][col], f, lt);
+          lt = fmaf(lS[z][col] * f2.x, f2.y, lt);
         }
         if (whole) {
           write_out<D>(a, y, col, cc, v, mt, lt);
@@ -742,18 +746,20 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
             float mn = mt;
 #pragma unroll
             for (int c = 0; c < AT_JOIN; ++c) mn = fmaxf(mn, ml[c].x);
-            const float fo = mt == -INFINITY ? 0.f : ex2(mt - mn);
+            const float2 f2 = down2(mt - mn);
+            const float fo = f2.x * f2.y;
             v.x *= fo; v.y *= fo; v.z *= fo; v.w *= fo;
-            lt *= fo;
+            lt = lt * f2.x * f2.y;
 #pragma unroll
             for (int c = 0; c < AT_JOIN; ++c)
               if (c0 + c < n) {                            // (a NaN in a part without a base stays one)
-                const float fn = ml[c].x == -INFINITY ? 0.f : ex2(ml[c].x - mn);
+                const float2 g2 = down2(ml[c].x - mn);
+                const float fn = g2.x * g2.y;
                 v.x = fmaf(b[c].x, fn, v.x);
                 v.y = fmaf(b[c].y, fn, v.y);
                 v.z = fmaf(b[c].z, fn, v.z);
                 v.w = fmaf(b[c].w, fn, v.w);
-                lt = fmaf(ml[c].y, fn, lt);
+                lt = fmaf(ml[c].y * g2.x, g2.y, lt);
               }
             mt = mn;
           }

@@ -1,8 +1,8 @@
 // Attention of many new tokens a sequence over the paged 8-bit cache, on tcgen05.
 //
 // The mathematics is that of kvpop_paged_attend.cu: f16 products that are exact for the logits,
-// the value scales in the exponent, p = 2^(x log2 e + ev - M + 7) as one f16 (bf16 results) or
-// the sum of two (fp32 results, SPLIT).  A CTA owns 256 consecutive rows (token, query head) of
+// the value scales in the weights' operand, p = 2^(x log2 e - M + 2) 2^(ev + 5) as one f16 (bf16
+// results) or the sum of two (fp32 results, SPLIT).  A CTA owns 256 consecutive rows (token, query head) of
 // one (sequence, KV head), as two halves of 128 rows, and streams the positions they see in blocks
 // of 64, the same bytes for both halves.  Roles:
 //  * 3 converter warps: bulk copies bring the bytes of keys and values into shared memory, two tiles
@@ -49,7 +49,6 @@ constexpr int PP_THREADS = 32 * (PP_CONV_WARP + PP_CONV);
 constexpr int PP_RING = 10, PP_SCALES = 16;              // tiles at most; blocks whose scales are held
 constexpr int PP_TMEM = 512;                             // O_h: 128 h (d = 64: and Q_h, 128 h + 64); S_h,b: 256 + 128 h + 64 b
 constexpr int PP_PARTS = 8, PP_LEAST = 8;                // parts of a tile at most; blocks of a part at least
-constexpr float PP_OFF = 7.f, PP_STEP = 8.f;
 // barriers
 constexpr int PB_FULL = 0;                               // [ring] converters -> MMA
 constexpr int PB_EMPTY = PB_FULL + PP_RING;              // [ring] MMA -> converters
@@ -91,8 +90,9 @@ struct PL {
   static constexpr int RING = D == 128 ? 7 : PP_RING, RAW = PP_KEYS * D;   // tiles of f16; bytes of a tile of codes
   static constexpr int OFF_RING = 2 * QB, OFF_RAW = OFF_RING + RING * KB, OFF_BAR = OFF_RAW + 2 * PP_CONV * RAW;
   static constexpr int OFF_TMEM = OFF_BAR + 8 * PB_N, OFF_NAN = (OFF_TMEM + 4 + 15) / 16 * 16;
-  static constexpr int OFF_SCALE = OFF_NAN + 4 * PP_NANW;   // [16 blocks] 4 key scales, 4 value exponents, 4 2^-those
-  static constexpr int OFF_KEEP = OFF_SCALE + PP_SCALES * 48;   // what only the end needs
+  // [16 blocks] of 4 groups: key scales, value exponents (-inf: not to be seen), value scales times 32, 0 or -inf
+  static constexpr int OFF_SCALE = OFF_NAN + 4 * PP_NANW, SCALES = 16;
+  static constexpr int OFF_KEEP = OFF_SCALE + PP_SCALES * SCALES * 4;   // what only the end needs
   static constexpr int BYTES = OFF_KEEP + 32;
   static_assert(PP_PARTS * PP_ROWS * 4 <= OFF_BAR, "");  // factors of the parts, where queries and ring were
 };
@@ -368,10 +368,13 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
         }
       }
       if (!(i & 1) && lane < 2 * PER) {                  // both scales with the keys, which the logits wait for
-        float* to = reinterpret_cast<float*>(smp + L::OFF_SCALE) + (i >> 1) % PP_SCALES * 12 + lane;
+        float* to = reinterpret_cast<float*>(smp + L::OFF_SCALE) + (i >> 1) % PP_SCALES * L::SCALES + lane;
         const uint32_t e = __float_as_uint(scale) >> 23;
         to[0] = lane < PER ? scale : scale > 0.f ? (float)((int)e - 127) : -INFINITY;
-        if (lane >= PER) to[PER] = scale > 0.f ? __uint_as_float((254u - e) << 23) : 0.f;
+        if (lane >= PER) {
+          to[PER] = scale * P_SCALE;
+          to[2 * PER] = scale > 0.f ? 0.f : -INFINITY;
+        }
       }
       if ((i & 1) && pos0 + PP_KEYS - 1 > lim_lo) {
         // Values that some row does not see: a NaN must not reach the rows before it, where its
@@ -471,10 +474,10 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
       float v[64];
       tmem_ld32(tS, *reinterpret_cast<float(*)[32]>(v));
       tmem_ld32(tS + 32, *reinterpret_cast<float(*)[32]>(v + 32));
-      const float4* sc = reinterpret_cast<const float4*>(smp + L::OFF_SCALE + j % PP_SCALES * 48);
-      const float4 ks4 = sc[0], ev4 = sc[1], vi4 = sc[2];
+      const float4* sc = reinterpret_cast<const float4*>(smp + L::OFF_SCALE + j % PP_SCALES * L::SCALES * 4);
+      const float4 ks4 = sc[0], ev4 = sc[1], pf4 = sc[2], see4 = sc[3];
       const float ks[4] = {ks4.x, ks4.y, ks4.z, ks4.w}, ev[4] = {ev4.x, ev4.y, ev4.z, ev4.w};
-      const float vi[4] = {vi4.x, vi4.y, vi4.z, vi4.w};
+      const float pf[4] = {pf4.x, pf4.y, pf4.z, pf4.w}, seen[4] = {see4.x, see4.y, see4.z, see4.w};
       tmem_wait_ld();
       const int see = lim - key0 - j * PP_KEYS;                 // last column the row sees
       if (edge) {
@@ -491,13 +494,14 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
         const float bm = fmaxf(fmax3(m0, m1, m2), fmax3(m3, m4, x[15]));
         top = fmaxf(top, fmaf(bm, rc * ks[e], ev[e]));
       }
-      const bool move = top > m + PP_STEP;
+      const bool move = top > m + BASE_STEP;
       if (__any_sync(0xffffffffu, move)) {
-        const float mn = move ? top : m, f = m == -INFINITY ? 0.f : ex2(m - mn);   // (1 where it stays)
+        const float mn = move ? top : m;
+        const float2 f = down2(m - mn);
         if (j > 0) {
           if (!wait(PB_O + hf, (j - 1) & 1)) return false;   // the product before has to be in O
           fence_after();
-          const float g = move ? f : 1.f;
+          const float g = move ? f.x * f.y : 1.f;
 #pragma unroll
           for (int c = 0; c < D / 32; ++c) {
             float o[32];
@@ -509,17 +513,17 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
           }
           tmem_wait_st();
         }
-        if (move) l *= f;
+        if (move) l = l * f.x * f.y;
         m = mn;
       }
-      const float base = m == -INFINITY ? 0.f : PP_OFF - m;
+      const float base = m == -INFINITY ? 0.f : W_OFF - m;
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         float hi[16], lo_[16];
 #pragma unroll
         for (int e = 2 * c; e < 2 * c + 2; ++e) {
-          const float cc = rc * ks[e], add = ev[e] + base;
-          const uint64_t c2 = f2_pack(cc, cc), a2 = f2_pack(add, add);
+          const float cc = rc * ks[e], add = seen[e] + base;
+          const uint64_t c2 = f2_pack(cc, cc), a2 = f2_pack(add, add), pf2 = f2_pack(pf[e], pf[e]);
           uint64_t s0 = 0ull, s1 = 0ull;
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
@@ -532,17 +536,19 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
             }
             x0 = ex2(x0);
             x1 = ex2(x1);
+            const uint64_t w2 = f2_pack(x0, x1);
+            if (i & 1) s1 = f2_add(s1, w2); else s0 = f2_add(s0, w2);
+            f2_unpack(f2_mul(w2, pf2), x0, x1);
             const uint32_t w = pack_h2(x0, x1);
             hi[k] = __uint_as_float(w);
             if (SPLIT) {
               const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&w));
               lo_[k] = __uint_as_float(pack_h2(x0 - b.x, x1 - b.y));
             }
-            if (i & 1) s1 = f2_add(s1, f2_pack(x0, x1)); else s0 = f2_add(s0, f2_pack(x0, x1));
           }
           float x0, x1;
           f2_unpack(f2_add(s0, s1), x0, x1);
-          l = fmaf(x0 + x1, vi[e], l);
+          l += x0 + x1;
         }
         tmem_st16(tS + 16 * c, hi);
         if (SPLIT) tmem_st16(tS + 32 + 16 * c, lo_);
@@ -591,7 +597,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     const uint32_t tO = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (warp >> 2) * 128;
     uint32_t any = 0;
     for (int i = 0; i < PP_NANW; ++i) any |= nanS[i];
-    const float inv = cut_ > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;   // (a part's rows stay as they are)
+    const float inv = cut_ > 1 ? 1.f : l == 0.f ? 0.f : (1.f / P_SCALE) / l;   // (a part's rows stay as they are)
     const long long row = row_of(row0_ + min(tid, rows_ - 1));
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {
@@ -640,7 +646,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     if (cut_ > 1) {
       __stcg(a.part_ml + slot * PP_ROWS + tid, make_float2(m, l));
     } else if (lim >= 0 && a.lse) {
-      a.lse[row] = l == 0.f ? -INFINITY : (m - PP_OFF + log2f(l)) * 0.69314718055994530942f;
+      a.lse[row] = l == 0.f ? -INFINITY : (m - W_OFF + log2f(l)) * 0.69314718055994530942f;
     }
   }
   fence_before();
@@ -671,15 +677,15 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
 #pragma unroll
         for (int c = 0; c < PP_PARTS; ++c)
           if (c < cut_) {
-            const float f = ml[c].x == -INFINITY ? 0.f : ex2(ml[c].x - mt);   // (times a NaN: a NaN)
-            lt = fmaf(ml[c].y, f, lt);
-            fS[c * PP_ROWS + rw] = f;
+            const float2 f = down2(ml[c].x - mt);          // (times a NaN: a NaN)
+            lt = fmaf(ml[c].y * f.x, f.y, lt);
+            fS[c * PP_ROWS + rw] = f.x * f.y;
           }
-        const float inv = lt == 0.f ? 0.f : 1.f / lt;
+        const float inv = lt == 0.f ? 0.f : (1.f / P_SCALE) / lt;
         for (int c = 0; c < cut_; ++c) fS[c * PP_ROWS + rw] *= inv;
         if (a.lse)
           a.lse[row_of(row0_ + rw)] =
-              lt == 0.f ? -INFINITY : (mt - PP_OFF + log2f(lt)) * 0.69314718055994530942f;
+              lt == 0.f ? -INFINITY : (mt - W_OFF + log2f(lt)) * 0.69314718055994530942f;
       }
       __syncthreads();
       constexpr int ITEMS = PP_ROWS * (D / 8);           // of 8 values, two a thread at once
