@@ -54,8 +54,12 @@ constexpr int PB_FULL = 0;                               // [ring] converters ->
 constexpr int PB_EMPTY = PB_FULL + PP_RING;              // [ring] MMA -> converters
 constexpr int PB_S = PB_EMPTY + PP_RING;                 // [2][2] MMA -> softmax: logits of even, odd blocks there
 constexpr int PB_P = PB_S + 4;                           // [2][2] softmax -> MMA: their probabilities there
+// A wait by parity does not tell the phase it is for from the one two before.  At block j the product
+// with block j - 2 is done (the logits of j follow it) and that with j is not begun, so that j - 1 can be
+// waited for; at the end nothing says that the last but one is done: the end has a barrier of its own.
 constexpr int PB_O = PB_P + 4;                           // [2] MMA -> softmax: a product done
-constexpr int PB_RAW = PB_O + 2;                         // [converters][2] bytes there
+constexpr int PB_END = PB_O + 2;                         // MMA -> softmax: all products done
+constexpr int PB_RAW = PB_END + 1;                       // [converters][2] bytes there
 constexpr int PB_N = PB_RAW + 2 * PP_CONV;
 constexpr int PP_NANW = (PP_ROWS + 2 * PP_KEYS) / 32;    // words of the map of NaN values
 
@@ -219,6 +223,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     for (int i = 0; i < 2 * PP_CONV; ++i) mbar_init(bar(PB_RAW + i), 1);
     mbar_init(bar(PB_O + 0), 1);
     mbar_init(bar(PB_O + 1), 1);
+    mbar_init(bar(PB_END), 1);
     mbar_fence_init();
   }
   if (tid < PP_NANW) nanS[tid] = 0;
@@ -461,6 +466,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
         if (j + 2 < nblk) issue_s(hf, j + 2);
       }
     }
+    if (lead && ok) commit(bar(PB_END));
+    __syncwarp();
   } else {
     // ---------------------------------------------------------------- softmax rows
     const int hf = warp >> 2;
@@ -566,7 +573,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     for (; j < whole && ok; ++j) ok = block(j, std::false_type{});
 #pragma unroll 1
     for (; j < nblk && ok; ++j) ok = block(j, std::true_type{});
-    if (ok) ok = wait(PB_O + hf, (nblk - 1) & 1);
+    if (ok) ok = wait(PB_END, 0);
   }
   fence_before();
   __syncthreads();                                       // every product is done; shared memory is free
