@@ -503,12 +503,13 @@ size_t kvpop_paged_workspace_bytes(void);
  *   y = sum_t softmax_t(q.k_t / sqrt(d)) v_t,   lse = log sum_t exp(q.k_t / sqrt(d)).
  *   q [n_tokens][n_q_heads][d] bf16, n_q_heads = H * G
  *   out_dev [n_tokens][n_q_heads][d] contiguous, 16-byte aligned, fp32 or bf16 (out_dtype); its
- *   type is also the precision of the softmax's weights: 22 bits for fp32, 11 for bf16 (with
- *   more than 64 rows (token, query head) of a sequence and KV head the sums run on tensor cores
- *   that cut them off: 8e-6 of an fp32 result over 8192 positions, 5e-7 otherwise)
+ *   type is also the precision of the softmax's weights: 22 bits for fp32, 11 for bf16.  Whatever
+ *   the length, fp32 results are within some 2e-6 of the weighted sum of magnitudes with more than
+ *   64 rows (token, query head) of a sequence and KV head, 5e-7 otherwise; the sums of bf16 results
+ *   run on tensor cores that cut them off, less than 5e-4 over a million positions
  *   lse_dev [n_tokens][n_q_heads] fp32, or NULL
  * An idle place's tokens get zeros and -inf.  workspace_dev: kvpop_paged_workspace_bytes()
- * bytes (some 70 MB: partial results of contexts that several SMs share), 256-byte aligned, owned
+ * bytes (some 90 MB: partial results of contexts that several SMs share, running sums), 256-byte aligned, owned
  * by the caller and zero before its first call; every call leaves it fit for the next one.  Calls
  * that share it have to be serialised; the layers of a model can share one.  Asynchronous on
  * `stream`; no allocation. */

@@ -15,15 +15,17 @@
 // Tensor memory: O (2 x 128 columns) and two buffers of logits (4 x 64), P in the place of its
 // logits.  The logits of block j + 2 follow the product with block j into its buffer in the order
 // the MMAs are issued, and those of block j + 1 are there when a row is done with block j, so a
-// block costs a softmax warp one wait and one signal.
+// block costs a softmax warp one wait and one signal.  O adds up cut off: after a chain of blocks the
+// softmax warps move it to running sums in L2, where it is added rounded, and the next product starts
+// from zero.
 //
 // What bounds it, for a block of 64 positions (d = 128, about 1950 clocks; the two products' share of
 // the tensor rate is 1024): the products, which the MMA warp issues for 1630 clocks, 1070 of them for
 // S, whose 128 query rows come from shared memory for every 64 keys (66 clocks a step of 16, 32 by
 // the tensor rate), and the softmax's 1270 clocks a warp, which wait for each other across the
 // halves.  A tile costs 7 to 9 us besides: queries, first products, output.
-// A prompt of 8192 tokens with 32 query and 8 KV heads takes 494 us (bf16 results; 630 with fp32
-// ones), 58% of the bf16 rate; at d = 64 329.  Measured before, in order: blocks of 128 in one
+// A prompt of 8192 tokens with 32 query and 8 KV heads takes 503 us (bf16 results; 773 with fp32
+// ones), 57% of the bf16 rate.  Measured before, in order: blocks of 128 in one
 // buffer, where a half's rows and its products took turns, 672; blocks of 64 with P in a place of its
 // own, two waits and two signals a block, 622; P over its logits 575; queries and results read and
 // written by rows, the converters' first tiles beside them 549; blocks that all rows see whole apart,
@@ -60,7 +62,14 @@ constexpr int PB_P = PB_S + 4;                           // [2][2] softmax -> MM
 constexpr int PB_O = PB_P + 4;                           // [2] MMA -> softmax: a product done
 constexpr int PB_END = PB_O + 2;                         // MMA -> softmax: all products done
 constexpr int PB_RAW = PB_END + 1;                       // [converters][2] bytes there
-constexpr int PB_N = PB_RAW + 2 * PP_CONV;
+constexpr int PB_SLOT = PB_RAW + 2 * PP_CONV;            // MMA -> softmax: the place for running sums claimed
+constexpr int PB_N = PB_SLOT + 1;
+// Blocks whose products add up in tensor memory before a row's sums move on.  The tensor cores cut off
+// what they add, by 0.7 of 2^-23 of the sum so far each time (values of one sign, 16384 positions in one
+// sum: 8.8e-5 of an fp32 result; in chains of 32, 16, 8 blocks 4e-6, 2.1e-6, 1.2e-6, and a prompt of 8192
+// takes 674, 707, 770 us, 629 in one sum).  256 blocks leave a bf16 result 3e-5, a 60th of its rounding;
+// where no tile has more, the kernel is without the moves (a prompt of 8192 503 us, 510 with them).
+constexpr int PP_CHAIN = 8, PP_CHAIN_BF16 = 256;
 constexpr int PP_NANW = (PP_ROWS + 2 * PP_KEYS) / 32;    // words of the map of NaN values
 
 struct PromptArgs {
@@ -74,6 +83,8 @@ struct PromptArgs {
   float* part;                                           // [slots][d / 8][256][8] sums of parts
   float2* part_ml;                                       // [slots][256] their bases and normalisers
   int* count;                                            // [slots] parts there, zero between calls
+  float* sum;                                            // [SMs][d / 4][256][4] running sums of CTAs
+  int* claim;                                            // [SMs] places of `sum` in use, zero between calls
   float c;                                               // log2(e) / sqrt(d)
   int G, out_f32, sms;
 };
@@ -97,7 +108,8 @@ struct PL {
   // [16 blocks] of 4 groups: key scales, value exponents (-inf: not to be seen), value scales times 32, 0 or -inf
   static constexpr int OFF_SCALE = OFF_NAN + 4 * PP_NANW, SCALES = 16;
   static constexpr int OFF_KEEP = OFF_SCALE + PP_SCALES * SCALES * 4;   // what only the end needs
-  static constexpr int BYTES = OFF_KEEP + 32;
+  static constexpr int OFF_BASE = OFF_KEEP + 32;         // [rows] bases of the running sums
+  static constexpr int BYTES = OFF_BASE + PP_ROWS * 4;
   static_assert(PP_PARTS * PP_ROWS * 4 <= OFF_BAR, "");  // factors of the parts, where queries and ring were
 };
 
@@ -146,10 +158,70 @@ __device__ __forceinline__ int share_of(int tiles, int most, float all, int sms,
   return __shfl_sync(0xffffffffu, b, key & 31u);
 }
 
-template <int D, bool SPLIT>
+// A place for running sums, of the first thread that asks; -1: none was free.  There is one for every
+// CTA that can run at once, and the SM's own is the one that its last CTA gave back.
+__device__ __noinline__ int claim_place(int* claim, int sms) {
+  unsigned at;
+  asm volatile("mov.u32 %0, %%smid;" : "=r"(at));
+  for (int i = 0; i < 64 * sms; ++i, ++at)
+    if (atomicCAS(claim + at % (unsigned)sms, 0, 1) == 0) return (int)(at % (unsigned)sms);
+  return -1;
+}
+// A row's sums in tensor memory (by all lanes) join the running ones: O 2^up is added to them, in L2; or
+// (set) they become O + 2^-up of them, or O.
+template <int D>
+__device__ __noinline__ void move_sums(uint32_t tO, float* to, float up, bool set, bool none) {
+  const float f = set ? ex2(-up) : ex2(up);
+#pragma unroll 1
+  for (int c = 0; c < D / 32; ++c) {
+    float o[32];
+    tmem_ld32(tO + c * 32, o);
+    tmem_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 8; ++i, to += 4 * PP_ROWS) {
+      float* v = o + 4 * i;
+      if (!set) {
+        asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(to), "f"(v[0] * f), "f"(v[1] * f),
+                     "f"(v[2] * f), "f"(v[3] * f)
+                     : "memory");
+      } else {
+        const float4 b = none ? make_float4(0.f, 0.f, 0.f, 0.f) : __ldcg(reinterpret_cast<const float4*>(to));
+        __stcg(reinterpret_cast<float4*>(to), make_float4(fmaf(b.x, f, v[0]), fmaf(b.y, f, v[1]), fmaf(b.z, f, v[2]),
+                                                          fmaf(b.w, f, v[3])));
+      }
+    }
+  }
+}
+
+// The sums in tensor memory become O + f times the running ones.
+template <int D>
+__device__ __noinline__ void fetch_sums(uint32_t tO, const float* from, float f) {
+  __threadfence();
+#pragma unroll 1
+  for (int c = 0; c < D / 32; ++c, tO += 32) {
+    float4 b[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i, from += 4 * PP_ROWS) b[i] = __ldcg(reinterpret_cast<const float4*>(from));
+    float o[32];
+    tmem_ld32(tO, o);
+    tmem_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      o[4 * i] = fmaf(b[i].x, f, o[4 * i]);
+      o[4 * i + 1] = fmaf(b[i].y, f, o[4 * i + 1]);
+      o[4 * i + 2] = fmaf(b[i].z, f, o[4 * i + 2]);
+      o[4 * i + 3] = fmaf(b[i].w, f, o[4 * i + 3]);
+    }
+    tmem_st32(tO, o);
+    tmem_wait_st();
+  }
+}
+
+// CHAINED: the sums move on after each chain of blocks.
+template <int D, bool SPLIT, bool CHAINED>
 __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs a) {
   using L = PL<D>;
-  constexpr int RING = L::RING;
+  constexpr int RING = L::RING, CHAIN = SPLIT ? PP_CHAIN : PP_CHAIN_BF16;
   extern __shared__ __align__(1024) unsigned char smp[];
   const uint32_t sb = smem_u32(smp);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -224,6 +296,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     mbar_init(bar(PB_O + 0), 1);
     mbar_init(bar(PB_O + 1), 1);
     mbar_init(bar(PB_END), 1);
+    mbar_init(bar(PB_SLOT), 1);
     mbar_fence_init();
   }
   if (tid < PP_NANW) nanS[tid] = 0;
@@ -237,6 +310,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     keep[4] = place;
     keep[5] = h;
     keep[6] = nan0;
+    keep[7] = -1;
   }
   if (warp == PP_MMA_WARP) tmem_alloc(sb + L::OFF_TMEM, PP_TMEM);
   fence_before();
@@ -415,6 +489,13 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     // ---------------------------------------------------------------- MMA issue
     const uint32_t idS = idesc_f16(128, PP_KEYS, 0), idO = idesc_f16(128, D, 1);
     const bool lead = elect_one();
+    if (CHAINED && nblk > CHAIN) {                       // (while the queries come)
+      if (lane == 0) {
+        keep[7] = claim_place(a.claim, a.sms);
+        mbar_arrive(bar(PB_SLOT));
+      }
+      __syncwarp();
+    }
     asm volatile("bar.sync 1, %0;" ::"n"(32 * PP_MMA_WARP + 32) : "memory");
     fence_after();
     const uint64_t qd0 = kmajor_desc(sb, PP_HALF, 0), kd0 = kmajor_desc(sb + L::OFF_RING, PP_KEYS, 0);
@@ -456,7 +537,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
 #pragma unroll
           for (int k = 0; k < PP_KEYS / 16; ++k) {
             const uint64_t vk = desc_at(vd, k * 16 * 128);
-            mma_bf16_ts(dO, tP + 8 * k, vk, idO, j > 0 || k > 0);
+            mma_bf16_ts(dO, tP + 8 * k, vk, idO, (CHAINED ? j & (CHAIN - 1) : j) > 0 || k > 0);
             if (SPLIT) mma_bf16_ts(dO, tP + 32 + 8 * k, vk, idO, 1);
           }
           commit(bar(PB_O + hf));
@@ -473,6 +554,24 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     const int hf = warp >> 2;
     const uint32_t trow = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tO = tmem + trow + hf * 128;
+    // The tensor cores cut their sums off, which adds up along a row: the sums of CHAIN blocks join the
+    // running ones, rounded, while the product with the next block waits for its probabilities.
+    float* const baseS = reinterpret_cast<float*>(smp + L::OFF_BASE) + tid;
+    auto move_on = [&](int j) {
+      if (!wait(PB_O + hf, (j - 1) & 1) || !wait(PB_SLOT, 0)) return false;
+      fence_after();
+      const int place = keep[7];
+      if (place < 0) {
+        report(a.err, ERR_WAIT);
+        return false;
+      }
+      float up = m - *baseS;                             // (no base before, no sums; no base at all: both are 0)
+      const bool none = j == CHAIN, set = __any_sync(0xffffffffu, none || !(up <= 40.f));
+      if (none || m == -INFINITY) up = 0.f;
+      move_sums<D>(tO, a.sum + ((long long)place * (D / 4) * PP_ROWS + tid) * 4, up, set, none);
+      if (set) *baseS = m;
+      return true;
+    };
     auto block = [&](int j, auto at_edge) {
       constexpr bool edge = decltype(at_edge)::value;
       if (!wait(PB_S + 2 * hf + (j & 1), j >> 1 & 1)) return false;
@@ -524,6 +623,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
         m = mn;
       }
       const float base = m == -INFINITY ? 0.f : W_OFF - m;
+      float lb = 0.f;
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         float hi[16], lo_[16];
@@ -555,12 +655,14 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
           }
           float x0, x1;
           f2_unpack(f2_add(s0, s1), x0, x1);
-          l += x0 + x1;
+          lb += x0 + x1;
         }
         tmem_st16(tS + 16 * c, hi);
         if (SPLIT) tmem_st16(tS + 32 + 16 * c, lo_);
       }
+      l += lb;
       tmem_wait_st();
+      if (CHAINED && (j & (CHAIN - 1)) == 0 && j > 0 && !move_on(j)) return false;
       fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(PB_P + 2 * hf + (j & 1)));
@@ -606,6 +708,9 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     for (int i = 0; i < PP_NANW; ++i) any |= nanS[i];
     const float inv = cut_ > 1 ? 1.f : l == 0.f ? 0.f : (1.f / P_SCALE) / l;   // (a part's rows stay as they are)
     const long long row = row_of(row0_ + min(tid, rows_ - 1));
+    if (CHAINED && keep[7] >= 0)
+      fetch_sums<D>(tO, a.sum + ((long long)keep[7] * (D / 4) * PP_ROWS + tid) * 4,
+                    ex2(fminf(reinterpret_cast<float*>(smp + L::OFF_BASE)[tid] - m, 0.f)));
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {
       float o[32];
@@ -660,6 +765,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
   if (cut_ > 1) __threadfence();
   __syncthreads();
   if (warp == PP_MMA_WARP) tmem_dealloc(tmem, PP_TMEM);
+  if (CHAINED && tid == 0 && keep[7] >= 0) atomicExch(a.claim + keep[7], 0);   // (its sums are read)
   if (cut_ > 1) {
     // the part that comes last joins them, in their order (a part whose waits ran out comes too)
     int* const count = a.count + pair;
@@ -735,9 +841,9 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
   }
 }
 
-template <int D, bool SPLIT>
+template <int D, bool SPLIT, bool CHAINED>
 cudaError_t launch(const PromptArgs& a, dim3 grid, cudaStream_t stream) {
-  auto k = paged_prompt_kernel<D, SPLIT>;
+  auto k = paged_prompt_kernel<D, SPLIT, CHAINED>;
   const size_t smem = PL<D>::BYTES;
   static std::atomic<unsigned long long> raised{0};
   const cudaError_t e = raise_smem_limit_once(raised, k, smem);
@@ -763,8 +869,9 @@ long long slots_of(int sms) { return 3ll * sms; }
 bool paged_prompt_fits(const Pool& pool, const Batch& b, int HQ) {
   return ((long long)b.n_tokens * (HQ / pool.H) / PP_ROWS + b.n_seq) * pool.H <= INT32_MAX;
 }
-size_t paged_prompt_counters(int sms) { return ((size_t)slots_of(sms) * 4 + 255) / 256 * 256; }
-size_t paged_prompt_parts(int sms) { return (size_t)slots_of(sms) * PP_ROWS * (128 + 2) * 4; }
+// [parts there][claims]; [sums of parts][their bases and normalisers][running sums]
+size_t paged_prompt_counters(int sms) { return ((size_t)(slots_of(sms) + sms) * 4 + 255) / 256 * 256; }
+size_t paged_prompt_parts(int sms) { return (size_t)slots_of(sms) * PP_ROWS * (128 + 2) * 4 + (size_t)sms * PP_ROWS * 128 * 4; }
 
 cudaError_t launch_paged_prompt(const Pool& pool, const Batch& b, const void* q, long long q_ts, long long q_hs,
                                 int HQ, void* out, int out_f32, float* lse, void* counters, void* parts, int sms,
@@ -785,12 +892,19 @@ cudaError_t launch_paged_prompt(const Pool& pool, const Batch& b, const void* q,
   a.count = static_cast<int*>(counters);
   a.part = static_cast<float*>(parts);
   a.part_ml = reinterpret_cast<float2*>(a.part + slots_of(sms) * PP_ROWS * pool.d);
+  a.sum = a.part + slots_of(sms) * PP_ROWS * (pool.d + 2);
+  a.claim = a.count + slots_of(sms);
   // Tiles are cut where there may be too few of them for the SMs; the most there can be counts, as
   // the lengths are not known here.
   const long long most = ((long long)b.n_tokens * a.G / PP_ROWS + b.n_seq) * pool.H, cuts = slots_of(sms) / most;
   const dim3 grid((unsigned)most, (unsigned)(cuts < 1 ? 1 : cuts < PP_PARTS ? cuts : PP_PARTS));
-  if (pool.d == 128) return out_f32 ? launch<128, true>(a, grid, stream) : launch<128, false>(a, grid, stream);
-  return out_f32 ? launch<64, true>(a, grid, stream) : launch<64, false>(a, grid, stream);
+  // what the table has room for bounds the blocks of a tile
+  const bool chained = ((long long)b.max_pages << pool.page_shift) > PP_CHAIN_BF16 * PP_KEYS;
+  if (pool.d == 128)
+    return out_f32 ? launch<128, true, true>(a, grid, stream)
+           : chained ? launch<128, false, true>(a, grid, stream) : launch<128, false, false>(a, grid, stream);
+  return out_f32 ? launch<64, true, true>(a, grid, stream)
+         : chained ? launch<64, false, true>(a, grid, stream) : launch<64, false, false>(a, grid, stream);
 }
 
 }  // namespace kvpop

@@ -46,7 +46,7 @@ def _want(what, name, t, dtype, shape):
 class PagedCache:
     """One layer's pages.  ``k_pages, v_pages [n_pages][H][page][d]`` (float8_e4m3fn) and
     ``k_scale, v_scale [n_pages][H][page / 16]`` (fp32) stay the caller's; ``PagedCache.empty``
-    makes them.  ``workspace``: another cache's, to share (some 70 MB; calls on both are then
+    makes them.  ``workspace``: another cache's, to share (some 90 MB; calls on both are then
     serialised, as those of a model's layers are)."""
 
     def __init__(self, k_pages, v_pages, k_scale, v_scale, workspace: Optional[torch.Tensor] = None):
