@@ -82,7 +82,7 @@ class PagedStack:
 
     def capture(self, x_in):
         """A step's layers as a CUDA graph on static ``x_in``; returns the hidden states it leaves.
-        The pages for the tokens to come have to be in the table before a replay."""
+        ``replay`` runs it."""
         stream = torch.cuda.Stream()
         stream.wait_stream(torch.cuda.current_stream())
         self.graph = torch.cuda.CUDAGraph()
@@ -90,9 +90,15 @@ class PagedStack:
             torch.matmul(x_in, self.layers[0]["Wqkv"])          # cuBLAS sets itself up outside a capture only
             with torch.cuda.graph(self.graph, stream=stream):
                 y = self.forward(x_in)
-                self.table.lens += 1
+                self.table.advance_lens()
         torch.cuda.current_stream().wait_stream(stream)
         return y
+
+    def replay(self):
+        """The captured step: one more token of every open place, as ``step``."""
+        self.table.grow(1)
+        self.graph.replay()
+        self.table.advance_held(1)
 
     def check(self):
         """Raises what a kernel recorded (bad tables, a wait that ran out)."""
@@ -122,11 +128,11 @@ def main():
     x = torch.randn((a.batch, a.hidden), generator=g, device="cuda").bfloat16()
     st.table.grow(a.steps + 1)
     st.capture(x)
-    st.graph.replay()
+    st.replay()
     torch.cuda.synchronize()
     t0 = time.perf_counter()
     for _ in range(a.steps):
-        st.graph.replay()
+        st.replay()
     st.check()
     t1 = time.perf_counter()
     print(f"decode: {a.steps} steps of {a.batch} tokens, {1e6 * (t1 - t0) / a.steps:.1f} us a step, "

@@ -260,10 +260,19 @@ class PageTable:
             at = torch.tensor(where, dtype=torch.int64, device=self.dev.device)
             self.dev[at[:, 0], at[:, 1]] = torch.tensor(ids, dtype=torch.int32, device=self.dev.device)
 
+    def advance_lens(self):
+        """One more token of every open place, on the device alone: what a captured step ends with
+        (``advance_held`` then tells the host at each replay)."""
+        self.lens += (self.lens >= 0).to(torch.int32)
+
+    def advance_held(self, new):
+        """The host's part of ``advance``, for tokens by which a replayed graph moved ``lens``."""
+        self.held = [h + c if h >= 0 else h for h, c in zip(self.held, self._new(new))]
+
     def advance(self, new):
         """The new tokens are in every layer's cache."""
         counts = self._new(new)
-        self.held = [h + c if h >= 0 else h for h, c in zip(self.held, counts)]
+        self.advance_held(counts)
         if len(set(counts)) == 1 and min(self.held) >= 0:
             self.lens += counts[0]
         else:
