@@ -67,9 +67,13 @@ class PagedStack:
         return x
 
     def chunk(self, x, new):
-        """``new[s]`` more tokens of every place, their rows in ``x`` one place after the other."""
+        """``new[s]`` more tokens of every open place, their rows in ``x`` one place after the other
+        (idle places have none)."""
+        counts = self.table.counts(new)
+        if x.shape[0] != sum(counts):
+            raise ValueError(f"PagedStack.chunk: {x.shape[0]} rows for {sum(counts)} tokens of the open places")
         self.table.grow(new)
-        y = self.forward(x, self.table.starts(new), max(new))
+        y = self.forward(x, self.table.starts(new), max(counts))
         self.table.advance(new)
         return y
 

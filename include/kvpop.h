@@ -450,7 +450,8 @@ typedef struct {
 /* New tokens of n_seq sequences.  Sequence s holds lens_dev[s] tokens before them (-1: an idle
  * place of the batch, whose tokens are passed over) and its new tokens are the rows starts_dev[s]
  * .. starts_dev[s + 1] - 1 of the token tensors, at the positions lens_dev[s] onwards; without
- * starts_dev each sequence has one, row s.  Entry p / page of row s of the table is the page of
+ * starts_dev each sequence has one, row s.  Rows from starts_dev[n_seq] on are nobody's: nothing of
+ * them is read, and outputs there keep what they held.  Entry p / page of row s of the table is the page of
  * position p.  An entry in use that is no page of the pool, a position past the table's row or
  * offsets that do not ascend are recorded (kvpop_standalone_status) and what they concern is left
  * out; nothing outside the given memory is touched.  Nothing here is changed: the caller advances

@@ -128,7 +128,8 @@ class PagedCache:
         ``cos, sin [positions][rot / 2]`` (none: no rotation) and writes k and ``v`` to the cache
         (q, k and v of one type, bf16 or fp32, any token and head strides of 16 bytes).  ``table
         [n][pages]`` int32, ``lens [n]`` int32 tokens held before (-1: idle), ``starts [n + 1]``
-        int32 first token of each sequence (none: one each).  Returns the rotated queries, bf16."""
+        int32 first token of each sequence (none: one each; rows past its last entry are nobody's and
+        stay as they are in the outputs).  Returns the rotated queries, bf16."""
         what, dtype, n_tokens = "PagedCache.append", k.dtype, k.shape[0]
         code = _CODES.get(dtype)
         if code is None:
@@ -220,7 +221,9 @@ class PageTable:
         self.dev = torch.full((n_seq, max_pages), -1, dtype=torch.int32, device=device)
         self.lens = torch.full((n_seq,), -1, dtype=torch.int32, device=device)
 
-    def _new(self, new) -> List[int]:
+    def counts(self, new) -> List[int]:
+        """Tokens of every place (``new``: a number, or one for each place): none of idle ones, which
+        have no rows among the tokens of a call with ``starts``."""
         n = len(self.held)
         counts = [int(new)] * n if isinstance(new, int) else [int(x) for x in new]
         if len(counts) != n or min(counts, default=0) < 0:
@@ -244,7 +247,7 @@ class PageTable:
     def grow(self, new):
         """Pages for ``new`` more tokens of every sequence (a number, or one for each place); none
         are handed out when they do not suffice (MemoryError)."""
-        counts = self._new(new)
+        counts = self.counts(new)
         need = [max(0, -(-(max(h, 0) + c) // self.page) - len(p)) for h, c, p in zip(self.held, counts, self.pages)]
         if any(len(p) + k > self.max_pages for p, k in zip(self.pages, need)):
             raise MemoryError(f"PageTable: a sequence needs more than {self.max_pages} pages")
@@ -267,11 +270,11 @@ class PageTable:
 
     def advance_held(self, new):
         """The host's part of ``advance``, for tokens by which a replayed graph moved ``lens``."""
-        self.held = [h + c if h >= 0 else h for h, c in zip(self.held, self._new(new))]
+        self.held = [h + c if h >= 0 else h for h, c in zip(self.held, self.counts(new))]
 
     def advance(self, new):
         """The new tokens are in every layer's cache."""
-        counts = self._new(new)
+        counts = self.counts(new)
         self.advance_held(counts)
         if len(set(counts)) == 1 and min(self.held) >= 0:
             self.lens += counts[0]
@@ -279,8 +282,9 @@ class PageTable:
             self.lens += torch.tensor(counts, dtype=torch.int32, device=self.lens.device)
 
     def starts(self, new: Sequence[int]) -> torch.Tensor:
-        """First token of every place, for the calls' ``starts``."""
+        """First token of every place, for the calls' ``starts``: the rows of the open places, one
+        after the other (see ``counts``); the last entry is how many there are."""
         at = [0]
-        for c in self._new(new):
+        for c in self.counts(new):
             at.append(at[-1] + c)
         return torch.tensor(at, dtype=torch.int32, device=self.dev.device)
