@@ -486,7 +486,7 @@ typedef struct {
  * and magnitudes of 2^108 and more are stored as NaN.  A block's first token starts its scale
  * anew; rows past the new tokens keep their bytes.
  *   q [n_tokens][n_q_heads][d] with q_out_dev [n_tokens][n_q_heads][d] bf16 (contiguous, may not
- *   overlap q), or both NULL; k, v [n_tokens][H][d]; dtype of q, k and v
+ *   overlap q, k or v), or both NULL; k, v [n_tokens][H][d]; dtype of q, k and v
  *   cos_dev, sin_dev [max_pos][rot_dim / 2] fp32, 16-byte aligned; rot_dim a multiple of 16, 0 ..
  *   d (0: no rotation, tables unused).  Tokens at max_pos and beyond are recorded and left out.
  * Asynchronous on `stream`; no allocation. */

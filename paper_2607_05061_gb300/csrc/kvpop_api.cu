@@ -5,6 +5,7 @@
 #include <cstdlib>
 #include <cstring>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "kvpop_argmin.cuh"
@@ -819,6 +820,32 @@ static bool paged_aligned(const kvpop_paged_pool* p, const kvpop_paged_batch* b)
   return aligned16(p->k_pages_dev) && aligned16(p->v_pages_dev) && aligned4(p->k_scale_dev) &&
          aligned4(p->v_scale_dev) && aligned4(b->table_dev) && aligned4(b->lens_dev) && aligned4(b->starts_dev);
 }
+// Whether some of rows [tokens][heads][d] lies in the `bytes` bytes from `out` on.
+static bool rows_meet(const kvpop_rows* r, long long tokens, long long heads, long long d, int esz, const void* out,
+                      long long bytes) {
+  typedef __int128 wide;                               // (strides are the caller's, whatever they are)
+  const wide o = (wide)reinterpret_cast<uintptr_t>(out) - (wide)reinterpret_cast<uintptr_t>(r->data_dev);
+  wide ts = (wide)r->token_stride * esz, hs = (wide)r->head_stride * esz, len = d * esz;
+  if (hs == len) {                                     // a token's heads lie together
+    len *= heads;
+    heads = 1;
+  }
+  if (heads > tokens) {                                // the shorter way through
+    std::swap(heads, tokens);
+    std::swap(hs, ts);
+  }
+  for (long long h = 0; h < heads; ++h) {              // runs [at + i step, .. + len) of i < tokens against [o, o + bytes)
+    wide at = h * hs, step = ts;
+    if (step < 0) {
+      at += (tokens - 1) * step;
+      step = -step;
+    }
+    const wide past = o - at - len;                    // the first run that ends behind o
+    const wide i = past < 0 || step == 0 ? (wide)0 : past / step + 1;
+    if (i < tokens && at + i * step + len > o && at + i * step < o + bytes) return true;
+  }
+  return false;
+}
 static paged::Pool paged_pool(const kvpop_paged_pool* p) {
   paged::Pool q;
   q.k = static_cast<unsigned char*>(p->k_pages_dev);
@@ -898,6 +925,12 @@ kvpop_status kvpop_paged_append(const kvpop_paged_pool* pool, const kvpop_paged_
       (q && (!rows_aligned(q, esz) || !aligned16(q_out))) ||
       (rot_dim > 0 && (!aligned16(cos_dev) || !aligned16(sin_dev))))
     return KVPOP_ERR_ALIGN;
+  // rows are read by other threads than those that write q_out
+  const long long out_bytes = 2ll * batch->n_tokens * n_q_heads * pool->head_dim;
+  if (q && (rows_meet(q, batch->n_tokens, n_q_heads, pool->head_dim, esz, q_out, out_bytes) ||
+            rows_meet(k, batch->n_tokens, pool->n_kv_heads, pool->head_dim, esz, q_out, out_bytes) ||
+            rows_meet(v, batch->n_tokens, pool->n_kv_heads, pool->head_dim, esz, q_out, out_bytes)))
+    return KVPOP_ERR_INVALID_ARG;
   const PagedDevice dev = paged_device();
   if (dev.sms <= 0) return KVPOP_ERR_CUDA;
   return from_cuda(NOTE(launch_paged_append(

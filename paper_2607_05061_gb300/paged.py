@@ -129,7 +129,8 @@ class PagedCache:
         (q, k and v of one type, bf16 or fp32, any token and head strides of 16 bytes).  ``table
         [n][pages]`` int32, ``lens [n]`` int32 tokens held before (-1: idle), ``starts [n + 1]``
         int32 first token of each sequence (none: one each; rows past its last entry are nobody's and
-        stay as they are in the outputs).  Returns the rotated queries, bf16."""
+        stay as they are in the outputs).  Returns the rotated queries, bf16, in ``q_out`` if given
+        (no memory of q, k or v)."""
         what, dtype, n_tokens = "PagedCache.append", k.dtype, k.shape[0]
         code = _CODES.get(dtype)
         if code is None:
