@@ -956,6 +956,12 @@ kvpop_status kvpop_paged_attend(const kvpop_paged_pool* pool, const kvpop_paged_
   if (!paged_aligned(pool, batch) || !rows_aligned(q, 2) || !aligned16(out) || !aligned4(lse) ||
       (reinterpret_cast<uintptr_t>(workspace) & 255u))
     return KVPOP_ERR_ALIGN;
+  // a row is written when all that read it are done, so the same place is fine, and another row's is not
+  const bool in_place = out == q->data_dev && out_dtype == KVPOP_BF16 && q->head_stride == pool->head_dim &&
+                        q->token_stride == (int64_t)n_q_heads * pool->head_dim;
+  if (!in_place && rows_meet(q, batch->n_tokens, n_q_heads, pool->head_dim, 2, out,
+                             (out_dtype == KVPOP_F32 ? 4ll : 2ll) * batch->n_tokens * n_q_heads * pool->head_dim))
+    return KVPOP_ERR_INVALID_ARG;
   const PagedDevice dev = paged_device();
   if (dev.sms <= 0) return KVPOP_ERR_CUDA;
   if (workspace_bytes < paged_attend_workspace(dev.sms)) return KVPOP_ERR_INVALID_ARG;

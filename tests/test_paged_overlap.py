@@ -4,7 +4,7 @@ import ctypes
 import pytest
 import torch
 
-from test_paged_arguments import append, batch, kv, pool, rows  # noqa: F401
+from test_paged_arguments import append, attend, batch, kv, pool, rows  # noqa: F401
 
 SIZE = 1 << 16
 BUF = (ctypes.c_char * (SIZE + 256))()
@@ -44,6 +44,35 @@ def test_rotated_queries_over_keys_or_values_are_refused(kv, which):  # noqa: F8
     a = dict(q=far, k=rows(kv, data_dev=AT + 32768), v=rows(kv, data_dev=AT + 32768))
     a[which] = rows(kv, data_dev=AT + 1024 - 16)
     assert append(kv, q_out=AT, **a) == 1
+
+
+@pytest.mark.parametrize("ts,hs", LAYOUTS)
+def test_attention_over_other_rows_of_the_queries_is_refused(kv, ts, hs):  # noqa: F811
+    n, heads, d = 3, 4, 64
+    base = AT + SIZE // 2
+    spans = [(base + 2 * (i * ts + h * hs), base + 2 * (i * ts + h * hs + d)) for i in range(n) for h in range(heads)]
+    for dtype, size in ((kv.KVPOP_F32, 4), (kv.KVPOP_BF16, 2)):
+        for out in range(base - 8192, base + 14000, 16):
+            same = size == 2 and out == base and (ts, hs) == (256, 64)
+            if meets(spans, out, out + size * n * heads * d) and not same:
+                assert attend(kv, b=batch(kv, n_seq=n, n_tokens=n),
+                              q=rows(kv, data_dev=base, token_stride=ts, head_stride=hs), out=out, dtype=dtype) == 1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("new", [1, 5, 70])
+def test_attention_in_place_of_the_queries(cuda_device, new):
+    from test_gpu_paged import make_cache, tables
+    H, G, d, page, held = 2, 4, 128, 16, [700, 30, 2000]
+    cache = make_cache(cuda_device, 190, H, d, page, seed=61)
+    table, lens, starts = tables(held, [new] * 3, page, 190, cuda_device, seed=62)
+    q = (torch.randn((3 * new, H * G, d), generator=torch.Generator().manual_seed(63)) * 0.02).bfloat16().cuda()
+    a = dict(starts=starts, max_new=new, out_dtype=torch.bfloat16)
+    want, _ = cache.attend(table, lens, q, **a)
+    for _ in range(10):
+        x = q.clone()
+        cache.attend(table, lens, x, out=x, **a)
+        assert torch.equal(x, want)
 
 
 @pytest.mark.gpu
