@@ -81,6 +81,11 @@ __device__ __forceinline__ int context(const Batch& b, const Pool& p, const SeqT
   return (int)min(all, cap);
 }
 
+// Last position that token `tok` of a sequence sees, -1 if none, for any length (len + tok may pass an int).
+__device__ __forceinline__ int last_seen(int len, int tok, int ctx) {
+  return (int)min((unsigned)len + 1u + (unsigned)tok, (unsigned)ctx) - 1;
+}
+
 // Whether a sequence's rows go to the tcgen05 kernel, where one is launched.
 constexpr int LONG_ROWS = 64;
 __device__ __forceinline__ bool long_rows(const SeqTokens& t, int G) {

@@ -188,7 +188,7 @@ __device__ __forceinline__ void seek(const AttendArgs& a, Unit& x, long long w) 
   x.rows = min(ROWS, x.u.n * a.G - x.row0);
   x.tok0 = x.row0 / a.G;
   x.rem0 = x.row0 - x.tok0 * a.G;
-  x.lim_hi = min(x.u.len + (x.row0 + x.rows - 1) / a.G, x.u.ctx - 1);
+  x.lim_hi = last_seen(x.u.len, (x.row0 + x.rows - 1) / a.G, x.u.ctx);
 }
 // Token and head of the unit's row i, without an integer division (i < 32, G up to 2^20: the
 // quotient is at most 32, and its distance from the next whole number at least 1 / (2 G)).
@@ -371,7 +371,7 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
     seek<ROWS>(a, x, w);
     if (tid == 0) unitS[turn ^ 1] = x;                     // (read again behind the next barrier)
     const int ta = (int)(w - x.start), tb = (int)min((long long)x.u.blocks, w1 - x.start);
-    const int lim_lo = min(x.u.len + x.tok0, x.u.ctx - 1), lim_hi = x.lim_hi;   // all rows see 0 .. lim_lo
+    const int lim_lo = last_seen(x.u.len, x.tok0, x.u.ctx), lim_hi = x.lim_hi;   // all rows see 0 .. lim_lo
     w = x.end();
 
     // ---- query rows, each scaled by a power of two, and what that makes of the logits
@@ -413,7 +413,7 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
       for (int e = 0; e < 2; ++e) {
         rc[j][e] = __shfl_sync(0xffffffffu, down, (2 * t4 + e) * 4);
         token_of(a, x, min(8 * j + 2 * t4 + e, x.rows - 1), tok, head);
-        lim[j][e] = min(x.u.len + tok, x.u.ctx - 1);
+        lim[j][e] = last_seen(x.u.len, tok, x.u.ctx);
       }
     }
     if (QS) __syncthreads();

@@ -274,8 +274,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
   if (!long_rows(t, G) || row0l < 0 || row0l >= all_rows) return;
   const int row0 = (int)row0l, rows = (int)min((long long)PP_ROWS, all_rows - row0l);
   const int ctx = context(a.b, a.pool, t, a.err);
-  const int lim_lo = min(t.len + row0 / G, ctx - 1);     // every row sees 0 .. lim_lo
-  const int lim_hi = min(t.len + (row0 + rows - 1) / G, ctx - 1);   // none sees past lim_hi
+  const int lim_lo = last_seen(t.len, row0 / G, ctx);    // every row sees 0 .. lim_lo
+  const int lim_hi = last_seen(t.len, (row0 + rows - 1) / G, ctx);   // none sees past lim_hi
   const int blocks = lim_hi / PP_KEYS + 1, part = blockIdx.y;
   const int cut = min((blocks - 1) / share + 1, (int)gridDim.y);
   if (part >= cut) return;
@@ -327,7 +327,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     const int r = row0 + min(tid, rows - 1), tok = r / G;
     const long long off = (t.first + tok) * a.q_ts + (long long)(h * G + (r - tok * G)) * a.q_hs;
     const int c = lane % LPR, sub = lane / LPR;
-    if (tid < rows) lim = min(t.len + tok, ctx - 1);
+    if (tid < rows) lim = last_seen(t.len, tok, ctx);
     uint4 v[IT];
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
