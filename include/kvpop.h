@@ -502,7 +502,7 @@ size_t kvpop_paged_workspace_bytes(void);
 /* Attention of the new tokens over the cache, their own keys (appended before) included: for
  * token i of a sequence and query head h * G + g, over the positions t <= lens + i,
  *   y = sum_t softmax_t(q.k_t / sqrt(d)) v_t,   lse = log sum_t exp(q.k_t / sqrt(d)).
- *   q [n_tokens][n_q_heads][d] bf16, n_q_heads = H * G
+ *   q [n_tokens][n_q_heads][d] bf16, n_q_heads = H * G, n_tokens * G below 2^31 - 1024
  *   out_dev [n_tokens][n_q_heads][d] contiguous, 16-byte aligned, fp32 or bf16 (out_dtype); q
  *   itself where that is contiguous and out bf16, else no memory of q.  Its
  *   type is also the precision of the softmax's weights: 22 bits for fp32, 11 for bf16.  Whatever

@@ -951,6 +951,8 @@ kvpop_status kvpop_paged_attend(const kvpop_paged_pool* pool, const kvpop_paged_
   if (!paged_pool_ok(pool) || !paged_batch_ok(batch) || !q || (out_dtype != KVPOP_F32 && out_dtype != KVPOP_BF16) ||
       n_q_heads < 1 || n_q_heads % pool->n_kv_heads != 0 || n_q_heads > (1 << 20))
     return KVPOP_ERR_INVALID_ARG;
+  // every row (token, query head) of a KV head has a number below 2^31
+  if ((long long)batch->n_tokens * (n_q_heads / pool->n_kv_heads) > INT32_MAX - 1024) return KVPOP_ERR_INVALID_ARG;
   if (batch->n_seq == 0 || batch->n_tokens == 0) return KVPOP_OK;
   if (!batch->table_dev || !batch->lens_dev || !q->data_dev || !out || !workspace) return KVPOP_ERR_INVALID_ARG;
   if (!paged_aligned(pool, batch) || !rows_aligned(q, 2) || !aligned16(out) || !aligned4(lse) ||
