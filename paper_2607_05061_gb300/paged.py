@@ -46,8 +46,9 @@ def _want(what, name, t, dtype, shape):
 class PagedCache:
     """One layer's pages.  ``k_pages, v_pages [n_pages][H][page][d]`` (float8_e4m3fn) and
     ``k_scale, v_scale [n_pages][H][page / 16]`` (fp32) stay the caller's; ``PagedCache.empty``
-    makes them.  ``workspace``: another cache's, to share (some 90 MB; calls on both are then
-    serialised, as those of a model's layers are)."""
+    makes them.  ``workspace``: another cache's, to share (some 90 MB).  Calls of ``attend`` that use
+    one workspace have to follow each other, on one stream or ordered by events, as those of a
+    model's layers do; the class does not see to it.  That goes for one cache used on two streams."""
 
     def __init__(self, k_pages, v_pages, k_scale, v_scale, workspace: Optional[torch.Tensor] = None):
         n, H, page, d = k_pages.shape
@@ -64,6 +65,10 @@ class PagedCache:
         self.k_pages, self.v_pages, self.k_scale, self.v_scale = k_pages, v_pages, k_scale, v_scale
         self.H, self.page, self.d = H, page, d
         self._pool = kvpop_paged_pool(_ptr(k_pages), _ptr(v_pages), _ptr(k_scale), _ptr(v_scale), n, H, d, page)
+        if workspace is not None and (workspace.dtype is not torch.uint8 or workspace.device != self.device or
+                                      not workspace.is_contiguous()):
+            raise ValueError(f"PagedCache: workspace is {workspace.dtype} on {workspace.device}, not another cache's "
+                             f"on {self.device}")
         if workspace is None and self.device.type == "cuda":
             with torch.cuda.device(self.device):
                 workspace = torch.zeros(int(kvpop_paged_workspace_bytes()), dtype=torch.uint8, device=self.device)
