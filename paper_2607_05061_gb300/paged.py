@@ -43,6 +43,16 @@ def _want(what, name, t, dtype, shape):
                          f"contiguous {dtype} {tuple(shape)}")
 
 
+def _output(shape, dtype, device, stream):
+    """A tensor of the stream that the call runs on: the current one's free memory may still be in use."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(_stream(stream), device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 class PagedCache:
     """One layer's pages.  ``k_pages, v_pages [n_pages][H][page][d]`` (float8_e4m3fn) and
     ``k_scale, v_scale [n_pages][H][page / 16]`` (fp32) stay the caller's; ``PagedCache.empty``
@@ -127,6 +137,7 @@ class PagedCache:
         return _rows_bytes(t.data_ptr(), stride[0], stride[1])
 
     # ------------------------------------------------------------------ calls
+    # (with a `stream`, outputs that are not given are that stream's)
     def append(self, table, lens, q, k, v, cos=None, sin=None, starts=None, max_new: Optional[int] = None,
                interleaved: bool = False, q_out=None, stream=None):
         """Rotates the new tokens' ``q [tokens][heads][d]`` and ``k [tokens][H][d]`` by the rows of
@@ -146,7 +157,7 @@ class PagedCache:
         if q is not None:
             qr, heads = self._rows(what, "q", q, dtype, n_tokens, None), q.shape[1]
             if q_out is None:
-                q_out = torch.empty((n_tokens, heads, self.d), dtype=torch.bfloat16, device=k.device)
+                q_out = _output((n_tokens, heads, self.d), torch.bfloat16, k.device, stream)
             _want(what, "q_out", q_out, torch.bfloat16, (n_tokens, heads, self.d))
             to = q_out.data_ptr()
         elif q_out is not None:
@@ -192,13 +203,13 @@ class PagedCache:
         if heads % self.H:
             raise ValueError(f"{what}: {heads} query heads over {self.H} KV heads")
         if out is None:
-            out = torch.empty((n_tokens, heads, self.d), dtype=out_dtype, device=q.device)
+            out = _output((n_tokens, heads, self.d), out_dtype, q.device, stream)
         code = _CODES.get(out.dtype)
         if code is None:
             raise ValueError(f"{what}: out is {out.dtype}, not fp32 or bf16")
         _want(what, "out", out, out.dtype, (n_tokens, heads, self.d))
         if lse is None and want_lse:
-            lse = torch.empty((n_tokens, heads), dtype=torch.float32, device=q.device)
+            lse = _output((n_tokens, heads), torch.float32, q.device, stream)
         if lse is not None:
             _want(what, "lse", lse, torch.float32, (n_tokens, heads))
         batch = self._batch(what, table, lens, starts, n_tokens, max_new)
