@@ -465,7 +465,8 @@ typedef struct {
   int32_t n_seq;               /* >= 0                                                      */
   int32_t n_tokens;            /* rows of the token tensors (n_seq without starts_dev)      */
   int32_t max_new;             /* most new tokens of a sequence, as far as known (>= 1): it
-                                  chooses among kernels, and outputs do not rest on it      */
+                                  chooses among kernels.  Too small a one is slower; outputs
+                                  differ by roundings, within the bounds of each kernel     */
 } kvpop_paged_batch;
 
 /* Rows [token][head][d] with strides in elements, multiples of 16 bytes; d is contiguous. */

@@ -32,7 +32,7 @@
 // several CTAs' parts is joined, in the order of the parts, by the CTA that arrives last, at its end (no
 // CTA waits); many parts join in groups first.
 //
-// 64 sequences of 8192 positions, 32 query and 8 KV heads: 168 us, 0.94 of the copy rate; one of
+// 64 sequences of 8192 positions, 32 query and 8 KV heads: 167 us, 0.94 of the copy rate; one of
 // 131072 52 us (40 by the copy rate: 7 until the stream runs, 5 for the join of 38 parts a head).
 // One CTA of 12 warps an SM took the same for the former and 93 instead of 66 for 40 ragged ones: it
 // streams nothing while its rows join.
@@ -816,13 +816,12 @@ cudaError_t launch_d(AttendArgs& a, int sms, cudaStream_t stream) {
   const int grid = AT_CTAS * sms;
   // Groups of 8 rows a warp takes at once, and its registers (2 CTAs of 6 warps of 168, of 4 of 255, or,
   // for one group at d = 64, of 8 of 128: 64 sequences of 8192 102 us, 108 with 6), by the rows that a
-  // sequence has on average.  One group streams at the rate of HBM and reads
-  // a cache once for each; more read it less often, and compute longer.  16 sequences of 10000
-  // positions and 4 heads, us for 16 / 24 / 32 / 64 rows: fp32 results, groups of 1 (6 warps) 103,
-  // 155, 200, 383; of 2 (4 warps) 80, 140, 141, 262; (6 warps) 93, 161, 162, 303; of 3 118, 122, 213,
-  // 308; of 4 169, 173, 177, -.  bf16: 1 101, 155, 199, 382; 2 (6 warps) 67, 109, 111, 206; (4 warps)
-  // 70, 117, 119, 220; 3 80, 85, 143, 204; 4 96, 100, 104, 179.  Lengths of 8 to 24 rows, 900 to 9000
-  // positions: fp32 68, 64, 74, 77, 104; bf16 61, 53, 56, 56, 65.
+  // sequence has on average.  One group streams at the rate of HBM and reads a cache once for each; more
+  // read it less often, and compute longer.  16 sequences of 10000 positions and 4 heads, us for 8 / 16 /
+  // 24 / 32 / 48 / 64 rows: fp32 results, groups of 1 38, 59, 77, 101, 141, 183; of 2 46, 50, 79, 79, 108,
+  // 139; of 3 67, 71, 75, 120, 122, 167.  bf16: 1 37, 58, 71, 97, 131, 163; 2 42, 45, 66, 67, 89, 114; 3 49,
+  // 52, 56, 87, 88, 119; 4 56, 59, 63, 67, 104, 106.  Lengths of 8 to 24 rows, 900 to 9000 positions: fp32
+  // 68, 63, 78; bf16 62, 54, 58, 66.  (fp32 results of 4 groups, and of 2 with 6 warps, were slower throughout.)
   const long long rows = !a.b.starts || a.skip_long ? a.G : ((long long)a.b.n_tokens * a.G + a.b.n_seq - 1) / a.b.n_seq;
   const int nt = rows <= 8 ? 1 : a.out_f32 ? (rows > 20 && rows <= 24 ? 3 : 2)
                  : rows <= 18 ? 2 : rows <= 24 || (rows > 32 && rows <= 48) ? 3 : 4;

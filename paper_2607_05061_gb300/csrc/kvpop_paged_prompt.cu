@@ -25,11 +25,11 @@
 // the tensor rate), and the softmax's 1270 clocks a warp, which wait for each other across the
 // halves.  A tile costs 7 to 9 us besides: queries, first products, output.
 // A prompt of 8192 tokens with 32 query and 8 KV heads takes 503 us (bf16 results; 773 with fp32
-// ones), 57% of the bf16 rate.  Measured before, in order: blocks of 128 in one
+// ones), 57% of the bf16 rate; at d = 64 331 (520).  Measured before, in order: blocks of 128 in one
 // buffer, where a half's rows and its products took turns, 672; blocks of 64 with P in a place of its
 // own, two waits and two signals a block, 622; P over its logits 575; queries and results read and
 // written by rows, the converters' first tiles beside them 549; blocks that all rows see whole apart,
-// without the masks' selects, 497.  Not kept: softmax warps that ask for the next logits before the
+// without the masks' selects, 497 (503 since the weights are apart from the products' operand).  Not kept: softmax warps that ask for the next logits before the
 // exponentials (642 then) or signal behind the next block's loads (504); register splits between the
 // roles (631); two threads a row (1799); a CTA that takes tile after tile (770: spills).
 #include <type_traits>
