@@ -439,7 +439,8 @@ kvpop_status kvpop_attend_noalloc(const void* slotK_dev, const void* slotV_dev,
 typedef struct {
   void* k_pages_dev;       /* [n_pages][H][page][d], 16-byte aligned                  */
   void* v_pages_dev;       /* the same                                                */
-  float* k_scale_dev;      /* [n_pages][H][page / 16], positive powers of two in use  */
+  float* k_scale_dev;      /* [n_pages][H][page / 16], in use 2^-96 .. 2^100, as append
+                              makes them: powers of two                               */
   float* v_scale_dev;      /* the same                                                */
   int32_t n_pages;         /* >= 1                                                    */
   int32_t n_kv_heads;      /* H >= 1                                                  */
