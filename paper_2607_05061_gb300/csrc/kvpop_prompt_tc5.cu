@@ -74,8 +74,13 @@ constexpr int B_FULL = 0;          // [4]  producers -> MMA
 constexpr int B_EMPTY = 4;         // [4]  MMA -> producers
 constexpr int B_SFULL = 8;         // [2 halves][2 buffers]  MMA -> softmax
 constexpr int B_PFULL = 12;        // [2][2]  softmax -> MMA
+// A wait by parity does not tell the phase it is for from the one two before.  At block j product j - 2
+// is done (the logits of j follow it) and product j is not begun, so that j - 1 can be waited for; at the
+// end the last but one may be open (or not issued: the other half goes first), and the end has a barrier
+// of its own.
 constexpr int B_ODONE = 16;        // [2]  MMA -> softmax (one per half)
 constexpr int B_QFULL = 18;
+constexpr int B_END = 19;          // MMA -> softmax: all products done
 enum : int { T5ERR_WAIT = 21 };
 
 // PACK: an M entry's position and the length of its run of queries share a word (below), so that
@@ -106,6 +111,7 @@ __global__ void __launch_bounds__(T5_THREADS, 1) prompt_t5_kernel(PromptArgs a) 
     mbar_init(bar(B_ODONE + 0), 1);
     mbar_init(bar(B_ODONE + 1), 1);
     mbar_init(bar(B_QFULL), T5_THREADS);
+    mbar_init(bar(B_END), 1);
     mbar_fence_init();
   }
   if (warp == T5_MMA_WARP) tmem_alloc(sb + L::OFF_TMEM, T5_TMEM_COLS);
@@ -235,6 +241,7 @@ __global__ void __launch_bounds__(T5_THREADS, 1) prompt_t5_kernel(PromptArgs a) 
         if (!ok) break;
         if (j + 2 < nblk) issue_s(j + 2);
       }
+      if (lead && ok) commit(bar(B_END));
       __syncwarp();
     } else {
       // ---------------------------------------------------------------- softmax rows
@@ -337,12 +344,11 @@ __global__ void __launch_bounds__(T5_THREADS, 1) prompt_t5_kernel(PromptArgs a) 
       }
       const size_t row = ((size_t)ti.seq * H * G + (size_t)ti.h * G + g) * S + q;
       if (ok && nblk > 0) {
-        ok = uniform(mbar_wait(bar(B_ODONE + h), (nblk - 1) & 1, a.err, T5ERR_WAIT));
+        ok = uniform(mbar_wait(bar(B_END), 0, a.err, T5ERR_WAIT));
         fence_after();
         if (ok) {
           // a warp's 32 rows pass through shared memory, so that a store writes one whole row:
-          // half 0 in the query tile (every S is done), half 1, whose last product is the last
-          // of all, in the first K/V stages
+          // half 0 in the query tile, half 1 in the first K/V stages (every product is done)
           const float inv = 1.f / l;
           const uint32_t tile = sb + (h ? OFF_KV : OFF_Q) + (warp & 3) * (32 * 512);
 #pragma unroll
