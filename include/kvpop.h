@@ -498,6 +498,21 @@ kvpop_status kvpop_paged_append(const kvpop_paged_pool* pool, const kvpop_paged_
                                 const float* sin_dev, int32_t rot_dim, int32_t max_pos,
                                 int32_t interleaved, void* q_out_dev, cudaStream_t stream);
 
+/* kvpop_paged_append for tokens whose positions are not their places in the cache: a cache that
+ * has shed tokens, or tokens with positions on several axes (time, height and width of an image's).
+ * Pair j of token i turns by row positions[i][axes[j]] of the tables; the token's place is
+ * lens + i of its sequence as before.
+ *   positions_dev [n_tokens][n_axes] int32, contiguous, n_axes 1 .. 4; rot_dim >= 16
+ *   axes (host, read by the call) [rot_dim / 2] bytes, each below n_axes; NULL: all 0
+ * A token with a position outside 0 .. max_pos - 1, used by a pair or not, is recorded and left out:
+ * its query row, keys and values keep what they held, and its block's scale does not count it. */
+kvpop_status kvpop_paged_append_at(const kvpop_paged_pool* pool, const kvpop_paged_batch* batch,
+                                   const kvpop_rows* q, int32_t n_q_heads, const kvpop_rows* k,
+                                   const kvpop_rows* v, kvpop_dtype dtype, const float* cos_dev,
+                                   const float* sin_dev, int32_t rot_dim, int32_t max_pos,
+                                   int32_t interleaved, const int32_t* positions_dev, int32_t n_axes,
+                                   const uint8_t* axes, void* q_out_dev, cudaStream_t stream);
+
 /* Bytes of device workspace kvpop_paged_attend needs on the current device (0 without one). */
 size_t kvpop_paged_workspace_bytes(void);
 
@@ -521,6 +536,44 @@ kvpop_status kvpop_paged_attend(const kvpop_paged_pool* pool, const kvpop_paged_
                                 const kvpop_rows* q, int32_t n_q_heads, void* out_dev,
                                 kvpop_dtype out_dtype, float* lse_dev, void* workspace_dev,
                                 size_t workspace_bytes, cudaStream_t stream);
+
+/* Attention weights of the cache's positions, added up over the new tokens and the G query heads of
+ * each KV head: for sequence s, head h and every position t < lens + n,
+ *   mass[s][h][t] = (t < lens ? mass[s][h][t] : 0) + sum_{i: t <= lens + i} sum_g exp(q.k_t / sqrt(d) - lse),
+ * so that the new tokens' own positions start from nothing, and a tensor that is kept along with the
+ * cache holds each position's accumulated weight.
+ *   q [n_tokens][n_q_heads][d] bf16, and lse_dev [n_tokens][n_q_heads] fp32, as the attention took
+ *   and returned them (a normaliser of -inf: a row that saw nothing, and gives nothing)
+ *   mass_dev [n_seq][H][positions] fp32, positions >= max_pages * page, no memory of q or lse
+ * Positions from lens + n on and idle places keep what they held.  Results do not depend on order.
+ * Asynchronous on `stream`; no allocation, no workspace. */
+kvpop_status kvpop_paged_weigh(const kvpop_paged_pool* pool, const kvpop_paged_batch* batch,
+                               const kvpop_rows* q, int32_t n_q_heads, const float* lse_dev,
+                               float* mass_dev, int64_t positions, cudaStream_t stream);
+
+/* Eviction: sequences with more than `keep` tokens are cut down to keep, for each KV head by itself,
+ * and every sequence moves to new pages.  Of L = lens tokens a head keeps all if L <= keep, else the
+ * first `sinks`, the last `window`, and of the others the keep - sinks - window of largest mass (NaN
+ * as -inf, zeros alike; the lower position first among equals), in the order of their positions.
+ * They become positions 0 .. min(L, keep) - 1 of the pages in the sequence's row of to_table_dev:
+ * scales and bytes as kvpop_paged_append would store the held values, but that a value that falls
+ * below 2^-6 of its new scale is rounded a second time.
+ *   batch: table, lens and n_seq are used      mass_dev [n_seq][H][positions], positions >= max_pages * page
+ *   to_table_dev [n_seq] rows of to_pages entries, to_stride apart, keep <= to_pages * page: no page
+ *   of them is one that the batch's sequences hold, or in two rows (pages read may be shared)
+ *   0 <= sinks, 0 <= window, sinks + window <= keep
+ *   kept_dev [n_seq][H][keep] int32 out: the positions kept, -1 behind them
+ *   new_mass_dev [n_seq][H][new_positions] fp32 out or NULL: their mass (new_positions >= keep; what
+ *   lies behind them stays); no memory of mass_dev or kept_dev
+ *   new_lens_dev [n_seq] int32 out or NULL: tokens held now, -1 for idle places; not lens_dev
+ * The token's positions are no longer their places: kvpop_paged_append_at takes what comes next.  Bad
+ * entries of either table are recorded (kvpop_standalone_status) and the rows that they concern left
+ * out.  Asynchronous on `stream`; no allocation, no workspace. */
+kvpop_status kvpop_paged_evict(const kvpop_paged_pool* pool, const kvpop_paged_batch* batch,
+                               const float* mass_dev, int64_t positions, const int32_t* to_table_dev,
+                               int64_t to_stride, int32_t to_pages, int32_t keep, int32_t sinks,
+                               int32_t window, int32_t* kept_dev, float* new_mass_dev,
+                               int64_t new_positions, int32_t* new_lens_dev, cudaStream_t stream);
 
 /* Description of the last failing CUDA call made by this library on the
  * calling thread ("" if none): call site, error name and message. */

@@ -84,3 +84,36 @@ def attend(q, k, v):
     top = x.max()
     p = np.exp(x - top)
     return p @ np.asarray(v, np.float64) / p.sum(), top + math.log(p.sum())
+
+
+def weights(q, k, lse):
+    """What one query row [d] with normaliser lse gives to k [t][d]: exp(q k / sqrt(d) - lse); nothing
+    where lse is -inf."""
+    if lse == -math.inf:
+        return np.zeros(len(k))
+    return np.exp(np.asarray(k, np.float64) @ np.asarray(q, np.float64) / math.sqrt(len(q)) - float(lse))
+
+
+def kept(mass, keep, sinks, window):
+    """Positions that stay, ascending, of those that mass [t] has: one head's, taken one at a time."""
+    n = len(mass)
+    if n <= keep:
+        return list(range(n))
+    stay = list(range(sinks)) + list(range(n - window, n))
+    rest = list(range(sinks, n - window))
+    for _ in range(keep - sinks - window):
+        best = rest[0]
+        for t in rest:                                   # strictly larger: the lower position among equals
+            a, b = (-math.inf if math.isnan(mass[i]) else float(mass[i]) for i in (t, best))
+            if a > b:
+                best = t
+        rest.remove(best)
+        stay.append(best)
+    return sorted(stay)
+
+
+def store_block(codes, scales):
+    """Bytes [n][d] (n <= 16) of one new block, and its scale, from codes [n][d] under scales [n]."""
+    x = E4M3[codes] * np.asarray(scales, np.float64)[:, None]
+    scale = 2.0 ** exponent(np.abs(x[np.isfinite(x)]).max(initial=0.0))
+    return round_e4m3(x / scale), scale

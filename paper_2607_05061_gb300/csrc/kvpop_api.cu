@@ -904,26 +904,35 @@ static PagedDevice paged_device() {
   return d;
 }
 
-kvpop_status kvpop_paged_append(const kvpop_paged_pool* pool, const kvpop_paged_batch* batch,
-                                const kvpop_rows* q, int32_t n_q_heads, const kvpop_rows* k,
-                                const kvpop_rows* v, kvpop_dtype dtype, const float* cos_dev,
-                                const float* sin_dev, int32_t rot_dim, int32_t max_pos,
-                                int32_t interleaved, void* q_out, cudaStream_t stream) {
+// `at`: whether positions are given
+static kvpop_status paged_append(const kvpop_paged_pool* pool, const kvpop_paged_batch* batch,
+                                 const kvpop_rows* q, int32_t n_q_heads, const kvpop_rows* k,
+                                 const kvpop_rows* v, kvpop_dtype dtype, const float* cos_dev,
+                                 const float* sin_dev, int32_t rot_dim, int32_t max_pos,
+                                 int32_t interleaved, bool at, const int32_t* positions, int32_t n_axes,
+                                 const uint8_t* axes, void* q_out, cudaStream_t stream) {
   if (!paged_pool_ok(pool) || !paged_batch_ok(batch) || !k || !v || (dtype != KVPOP_F32 && dtype != KVPOP_BF16) ||
       (q == nullptr) != (q_out == nullptr) || (q && (n_q_heads < 1 || n_q_heads > (1 << 20))) || rot_dim < 0 ||
       rot_dim > pool->head_dim || rot_dim % 16 != 0 || (rot_dim > 0 && (!cos_dev || !sin_dev || max_pos < 1)) ||
       (interleaved != 0 && interleaved != 1))
     return KVPOP_ERR_INVALID_ARG;
+  if (at) {
+    if (rot_dim == 0 || n_axes < 1 || n_axes > 4) return KVPOP_ERR_INVALID_ARG;
+    if (axes)
+      for (int j = 0; j < rot_dim / 2; ++j)
+        if (axes[j] >= n_axes) return KVPOP_ERR_INVALID_ARG;
+  }
   // every (block of tokens, head) has a number below 2^31
   const long long units = (long long)batch->n_tokens / paged::BLK + 2ll * batch->n_seq;
   if (units * (2ll * pool->n_kv_heads + (q ? n_q_heads : 0)) > INT32_MAX - 1024) return KVPOP_ERR_INVALID_ARG;
   if (batch->n_seq == 0 || batch->n_tokens == 0) return KVPOP_OK;
-  if (!batch->table_dev || !batch->lens_dev || !k->data_dev || !v->data_dev || (q && !q->data_dev))
+  if (!batch->table_dev || !batch->lens_dev || !k->data_dev || !v->data_dev || (q && !q->data_dev) ||
+      (at && !positions))
     return KVPOP_ERR_INVALID_ARG;
   const int esz = dtype == KVPOP_BF16 ? 2 : 4;
   if (!paged_aligned(pool, batch) || !rows_aligned(k, esz) || !rows_aligned(v, esz) ||
       (q && (!rows_aligned(q, esz) || !aligned16(q_out))) ||
-      (rot_dim > 0 && (!aligned16(cos_dev) || !aligned16(sin_dev))))
+      (rot_dim > 0 && (!aligned16(cos_dev) || !aligned16(sin_dev))) || !aligned4(positions))
     return KVPOP_ERR_ALIGN;
   // rows are read by other threads than those that write q_out
   const long long out_bytes = 2ll * batch->n_tokens * n_q_heads * pool->head_dim;
@@ -936,8 +945,27 @@ kvpop_status kvpop_paged_append(const kvpop_paged_pool* pool, const kvpop_paged_
   return from_cuda(NOTE(launch_paged_append(
       paged_pool(pool), paged_batch(batch), q ? q->data_dev : nullptr, q ? q->token_stride : 0,
       q ? q->head_stride : 0, n_q_heads, k->data_dev, k->token_stride, k->head_stride, v->data_dev,
-      v->token_stride, v->head_stride, dtype, cos_dev, sin_dev, rot_dim, max_pos, interleaved, q_out,
-      dev.err, stream)));
+      v->token_stride, v->head_stride, dtype, cos_dev, sin_dev, rot_dim, max_pos, interleaved,
+      at ? positions : nullptr, n_axes, axes, q_out, dev.err, stream)));
+}
+
+kvpop_status kvpop_paged_append(const kvpop_paged_pool* pool, const kvpop_paged_batch* batch,
+                                const kvpop_rows* q, int32_t n_q_heads, const kvpop_rows* k,
+                                const kvpop_rows* v, kvpop_dtype dtype, const float* cos_dev,
+                                const float* sin_dev, int32_t rot_dim, int32_t max_pos,
+                                int32_t interleaved, void* q_out, cudaStream_t stream) {
+  return paged_append(pool, batch, q, n_q_heads, k, v, dtype, cos_dev, sin_dev, rot_dim, max_pos, interleaved,
+                      false, nullptr, 1, nullptr, q_out, stream);
+}
+
+kvpop_status kvpop_paged_append_at(const kvpop_paged_pool* pool, const kvpop_paged_batch* batch,
+                                   const kvpop_rows* q, int32_t n_q_heads, const kvpop_rows* k,
+                                   const kvpop_rows* v, kvpop_dtype dtype, const float* cos_dev,
+                                   const float* sin_dev, int32_t rot_dim, int32_t max_pos,
+                                   int32_t interleaved, const int32_t* positions_dev, int32_t n_axes,
+                                   const uint8_t* axes, void* q_out, cudaStream_t stream) {
+  return paged_append(pool, batch, q, n_q_heads, k, v, dtype, cos_dev, sin_dev, rot_dim, max_pos, interleaved,
+                      true, positions_dev, n_axes, axes, q_out, stream);
 }
 
 size_t kvpop_paged_workspace_bytes(void) {
@@ -970,6 +998,87 @@ kvpop_status kvpop_paged_attend(const kvpop_paged_pool* pool, const kvpop_paged_
   return from_cuda(NOTE(launch_paged_attend(paged_pool(pool), paged_batch(batch), q->data_dev, q->token_stride,
                                             q->head_stride, n_q_heads, out, out_dtype == KVPOP_F32, lse, workspace,
                                             dev.sms, dev.err, stream)));
+}
+
+// Whether two ranges of memory share a byte.
+static bool ranges_meet(const void* p, long long p_bytes, const void* q, long long q_bytes) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return a < b + (uintptr_t)q_bytes && b < a + (uintptr_t)p_bytes;
+}
+// Whether [n_seq][H][positions] floats can be counted in bytes, and have room for what the table holds.
+static bool mass_ok(const kvpop_paged_pool* p, long long n_seq, long long positions, long long pages) {
+  return positions >= pages * p->page && (__int128)n_seq * p->n_kv_heads * positions < ((__int128)1 << 60);
+}
+
+kvpop_status kvpop_paged_weigh(const kvpop_paged_pool* pool, const kvpop_paged_batch* batch,
+                               const kvpop_rows* q, int32_t n_q_heads, const float* lse_dev, float* mass_dev,
+                               int64_t positions, cudaStream_t stream) {
+  if (!paged_pool_ok(pool) || !paged_batch_ok(batch) || !q || n_q_heads < 1 || n_q_heads % pool->n_kv_heads != 0 ||
+      n_q_heads > (1 << 20) || !mass_ok(pool, batch->n_seq, positions, batch->max_pages))
+    return KVPOP_ERR_INVALID_ARG;
+  if ((long long)batch->n_tokens * (n_q_heads / pool->n_kv_heads) > INT32_MAX - 1024) return KVPOP_ERR_INVALID_ARG;
+  if (batch->n_seq == 0 || batch->n_tokens == 0) return KVPOP_OK;
+  if (!batch->table_dev || !batch->lens_dev || !q->data_dev || !lse_dev || !mass_dev) return KVPOP_ERR_INVALID_ARG;
+  if (!paged_aligned(pool, batch) || !rows_aligned(q, 2) || !aligned4(lse_dev) || !aligned4(mass_dev))
+    return KVPOP_ERR_ALIGN;
+  const long long bytes = 4ll * batch->n_seq * pool->n_kv_heads * positions;
+  if (rows_meet(q, batch->n_tokens, n_q_heads, pool->head_dim, 2, mass_dev, bytes) ||
+      ranges_meet(lse_dev, 4ll * batch->n_tokens * n_q_heads, mass_dev, bytes))
+    return KVPOP_ERR_INVALID_ARG;
+  const PagedDevice dev = paged_device();
+  if (dev.sms <= 0) return KVPOP_ERR_CUDA;
+  return from_cuda(NOTE(launch_paged_weigh(paged_pool(pool), paged_batch(batch), q->data_dev, q->token_stride,
+                                           q->head_stride, n_q_heads, lse_dev, mass_dev, positions, dev.sms,
+                                           dev.err, stream)));
+}
+
+kvpop_status kvpop_paged_evict(const kvpop_paged_pool* pool, const kvpop_paged_batch* batch,
+                               const float* mass_dev, int64_t positions, const int32_t* to_table_dev,
+                               int64_t to_stride, int32_t to_pages, int32_t keep, int32_t sinks,
+                               int32_t window, int32_t* kept_dev, float* new_mass_dev,
+                               int64_t new_positions, int32_t* new_lens_dev, cudaStream_t stream) {
+  if (!paged_pool_ok(pool) || !batch || batch->n_seq < 0 || batch->max_pages < 1 ||
+      batch->table_stride < batch->max_pages || !mass_ok(pool, batch->n_seq, positions, batch->max_pages) ||
+      to_pages < 1 || to_stride < to_pages || keep < 1 || keep > (long long)to_pages * pool->page || sinks < 0 ||
+      window < 0 || (long long)sinks + window > keep)
+    return KVPOP_ERR_INVALID_ARG;
+  if (new_mass_dev && (new_positions < keep || !mass_ok(pool, batch->n_seq, new_positions, 0)))
+    return KVPOP_ERR_INVALID_ARG;
+  // every (sequence, head, 16 kept tokens) has a number that a grid can hold, and so has every cluster's CTA
+  const long long rows = (long long)batch->n_seq * pool->n_kv_heads;
+  if (rows > INT32_MAX / 8 || (__int128)rows * ((keep + paged::BLK - 1) / paged::BLK) > (__int128)INT32_MAX * 4)
+    return KVPOP_ERR_INVALID_ARG;
+  if (rows == 0) return KVPOP_OK;
+  if (!batch->table_dev || !batch->lens_dev || !mass_dev || !to_table_dev || !kept_dev) return KVPOP_ERR_INVALID_ARG;
+  if (!aligned16(pool->k_pages_dev) || !aligned16(pool->v_pages_dev) || !aligned4(pool->k_scale_dev) ||
+      !aligned4(pool->v_scale_dev) || !aligned4(batch->table_dev) || !aligned4(batch->lens_dev) ||
+      !aligned4(mass_dev) || !aligned4(to_table_dev) || !aligned4(kept_dev) || !aligned4(new_mass_dev) ||
+      !aligned4(new_lens_dev))
+    return KVPOP_ERR_ALIGN;
+  // weights are read while others' are written, and lengths
+  const long long mass_bytes = 4 * rows * positions, kept_bytes = 4 * rows * keep;
+  const long long new_bytes = new_mass_dev ? 4 * rows * new_positions : 0, lens_bytes = 4ll * batch->n_seq;
+  if (ranges_meet(mass_dev, mass_bytes, kept_dev, kept_bytes) ||
+      (new_mass_dev && (ranges_meet(mass_dev, mass_bytes, new_mass_dev, new_bytes) ||
+                        ranges_meet(kept_dev, kept_bytes, new_mass_dev, new_bytes))) ||
+      (new_lens_dev && ranges_meet(batch->lens_dev, lens_bytes, new_lens_dev, lens_bytes)))
+    return KVPOP_ERR_INVALID_ARG;
+  const PagedDevice dev = paged_device();
+  if (dev.sms <= 0) return KVPOP_ERR_CUDA;
+  PagedEvict e{};
+  e.mass = mass_dev;
+  e.to = to_table_dev;
+  e.kept = kept_dev;
+  e.new_mass = new_mass_dev;
+  e.new_lens = new_lens_dev;
+  e.positions = positions;
+  e.new_positions = new_positions;
+  e.to_stride = to_stride;
+  e.to_pages = to_pages;
+  e.keep = keep;
+  e.sinks = sinks;
+  e.window = window;
+  return from_cuda(NOTE(launch_paged_evict(paged_pool(pool), paged_batch(batch), e, dev.sms, dev.err, stream)));
 }
 
 kvpop_status kvpop_decode_ingest(kvpop_cache* c, const void* q, const void* k, const void* v,

@@ -112,6 +112,65 @@ __device__ __forceinline__ float2 down2(float d) {
   return make_float2(ex2(fmaxf(d, -90.f)), ex2(fminf(d + 90.f, 0.f)));
 }
 
+// Least e with amax <= 448 * 2^e, at least E_MIN; amax finite.
+__device__ __forceinline__ int scale_exponent(float amax) {
+  const uint32_t u = __float_as_uint(amax);
+  return max((int)(u >> 23) - 135 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0), E_MIN);
+}
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
+__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// Codes multiplied by f (a power of two) and rounded again; NaN stays NaN.
+__device__ __forceinline__ uint32_t rescale2(uint32_t two, float f) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)two));
+  const float2 v = __half22float2(*reinterpret_cast<__half2*>(&h));
+  return e4m3x2(v.x * f, v.y * f);
+}
+__device__ __forceinline__ uint32_t rescale4(uint32_t w, float f) {
+  return rescale2(w & 0xffffu, f) | rescale2(w >> 16, f) << 16;
+}
+
+// m16n8k16 of f16 with fp32 sums
+__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                        uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9},"
+      " {%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// the same from zero
+__device__ __forceinline__ void mma_f16_0(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                          uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9},"
+      " {%10, %10, %10, %10};"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+// four e4m3 bytes -> two words of two f16
+__device__ __forceinline__ void cvt4(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\t"
+      "cvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
+      : "=r"(lo), "=r"(hi)
+      : "r"(w));
+}
+__device__ __forceinline__ uint32_t movm(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<uint32_t*>(&v);
+}
+
 // raise_smem_limit once per device (`done`: one bit each, of one kernel): it takes longer on the
 // host than a launch.
 template <typename K>
@@ -131,8 +190,26 @@ inline cudaError_t raise_smem_limit_once(std::atomic<unsigned long long>& done, 
 cudaError_t launch_paged_append(const paged::Pool& pool, const paged::Batch& b, const void* q, long long q_ts,
                                 long long q_hs, int HQ, const void* k, long long k_ts, long long k_hs,
                                 const void* v, long long v_ts, long long v_hs, int dtype, const float* cos_,
-                                const float* sin_, int rot, int max_pos, int interleaved, void* q_out,
+                                const float* sin_, int rot, int max_pos, int interleaved,
+                                const int32_t* positions, int n_axes, const uint8_t* axes, void* q_out,
                                 int32_t* err, cudaStream_t stream);
+
+// Selection and move of kept tokens: `kept` [n_seq][H][keep], to: rows of to_pages pages, to_stride apart.
+struct PagedEvict {
+  const float* mass;                   // [n_seq][H][positions]
+  const int32_t* to;
+  int32_t* kept;
+  float* new_mass;                     // [n_seq][H][new_positions], or null
+  int32_t* new_lens;                   // [n_seq], or null
+  long long positions, new_positions, to_stride;
+  int to_pages, keep, sinks, window;
+};
+cudaError_t launch_paged_evict(const paged::Pool& pool, const paged::Batch& b, const PagedEvict& e, int sms,
+                               int32_t* err, cudaStream_t stream);
+
+cudaError_t launch_paged_weigh(const paged::Pool& pool, const paged::Batch& b, const void* q, long long q_ts,
+                               long long q_hs, int HQ, const float* lse, float* mass, long long positions, int sms,
+                               int32_t* err, cudaStream_t stream);
 
 // Bytes of the attention's workspace on a device with that many SMs.  The counters at its start have
 // to be zero before the first call and are zero after every call.

@@ -11,6 +11,9 @@
 // codes that fall below 2^-6.  A block's first token starts its scale anew, so what a page held
 // for an earlier owner does not matter; rows past the new tokens are not touched.
 //
+// With positions given (AT), token i turns by them instead of p: pair j by row positions[i][axes[j]] of
+// the tables.  Its place in the cache stays p.
+//
 // Bound by memory: K, V and q are read once, codes and rotated queries written once.  One warp
 // takes one head of K or V, or two of q, over the (at most 16) new tokens of one block, so that a
 // block's scale and codes have one writer; with one token a sequence, D / 8 lanes take a head.  16384
@@ -38,6 +41,9 @@ struct AppendArgs {
   bf16* q_out;
   int32_t* err;
   int tasks, HQ, rot, max_pos, interleaved;
+  const int32_t* at;                   // [n_tokens][n_axes] positions that turn the tokens, or null: their places
+  int n_axes;
+  uint32_t axes[16];                   // a byte for each pair: the axis that it turns with
 };
 
 // Loads that no store of this kernel can change.  (As volatile assembly they stay behind
@@ -119,6 +125,41 @@ __device__ __forceinline__ Turn turn_of(const AppendArgs& a, const Lane& n, cons
     for (int i = 0; i < 8; ++i) t.sn[i] = -t.sn[i];
   return t;
 }
+// The same by a token's positions: 4 neighbouring pairs of one axis are one load.
+__device__ __forceinline__ Turn turn_at(const AppendArgs& a, const Lane& n, const int32_t* at) {
+  Turn t;
+  if (!n.turned) return t;
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    if (e && a.interleaved) break;                  // (4 pairs)
+    const uint32_t ax = a.axes[(n.angle >> 2) + e];
+    const int j = n.angle + 4 * e;
+    const long long half = a.rot >> 1, row = at[ax & 255] * half;
+    float4 c, s;
+    if (ax == (ax & 255) * 0x01010101u) {
+      c = ld16f(a.cosT + row + j);
+      s = ld16f(a.sinT + row + j);
+    } else {
+      const long long r1 = at[ax >> 8 & 255] * half, r2 = at[ax >> 16 & 255] * half;
+      const long long r3 = at[ax >> 24] * half;
+      c = make_float4(a.cosT[row + j], a.cosT[r1 + j + 1], a.cosT[r2 + j + 2], a.cosT[r3 + j + 3]);
+      s = make_float4(a.sinT[row + j], a.sinT[r1 + j + 1], a.sinT[r2 + j + 2], a.sinT[r3 + j + 3]);
+    }
+    t.cs[4 * e] = c.x; t.cs[4 * e + 1] = c.y; t.cs[4 * e + 2] = c.z; t.cs[4 * e + 3] = c.w;
+    t.sn[4 * e] = s.x; t.sn[4 * e + 1] = s.y; t.sn[4 * e + 2] = s.z; t.sn[4 * e + 3] = s.w;
+  }
+  if (n.low && !a.interleaved)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t.sn[i] = -t.sn[i];
+  return t;
+}
+// Whether all of a token's positions are in the tables.
+__device__ __forceinline__ bool in_tables(const AppendArgs& a, const int32_t* at) {
+  bool ok = true;
+  for (int i = 0; i < a.n_axes; ++i) ok &= (unsigned)at[i] < (unsigned)a.max_pos;
+  if (!ok) report(a.err, ERR_ROTATION);
+  return ok;
+}
 template <typename T>
 __device__ __forceinline__ void rotated(const AppendArgs& a, const Lane& n, const Turn& t, const Raw<T>& own,
                                         const Raw<T>& other, float (&x)[8]) {
@@ -139,18 +180,6 @@ __device__ __forceinline__ void rotated(const AppendArgs& a, const Lane& n, cons
   }
 }
 
-// Least e with amax <= 448 * 2^e, at least E_MIN; amax finite.
-__device__ __forceinline__ int scale_exponent(float amax) {
-  const uint32_t u = __float_as_uint(amax);
-  return max((int)(u >> 23) - 135 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0), E_MIN);
-}
-__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
-
-__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-  return r;
-}
 // Codes of 8 values under the scale 2^e (inv = 2^-e); all finite ones are at most 448 * 2^e, unless
 // `special`: then those that no scale holds become NaN (a NaN does by itself).
 __device__ __forceinline__ uint2 codes8(const float (&x)[8], float inv, bool special) {
@@ -163,17 +192,6 @@ __device__ __forceinline__ uint2 codes8(const float (&x)[8], float inv, bool spe
       if (!(fabsf(x[i]) < VALUE_LIMIT)) y[i] = __uint_as_float(0x7fffffffu);
   return make_uint2(e4m3x2(y[0], y[1]) | e4m3x2(y[2], y[3]) << 16, e4m3x2(y[4], y[5]) | e4m3x2(y[6], y[7]) << 16);
 }
-// Codes multiplied by f (a power of two) and rounded again; NaN stays NaN.
-__device__ __forceinline__ uint32_t rescale2(uint32_t two, float f) {
-  uint32_t h;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)two));
-  const float2 v = __half22float2(*reinterpret_cast<__half2*>(&h));
-  return e4m3x2(v.x * f, v.y * f);
-}
-__device__ __forceinline__ uint32_t rescale4(uint32_t w, float f) {
-  return rescale2(w & 0xffffu, f) | rescale2(w >> 16, f) << 16;
-}
-
 // Sends every RPI-th of a lane's `rows` rows to L2, for up to NH heads: the loads that follow, a few
 // rows at a time, then wait for L2 only.
 template <typename T, int IT, int RPI, int NH>
@@ -188,8 +206,8 @@ __device__ __forceinline__ void ahead(const T* p, long long ts, long long hs, in
 }
 
 // ONE: one token a sequence.  D / 8 lanes per row; a warp takes one (block, head) of up to 16 rows,
-// or, with ONE, 32 / (D / 8) of them with one row each.
-template <typename T, int D, bool ONE>
+// or, with ONE, 32 / (D / 8) of them with one row each.  AT: positions are given.
+template <typename T, int D, bool ONE, bool AT>
 __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendArgs a) {
   constexpr int LPR = D / 8, RPI = 32 / LPR, IT = ONE ? 1 : BLK / RPI, QH = ONE ? 1 : AP_QH;
   const int lane = threadIdx.x & 31, c = lane % LPR, sub = lane / LPR;
@@ -228,12 +246,13 @@ __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendAr
       p0 = (int)max(first, (long long)t.len);
       end = (int)min(min(all, first + BLK), (long long)cap);
       if (min(all, first + BLK) > cap) report(a.err, ERR_PAGE);
-      if (a.rot > 0 && end > a.max_pos) {
+      if (!AT && a.rot > 0 && end > a.max_pos) {
         report(a.err, ERR_ROTATION);
         end = a.max_pos;
       }
     }
   }
+  if (AT && ONE && p0 < end && !in_tables(a, a.at + (long long)t.first * a.n_axes)) end = p0;
   const bool some = p0 < end;
   if (!ONE && !some) return;                        // warp-uniform
 
@@ -243,13 +262,15 @@ __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendAr
     int pos = ONE ? p0 : p0 + sub;
     const long long tok = t.first + (pos - t.len);
     const T* from = static_cast<const T*>(a.q) + tok * a.q_ts + h0 * a.q_hs;
-    const float *cosR = a.cosT + (long long)pos * (a.rot >> 1) + n.angle, *sinR = a.sinT + (cosR - a.cosT);
+    const float *cosR = AT ? nullptr : a.cosT + (long long)pos * (a.rot >> 1) + n.angle;
+    const float* sinR = AT ? nullptr : a.sinT + (cosR - a.cosT);
     bf16* to = a.q_out + (tok * a.HQ + h0) * D + n.own;
     if (!ONE) ahead<T, IT, RPI, QH>(from + n.own, a.q_ts, a.q_hs, min(a.HQ - h0, QH), end - pos, c);
 #pragma unroll 1
     for (int it = 0; it < IT; ++it) {
-      if (pos < end) {
-        const Turn turn = turn_of(a, n, cosR, sinR);
+      const int32_t* at = AT ? a.at + (t.first + (pos - t.len)) * (long long)a.n_axes : nullptr;
+      if (pos < end && (!AT || ONE || in_tables(a, at))) {
+        const Turn turn = AT ? turn_at(a, n, at) : turn_of(a, n, cosR, sinR);
         Raw<T> own[QH], other[QH];
 #pragma unroll
         for (int e = 0; e < QH; ++e) {
@@ -267,8 +288,10 @@ __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendAr
       }
       pos += RPI;
       from += RPI * a.q_ts;
-      cosR += RPI * (a.rot >> 1);
-      sinR += RPI * (a.rot >> 1);
+      if (!AT) {
+        cosR += RPI * (a.rot >> 1);
+        sinR += RPI * (a.rot >> 1);
+      }
       to += (long long)RPI * a.HQ * D;
     }
     if (!ONE) return;
@@ -296,13 +319,21 @@ __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendAr
   const T* const from = src + (t.first + (pos0 - t.len)) * ts;
   const long long angle0 = (long long)pos0 * (a.rot >> 1) + n.angle;
   if (!ONE && id >= 0) ahead<T, IT, RPI, 1>(from + n.own, ts, 0, 1, end - pos0, c);
+  const int32_t* const at0 = AT ? a.at + (t.first + (pos0 - t.len)) * (long long)a.n_axes : nullptr;
+  uint32_t ok = 0;                                  // AT: the lane's rows whose positions are in the tables
+  if (AT && id >= 0)
+#pragma unroll
+    for (int it = 0; it < IT; ++it)
+      if (pos0 + it * RPI < end && (ONE || in_tables(a, at0 + (long long)it * RPI * a.n_axes))) ok |= 1u << it;
+  auto taken = [&](int it) { return AT ? (ok >> it & 1u) != 0 : pos0 + it * RPI < end; };
   auto read = [&](int it, float (&x)[8]) {
     const T* row = from + it * RPI * ts;
     const long long at = angle0 + it * RPI * (a.rot >> 1);
     Raw<T> own, other;
     own.load(row + n.own);
     other.load(row + n.other);
-    rotated(a, n, turn_of(a, n, a.cosT + at, a.sinT + at), own, other, x);
+    rotated(a, n, AT ? turn_at(a, n, at0 + (long long)it * RPI * a.n_axes) : turn_of(a, n, a.cosT + at, a.sinT + at),
+            own, other, x);
   };
   auto value = [&](int it, float (&x)[8], bool again) {
     if (!KEEP || !again) {
@@ -318,7 +349,7 @@ __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendAr
     if (id >= 0)
 #pragma unroll 2
       for (int it = 0; it < IT; ++it)
-        if (pos0 + it * RPI < end) {
+        if (taken(it)) {
           float x[8];
           value(it, x, limit > 0.f);
           if (KEEP && limit == 0.f) {
@@ -357,7 +388,7 @@ __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendAr
   unsigned char* to = rows + (head + (pos0 - p0)) * D + n.own;
 #pragma unroll 2
   for (int it = 0; it < IT; ++it)
-    if (pos0 + it * RPI < end) {
+    if (taken(it)) {
       float x[8];
       value(it, x, true);
       *reinterpret_cast<uint2*>(to + it * RPI * D) = codes8(x, inv, special);
@@ -381,8 +412,11 @@ cudaError_t launch(AppendArgs& a, cudaStream_t stream) {
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  return one ? cudaLaunchKernelEx(&cfg, paged_append_kernel<T, D, true>, a)
-             : cudaLaunchKernelEx(&cfg, paged_append_kernel<T, D, false>, a);
+  if (a.at)
+    return one ? cudaLaunchKernelEx(&cfg, paged_append_kernel<T, D, true, true>, a)
+               : cudaLaunchKernelEx(&cfg, paged_append_kernel<T, D, false, true>, a);
+  return one ? cudaLaunchKernelEx(&cfg, paged_append_kernel<T, D, true, false>, a)
+             : cudaLaunchKernelEx(&cfg, paged_append_kernel<T, D, false, false>, a);
 }
 
 }  // namespace
@@ -390,9 +424,13 @@ cudaError_t launch(AppendArgs& a, cudaStream_t stream) {
 cudaError_t launch_paged_append(const Pool& pool, const Batch& b, const void* q, long long q_ts, long long q_hs,
                                 int HQ, const void* k, long long k_ts, long long k_hs, const void* v,
                                 long long v_ts, long long v_hs, int dtype, const float* cos_, const float* sin_,
-                                int rot, int max_pos, int interleaved, void* q_out, int32_t* err,
-                                cudaStream_t stream) {
+                                int rot, int max_pos, int interleaved, const int32_t* positions, int n_axes,
+                                const uint8_t* axes, void* q_out, int32_t* err, cudaStream_t stream) {
   AppendArgs a{};
+  a.at = positions;
+  a.n_axes = n_axes;
+  if (axes)
+    for (int j = 0; j < rot / 2; ++j) a.axes[j >> 2] |= (uint32_t)axes[j] << 8 * (j & 3);
   a.pool = pool;
   a.b = b;
   a.q = q;

@@ -112,8 +112,13 @@ _SIGS = {
     "kvpop_project_out_settled": (ctypes.c_int, [_P, _P, _P, c_int32, c_int32, c_int32, _P, _P]),
     "kvpop_paged_append": (ctypes.c_int, [_P, _P, _P, c_int32, _P, _P, ctypes.c_int, _P, _P, c_int32, c_int32,
                                           c_int32, _P, _P]),
+    "kvpop_paged_append_at": (ctypes.c_int, [_P, _P, _P, c_int32, _P, _P, ctypes.c_int, _P, _P, c_int32, c_int32,
+                                             c_int32, _P, c_int32, _P, _P, _P]),
     "kvpop_paged_workspace_bytes": (c_size_t, []),
     "kvpop_paged_attend": (ctypes.c_int, [_P, _P, _P, c_int32, _P, ctypes.c_int, _P, _P, c_size_t, _P]),
+    "kvpop_paged_weigh": (ctypes.c_int, [_P, _P, _P, c_int32, _P, _P, ctypes.c_int64, _P]),
+    "kvpop_paged_evict": (ctypes.c_int, [_P, _P, _P, ctypes.c_int64, _P, ctypes.c_int64, c_int32, c_int32, c_int32,
+                                         c_int32, _P, _P, ctypes.c_int64, _P, _P]),
     "kvpop_standalone_status": (ctypes.c_int, [_P]),
     "kvpop_last_error": (ctypes.c_char_p, []),
     "kvpop_debug_fail_alloc_after": (None, [c_int32]),

@@ -22,8 +22,8 @@ from typing import List, Optional, Sequence
 
 import torch
 
-from .kvpop import (KVPOP_BF16, KVPOP_F32, _ck, _ptr, _raw_stream, _stream, kvpop_paged_append,
-                    kvpop_paged_attend, kvpop_paged_batch, kvpop_paged_pool, kvpop_paged_workspace_bytes, kvpop_rows)
+from .kvpop import (KVPOP_BF16, KVPOP_F32, _ck, _ptr, _raw_stream, _stream, kvpop_paged_append, kvpop_paged_append_at,
+                    kvpop_paged_evict, kvpop_paged_weigh, kvpop_paged_attend, kvpop_paged_batch, kvpop_paged_pool, kvpop_paged_workspace_bytes, kvpop_rows)
 
 BLOCK = 16               # tokens that share a scale
 _F8 = torch.float8_e4m3fn
@@ -139,14 +139,16 @@ class PagedCache:
     # ------------------------------------------------------------------ calls
     # (with a `stream`, outputs that are not given are that stream's)
     def append(self, table, lens, q, k, v, cos=None, sin=None, starts=None, max_new: Optional[int] = None,
-               interleaved: bool = False, q_out=None, stream=None):
+               interleaved: bool = False, q_out=None, stream=None, positions=None, axes=None):
         """Rotates the new tokens' ``q [tokens][heads][d]`` and ``k [tokens][H][d]`` by the rows of
         ``cos, sin [positions][rot / 2]`` (none: no rotation) and writes k and ``v`` to the cache
         (q, k and v of one type, bf16 or fp32, any token and head strides of 16 bytes).  ``table
         [n][pages]`` int32, ``lens [n]`` int32 tokens held before (-1: idle), ``starts [n + 1]``
         int32 first token of each sequence (none: one each; rows past its last entry are nobody's and
-        stay as they are in the outputs).  Returns the rotated queries, bf16, in ``q_out`` if given
-        (no memory of q, k or v)."""
+        stay as they are in the outputs).  ``positions [tokens]`` or ``[tokens][up to 4 axes]`` int32:
+        what turns the tokens, where that is not their place in the cache (none: ``lens`` onwards);
+        ``axes``: the axis of each of the rot / 2 pairs (bytes, or numbers; with one axis not needed).
+        Returns the rotated queries, bf16, in ``q_out`` if given (no memory of q, k or v)."""
         what, dtype, n_tokens = "PagedCache.append", k.dtype, k.shape[0]
         code = _CODES.get(dtype)
         if code is None:
@@ -162,21 +164,41 @@ class PagedCache:
             to = q_out.data_ptr()
         elif q_out is not None:
             raise ValueError(f"{what}: q_out without q")
-        rot = positions = 0
+        rot = rows = 0
         cos_ptr = sin_ptr = None
         if cos is not None and sin is not None:
             angles = cos.shape
-            positions, rot = angles[0], 2 * angles[1]
-            if positions < 1 or rot < 16 or rot > self.d or rot % 16:
+            rows, rot = angles[0], 2 * angles[1]
+            if rows < 1 or rot < 16 or rot > self.d or rot % 16:
                 raise ValueError(f"{what}: cos is {tuple(cos.shape)}: 2 * {rot // 2} values of {self.d} cannot be "
                                  "rotated (a multiple of 16 can)")
             if cos.dtype is not torch.float32 or sin.dtype is not torch.float32 or sin.shape != angles or \
                     len(angles) != 2 or not cos.is_contiguous() or not sin.is_contiguous():
-                _want(what, "cos", cos, torch.float32, (positions, rot // 2))
-                _want(what, "sin", sin, torch.float32, (positions, rot // 2))
+                _want(what, "cos", cos, torch.float32, (rows, rot // 2))
+                _want(what, "sin", sin, torch.float32, (rows, rot // 2))
             cos_ptr, sin_ptr = cos.data_ptr(), sin.data_ptr()
         elif cos is not None or sin is not None:
             raise ValueError(f"{what}: cos and sin come together")
+        if positions is not None:
+            if cos is None:
+                raise ValueError(f"{what}: positions without cos and sin")
+            shape = positions.shape
+            n_axes = shape[1] if len(shape) == 2 else 1
+            if not 1 <= n_axes <= 4 or len(shape) > 2:
+                raise ValueError(f"{what}: positions are {tuple(shape)}, not ({n_tokens}, up to 4)")
+            _want(what, "positions", positions, torch.int32, (n_tokens,) if len(shape) < 2 else (n_tokens, n_axes))
+            if positions.get_device() != self._index:
+                self._elsewhere(what, positions)
+            if axes is None:
+                if n_axes > 1:
+                    raise ValueError(f"{what}: positions on {n_axes} axes without axes")
+            else:
+                axes = bytes(axes)
+                if len(axes) != rot // 2 or max(axes) >= n_axes:
+                    raise ValueError(f"{what}: axes are {len(axes)} numbers up to {max(axes, default=0)}, not {rot // 2} "
+                                     f"below {n_axes}")
+        elif axes is not None:
+            raise ValueError(f"{what}: axes without positions")
         batch = self._batch(what, table, lens, starts, n_tokens, max_new)
         at = self._index
         if not (table.get_device() == lens.get_device() == k.get_device() == v.get_device() == at and
@@ -185,10 +207,14 @@ class PagedCache:
                 (starts is None or starts.get_device() == at)):
             self._elsewhere(what, table, lens, starts, q, k, v, cos, sin, q_out)
         on = self._on(what, stream)
-        status = kvpop_paged_append(self._pool_ptr, batch, qr, heads, kr, vr, code, cos_ptr, sin_ptr, rot, positions,
-                                    1 if interleaved else 0, to, on)
+        if positions is None:
+            status = kvpop_paged_append(self._pool_ptr, batch, qr, heads, kr, vr, code, cos_ptr, sin_ptr, rot, rows,
+                                        1 if interleaved else 0, to, on)
+        else:
+            status = kvpop_paged_append_at(self._pool_ptr, batch, qr, heads, kr, vr, code, cos_ptr, sin_ptr, rot, rows,
+                                           1 if interleaved else 0, positions.data_ptr(), n_axes, axes, to, on)
         if status != 0:
-            _ck(status, "kvpop_paged_append")
+            _ck(status, "kvpop_paged_append" if positions is None else "kvpop_paged_append_at")
         return q_out
 
     def attend(self, table, lens, q, starts=None, max_new: Optional[int] = None, out=None, lse=None,
@@ -223,6 +249,76 @@ class PagedCache:
         if status != 0:
             _ck(status, "kvpop_paged_attend")
         return out, lse
+
+
+    def _mass(self, what, name, mass, n, room):
+        shape = mass.shape
+        if mass.dtype is not torch.float32 or len(shape) != 3 or shape[0] != n or shape[1] != self.H or \
+                shape[2] < room or not mass.is_contiguous():
+            raise ValueError(f"{what}: {name} is {mass.dtype} {tuple(shape)} (strides {tuple(mass.stride())}), not "
+                             f"contiguous {torch.float32} ({n}, {self.H}, {room} or more)")
+
+    def weigh(self, table, lens, q, lse, mass, starts=None, max_new: Optional[int] = None, stream=None):
+        """Adds the attention weights of the new tokens' ``q`` (as ``attend`` took it, with the ``lse``
+        that it returned) to ``mass [n][H][positions]`` fp32, positions at least the table's pages times
+        the page: over all query heads of a KV head, for each position of its sequence.  The new tokens'
+        own positions start from nothing, so that a tensor kept along with the cache holds what each
+        position has got so far.  Returns ``mass``."""
+        what = "PagedCache.weigh"
+        n_tokens, heads = q.shape[0], q.shape[1]
+        qr = self._rows(what, "q", q, torch.bfloat16, n_tokens, None)
+        if heads % self.H:
+            raise ValueError(f"{what}: {heads} query heads over {self.H} KV heads")
+        _want(what, "lse", lse, torch.float32, (n_tokens, heads))
+        batch = self._batch(what, table, lens, starts, n_tokens, max_new)
+        self._mass(what, "mass", mass, table.shape[0], table.shape[1] * self.page)
+        self._elsewhere(what, table, lens, starts, q, lse, mass)
+        on = self._on(what, stream)
+        status = kvpop_paged_weigh(self._pool_ptr, batch, qr, heads, lse.data_ptr(), mass.data_ptr(), mass.shape[2], on)
+        if status != 0:
+            _ck(status, "kvpop_paged_weigh")
+        return mass
+
+    def evict(self, table, lens, mass, to, keep: int, sinks: int = 0, window: int = 0, kept=None, new_mass=None,
+              new_lens=None, stream=None):
+        """Cuts sequences of more than ``keep`` tokens down to that, for each KV head by itself: the first
+        ``sinks``, the last ``window``, and of the others those of largest ``mass`` (see ``weigh``; the
+        lower position first among equals), in their order.  All sequences' tokens move to the pages of
+        ``to [n][pages]`` int32, none of which the sequences hold (``PageTable.shrink`` hands them out);
+        the old ones are not changed.  Returns (lengths ``[n]`` int32, the kept positions ``[n][H][keep]``
+        int32, -1 behind them), in ``new_lens`` and ``kept`` if given; their weights go to ``new_mass
+        [n][H][keep or more]`` if given.  What is appended next needs ``positions``: places are no longer
+        those."""
+        what = "PagedCache.evict"
+        n = lens.shape[0] if len(lens.shape) else 0
+        batch = self._batch(what, table, lens, None, n, None)
+        keep, sinks, window = int(keep), int(sinks), int(window)
+        shape, stride = to.shape, to.stride()
+        if to.dtype is not torch.int32 or len(shape) != 2 or shape[0] != n or shape[1] < 1 or stride[1] != 1 or \
+                (n > 1 and stride[0] < shape[1]):
+            raise ValueError(f"{what}: to is {to.dtype} {tuple(shape)} (strides {tuple(stride)}), not {torch.int32} "
+                             f"({n}, pages) with neighbouring entries")
+        if not 1 <= keep <= min(shape[1] * self.page, 0x7fffffff) or sinks < 0 or window < 0 or sinks + window > keep:
+            raise ValueError(f"{what}: keep {keep} of at most {shape[1] * self.page} places, {sinks} sinks and a window "
+                             f"of {window}")
+        self._mass(what, "mass", mass, n, table.shape[1] * self.page)
+        if kept is None:
+            kept = _output((n, self.H, keep), torch.int32, mass.device, stream)
+        _want(what, "kept", kept, torch.int32, (n, self.H, keep))
+        if new_lens is None:
+            new_lens = _output((n,), torch.int32, mass.device, stream)
+        _want(what, "new_lens", new_lens, torch.int32, (n,))
+        if new_mass is not None:
+            self._mass(what, "new_mass", new_mass, n, keep)
+        self._elsewhere(what, table, lens, mass, to, kept, new_mass, new_lens)
+        on = self._on(what, stream)
+        status = kvpop_paged_evict(self._pool_ptr, batch, mass.data_ptr(), mass.shape[2], to.data_ptr(),
+                                   max(stride[0], shape[1]), shape[1], keep, sinks, window, kept.data_ptr(),
+                                   None if new_mass is None else new_mass.data_ptr(),
+                                   0 if new_mass is None else new_mass.shape[2], new_lens.data_ptr(), on)
+        if status != 0:
+            _ck(status, "kvpop_paged_evict")
+        return new_lens, kept
 
 
 class PageTable:
