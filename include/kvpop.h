@@ -537,6 +537,27 @@ kvpop_status kvpop_paged_attend(const kvpop_paged_pool* pool, const kvpop_paged_
                                 kvpop_dtype out_dtype, float* lse_dev, void* workspace_dev,
                                 size_t workspace_bytes, cudaStream_t stream);
 
+/* The same for sequences that share prefixes, each of which is read once for all tokens of its group.
+ *   groups_dev [n_groups + 1] int32, ascending, 0 .. n_seq: group g is the places groups[g] ..
+ *     groups[g + 1] - 1 of the batch; places of no group are computed as kvpop_paged_attend does
+ *   prefix_dev [n_groups] int32: the first prefix[g] positions of group g's sequences are the same
+ *     (their rows of the table need not be: one member's are read; idle places do not matter).  What
+ *     passes the shortest member's tokens is not taken as shared, nor is what is left of a multiple
+ *     of 64; a group with fewer than two members that have tokens, or fewer than 64 positions, is none
+ * Offsets that do not ascend are recorded, and what they concern is left out.  Other arguments and the
+ * precision as kvpop_paged_attend, whose workspace it shares.
+ *   scratch_dev: kvpop_paged_shared_bytes(...) bytes (0: arguments that the call refuses; some
+ *     8 (d + 2) a token and query head), 256-byte aligned, of no content before or after
+ * Asynchronous on `stream`; no allocation. */
+size_t kvpop_paged_shared_bytes(const kvpop_paged_pool* pool, const kvpop_paged_batch* batch,
+                                int32_t n_groups, int32_t n_q_heads);
+kvpop_status kvpop_paged_attend_shared(const kvpop_paged_pool* pool, const kvpop_paged_batch* batch,
+                                       const kvpop_rows* q, int32_t n_q_heads, const int32_t* groups_dev,
+                                       const int32_t* prefix_dev, int32_t n_groups, void* out_dev,
+                                       kvpop_dtype out_dtype, float* lse_dev, void* workspace_dev,
+                                       size_t workspace_bytes, void* scratch_dev, size_t scratch_bytes,
+                                       cudaStream_t stream);
+
 /* Attention weights of the cache's positions, added up over the new tokens and the G query heads of
  * each KV head: for sequence s, head h and every position t < lens + n,
  *   mass[s][h][t] = (t < lens ? mass[s][h][t] : 0) + sum_{i: t <= lens + i} sum_g exp(q.k_t / sqrt(d) - lse),

@@ -973,15 +973,18 @@ size_t kvpop_paged_workspace_bytes(void) {
   return sms > 0 ? paged_attend_workspace(sms) : 0;
 }
 
-kvpop_status kvpop_paged_attend(const kvpop_paged_pool* pool, const kvpop_paged_batch* batch,
-                                const kvpop_rows* q, int32_t n_q_heads, void* out, kvpop_dtype out_dtype,
-                                float* lse, void* workspace, size_t workspace_bytes, cudaStream_t stream) {
+// What both attention calls ask of their arguments (KVPOP_OK: go on; `none`: there is nothing to do).
+static kvpop_status paged_attend_check(const kvpop_paged_pool* pool, const kvpop_paged_batch* batch,
+                                       const kvpop_rows* q, int32_t n_q_heads, const void* out,
+                                       kvpop_dtype out_dtype, const float* lse, const void* workspace, bool& none) {
+  none = false;
   if (!paged_pool_ok(pool) || !paged_batch_ok(batch) || !q || (out_dtype != KVPOP_F32 && out_dtype != KVPOP_BF16) ||
       n_q_heads < 1 || n_q_heads % pool->n_kv_heads != 0 || n_q_heads > (1 << 20))
     return KVPOP_ERR_INVALID_ARG;
   // every row (token, query head) of a KV head has a number below 2^31
   if ((long long)batch->n_tokens * (n_q_heads / pool->n_kv_heads) > INT32_MAX - 1024) return KVPOP_ERR_INVALID_ARG;
-  if (batch->n_seq == 0 || batch->n_tokens == 0) return KVPOP_OK;
+  none = batch->n_seq == 0 || batch->n_tokens == 0;
+  if (none) return KVPOP_OK;
   if (!batch->table_dev || !batch->lens_dev || !q->data_dev || !out || !workspace) return KVPOP_ERR_INVALID_ARG;
   if (!paged_aligned(pool, batch) || !rows_aligned(q, 2) || !aligned16(out) || !aligned4(lse) ||
       (reinterpret_cast<uintptr_t>(workspace) & 255u))
@@ -992,12 +995,59 @@ kvpop_status kvpop_paged_attend(const kvpop_paged_pool* pool, const kvpop_paged_
   if (!in_place && rows_meet(q, batch->n_tokens, n_q_heads, pool->head_dim, 2, out,
                              (out_dtype == KVPOP_F32 ? 4ll : 2ll) * batch->n_tokens * n_q_heads * pool->head_dim))
     return KVPOP_ERR_INVALID_ARG;
+  return KVPOP_OK;
+}
+
+kvpop_status kvpop_paged_attend(const kvpop_paged_pool* pool, const kvpop_paged_batch* batch,
+                                const kvpop_rows* q, int32_t n_q_heads, void* out, kvpop_dtype out_dtype,
+                                float* lse, void* workspace, size_t workspace_bytes, cudaStream_t stream) {
+  bool none;
+  const kvpop_status s = paged_attend_check(pool, batch, q, n_q_heads, out, out_dtype, lse, workspace, none);
+  if (s != KVPOP_OK || none) return s;
   const PagedDevice dev = paged_device();
   if (dev.sms <= 0) return KVPOP_ERR_CUDA;
   if (workspace_bytes < paged_attend_workspace(dev.sms)) return KVPOP_ERR_INVALID_ARG;
   return from_cuda(NOTE(launch_paged_attend(paged_pool(pool), paged_batch(batch), q->data_dev, q->token_stride,
                                             q->head_stride, n_q_heads, out, out_dtype == KVPOP_F32, lse, workspace,
                                             dev.sms, dev.err, stream)));
+}
+
+static bool paged_shared_ok(const kvpop_paged_pool* pool, const kvpop_paged_batch* batch, int32_t n_groups,
+                            int32_t n_q_heads) {
+  return paged_pool_ok(pool) && paged_batch_ok(batch) && n_groups >= 1 && n_q_heads >= 1 &&
+         n_q_heads % pool->n_kv_heads == 0 && n_q_heads <= (1 << 20) &&
+         (long long)batch->n_tokens * (n_q_heads / pool->n_kv_heads) <= INT32_MAX - 1024 &&
+         paged_shared_fits(paged_pool(pool), paged_batch(batch), n_groups, n_q_heads);
+}
+
+size_t kvpop_paged_shared_bytes(const kvpop_paged_pool* pool, const kvpop_paged_batch* batch, int32_t n_groups,
+                                int32_t n_q_heads) {
+  if (!paged_shared_ok(pool, batch, n_groups, n_q_heads)) return 0;
+  return paged_shared_scratch(paged_pool(pool), paged_batch(batch), n_groups, n_q_heads);
+}
+
+kvpop_status kvpop_paged_attend_shared(const kvpop_paged_pool* pool, const kvpop_paged_batch* batch,
+                                       const kvpop_rows* q, int32_t n_q_heads, const int32_t* groups_dev,
+                                       const int32_t* prefix_dev, int32_t n_groups, void* out,
+                                       kvpop_dtype out_dtype, float* lse, void* workspace,
+                                       size_t workspace_bytes, void* scratch, size_t scratch_bytes,
+                                       cudaStream_t stream) {
+  bool none;
+  const kvpop_status s = paged_attend_check(pool, batch, q, n_q_heads, out, out_dtype, lse, workspace, none);
+  if (s != KVPOP_OK) return s;
+  if (!paged_shared_ok(pool, batch, n_groups, n_q_heads)) return KVPOP_ERR_INVALID_ARG;
+  if (none) return KVPOP_OK;
+  if (!groups_dev || !prefix_dev || !scratch) return KVPOP_ERR_INVALID_ARG;
+  if (!aligned4(groups_dev) || !aligned4(prefix_dev) || (reinterpret_cast<uintptr_t>(scratch) & 255u))
+    return KVPOP_ERR_ALIGN;
+  const PagedDevice dev = paged_device();
+  if (dev.sms <= 0) return KVPOP_ERR_CUDA;
+  if (workspace_bytes < paged_attend_workspace(dev.sms) ||
+      scratch_bytes < kvpop_paged_shared_bytes(pool, batch, n_groups, n_q_heads))
+    return KVPOP_ERR_INVALID_ARG;
+  return from_cuda(NOTE(launch_paged_shared(paged_pool(pool), paged_batch(batch), groups_dev, prefix_dev, n_groups,
+                                            q->data_dev, q->token_stride, q->head_stride, n_q_heads, out,
+                                            out_dtype == KVPOP_F32, lse, workspace, scratch, dev.sms, dev.err, stream)));
 }
 
 // Whether two ranges of memory share a byte.

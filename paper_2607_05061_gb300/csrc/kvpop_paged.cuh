@@ -171,6 +171,27 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   return *reinterpret_cast<uint32_t*>(&v);
 }
 
+// Attention over shared prefixes reads the positions of a batch in parts: those that the sequences of a
+// group share, for all their tokens at once, and each sequence's own.  An entry is one such part; the
+// groups come first.
+struct Entry {
+  int first, n;                        // tokens
+  int len;                             // as a sequence's; larger than any position for a group's part, which all tokens see
+  int ctx, begin;                      // positions [begin, ctx), begin a multiple of SHARED_STEP
+  int row;                             // of the page table
+  int group;                           // a sequence's group, -1: none
+  int place;                           // first tile of the tcgen05 kernel, -1: has few rows
+};
+constexpr int SHARED_STEP = 64;        // blocks of the tcgen05 kernel
+struct Parts {
+  const Entry* entries;                // [groups + sequences]
+  int n_groups;
+  long long rows;                      // n_tokens * query heads
+  float* sums;                         // [own, group's][rows][d]
+  float2* ml;                          // [own, group's][rows] what the sums are relative to, and the weights' sums
+  int* cuts;                           // [tiles] parts that a tile's positions were cut into
+};
+
 // raise_smem_limit once per device (`done`: one bit each, of one kernel): it takes longer on the
 // host than a launch.
 template <typename K>
@@ -217,6 +238,15 @@ size_t paged_attend_workspace(int sms);
 cudaError_t launch_paged_attend(const paged::Pool& pool, const paged::Batch& b, const void* q, long long q_ts,
                                 long long q_hs, int HQ, void* out, int out_f32, float* lse, void* workspace,
                                 int sms, int32_t* err, cudaStream_t stream);
+
+// Attention of batches whose sequences share prefixes (groups [n_groups + 1], prefix [n_groups]), where
+// paged_shared_fits; the workspace is the attention's.
+bool paged_shared_fits(const paged::Pool& pool, const paged::Batch& b, int n_groups, int HQ);
+size_t paged_shared_scratch(const paged::Pool& pool, const paged::Batch& b, int n_groups, int HQ);
+cudaError_t launch_paged_shared(const paged::Pool& pool, const paged::Batch& b, const int32_t* groups,
+                                const int32_t* prefix, int n_groups, const void* q, long long q_ts, long long q_hs,
+                                int HQ, void* out, int out_f32, float* lse, void* workspace, void* scratch, int sms,
+                                int32_t* err, cudaStream_t stream);
 
 // The same for sequences with long_rows, where paged_prompt_fits.  Its share of the workspace:
 // counters (zero between calls) and partial results.

@@ -1,0 +1,382 @@
+// Attention over the paged 8-bit cache for sequences that share prefixes.
+//
+// The sequences of a group have the same first positions.  With S the shared ones and O_s a
+// sequence's own, a row's softmax over both is joined from two:
+//   m = max(m_S, m_O),  l = l_S 2^(m_S - m) + l_O 2^(m_O - m),  y = (A_S 2^(m_S - m) + A_O 2^(m_O - m)) / l,
+// A being the sums of weights times values relative to m.  S is read once for the rows of all the
+// group's tokens, as a sequence with that many tokens whose positions all of them see.
+//
+// Four kernels in a row: the plan writes the list of parts (each group's, each sequence's own); the
+// attention's two kernels take them as they take sequences, those with many rows on tcgen05, whose
+// positions are cut over all SMs, and beside them the stream for few rows; the join reads each row's
+// sums.  The number of shared positions is a multiple of 64 (blocks of the tcgen05 kernel): what is
+// left of a prefix counts as the sequences' own.
+#include "kvpop_paged_attend.cuh"
+#include "kvpop_paged_prompt.cuh"
+
+namespace kvpop {
+namespace {
+
+constexpr int PLAN_THREADS = 256;
+constexpr int ANY_LEN = 0x7fffff00;    // as a length: its tokens see all positions there are
+
+struct PlanArgs {
+  Pool pool;
+  Batch b;
+  const int32_t *groups, *prefix;
+  int32_t* err;
+  Entry* entries;
+  int n_groups, G, tiles;              // tiles of the tcgen05 kernel that there is room for, of one head (0: not launched)
+  int own_tiles;                       // whether it takes sequences' own parts
+};
+
+__global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(PlanArgs a) {
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n = a.b.n_seq, ng = a.n_groups;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  for (int s = tid; s < n; s += PLAN_THREADS) {
+    const SeqTokens t = seq_tokens(a.b, s, a.err);
+    Entry e;
+    e.first = t.first;
+    e.n = t.n;
+    e.len = t.len;
+    e.ctx = t.n > 0 ? context(a.b, a.pool, t, a.err) : 0;
+    e.begin = 0;
+    e.row = s;
+    e.group = e.place = -1;
+    a.entries[ng + s] = e;
+  }
+  __syncthreads();
+  for (int g = warp; g < ng; g += PLAN_THREADS / 32) {
+    int from = a.groups[g], to = a.groups[g + 1];
+    if (from < 0 || to < from || to > n) {
+      if (lane == 0) report(a.err, ERR_BATCH);
+      from = to = 0;
+    }
+    int least = a.prefix[g], members = 0, lead = INT32_MAX, first = INT32_MAX, end = 0;
+    for (int s = from + lane; s < to; s += 32) {
+      const Entry& e = a.entries[ng + s];
+      if (e.n <= 0) continue;
+      first = min(first, e.first);
+      end = max(end, e.first + e.n);
+      if (e.len < 0) continue;
+      ++members;
+      lead = min(lead, s);
+      least = min(least, min(e.len, e.ctx));
+    }
+    members = __reduce_add_sync(0xffffffffu, members);
+    lead = __reduce_min_sync(0xffffffffu, lead);
+    least = __reduce_min_sync(0xffffffffu, least);
+    first = __reduce_min_sync(0xffffffffu, first);
+    end = __reduce_max_sync(0xffffffffu, end);
+    const int shared = members < 2 ? 0 : max(least, 0) / SHARED_STEP * SHARED_STEP;
+    if (lane == 0) {
+      Entry e;
+      e.first = shared > 0 ? first : 0;
+      e.n = shared > 0 ? end - first : 0;
+      e.len = ANY_LEN;
+      e.ctx = shared;
+      e.begin = 0;
+      e.row = shared > 0 ? lead : 0;
+      e.group = e.place = -1;
+      a.entries[g] = e;
+    }
+    if (shared > 0)
+      for (int s = from + lane; s < to; s += 32) {
+        Entry& e = a.entries[ng + s];
+        if (e.n > 0 && e.len >= 0) {
+          e.begin = shared;
+          e.group = g;
+        }
+      }
+  }
+  if (a.tiles == 0) return;
+  __syncthreads();
+  if (warp == 0) {                     // tiles of those with many rows
+    int place = 0;
+    for (int i0 = 0; i0 < ng + n; i0 += 32) {
+      const int i = i0 + lane;
+      int k = 0;
+      if (i < ng + n && (i < ng || a.own_tiles)) {
+        const Entry& e = a.entries[i];
+        const long long rows = (long long)e.n * a.G;
+        if (e.len >= 0 && rows > LONG_ROWS) k = (int)min((rows + PP_ROWS - 1) / PP_ROWS, (long long)(1 << 24));
+      }
+      int pre = k;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, pre, o);
+        if (lane >= o) pre = min(pre + y, 1 << 28);
+      }
+      if (k > 0) {
+        if (place + pre <= a.tiles) a.entries[i].place = place + pre - k;
+        else report(a.err, ERR_BATCH); // (offsets that do not ascend: the other kernel takes it)
+      }
+      place = min(place + __shfl_sync(0xffffffffu, pre, 31), 1 << 28);
+    }
+  }
+}
+
+struct JoinArgs {
+  Batch b;
+  Parts from;
+  const float* part;                   // sums of the tcgen05 kernel's cut tiles
+  const float2* part_ml;
+  void* out;
+  float* lse;
+  int H, G, out_f32, places;           // places: parts that a tile has room for
+};
+constexpr int JOIN_WARPS = 8, JOIN_HEADS = 4;   // query heads that a warp takes in turn
+
+template <int D>
+__global__ void __launch_bounds__(32 * JOIN_WARPS) shared_join_kernel(JoinArgs a) {
+  constexpr int CH = D / 4, AT_ONCE = 32 / CH;   // lanes of a row, parts at once
+  const int lane = threadIdx.x & 31, cc = lane % CH, sub = lane / CH, HQ = a.H * a.G;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int per = (HQ + JOIN_HEADS - 1) / JOIN_HEADS;
+  const long long task = (long long)blockIdx.x * JOIN_WARPS + (threadIdx.x >> 5);
+  const int tok = (int)(task / per), h0 = (int)(task - (long long)tok * per) * JOIN_HEADS;
+  if (tok >= a.b.n_tokens) return;
+  int s = tok;
+  if (a.b.starts) {
+    if (tok >= a.b.starts[a.b.n_seq]) return;    // nobody's
+    int lo = 0, hi = a.b.n_seq - 1;              // the last sequence that starts at or before the token
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (a.b.starts[mid] <= tok) lo = mid; else hi = mid - 1;
+    }
+    s = lo;
+  }
+  const Entry own = a.from.entries[a.from.n_groups + s];
+  const Entry shared = own.group >= 0 ? a.from.entries[own.group] : Entry{};
+#pragma unroll 1
+  for (int hq = h0; hq < min(h0 + JOIN_HEADS, HQ); ++hq) {
+    const int h = hq / a.G, g = hq - h * a.G;
+    const long long row = (long long)tok * HQ + hq;
+    float M = -INFINITY, L = 0.f;
+    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+    for (int w = 0; w < (own.group >= 0 ? 2 : 1); ++w) {
+      const Entry& e = w ? shared : own;
+      const int r = (tok - e.first) * a.G + g;
+      const int pair = e.place >= 0 ? (e.place + r / PP_ROWS) * a.H + h : 0;
+      const int cut = e.place >= 0 ? a.from.cuts[pair] : 1;
+      const long long at = row + (w ? a.from.rows : 0), slot0 = (long long)pair * a.places;
+      const bool split = cut > 1;
+      float2 ml = make_float2(-INFINITY, 0.f);
+      if (lane < cut) ml = split ? __ldcg(a.part_ml + (slot0 + lane) * PP_ROWS + r % PP_ROWS) : __ldcg(a.from.ml + at);
+      float top = ml.x;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      top = fmaxf(top, M);
+      const float2 b = down2(M - top), f2 = down2(ml.x - top);
+      const float f = f2.x * f2.y, fb = b.x * b.y;
+      float l = lane < cut ? ml.y * f2.x * f2.y : 0.f;     // (a NaN stays one)
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+      L = L * b.x * b.y + l;
+      M = top;
+      y.x *= fb; y.y *= fb; y.z *= fb; y.w *= fb;
+      constexpr int BATCH = 4;
+#pragma unroll 1
+      for (int c0 = 0; c0 < cut; c0 += BATCH * AT_ONCE) {
+        float4 v[BATCH];
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {                  // (past the last: the last again)
+          const int c = min(c0 + i * AT_ONCE + sub, cut - 1);
+          const float* p = split ? a.part + (((slot0 + c) * (D / 8) + (cc >> 1)) * PP_ROWS + r % PP_ROWS) * 8 + 4 * (cc & 1)
+                                 : a.from.sums + at * D + 4 * cc;
+          v[i] = __ldcg(reinterpret_cast<const float4*>(p));
+        }
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+          const int c = c0 + i * AT_ONCE + sub;
+          const float fc = __shfl_sync(0xffffffffu, f, c & 31);
+          if (c < cut) {
+            y.x = fmaf(v[i].x, fc, y.x);
+            y.y = fmaf(v[i].y, fc, y.y);
+            y.z = fmaf(v[i].z, fc, y.z);
+            y.w = fmaf(v[i].w, fc, y.w);
+          }
+        }
+      }
+    }
+    if (AT_ONCE == 2) {
+      y.x += __shfl_xor_sync(0xffffffffu, y.x, 16);
+      y.y += __shfl_xor_sync(0xffffffffu, y.y, 16);
+      y.z += __shfl_xor_sync(0xffffffffu, y.z, 16);
+      y.w += __shfl_xor_sync(0xffffffffu, y.w, 16);
+    }
+    const float inv = L == 0.f ? 0.f : (1.f / P_SCALE) / L;
+    y.x *= inv; y.y *= inv; y.z *= inv; y.w *= inv;
+    if (sub == 0) {
+      if (a.out_f32)
+        reinterpret_cast<float4*>(a.out)[row * CH + cc] = y;
+      else
+        reinterpret_cast<uint2*>(a.out)[row * CH + cc] = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
+    }
+    if (lane == 0 && a.lse) a.lse[row] = L == 0.f ? -INFINITY : (M - W_OFF + log2f(L)) * 0.69314718055994530942f;
+  }
+}
+
+template <typename A>
+cudaError_t launch_after(void (*k)(A), long long grid, int threads, const A& a, cudaStream_t stream) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3(threads);
+  cfg.stream = stream;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, k, a);
+}
+
+// Tiles of the tcgen05 kernel at most, of one head: groups' parts, and sequences' own.
+long long group_tiles(const Batch& b, int n_groups, int G) {
+  const long long rows = (long long)b.n_tokens * G;
+  return rows > LONG_ROWS ? rows / PP_ROWS + std::min<long long>(n_groups, rows / (LONG_ROWS + 1)) : 0;
+}
+long long own_tiles(const Batch& b, int G) {
+  const long long rows = (long long)b.n_tokens * G;
+  return b.starts && (long long)b.max_new * G > LONG_ROWS ? rows / PP_ROWS + std::min<long long>(b.n_seq, rows / (LONG_ROWS + 1)) : 0;
+}
+
+struct Layout {
+  size_t cuts, ml, sums, bytes;
+};
+Layout layout(const Batch& b, int n_groups, int HQ, int H, int d) {
+  const long long rows = (long long)b.n_tokens * HQ, tiles = (group_tiles(b, n_groups, HQ / H) + own_tiles(b, HQ / H)) * H;
+  auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  Layout l;
+  l.cuts = up((size_t)((long long)n_groups + b.n_seq) * sizeof(Entry));
+  l.ml = l.cuts + up((size_t)tiles * 4);
+  l.sums = l.ml + up((size_t)rows * 2 * sizeof(float2));
+  l.bytes = l.sums + (size_t)rows * 2 * d * 4;
+  return l;
+}
+
+template <int D>
+cudaError_t launch_few(AttendArgs& a, int n_groups, int sms, bool precise, cudaStream_t stream) {
+  const int grid = AT_CTAS * sms;
+  const long long rows = !a.b.starts || a.skip_long ? a.G : ((long long)a.b.n_tokens * a.G + a.b.n_seq - 1) / a.b.n_seq;
+  const int nt = rows <= 8 ? 1 : 2;
+  a.one = (a.G + 8 * nt - 1) / (8 * nt);
+  if (precise)
+    return nt == 1 ? launch_attend<D, 1, D == 64 ? 8 : 6, true, true>(a, grid, stream) : launch_attend<D, 2, 4, true, true>(a, grid, stream);
+  return nt == 1 ? launch_attend<D, 1, D == 64 ? 8 : 6, false, true>(a, grid, stream) : launch_attend<D, 2, 6, false, true>(a, grid, stream);
+}
+
+}  // namespace
+
+bool paged_shared_fits(const Pool& pool, const Batch& b, int n_groups, int HQ) {
+  const int G = HQ / pool.H;
+  return ((long long)b.n_tokens * G / PP_ROWS + b.n_seq + ((long long)b.n_tokens * G / PP_ROWS + n_groups)) * pool.H <= INT32_MAX &&
+         (long long)n_groups + b.n_seq <= INT32_MAX / 2 &&
+         ((long long)b.n_tokens * ((HQ + JOIN_HEADS - 1) / JOIN_HEADS) + JOIN_WARPS) / JOIN_WARPS <= INT32_MAX;
+}
+size_t paged_shared_scratch(const Pool& pool, const Batch& b, int n_groups, int HQ) {
+  return layout(b, n_groups, HQ, pool.H, pool.d).bytes;
+}
+
+cudaError_t launch_paged_shared(const Pool& pool, const Batch& b, const int32_t* groups, const int32_t* prefix,
+                                int n_groups, const void* q, long long q_ts, long long q_hs, int HQ, void* out,
+                                int out_f32, float* lse, void* workspace, void* scratch, int sms, int32_t* err,
+                                cudaStream_t stream) {
+  const int H = pool.H, G = HQ / H;
+  const Layout lay = layout(b, n_groups, HQ, H, pool.d);
+  char* const base = static_cast<char*>(scratch);
+  const long long own = own_tiles(b, G), tiles = group_tiles(b, n_groups, G) + own;
+  PlanArgs plan{};
+  plan.pool = pool;
+  plan.b = b;
+  plan.groups = groups;
+  plan.prefix = prefix;
+  plan.err = err;
+  plan.entries = reinterpret_cast<Entry*>(base);
+  plan.n_groups = n_groups;
+  plan.G = G;
+  plan.tiles = (int)tiles;
+  plan.own_tiles = own > 0;
+  cudaError_t e = launch_after(shared_plan_kernel, 1, PLAN_THREADS, plan, stream);
+  if (e != cudaSuccess) return e;
+  Parts to{};
+  to.entries = plan.entries;
+  to.n_groups = n_groups;
+  to.rows = (long long)b.n_tokens * HQ;
+  to.cuts = reinterpret_cast<int*>(base + lay.cuts);
+  to.ml = reinterpret_cast<float2*>(base + lay.ml);
+  to.sums = reinterpret_cast<float*>(base + lay.sums);
+  Batch list = b;                      // of parts
+  list.n_seq = n_groups + b.n_seq;
+  char* const counters = static_cast<char*>(workspace) + counter_bytes(sms);
+  char* const parts = counters + paged_prompt_counters(sms);
+
+  const float c = (float)(1.4426950408889634 / sqrt((double)pool.d));
+  JoinArgs join{};
+  join.places = 1;
+  if (tiles > 0) {
+    PromptArgs a{};
+    a.pool = pool;
+    a.b = list;
+    a.q = static_cast<const bf16*>(q);
+    a.q_ts = q_ts;
+    a.q_hs = q_hs;
+    a.out = to.sums;
+    a.out_f32 = 1;
+    a.err = err;
+    a.c = c;
+    a.G = G;
+    a.sms = sms;
+    a.count = reinterpret_cast<int*>(counters);
+    a.part = reinterpret_cast<float*>(parts + part_bytes(sms));
+    a.part_ml = reinterpret_cast<float2*>(a.part + slots_of(sms) * PP_ROWS * pool.d);
+    a.sum = a.part + slots_of(sms) * PP_ROWS * (pool.d + 2);
+    a.claim = a.count + slots_of(sms);
+    a.to = to;
+    const long long cuts = slots_of(sms) / (tiles * H);
+    const dim3 grid((unsigned)(tiles * H), (unsigned)(cuts < 1 ? 1 : std::min<long long>(cuts, PP_MORE_PARTS)));
+    const bool chained = ((long long)b.max_pages << pool.page_shift) > PP_CHAIN_BF16 * PP_KEYS;
+    if (pool.d == 128)
+      e = out_f32 ? launch_prompt<128, true, true, true>(a, grid, stream)
+          : chained ? launch_prompt<128, false, true, true>(a, grid, stream) : launch_prompt<128, false, false, true>(a, grid, stream);
+    else
+      e = out_f32 ? launch_prompt<64, true, true, true>(a, grid, stream)
+          : chained ? launch_prompt<64, false, true, true>(a, grid, stream) : launch_prompt<64, false, false, true>(a, grid, stream);
+    if (e != cudaSuccess) return e;
+    join.part = a.part;
+    join.part_ml = a.part_ml;
+    join.places = (int)grid.y;
+  }
+  AttendArgs a{};
+  a.pool = pool;
+  a.b = list;
+  a.q = static_cast<const bf16*>(q);
+  a.q_ts = q_ts;
+  a.q_hs = q_hs;
+  a.count = static_cast<int*>(workspace);
+  a.part = reinterpret_cast<float*>(parts);
+  a.err = err;
+  a.c = c;
+  a.G = G;
+  a.inv_g = 1.f / (float)G;
+  a.skip_long = tiles > 0;
+  a.to = to;
+  e = pool.d == 128 ? launch_few<128>(a, n_groups, sms, out_f32 != 0, stream) : launch_few<64>(a, n_groups, sms, out_f32 != 0, stream);
+  if (e != cudaSuccess) return e;
+  join.b = b;
+  join.from = to;
+  join.out = out;
+  join.lse = lse;
+  join.H = H;
+  join.G = G;
+  join.out_f32 = out_f32;
+  const long long tasks = (long long)b.n_tokens * ((HQ + JOIN_HEADS - 1) / JOIN_HEADS);
+  const long long grid = (tasks + JOIN_WARPS - 1) / JOIN_WARPS;
+  return pool.d == 128 ? launch_after(shared_join_kernel<128>, grid, 32 * JOIN_WARPS, join, stream)
+                       : launch_after(shared_join_kernel<64>, grid, 32 * JOIN_WARPS, join, stream);
+}
+
+}  // namespace kvpop

@@ -23,7 +23,7 @@ from typing import List, Optional, Sequence
 import torch
 
 from .kvpop import (KVPOP_BF16, KVPOP_F32, _ck, _ptr, _raw_stream, _stream, kvpop_paged_append, kvpop_paged_append_at,
-                    kvpop_paged_evict, kvpop_paged_weigh, kvpop_paged_attend, kvpop_paged_batch, kvpop_paged_pool, kvpop_paged_workspace_bytes, kvpop_rows)
+                    kvpop_paged_attend_shared, kvpop_paged_evict, kvpop_paged_shared_bytes, kvpop_paged_weigh, kvpop_paged_attend, kvpop_paged_batch, kvpop_paged_pool, kvpop_paged_workspace_bytes, kvpop_rows)
 
 BLOCK = 16               # tokens that share a scale
 _F8 = torch.float8_e4m3fn
@@ -218,10 +218,12 @@ class PagedCache:
         return q_out
 
     def attend(self, table, lens, q, starts=None, max_new: Optional[int] = None, out=None, lse=None,
-               out_dtype=torch.float32, want_lse: bool = False, stream=None):
+               out_dtype=torch.float32, want_lse: bool = False, stream=None, groups=None, prefix=None):
         """Attention of the new tokens' ``q [tokens][H * G][d]`` (bf16, rotated) over positions
         0 .. lens + i of their sequences; arguments as ``append``, with which the tokens' own keys
-        came.  Returns (out fp32 or bf16 ``[tokens][H * G][d]``, natural-log normalisers
+        came.  Sequences that share prefixes: ``groups [n + 1]`` int32, group g being the places groups[g]
+        .. groups[g + 1] - 1, and ``prefix [n]`` int32 the positions that its sequences begin with in
+        common (``PageTable.groups``); each is read once for all of them.  Returns (out fp32 or bf16 ``[tokens][H * G][d]``, natural-log normalisers
         ``[tokens][H * G]`` or None)."""
         what = "PagedCache.attend"
         n_tokens, heads = q.shape[0], q.shape[1]
@@ -243,6 +245,8 @@ class PagedCache:
         if not (table.get_device() == lens.get_device() == q.get_device() == out.get_device() == at and
                 (starts is None or starts.get_device() == at) and (lse is None or lse.get_device() == at)):
             self._elsewhere(what, table, lens, starts, q, out, lse)
+        if groups is not None or prefix is not None:
+            return self._attend_shared(what, batch, qr, heads, n_tokens, out, code, lse, groups, prefix, stream)
         on = self._on(what, stream)
         status = kvpop_paged_attend(self._pool_ptr, batch, qr, heads, out.data_ptr(), code,
                                     None if lse is None else lse.data_ptr(), *self._work, on)
@@ -250,6 +254,25 @@ class PagedCache:
             _ck(status, "kvpop_paged_attend")
         return out, lse
 
+
+    def _attend_shared(self, what, batch, qr, heads, n_tokens, out, code, lse, groups, prefix, stream):
+        if groups is None or prefix is None:
+            raise ValueError(f"{what}: groups and prefix come together")
+        n_groups = prefix.shape[0] if len(prefix.shape) else 0
+        if n_groups < 1:
+            raise ValueError(f"{what}: prefix is {tuple(prefix.shape)}, not one number for each group")
+        _want(what, "prefix", prefix, torch.int32, (n_groups,))
+        _want(what, "groups", groups, torch.int32, (n_groups + 1,))
+        self._elsewhere(what, groups, prefix)
+        on = self._on(what, stream)
+        need = kvpop_paged_shared_bytes(self._pool_ptr, batch, n_groups, heads)
+        scratch = _output((max(need, 1),), torch.uint8, out.device, stream)
+        status = kvpop_paged_attend_shared(self._pool_ptr, batch, qr, heads, groups.data_ptr(), prefix.data_ptr(),
+                                           n_groups, out.data_ptr(), code, None if lse is None else lse.data_ptr(),
+                                           *self._work, scratch.data_ptr(), need, on)
+        if status != 0:
+            _ck(status, "kvpop_paged_attend_shared")
+        return out, lse
 
     def _mass(self, what, name, mass, n, room):
         shape = mass.shape

@@ -161,3 +161,58 @@ def test_evict_refuses(cache, what):  # noqa: F811
               "lens type": dict(lens=lens.long()), "device": {}}[what])
     with pytest.raises(ValueError):
         cache.evict(**a)
+
+
+# ------------------------------------------------------------------ shared prefixes
+def shared(kv, p=None, b=None, q=None, **kw):
+    a = dict(heads=4, groups=PTR, prefix=PTR, n=1, out=PTR + 2048, dtype=kv.KVPOP_F32, lse=PTR, ws=PTR, nbytes=1 << 40,
+             scratch=PTR, sbytes=1 << 40)
+    a.update(kw)
+    return kv.kvpop_paged_attend_shared(
+        ctypes.byref(p or pool(kv)), ctypes.byref(b or batch(kv)), ctypes.byref(q or rows(kv)), a["heads"], a["groups"],
+        a["prefix"], a["n"], a["out"], a["dtype"], a["lse"], a["ws"], a["nbytes"], a["scratch"], a["sbytes"], None)
+
+
+@pytest.mark.parametrize("bad", BAD_POOL)
+def test_pools_that_shared_attention_refuses(kv, bad):
+    assert shared(kv, p=pool(kv, **bad)) == 1
+
+
+@pytest.mark.parametrize("bad", BAD_BATCH)
+def test_batches_that_shared_attention_refuses(kv, bad):
+    assert shared(kv, b=batch(kv, **bad)) == 1
+
+
+@pytest.mark.parametrize("kw", [dict(heads=0), dict(heads=3), dict(groups=None), dict(prefix=None), dict(n=0), dict(n=-1),
+                                dict(n=2 ** 30), dict(out=None), dict(dtype=5), dict(ws=None), dict(scratch=None),
+                                dict(out=PTR)])
+def test_shared_arguments_that_are_refused(kv, kw):
+    assert shared(kv, **kw) == 1
+
+
+def test_shared_alignment_and_nothing_to_do(kv):
+    assert shared(kv, groups=PTR + 2) == 2 and shared(kv, prefix=PTR + 1) == 2 and shared(kv, scratch=PTR + 16) == 2
+    assert shared(kv, b=batch(kv, n_seq=0, n_tokens=0)) == 0
+    assert shared(kv, b=batch(kv, starts_dev=PTR, n_tokens=0)) == 0
+
+
+def test_shared_bytes(kv):
+    def need(n=1, heads=4, **kw):
+        return kv.kvpop_paged_shared_bytes(ctypes.byref(pool(kv)), ctypes.byref(batch(kv, **kw)), n, heads)
+    assert need() >= 2 * 4 * 2 * (64 + 2) * 4
+    assert need(n=0) == 0 and need(heads=3) == 0 and need(n_seq=-1) == 0
+    assert need(starts_dev=PTR, n_tokens=1000) > need(starts_dev=PTR, n_tokens=10)
+
+
+@pytest.mark.parametrize("what", ["groups alone", "prefix alone", "groups type", "prefix type", "groups shape",
+                                  "no groups", "device"])
+def test_attend_refuses_groups(cache, what):  # noqa: F811
+    table, lens = batch_args()
+    i32 = torch.int32
+    a = dict(table=table, lens=lens, q=torch.zeros(3, 4, 64, dtype=torch.bfloat16), groups=torch.zeros(2, dtype=i32),
+             prefix=torch.zeros(1, dtype=i32))
+    a.update({"groups alone": dict(prefix=None), "prefix alone": dict(groups=None), "groups type": dict(groups=torch.zeros(2)),
+              "prefix type": dict(prefix=torch.zeros(1, dtype=torch.int64)), "groups shape": dict(groups=torch.zeros(3, dtype=i32)),
+              "no groups": dict(groups=torch.zeros(1, dtype=i32), prefix=torch.zeros(0, dtype=i32)), "device": {}}[what])
+    with pytest.raises(ValueError):
+        cache.attend(**a)
