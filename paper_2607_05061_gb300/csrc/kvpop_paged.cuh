@@ -189,7 +189,8 @@ struct Parts {
   long long rows;                      // n_tokens * query heads
   float* sums;                         // [own, group's][rows][d]
   float2* ml;                          // [own, group's][rows] what the sums are relative to, and the weights' sums
-  int* cuts;                           // [tiles] parts that a tile's positions were cut into
+  int* tiles;                          // tiles there are, blocks of a part at most, and for each tile its parts
+  int room;                            // places for sums of parts
 };
 
 // raise_smem_limit once per device (`done`: one bit each, of one kernel): it takes longer on the

@@ -242,26 +242,25 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
   // ---- the tile: sequence s owns the places from starts[s] G / 256 + s on, which leaves one for
   // each of its tiles.  Later tokens see more, and go first.
   const unsigned order = gridDim.x - 1 - blockIdx.x;
-  const int place = (int)(order / (unsigned)H), h = (int)(order % (unsigned)H);
+  int place = (int)(order / (unsigned)H), h = (int)(order % (unsigned)H), part = blockIdx.y;
   auto first_place = [&](int s) { return (long long)a.b.starts[s] * G / PP_ROWS + s; };
   int s = -1, tiles = 0, most = 0;                       // tiles of all sequences, blocks of the longest
   float all_blocks = 0.f;
+  int all_tiles = 0;
   if constexpr (PARTS) {
-    for (int i0 = 0; i0 < a.b.n_seq; i0 += 32) {
+    // all tiles' first parts, then their second ones, ...; the plan has made the list
+    all_tiles = a.to.tiles[0];
+    if (all_tiles == 0) return;
+    part = (int)(blockIdx.x / (unsigned)all_tiles);
+    const int tile = all_tiles - 1 - (int)(blockIdx.x % (unsigned)all_tiles);
+    place = tile / H;
+    h = tile - place * H;
+    for (int i0 = 0; i0 < a.b.n_seq && s < 0; i0 += 32) {
       const int i = i0 + lane;
-      const bool in = i < a.b.n_seq;
-      const Entry e = a.to.entries[in ? i : 0];
-      const int k = in && e.place >= 0 ? (int)(((long long)e.n * G + PP_ROWS - 1) / PP_ROWS) : 0;
+      const Entry e = a.to.entries[i < a.b.n_seq ? i : 0];
+      const int k = i < a.b.n_seq && e.place >= 0 ? (int)(((long long)e.n * G + PP_ROWS - 1) / PP_ROWS) : 0;
       const unsigned who = __ballot_sync(0xffffffffu, k > 0 && e.place <= place && place < e.place + k);
       if (who) s = i0 + __ffs(who) - 1;
-      if (k > 0) {
-        const int b = e.ctx / PP_KEYS + 1 - e.begin / PP_KEYS;
-        tiles += k * H;
-        most = max(most, b);
-        // a group's tokens see all positions, a sequence's half of its new ones on average
-        const int lo = i < a.to.n_groups ? b : max((e.len - e.begin) / PP_KEYS + 1, 1);
-        all_blocks += (float)(k * H) * 0.5f * (float)(min(lo, b) + b);
-      }
     }
   } else
   for (int i0 = 0; i0 < a.b.n_seq; i0 += 32) {           // (each warp for itself)
@@ -286,13 +285,13 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     }
   }
   if (s < 0) return;                                     // (offsets that do not ascend)
-  int share = INT32_MAX;                                 // blocks of a part at most
-  if (gridDim.y > 1) {
+  int share = PARTS ? a.to.tiles[1] : INT32_MAX;         // blocks of a part at most
+  if (!PARTS && gridDim.y > 1) {
     tiles = __reduce_add_sync(0xffffffffu, tiles);
     most = __reduce_max_sync(0xffffffffu, most);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) all_blocks += __shfl_xor_sync(0xffffffffu, all_blocks, o);
-    share = max(share_of<!PARTS>(tiles, most, all_blocks, a.sms, (int)gridDim.y, lane), 1);
+    share = max(share_of<true>(tiles, most, all_blocks, a.sms, (int)gridDim.y, lane), 1);
   }
   Entry e{};
   SeqTokens t;
@@ -310,8 +309,8 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
   const int32_t* const trow = a.b.table + (long long)(PARTS ? e.row : s) * a.b.table_stride;
   const int lim_lo = last_seen(t.len, row0 / G, ctx);    // every row sees 0 .. lim_lo
   const int lim_hi = last_seen(t.len, (row0 + rows - 1) / G, ctx);   // none sees past lim_hi
-  const int blocks = PARTS ? max(lim_hi / PP_KEYS + 1 - begin, 1) : lim_hi / PP_KEYS + 1, part = blockIdx.y;
-  const int cut = min((blocks - 1) / share + 1, (int)gridDim.y);
+  const int blocks = PARTS ? max(lim_hi / PP_KEYS + 1 - begin, 1) : lim_hi / PP_KEYS + 1;
+  const int cut = min((blocks - 1) / share + 1, PARTS ? max(min(a.to.room / all_tiles, PP_MORE_PARTS), 1) : (int)gridDim.y);
   if (part >= cut) return;
   const int blk0 = (int)((long long)blocks * part / cut), nblk = (int)((long long)blocks * (part + 1) / cut) - blk0;
   const int key0 = (begin + blk0) * PP_KEYS;             // first position of the part
@@ -347,7 +346,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     keep[7] = -1;
     if (PARTS) {
       keep[8] = s;
-      if (part == 0) a.to.cuts[place * H + h] = cut;
+      if (part == 0) a.to.tiles[2 + place * H + h] = cut;
     }
   }
   if (warp == PP_MMA_WARP) tmem_alloc(sb + L::OFF_TMEM, PP_TMEM);
@@ -726,7 +725,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
   fence_after();
 
   const int first = keep[0], row0_ = keep[1], rows_ = keep[2], cut_ = keep[3], h_ = keep[5], nan0_ = keep[6];
-  const long long HQ = (long long)H * G, pair = (long long)keep[4] * H + h_, slot = pair * gridDim.y + blockIdx.y;
+  const long long HQ = (long long)H * G, pair = (long long)keep[4] * H + h_, slot = PARTS ? blockIdx.x : pair * gridDim.y + blockIdx.y;
   auto row_of = [&](int r) {                             // of the outputs
     const int tok = r / G;
     return (first + tok) * HQ + h_ * G + (r - tok * G);
@@ -779,7 +778,9 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
         for (int i = 0; i < 32; ++i) o[i] *= inv;
         if (cut_ > 1) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) st32(a.part + ((slot * (D / 8) + 4 * c + i) * PP_ROWS + tid) * 8, o + 8 * i);
+          for (int i = 0; i < 4; ++i)
+            st32(a.part + (PARTS ? (slot * PP_ROWS + tid) * D + 32 * c + 8 * i : ((slot * (D / 8) + 4 * c + i) * PP_ROWS + tid) * 8),
+                 o + 8 * i);
         } else if (a.out_f32) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) write(row, 4 * c + i, o + 8 * i);

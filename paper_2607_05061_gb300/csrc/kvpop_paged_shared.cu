@@ -28,6 +28,8 @@ struct PlanArgs {
   Entry* entries;
   int n_groups, G, tiles;              // tiles of the tcgen05 kernel that there is room for, of one head (0: not launched)
   int own_tiles;                       // whether it takes sequences' own parts
+  int* tiles_out;                      // Parts::tiles
+  int room, sms;                       // CTAs that parts may take
 };
 
 __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(PlanArgs a) {
@@ -93,7 +95,8 @@ __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(PlanArgs a) {
   if (a.tiles == 0) return;
   __syncthreads();
   if (warp == 0) {                     // tiles of those with many rows
-    int place = 0;
+    int place = 0, most = 0;           // blocks of the longest
+    float all_blocks = 0.f;
     for (int i0 = 0; i0 < ng + n; i0 += 32) {
       const int i = i0 + lane;
       int k = 0;
@@ -109,10 +112,32 @@ __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(PlanArgs a) {
         if (lane >= o) pre = min(pre + y, 1 << 28);
       }
       if (k > 0) {
-        if (place + pre <= a.tiles) a.entries[i].place = place + pre - k;
-        else report(a.err, ERR_BATCH); // (offsets that do not ascend: the other kernel takes it)
+        if (place + pre <= a.tiles) {
+          Entry& e = a.entries[i];
+          e.place = place + pre - k;
+          const int b = max((e.ctx + PP_KEYS - 1) / PP_KEYS - e.begin / PP_KEYS, 1);
+          most = max(most, b);
+          // a group's tokens see all positions, a sequence's half of its new ones on average
+          const int lo = i < ng ? b : min(max((e.len - e.begin) / PP_KEYS + 1, 1), b);
+          all_blocks += (float)(k * a.pool.H) * 0.5f * (float)(lo + b);
+        } else {
+          report(a.err, ERR_BATCH);    // (offsets that do not ascend: the other kernel takes it)
+          pre = 0;
+        }
       }
-      place = min(place + __shfl_sync(0xffffffffu, pre, 31), 1 << 28);
+      place += __reduce_max_sync(0xffffffffu, place + pre <= a.tiles ? pre : 0);
+    }
+    // all of them cut alike, so that their parts have a CTA each
+    most = __reduce_max_sync(0xffffffffu, most);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) all_blocks += __shfl_xor_sync(0xffffffffu, all_blocks, o);
+    const int all = place * a.pool.H;
+    int share = INT32_MAX;
+    if (all > 0 && a.room / all > 1)
+      share = max(share_of<false>(all, most, all_blocks, a.sms, min(a.room / all, PP_MORE_PARTS), lane), 1);
+    if (lane == 0) {
+      a.tiles_out[0] = all;
+      a.tiles_out[1] = share;
     }
   }
 }
@@ -124,19 +149,19 @@ struct JoinArgs {
   const float2* part_ml;
   void* out;
   float* lse;
-  int H, G, out_f32, places;           // places: parts that a tile has room for
+  int H, G, out_f32;
 };
-constexpr int JOIN_WARPS = 8, JOIN_HEADS = 4;   // query heads that a warp takes in turn
+constexpr int JOIN_WARPS = 4;
 
+// A warp joins one row: a lane has one or two parts' bases, then four (d = 128) values of all parts.
 template <int D>
 __global__ void __launch_bounds__(32 * JOIN_WARPS) shared_join_kernel(JoinArgs a) {
-  constexpr int CH = D / 4, AT_ONCE = 32 / CH;   // lanes of a row, parts at once
+  constexpr int CH = D / 4, AT_ONCE = 32 / CH, BATCH = 10;   // lanes of a row, parts at once, and on their way
   const int lane = threadIdx.x & 31, cc = lane % CH, sub = lane / CH, HQ = a.H * a.G;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int per = (HQ + JOIN_HEADS - 1) / JOIN_HEADS;
-  const long long task = (long long)blockIdx.x * JOIN_WARPS + (threadIdx.x >> 5);
-  const int tok = (int)(task / per), h0 = (int)(task - (long long)tok * per) * JOIN_HEADS;
+  const long long row = (long long)blockIdx.x * JOIN_WARPS + (threadIdx.x >> 5);
+  const int tok = (int)(row / HQ), hq = (int)(row - (long long)tok * HQ), h = hq / a.G, g = hq - h * a.G;
   if (tok >= a.b.n_tokens) return;
   int s = tok;
   if (a.b.starts) {
@@ -148,76 +173,92 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) shared_join_kernel(JoinArgs a
     }
     s = lo;
   }
+  const int all = a.part ? a.from.tiles[0] : 0;  // a tile's parts lie that far apart
+  // a row's sums: one row of `sums`, or a tile's parts
+  struct Source {
+    const float* p;
+    const float2* ml;
+    int n;
+  };
+  auto source = [&](const Entry& e, bool group) {
+    Source x;
+    const int r = (tok - e.first) * a.G + g;
+    const int pair = e.place >= 0 ? (e.place + r / PP_ROWS) * a.H + h : 0;
+    x.n = e.place >= 0 ? a.from.tiles[2 + pair] : 1;
+    const long long at = row + (group ? a.from.rows : 0), slot0 = all - 1 - pair;
+    x.p = x.n > 1 ? a.part + (slot0 * PP_ROWS + r % PP_ROWS) * D + 4 * cc : a.from.sums + at * D + 4 * cc;
+    x.ml = x.n > 1 ? a.part_ml + slot0 * PP_ROWS + r % PP_ROWS : a.from.ml + at;
+    return x;
+  };
   const Entry own = a.from.entries[a.from.n_groups + s];
-  const Entry shared = own.group >= 0 ? a.from.entries[own.group] : Entry{};
+  const Source o = source(own, false);
+  Source sh{};
+  if (own.group >= 0) sh = source(a.from.entries[own.group], true);
+  const int n = o.n + sh.n;                      // (at most 64 parts)
+  float2 ml[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int c = lane + 32 * i;
+    ml[i] = make_float2(-INFINITY, 0.f);
+    if (c < n) ml[i] = __ldcg(c < o.n ? o.ml + (long long)c * all * PP_ROWS : sh.ml + (long long)(c - o.n) * all * PP_ROWS);
+  }
+  float4 v[BATCH];
+  const long long step = (long long)all * D * PP_ROWS;
+  auto fetch = [&](int c0) {
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      const int c = c0 + i * AT_ONCE + sub;
+      const float* p = c < o.n ? o.p + c * step : sh.p + (c - o.n) * step;
+      if (c < n) v[i] = __ldcg(reinterpret_cast<const float4*>(p));
+    }
+  };
+  fetch(0);
+  float top = fmaxf(ml[0].x, ml[1].x);
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+  float f[2], l = 0.f;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float2 f2 = down2(ml[i].x - top);
+    f[i] = f2.x * f2.y;
+    l = fmaf(ml[i].y * f2.x, f2.y, l);           // (a NaN stays one; no part: 0)
+  }
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
+  float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
-  for (int hq = h0; hq < min(h0 + JOIN_HEADS, HQ); ++hq) {
-    const int h = hq / a.G, g = hq - h * a.G;
-    const long long row = (long long)tok * HQ + hq;
-    float M = -INFINITY, L = 0.f;
-    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 1
-    for (int w = 0; w < (own.group >= 0 ? 2 : 1); ++w) {
-      const Entry& e = w ? shared : own;
-      const int r = (tok - e.first) * a.G + g;
-      const int pair = e.place >= 0 ? (e.place + r / PP_ROWS) * a.H + h : 0;
-      const int cut = e.place >= 0 ? a.from.cuts[pair] : 1;
-      const long long at = row + (w ? a.from.rows : 0), slot0 = (long long)pair * a.places;
-      const bool split = cut > 1;
-      float2 ml = make_float2(-INFINITY, 0.f);
-      if (lane < cut) ml = split ? __ldcg(a.part_ml + (slot0 + lane) * PP_ROWS + r % PP_ROWS) : __ldcg(a.from.ml + at);
-      float top = ml.x;
+  for (int c0 = 0;;) {
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      top = fmaxf(top, M);
-      const float2 b = down2(M - top), f2 = down2(ml.x - top);
-      const float f = f2.x * f2.y, fb = b.x * b.y;
-      float l = lane < cut ? ml.y * f2.x * f2.y : 0.f;     // (a NaN stays one)
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-      L = L * b.x * b.y + l;
-      M = top;
-      y.x *= fb; y.y *= fb; y.z *= fb; y.w *= fb;
-      constexpr int BATCH = 4;
-#pragma unroll 1
-      for (int c0 = 0; c0 < cut; c0 += BATCH * AT_ONCE) {
-        float4 v[BATCH];
-#pragma unroll
-        for (int i = 0; i < BATCH; ++i) {                  // (past the last: the last again)
-          const int c = min(c0 + i * AT_ONCE + sub, cut - 1);
-          const float* p = split ? a.part + (((slot0 + c) * (D / 8) + (cc >> 1)) * PP_ROWS + r % PP_ROWS) * 8 + 4 * (cc & 1)
-                                 : a.from.sums + at * D + 4 * cc;
-          v[i] = __ldcg(reinterpret_cast<const float4*>(p));
-        }
-#pragma unroll
-        for (int i = 0; i < BATCH; ++i) {
-          const int c = c0 + i * AT_ONCE + sub;
-          const float fc = __shfl_sync(0xffffffffu, f, c & 31);
-          if (c < cut) {
-            y.x = fmaf(v[i].x, fc, y.x);
-            y.y = fmaf(v[i].y, fc, y.y);
-            y.z = fmaf(v[i].z, fc, y.z);
-            y.w = fmaf(v[i].w, fc, y.w);
-          }
-        }
+    for (int i = 0; i < BATCH; ++i) {
+      const int c = c0 + i * AT_ONCE + sub;
+      const float f0 = __shfl_sync(0xffffffffu, f[0], c & 31), f1 = __shfl_sync(0xffffffffu, f[1], c & 31);
+      if (c < n) {
+        const float fc = c < 32 ? f0 : f1;
+        y.x = fmaf(v[i].x, fc, y.x);
+        y.y = fmaf(v[i].y, fc, y.y);
+        y.z = fmaf(v[i].z, fc, y.z);
+        y.w = fmaf(v[i].w, fc, y.w);
       }
     }
-    if (AT_ONCE == 2) {
-      y.x += __shfl_xor_sync(0xffffffffu, y.x, 16);
-      y.y += __shfl_xor_sync(0xffffffffu, y.y, 16);
-      y.z += __shfl_xor_sync(0xffffffffu, y.z, 16);
-      y.w += __shfl_xor_sync(0xffffffffu, y.w, 16);
-    }
-    const float inv = L == 0.f ? 0.f : (1.f / P_SCALE) / L;
-    y.x *= inv; y.y *= inv; y.z *= inv; y.w *= inv;
-    if (sub == 0) {
-      if (a.out_f32)
-        reinterpret_cast<float4*>(a.out)[row * CH + cc] = y;
-      else
-        reinterpret_cast<uint2*>(a.out)[row * CH + cc] = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
-    }
-    if (lane == 0 && a.lse) a.lse[row] = L == 0.f ? -INFINITY : (M - W_OFF + log2f(L)) * 0.69314718055994530942f;
+    c0 += BATCH * AT_ONCE;
+    if (c0 >= n) break;
+    fetch(c0);
   }
+  if (AT_ONCE == 2) {
+    y.x += __shfl_xor_sync(0xffffffffu, y.x, 16);
+    y.y += __shfl_xor_sync(0xffffffffu, y.y, 16);
+    y.z += __shfl_xor_sync(0xffffffffu, y.z, 16);
+    y.w += __shfl_xor_sync(0xffffffffu, y.w, 16);
+  }
+  const float inv = l == 0.f ? 0.f : (1.f / P_SCALE) / l;
+  y.x *= inv; y.y *= inv; y.z *= inv; y.w *= inv;
+  if (sub == 0) {
+    if (a.out_f32)
+      reinterpret_cast<float4*>(a.out)[row * CH + cc] = y;
+    else
+      reinterpret_cast<uint2*>(a.out)[row * CH + cc] = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
+  }
+  if (lane == 0 && a.lse) a.lse[row] = l == 0.f ? -INFINITY : (top - W_OFF + log2f(l)) * 0.69314718055994530942f;
 }
 
 template <typename A>
@@ -245,14 +286,14 @@ long long own_tiles(const Batch& b, int G) {
 }
 
 struct Layout {
-  size_t cuts, ml, sums, bytes;
+  size_t tiles, ml, sums, bytes;
 };
 Layout layout(const Batch& b, int n_groups, int HQ, int H, int d) {
   const long long rows = (long long)b.n_tokens * HQ, tiles = (group_tiles(b, n_groups, HQ / H) + own_tiles(b, HQ / H)) * H;
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   Layout l;
-  l.cuts = up((size_t)((long long)n_groups + b.n_seq) * sizeof(Entry));
-  l.ml = l.cuts + up((size_t)tiles * 4);
+  l.tiles = up((size_t)((long long)n_groups + b.n_seq) * sizeof(Entry));
+  l.ml = l.tiles + up((size_t)(tiles + 2) * 4);
   l.sums = l.ml + up((size_t)rows * 2 * sizeof(float2));
   l.bytes = l.sums + (size_t)rows * 2 * d * 4;
   return l;
@@ -275,7 +316,7 @@ bool paged_shared_fits(const Pool& pool, const Batch& b, int n_groups, int HQ) {
   const int G = HQ / pool.H;
   return ((long long)b.n_tokens * G / PP_ROWS + b.n_seq + ((long long)b.n_tokens * G / PP_ROWS + n_groups)) * pool.H <= INT32_MAX &&
          (long long)n_groups + b.n_seq <= INT32_MAX / 2 &&
-         ((long long)b.n_tokens * ((HQ + JOIN_HEADS - 1) / JOIN_HEADS) + JOIN_WARPS) / JOIN_WARPS <= INT32_MAX;
+         ((long long)b.n_tokens * HQ + JOIN_WARPS) / JOIN_WARPS <= INT32_MAX;
 }
 size_t paged_shared_scratch(const Pool& pool, const Batch& b, int n_groups, int HQ) {
   return layout(b, n_groups, HQ, pool.H, pool.d).bytes;
@@ -300,23 +341,28 @@ cudaError_t launch_paged_shared(const Pool& pool, const Batch& b, const int32_t*
   plan.G = G;
   plan.tiles = (int)tiles;
   plan.own_tiles = own > 0;
+  plan.tiles_out = reinterpret_cast<int*>(base + lay.tiles);
+  // a CTA for every tile there may be, and a part on every SM beside them; parts have a place for their sums
+  const long long grid_tc = tiles * H + sms;
+  plan.room = (int)std::min<long long>(grid_tc, slots_of(sms));
+  plan.sms = sms;
   cudaError_t e = launch_after(shared_plan_kernel, 1, PLAN_THREADS, plan, stream);
   if (e != cudaSuccess) return e;
   Parts to{};
   to.entries = plan.entries;
   to.n_groups = n_groups;
   to.rows = (long long)b.n_tokens * HQ;
-  to.cuts = reinterpret_cast<int*>(base + lay.cuts);
+  to.tiles = plan.tiles_out;
   to.ml = reinterpret_cast<float2*>(base + lay.ml);
   to.sums = reinterpret_cast<float*>(base + lay.sums);
   Batch list = b;                      // of parts
   list.n_seq = n_groups + b.n_seq;
+  to.room = plan.room;
   char* const counters = static_cast<char*>(workspace) + counter_bytes(sms);
   char* const parts = counters + paged_prompt_counters(sms);
 
   const float c = (float)(1.4426950408889634 / sqrt((double)pool.d));
   JoinArgs join{};
-  join.places = 1;
   if (tiles > 0) {
     PromptArgs a{};
     a.pool = pool;
@@ -336,8 +382,7 @@ cudaError_t launch_paged_shared(const Pool& pool, const Batch& b, const int32_t*
     a.sum = a.part + slots_of(sms) * PP_ROWS * (pool.d + 2);
     a.claim = a.count + slots_of(sms);
     a.to = to;
-    const long long cuts = slots_of(sms) / (tiles * H);
-    const dim3 grid((unsigned)(tiles * H), (unsigned)(cuts < 1 ? 1 : std::min<long long>(cuts, PP_MORE_PARTS)));
+    const dim3 grid((unsigned)grid_tc);
     const bool chained = ((long long)b.max_pages << pool.page_shift) > PP_CHAIN_BF16 * PP_KEYS;
     if (pool.d == 128)
       e = out_f32 ? launch_prompt<128, true, true, true>(a, grid, stream)
@@ -348,7 +393,6 @@ cudaError_t launch_paged_shared(const Pool& pool, const Batch& b, const int32_t*
     if (e != cudaSuccess) return e;
     join.part = a.part;
     join.part_ml = a.part_ml;
-    join.places = (int)grid.y;
   }
   AttendArgs a{};
   a.pool = pool;
@@ -373,8 +417,7 @@ cudaError_t launch_paged_shared(const Pool& pool, const Batch& b, const int32_t*
   join.H = H;
   join.G = G;
   join.out_f32 = out_f32;
-  const long long tasks = (long long)b.n_tokens * ((HQ + JOIN_HEADS - 1) / JOIN_HEADS);
-  const long long grid = (tasks + JOIN_WARPS - 1) / JOIN_WARPS;
+  const long long grid = (to.rows + JOIN_WARPS - 1) / JOIN_WARPS;
   return pool.d == 128 ? launch_after(shared_join_kernel<128>, grid, 32 * JOIN_WARPS, join, stream)
                        : launch_after(shared_join_kernel<64>, grid, 32 * JOIN_WARPS, join, stream);
 }
