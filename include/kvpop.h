@@ -567,10 +567,12 @@ kvpop_status kvpop_paged_attend_shared(const kvpop_paged_pool* pool, const kvpop
  *   and returned them (a normaliser of -inf: a row that saw nothing, and gives nothing)
  *   mass_dev [n_seq][H][positions] fp32, positions >= max_pages * page, no memory of q or lse
  * Positions from lens + n on and idle places keep what they held.  Results do not depend on order.
- * Asynchronous on `stream`; no allocation, no workspace. */
+ * max_new chooses among kernels, as for the attention, whose workspace it shares.  Asynchronous on
+ * `stream`; no allocation. */
 kvpop_status kvpop_paged_weigh(const kvpop_paged_pool* pool, const kvpop_paged_batch* batch,
                                const kvpop_rows* q, int32_t n_q_heads, const float* lse_dev,
-                               float* mass_dev, int64_t positions, cudaStream_t stream);
+                               float* mass_dev, int64_t positions, void* workspace_dev,
+                               size_t workspace_bytes, cudaStream_t stream);
 
 /* Eviction: sequences with more than `keep` tokens are cut down to keep, for each KV head by itself,
  * and every sequence moves to new pages.  Of L = lens tokens a head keeps all if L <= keep, else the

@@ -1062,14 +1062,17 @@ static bool mass_ok(const kvpop_paged_pool* p, long long n_seq, long long positi
 
 kvpop_status kvpop_paged_weigh(const kvpop_paged_pool* pool, const kvpop_paged_batch* batch,
                                const kvpop_rows* q, int32_t n_q_heads, const float* lse_dev, float* mass_dev,
-                               int64_t positions, cudaStream_t stream) {
+                               int64_t positions, void* workspace, size_t workspace_bytes,
+                               cudaStream_t stream) {
   if (!paged_pool_ok(pool) || !paged_batch_ok(batch) || !q || n_q_heads < 1 || n_q_heads % pool->n_kv_heads != 0 ||
       n_q_heads > (1 << 20) || !mass_ok(pool, batch->n_seq, positions, batch->max_pages))
     return KVPOP_ERR_INVALID_ARG;
   if ((long long)batch->n_tokens * (n_q_heads / pool->n_kv_heads) > INT32_MAX - 1024) return KVPOP_ERR_INVALID_ARG;
   if (batch->n_seq == 0 || batch->n_tokens == 0) return KVPOP_OK;
-  if (!batch->table_dev || !batch->lens_dev || !q->data_dev || !lse_dev || !mass_dev) return KVPOP_ERR_INVALID_ARG;
-  if (!paged_aligned(pool, batch) || !rows_aligned(q, 2) || !aligned4(lse_dev) || !aligned4(mass_dev))
+  if (!batch->table_dev || !batch->lens_dev || !q->data_dev || !lse_dev || !mass_dev || !workspace)
+    return KVPOP_ERR_INVALID_ARG;
+  if (!paged_aligned(pool, batch) || !rows_aligned(q, 2) || !aligned4(lse_dev) || !aligned4(mass_dev) ||
+      (reinterpret_cast<uintptr_t>(workspace) & 255u))
     return KVPOP_ERR_ALIGN;
   const long long bytes = 4ll * batch->n_seq * pool->n_kv_heads * positions;
   if (rows_meet(q, batch->n_tokens, n_q_heads, pool->head_dim, 2, mass_dev, bytes) ||
@@ -1077,9 +1080,10 @@ kvpop_status kvpop_paged_weigh(const kvpop_paged_pool* pool, const kvpop_paged_b
     return KVPOP_ERR_INVALID_ARG;
   const PagedDevice dev = paged_device();
   if (dev.sms <= 0) return KVPOP_ERR_CUDA;
+  if (workspace_bytes < paged_attend_workspace(dev.sms)) return KVPOP_ERR_INVALID_ARG;
   return from_cuda(NOTE(launch_paged_weigh(paged_pool(pool), paged_batch(batch), q->data_dev, q->token_stride,
-                                           q->head_stride, n_q_heads, lse_dev, mass_dev, positions, dev.sms,
-                                           dev.err, stream)));
+                                           q->head_stride, n_q_heads, lse_dev, mass_dev, positions, workspace,
+                                           dev.sms, dev.err, stream)));
 }
 
 kvpop_status kvpop_paged_evict(const kvpop_paged_pool* pool, const kvpop_paged_batch* batch,

@@ -230,12 +230,18 @@ cudaError_t launch_paged_evict(const paged::Pool& pool, const paged::Batch& b, c
                                int32_t* err, cudaStream_t stream);
 
 cudaError_t launch_paged_weigh(const paged::Pool& pool, const paged::Batch& b, const void* q, long long q_ts,
-                               long long q_hs, int HQ, const float* lse, float* mass, long long positions, int sms,
-                               int32_t* err, cudaStream_t stream);
+                               long long q_hs, int HQ, const float* lse, float* mass, long long positions,
+                               void* workspace, int sms, int32_t* err, cudaStream_t stream);
+// The same for sequences with more than `least` rows: counters of a CTA each, zero between calls, and sums.
+size_t paged_weigh_workspace(int sms);
+cudaError_t launch_paged_weigh_tc(const paged::Pool& pool, const paged::Batch& b, const void* q, long long q_ts,
+                                  long long q_hs, int HQ, const float* lse, float* mass, long long positions,
+                                  int least, int* count, float* part, int sms, int32_t* err, cudaStream_t stream);
 
 // Bytes of the attention's workspace on a device with that many SMs.  The counters at its start have
 // to be zero before the first call and are zero after every call.
 size_t paged_attend_workspace(int sms);
+size_t paged_attend_parts(int sms);    // where its partial results begin
 cudaError_t launch_paged_attend(const paged::Pool& pool, const paged::Batch& b, const void* q, long long q_ts,
                                 long long q_hs, int HQ, void* out, int out_f32, float* lse, void* workspace,
                                 int sms, int32_t* err, cudaStream_t stream);

@@ -32,6 +32,7 @@ cudaError_t launch_d(AttendArgs& a, int sms, cudaStream_t stream) {
 size_t paged_attend_workspace(int sms) {
   return counter_bytes(sms) + paged_prompt_counters(sms) + part_bytes(sms) + paged_prompt_parts(sms);
 }
+size_t paged_attend_parts(int sms) { return counter_bytes(sms) + paged_prompt_counters(sms); }
 
 cudaError_t launch_paged_attend(const Pool& pool, const Batch& b, const void* q, long long q_ts, long long q_hs,
                                 int HQ, void* out, int out_f32, float* lse, void* workspace, int sms,

@@ -21,6 +21,7 @@ namespace {
 using namespace paged;
 
 constexpr int WG_WARPS = 8, WG_CTAS = 2;
+constexpr int WG_ROWS = 32;            // rows of a sequence from which on it goes to the tcgen05 kernel
 
 struct WeighArgs {
   Pool pool;
@@ -33,6 +34,7 @@ struct WeighArgs {
   int32_t* err;
   float c;                             // log2(e) / sqrt(d)
   int G;
+  int most;                            // sequences with more rows are the tcgen05 kernel's
 };
 
 // A warp's ring of blocks: 16 rows of keys, their weights so far and their scale.  The 16-byte chunk c
@@ -56,6 +58,7 @@ template <int ROWS>
 __device__ __forceinline__ WSeq wseq(const WeighArgs& a, int s) {
   WSeq w;
   w.t = seq_tokens(a.b, s, a.err);
+  if ((long long)w.t.n * a.G > a.most) w.t.n = 0;
   w.ctx = w.t.n > 0 ? context(a.b, a.pool, w.t, a.err) : 0;
   w.blocks = (w.ctx + BLK - 1) / BLK;
   w.passes = (int)(((long long)w.t.n * a.G + ROWS - 1) / ROWS);
@@ -68,18 +71,24 @@ __global__ void __launch_bounds__(32 * WG_WARPS, WG_CTAS) paged_weigh_kernel(Wei
   constexpr int ROWS = 8 * NT, KW = D / 16;
   extern __shared__ __align__(128) unsigned char smw[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3, H = a.pool.H;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  // Behind the tcgen05 kernel, which lets this one start when all that came before is done, nothing is to be
+  // waited for but that this one does not end first: its last CTA sees to that.
+  const bool beside = a.most < INT32_MAX;
+  if (!beside) asm volatile("griddepcontrol.wait;" ::: "memory");
+  auto leave = [&] {
+    if (beside && blockIdx.x == gridDim.x - 1) asm volatile("griddepcontrol.wait;" ::: "memory");
+  };
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   // ---- the list of all blocks, and the warp's part of it: the blocks that begin in [w0, w1)
   long long total = 0;
   for (int s = lane; s < a.b.n_seq; s += 32) total += wseq<ROWS>(a, s).work(H);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-  if (total == 0) return;
+  if (total == 0) return leave();
   const long long parts = (long long)gridDim.x * WG_WARPS, part = (long long)blockIdx.x * WG_WARPS + warp;
   const long long w0 = total / parts * part + total % parts * part / parts;
   const long long w1 = total / parts * (part + 1) + total % parts * (part + 1) / parts;
-  if (w0 >= w1) return;
+  if (w0 >= w1) return leave();
   int s = -1;
   long long base = 0;
   for (int s0 = 0; s0 < a.b.n_seq && s < 0; s0 += 32) {
@@ -108,7 +117,7 @@ __global__ void __launch_bounds__(32 * WG_WARPS, WG_CTAS) paged_weigh_kernel(Wei
   for (long long w = w0; w < w1;) {
     while (w >= base + x.work(H)) {
       base += x.work(H);
-      if (++s >= a.b.n_seq) return;
+      if (++s >= a.b.n_seq) return leave();
       x = wseq<ROWS>(a, s);
     }
     // blocks [k0, k1) of KV head h
@@ -257,6 +266,7 @@ __global__ void __launch_bounds__(32 * WG_WARPS, WG_CTAS) paged_weigh_kernel(Wei
       __syncwarp();
     }
   }
+  leave();
 }
 
 template <int D, int NT>
@@ -281,9 +291,21 @@ cudaError_t launch(const WeighArgs& a, int grid, cudaStream_t stream) {
 }  // namespace
 
 cudaError_t launch_paged_weigh(const Pool& pool, const Batch& b, const void* q, long long q_ts, long long q_hs,
-                               int HQ, const float* lse, float* mass, long long positions, int sms, int32_t* err,
-                               cudaStream_t stream) {
+                               int HQ, const float* lse, float* mass, long long positions, void* workspace, int sms,
+                               int32_t* err, cudaStream_t stream) {
+  const int G = HQ / pool.H;
+  const long long most_rows = b.starts ? (long long)b.max_new * G : G;
   WeighArgs a{};
+  a.most = INT32_MAX;
+  if (most_rows > WG_ROWS) {
+    a.most = WG_ROWS;
+    // [counters][sums of parts], where the attention has its own
+    char* const w = static_cast<char*>(workspace);
+    const cudaError_t e = launch_paged_weigh_tc(pool, b, q, q_ts, q_hs, HQ, lse, mass, positions, WG_ROWS,
+                                                reinterpret_cast<int*>(w),
+                                                reinterpret_cast<float*>(w + paged_attend_parts(sms)), sms, err, stream);
+    if (e != cudaSuccess || !b.starts) return e;         // (without offsets all sequences have G rows)
+  }
   a.pool = pool;
   a.b = b;
   a.q = static_cast<const bf16*>(q);
@@ -294,9 +316,9 @@ cudaError_t launch_paged_weigh(const Pool& pool, const Batch& b, const void* q, 
   a.positions = positions;
   a.err = err;
   a.c = (float)(1.4426950408889634 / sqrt((double)pool.d));
-  a.G = HQ / pool.H;
+  a.G = G;
   const int grid = WG_CTAS * sms;
-  const bool few = (b.starts ? (long long)b.max_new * a.G : a.G) <= 8;
+  const bool few = most_rows <= 8;
   if (pool.d == 128) return few ? launch<128, 1>(a, grid, stream) : launch<128, 4>(a, grid, stream);
   return few ? launch<64, 1>(a, grid, stream) : launch<64, 4>(a, grid, stream);
 }

@@ -1,0 +1,594 @@
+// Attention weights of the paged 8-bit cache's positions for many query rows, on tcgen05.
+//
+// The mathematics is that of kvpop_paged_weigh.cu.  Positions are the rows of the products: a tile is
+// 256 positions of one (sequence, KV head), as bf16 (which holds every e4m3 value) in tensor memory,
+// and its query rows (token, query head) come as blocks of 128 columns, unchanged.  A thread owns one
+// position and 64 columns of every block:
+//   x = S ks c - lse log2 e,   sum += 2^x,
+// one fma, one exponential and one addition a value; there is no maximum to keep, since a weight is
+// no more than 1.  A position's sum is added to its weight at the end of the tile.
+//
+// All (tile, block) pairs form one list, tile after tile, that is cut evenly over the SMs; a tile that
+// lies in several CTAs' parts is added up, in their order, by the CTA that arrives last, at its end.
+// Roles:
+//  * 16 softmax warps, which also bring the next tile's positions into the other half of the
+//    operand's tensor memory (their bytes are on their way one tile before, their pages two);
+//  * 1 MMA warp: S = K Q^T (M 128, N 128, K d) per half of the tile, one buffer a half;
+//  * 2 producer warps: query rows by 16-byte cp.async into 128B-swizzled slots, with lse and the last
+//    position that each row sees beside them.  Where all of a sequence's rows fit the slots they stay
+//    there for all tiles of the head.
+// Tensor memory: S 2 x 128 columns, operands 2 x (2 x d / 2).
+#include "kvpop_mma.cuh"
+#include "kvpop_paged.cuh"
+#include "kvpop_ptx.cuh"
+#include "kvpop_tc05.cuh"
+
+namespace kvpop {
+namespace {
+
+using namespace paged;
+using namespace tc05;
+
+constexpr int WT_HALF = 128, WT_KEYS = 256, WT_BN = 128;
+constexpr int WT_SOFT = 16, WT_MMA_WARP = WT_SOFT, WT_COPY_WARP = WT_SOFT + 1, WT_COPY = 2;
+constexpr int WT_THREADS = 32 * (WT_COPY_WARP + WT_COPY);
+constexpr int WT_WHOLE = 8;                              // tiles of up to that many blocks are not cut
+constexpr float kLog2E = 1.4426950408889634f;
+
+struct WeighTcArgs {
+  Pool pool;
+  Batch b;
+  const bf16* q;
+  long long q_ts, q_hs;
+  const float* lse;
+  float* mass;
+  long long positions;
+  float* part;                                           // [CTAs][2][256] sums of cut tiles
+  int* count;                                            // [CTAs] parts there, zero between calls
+  int32_t* err;
+  float c;                                               // log2(e) / sqrt(d)
+  int G, least;                                          // sequences with more than `least` rows
+};
+
+template <int D>
+struct WL {
+  static constexpr int ST = D == 128 ? 5 : 8, SLOT = WT_BN * D * 2;
+  static constexpr int OFF_NL = ST * SLOT;               // [slot][128] -lse log2 e
+  static constexpr int OFF_LIM = OFF_NL + ST * WT_BN * 4;   // [slot][128] last position seen, -1: none
+  static constexpr int OFF_FLAG = OFF_LIM + ST * WT_BN * 4; // [slot][copy warp] whether one sees none
+  static constexpr int OFF_X = OFF_FLAG + ST * WT_COPY * 4; // [2][256] sums of the upper columns
+  static constexpr int OFF_BAR = (OFF_X + 2 * WT_KEYS * 4 + 7) / 8 * 8;
+  static constexpr int FULL = 0, EMPTY = ST, SFULL = 2 * ST, PFULL = SFULL + 2, AFULL = PFULL + 2, XFULL = AFULL + 2,
+                       END = XFULL + 8, N_BAR = END + 1;
+  static constexpr int OFF_TMEM = OFF_BAR + 8 * N_BAR, BYTES = OFF_TMEM + 16;
+  static_assert(ST <= WT_WHOLE, "");
+};
+
+// A sequence's tiles, of one head.
+struct WSeqT {
+  int first, n, len, ctx, tiles, blocks;                 // blocks of all its rows; 0 tiles: not this kernel's
+  __device__ __forceinline__ int skipped(int G, int kt) const {   // blocks whose rows all lie before the tile
+    const long long t0 = (long long)kt * WT_KEYS;
+    return t0 <= len ? 0 : (int)((t0 - len) * G / WT_BN);
+  }
+  __device__ __forceinline__ int here(int G, int kt) const { return blocks - skipped(G, kt); }
+  // blocks of the tiles before kt
+  __device__ __forceinline__ long long before(int G, int kt) const {
+    const int full = min(kt, min(tiles, len / WT_KEYS + 1));
+    long long w = (long long)full * blocks;
+    if (kt > full) {                                     // sum of blocks - (2 G k - up), k from full to kt - 1
+      const long long up = ((long long)len * G + WT_BN - 1) / WT_BN, k = kt - full;
+      w += k * (blocks + up) - (long long)G * ((long long)kt * (kt - 1) - (long long)full * (full - 1));
+    }
+    return w;
+  }
+};
+__device__ __forceinline__ WSeqT wseq_t(const WeighTcArgs& a, int s) {
+  const SeqTokens t = seq_tokens(a.b, s, a.err);
+  WSeqT x;
+  x.first = t.first;
+  x.n = t.n;
+  x.len = t.len;
+  x.ctx = x.tiles = x.blocks = 0;
+  if (t.len >= 0 && (long long)t.n * a.G > a.least) {
+    x.ctx = context(a.b, a.pool, t, a.err);
+    x.tiles = (x.ctx + WT_KEYS - 1) / WT_KEYS;
+    x.blocks = (int)(((long long)t.n * a.G + WT_BN - 1) / WT_BN);
+  }
+  return x;
+}
+// A tile of the list: blocks [b0, b1) of it are this CTA's.
+struct Tile {
+  WSeqT x;
+  int s, h, kt, b0, b1;
+  long long at, end;                                     // list positions of b0, and of the CTA's end
+  __device__ __forceinline__ bool valid() const { return at < end; }
+  __device__ __forceinline__ void cut() { b1 = (int)min((long long)x.blocks, b0 + (end - at)); }
+  __device__ __forceinline__ bool same_head(const Tile& o) const { return s == o.s && h == o.h; }
+};
+__device__ __forceinline__ void advance(const WeighTcArgs& a, Tile& t) {
+  t.at += t.b1 - t.b0;
+  if (t.at >= t.end) return;
+  if (++t.kt == t.x.tiles) {
+    t.kt = 0;
+    if (++t.h == a.pool.H) {
+      t.h = 0;
+      do t.x = wseq_t(a, ++t.s);                         // (there is one: the list goes on)
+      while (t.x.tiles == 0);
+    }
+  }
+  t.b0 = t.x.skipped(a.G, t.kt);
+  t.cut();
+}
+// The tile that list position w lies in (by a whole warp); w: below the total.
+__device__ Tile find(const WeighTcArgs& a, long long w, int lane) {
+  Tile t;
+  long long base = 0;
+  t.s = -1;
+  for (int s0 = 0; s0 < a.b.n_seq && t.s < 0; s0 += 32) {
+    long long mine = 0;
+    if (s0 + lane < a.b.n_seq) {
+      const WSeqT x = wseq_t(a, s0 + lane);
+      mine = x.before(a.G, x.tiles) * a.pool.H;
+    }
+    long long pre = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, pre, o);
+      if (lane >= o) pre += y;
+    }
+    const unsigned has = __ballot_sync(0xffffffffu, w < base + pre);
+    const int who = has ? __ffs(has) - 1 : 31;
+    if (has) t.s = s0 + who;
+    base += __shfl_sync(0xffffffffu, has ? pre - mine : pre, who);
+  }
+  t.s = max(t.s, 0);
+  t.x = wseq_t(a, t.s);
+  const long long each = max(t.x.before(a.G, t.x.tiles), 1ll), rem = w - base;
+  t.h = (int)(rem / each);
+  const long long in = rem - each * t.h;
+  int lo = 0, hi = max(t.x.tiles - 1, 0);                // the last tile that begins at or before it
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (t.x.before(a.G, mid) <= in) lo = mid; else hi = mid - 1;
+  }
+  t.kt = lo;
+  t.b0 = t.x.skipped(a.G, lo) + (int)(in - t.x.before(a.G, lo));
+  t.at = w;
+  return t;
+}
+
+template <int D>
+__global__ void __launch_bounds__(WT_THREADS, 1) paged_weigh_tc_kernel(WeighTcArgs a) {
+  using L = WL<D>;
+  constexpr int ST = L::ST, RAW = D / 32;                // 16-byte pieces of a thread's half of a row
+  extern __shared__ __align__(1024) unsigned char smt[];
+  __shared__ Tile edgeS[2], aheadS[WT_SOFT];
+  __shared__ long long edgeW[2], shareS;
+  __shared__ int lastS;
+  const uint32_t sb = smem_u32(smt);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, H = a.pool.H, G = a.G;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  auto bar = [&](int i) { return sb + L::OFF_BAR + 8u * (uint32_t)i; };
+
+  // ---- the CTA's part of the list.  A tile of few blocks is not cut: it belongs to the part that it begins in.
+  if (warp < 2) {
+    long long total = 0;
+    for (int s = lane; s < a.b.n_seq; s += 32) {
+      const WSeqT x = wseq_t(a, s);
+      total += x.before(G, x.tiles) * H;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    const long long share = (total + gridDim.x - 1) / gridDim.x;
+    long long w = min(share * (blockIdx.x + warp), total);
+    Tile t{};
+    if (w < total) {
+      t = find(a, w, lane);
+      const int skip = t.x.skipped(G, t.kt);
+      if (t.b0 > skip && t.x.blocks - skip <= WT_WHOLE) {
+        w += t.x.blocks - t.b0;
+        t = w < total ? find(a, w, lane) : Tile{};
+      }
+    }
+    if (lane == 0) {
+      edgeS[warp] = t;
+      edgeW[warp] = w;
+      shareS = share;
+    }
+  }
+  if (tid == 64) {
+    for (int i = 0; i < ST; ++i) {
+      mbar_init(bar(L::FULL + i), 32 * WT_COPY + WT_COPY);
+      mbar_init(bar(L::EMPTY + i), 1 + WT_SOFT);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar(L::SFULL + i), 1);
+      mbar_init(bar(L::PFULL + i), WT_SOFT / 2);
+      mbar_init(bar(L::AFULL + i), WT_SOFT);
+    }
+    for (int i = 0; i < 8; ++i) mbar_init(bar(L::XFULL + i), 1);
+    mbar_init(bar(L::END), 1);
+    mbar_fence_init();
+  }
+  if (warp == WT_MMA_WARP) tmem_alloc(sb + L::OFF_TMEM, 512);
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smt + L::OFF_TMEM);
+  Tile t = edgeS[0];
+  t.at = edgeW[0];
+  t.end = edgeW[1];
+  const long long share = shareS;
+  if (t.valid()) t.cut();
+  auto wait = [&](int b, uint32_t parity) {              // the whole warp; false: gave up
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar(b), parity))) return true;
+    return (bool)__all_sync(0xffffffffu, mbar_wait(bar(b), parity, a.err, ERR_WAIT));
+  };
+  // All of a head's rows fit the slots: its blocks from the first tile's on are loaded once.  `pos` counts
+  // the loads so far, the same in every role.
+  auto stays = [&](const Tile& x) { return x.x.blocks <= ST; };
+  uint32_t pos = 0;
+  bool ok = true;
+
+  if (warp >= WT_COPY_WARP) {
+    // ---------------------------------------------------------------- query rows
+    const int cw = warp - WT_COPY_WARP;
+    auto load = [&](const Tile& x, int b) {
+      const int st = pos % ST;
+      if (pos >= (uint32_t)ST && !wait(L::EMPTY + st, (pos / ST - 1) & 1)) return false;
+      // a lane knows two of the warp's 64 rows
+      long long off[2];
+      int lim[2];
+      float nl[2];
+      bool none = false;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const long long r = (long long)b * WT_BN + cw * 64 + 32 * i + lane, rows = (long long)x.x.n * G;
+        off[i] = -1;
+        lim[i] = -1;
+        nl[i] = 0.f;
+        if (r < rows) {
+          const int tok = (int)(r / G), g = (int)(r - (long long)tok * G);
+          off[i] = (x.x.first + tok) * a.q_ts + (long long)(x.h * G + g) * a.q_hs;
+          const float l = a.lse[((long long)(x.x.first + tok) * H + x.h) * G + g];
+          if (l != -INFINITY) {
+            lim[i] = last_seen(x.x.len, tok, x.x.ctx);
+            nl[i] = -l * kLog2E;
+          }
+        }
+        none |= lim[i] < 0;
+      }
+      const uint32_t dst = sb + st * L::SLOT;
+      constexpr int LPR = D / 8, RPI = 32 / LPR;         // lanes of a row, rows at a time
+      const int c = lane % LPR, sub = lane / LPR;
+#pragma unroll
+      for (int i = 0; i < 64 / RPI; ++i) {
+        const int rr = i * RPI + sub;
+        const long long o = __shfl_sync(0xffffffffu, off[i * RPI / 32], rr & 31);
+        cp_async16(dst + tile_off(cw * 64 + rr, c, WT_BN), a.q + (o < 0 ? 0 : o) + 8 * c, o < 0 ? 0 : 16);
+      }
+      cp_async_arrive_noinc(bar(L::FULL + st));
+      float* nls = reinterpret_cast<float*>(smt + L::OFF_NL) + st * WT_BN + cw * 64;
+      int* lims = reinterpret_cast<int*>(smt + L::OFF_LIM) + st * WT_BN + cw * 64;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        nls[32 * i + lane] = nl[i];
+        lims[32 * i + lane] = lim[i];
+      }
+      none = __any_sync(0xffffffffu, none);
+      if (lane == 0) reinterpret_cast<int*>(smt + L::OFF_FLAG)[st * WT_COPY + cw] = none;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(L::FULL + st));
+      ++pos;
+      return true;
+    };
+    Tile head = t;                                       // the first tile of the head
+    bool fresh = true;
+    while (t.valid() && ok) {
+      if (!stays(t) || fresh)
+        for (int b = t.b0; b < (stays(t) ? t.x.blocks : t.b1) && ok; ++b) ok = load(t, b);
+      advance(a, t);
+      fresh = !t.valid() || !t.same_head(head);
+      if (fresh) head = t;
+    }
+    cp_wait<0>();
+  } else if (warp == WT_MMA_WARP) {
+    // ---------------------------------------------------------------- MMA issue
+    const uint32_t idS = idesc_bf16(128, WT_BN, 0);
+    const bool lead = elect_one();
+    const uint64_t bd0 = kmajor_desc(sb, WT_BN, 0);
+    uint32_t step = 0;
+    int first = t.b0;                                    // block that lies in the head's first slot
+    for (uint32_t i = 0; t.valid() && ok; ++i) {
+      if (!(ok = wait(L::AFULL + (i & 1), i >> 1 & 1))) break;
+      fence_after();
+      const uint32_t tA = tmem + 256 + (i & 1) * D;
+      const bool stay = stays(t);
+      for (int b = t.b0; b < t.b1 && ok; ++b, ++step) {
+        const uint32_t p = stay ? pos + (b - first) : pos;
+        const int st = p % ST;
+        if (!(ok = wait(L::FULL + st, p / ST & 1))) break;
+        fence_async_smem();
+        const uint64_t bd = desc_at(bd0, st * L::SLOT);
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+          if (step > 0 && !(ok = ok && wait(L::PFULL + hh, (step - 1) & 1))) break;
+          fence_after();
+          if (lead) {
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks)
+              mma_bf16_ts(tmem + hh * 128, tA + hh * (D / 2) + ks * 8, kmajor_step(bd, WT_BN, ks), idS, ks > 0);
+            commit(bar(L::SFULL + hh));
+            if (hh == 1 && !stay) commit(bar(L::EMPTY + st));
+          }
+          __syncwarp();
+        }
+        if (!stay) ++pos;
+      }
+      const Tile was = t;
+      advance(a, t);
+      if (!t.valid() || !t.same_head(was)) {
+        if (stay && ok) {                                // the head's slots are free
+          const int k = was.x.blocks - first;
+          if (lead)
+            for (int j = 0; j < k; ++j) commit(bar(L::EMPTY + (pos + j) % ST));
+          __syncwarp();
+          pos += k;
+        }
+        first = t.b0;
+      }
+    }
+    if (lead) commit(bar(L::END));                       // every product is done before the CTA ends
+    __syncwarp();
+    wait(L::END, 0);
+  } else {
+    // ---------------------------------------------------------------- softmax
+    // warp: half hh of the tile, rows 32 (warp mod 4) + lane, columns 64 cs .. of every block
+    const int hh = (warp >> 2) & 1, cs = warp >> 3, r = hh * WT_HALF + (warp & 3) * 32 + lane;
+    const uint32_t tl = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    const float* const nlS = reinterpret_cast<const float*>(smt + L::OFF_NL) + 64 * cs;
+    const int* const limS = reinterpret_cast<const int*>(smt + L::OFF_LIM) + 64 * cs;
+    const int* const flagS = reinterpret_cast<const int*>(smt + L::OFF_FLAG);
+    float* const xS = reinterpret_cast<float*>(smt + L::OFF_X);
+    // the tiles to come: the page of one, the bytes and scale of the one before it
+    if (lane == 0) aheadS[warp] = t;
+    __syncwarp();
+    int id = -1, id_t = 0, id_h = 0;
+    uint4 raw[RAW];
+    float raw_scale = 0.f, next_scale = 0.f;
+    auto look = [&] {                                    // the page of the row in `ahead`
+      id = -1;
+      Tile ahead = aheadS[warp];
+      if (!ahead.valid()) return;
+      id_t = ahead.kt * WT_KEYS + r;
+      id_h = ahead.h;
+      if (id_t < ahead.x.ctx) {
+        id = a.b.table[(long long)ahead.s * a.b.table_stride + (id_t >> a.pool.page_shift)];
+        if ((unsigned)id >= (unsigned)a.pool.n_pages) {
+          report(a.err, ERR_PAGE);
+          id = -1;
+        }
+      }
+      advance(a, ahead);
+      __syncwarp();
+      if (lane == 0) aheadS[warp] = ahead;
+      __syncwarp();
+    };
+    auto fetch = [&] {                                   // its bytes
+      raw_scale = 0.f;
+#pragma unroll
+      for (int i = 0; i < RAW; ++i) raw[i] = make_uint4(0, 0, 0, 0);
+      if (id >= 0) {
+        const long long at = ((long long)id * H + id_h) * a.pool.page + (id_t & (a.pool.page - 1));
+        const uint4* p = reinterpret_cast<const uint4*>(a.pool.k + at * D + cs * (D / 2));
+#pragma unroll
+        for (int i = 0; i < RAW; ++i) raw[i] = p[i];
+        raw_scale = a.pool.ks[at / BLK];
+      }
+    };
+    auto store = [&](int buf) {                          // into the operand
+      float w[D / 4];
+#pragma unroll
+      for (int i = 0; i < RAW; ++i) {
+        const uint32_t u[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          uint32_t lo, hi;
+          cvt4(u[k], lo, hi);
+          const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&lo));
+          const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+          w[8 * i + 2 * k] = __uint_as_float(pack_bf16(x.x, x.y));
+          w[8 * i + 2 * k + 1] = __uint_as_float(pack_bf16(y.x, y.y));
+        }
+      }
+      const uint32_t to = tl + 256 + buf * D + hh * (D / 2) + cs * (D / 4);
+      if constexpr (D == 128) tmem_st32(to, w); else tmem_st16(to, w);
+      tmem_wait_st();
+      fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(L::AFULL + buf));
+      next_scale = raw_scale;
+    };
+    look();
+    fetch();
+    look();
+    if (t.valid()) store(0);
+    uint32_t step = 0;
+    int first = t.b0;
+    for (uint32_t i = 0; t.valid() && ok; ++i) {
+      const float scale = next_scale;                    // 0: no position, or a bad page
+      const uint64_t cc = f2_pack(a.c * scale, a.c * scale);
+      fetch();
+      look();
+      const int t0 = t.kt * WT_KEYS, tp = t0 + r, t1 = min(t0 + WT_KEYS, t.x.ctx) - 1;
+      float* const to = a.mass + ((long long)t.s * H + t.h) * a.positions + tp;
+      const bool whole = t.b0 == t.x.skipped(G, t.kt) && t.b1 == t.x.blocks;
+      float before = 0.f;
+      if (cs == 0 && whole && tp < t.x.ctx && tp < t.x.len) before = *to;
+      const bool stay = stays(t);
+      float sum = 0.f;
+      for (int b = t.b0; b < t.b1; ++b, ++step) {
+        const uint32_t p = stay ? pos + (b - first) : pos;
+        const int st = p % ST;
+        if (!(ok = wait(L::SFULL + hh, step & 1) && wait(L::FULL + st, p / ST & 1))) break;
+        fence_after();
+        // (all products of the tile before are done: the other operand is free)
+        if (b == t.b1 - 1 && t.at + (t.b1 - t.b0) < t.end) store((i + 1) & 1);
+        float s[64];
+        tmem_ld32(tl + hh * 128 + 64 * cs, *reinterpret_cast<float(*)[32]>(s));
+        tmem_ld32(tl + hh * 128 + 64 * cs + 32, *reinterpret_cast<float(*)[32]>(s + 32));
+        tmem_wait_ld();
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(L::PFULL + hh));
+        const float4* nl = reinterpret_cast<const float4*>(nlS + st * WT_BN);
+        uint64_t s0 = 0ull, s1 = 0ull;
+        const bool edge = last_seen(t.x.len, (int)((long long)b * WT_BN / G), t.x.ctx) < t1 || flagS[st * WT_COPY] || flagS[st * WT_COPY + 1];
+        if (!edge) {
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            const float4 n4 = nl[k];
+            float x0, x1, x2, x3;
+            f2_unpack(f2_fma(f2_pack(s[4 * k], s[4 * k + 1]), cc, f2_pack(n4.x, n4.y)), x0, x1);
+            f2_unpack(f2_fma(f2_pack(s[4 * k + 2], s[4 * k + 3]), cc, f2_pack(n4.z, n4.w)), x2, x3);
+            s0 = f2_add(s0, f2_pack(ex2(x0), ex2(x1)));
+            s1 = f2_add(s1, f2_pack(ex2(x2), ex2(x3)));
+          }
+        } else {
+          const int4* lim = reinterpret_cast<const int4*>(limS + st * WT_BN);
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            const float4 n4 = nl[k];
+            const int4 l4 = lim[k];
+            float x0, x1, x2, x3;
+            f2_unpack(f2_fma(f2_pack(s[4 * k], s[4 * k + 1]), cc, f2_pack(n4.x, n4.y)), x0, x1);
+            f2_unpack(f2_fma(f2_pack(s[4 * k + 2], s[4 * k + 3]), cc, f2_pack(n4.z, n4.w)), x2, x3);
+            s0 = f2_add(s0, f2_pack(ex2(tp <= l4.x ? x0 : -INFINITY), ex2(tp <= l4.y ? x1 : -INFINITY)));
+            s1 = f2_add(s1, f2_pack(ex2(tp <= l4.z ? x2 : -INFINITY), ex2(tp <= l4.w ? x3 : -INFINITY)));
+          }
+        }
+        float y0, y1;
+        f2_unpack(f2_add(s0, s1), y0, y1);
+        sum += y0 + y1;
+        if (!stay) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(L::EMPTY + st));
+          ++pos;
+        }
+      }
+      if (!ok) break;
+      // ---- the columns' halves meet
+      float* const x = xS + (i & 1) * WT_KEYS + r;
+      if (cs == 1) {
+        *x = sum;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(L::XFULL + (warp & 7)));
+      } else {
+        if (!(ok = wait(L::XFULL + warp, i & 1))) break;
+        sum += *x;
+        if (scale == 0.f) sum = 0.f;
+        if (whole) {
+          if (tp < t.x.ctx) *to = before + sum;
+        } else {                                         // (the part's first tile, or its last)
+          const bool begins = t.b0 == t.x.skipped(G, t.kt);
+          __stcg(a.part + ((long long)blockIdx.x * 2 + begins) * WT_KEYS + r, sum);
+        }
+      }
+      const Tile was = t;
+      advance(a, t);
+      if (!t.valid() || !t.same_head(was)) {
+        if (stay) {
+          const int k = was.x.blocks - first;
+          __syncwarp();
+          if (lane == 0)
+            for (int j = 0; j < k; ++j) mbar_arrive(bar(L::EMPTY + (pos + j) % ST));
+          pos += k;
+        }
+        first = t.b0;
+      }
+    }
+  }
+  fence_before();
+  __syncthreads();
+  if (warp == WT_MMA_WARP) tmem_dealloc(tmem, 512);
+
+  // ---- tiles in several parts: the CTA that comes last adds them up
+#pragma unroll 1
+  for (int e = 0; e < 2; ++e) {
+    Tile c = edgeS[e];                                   // the first tile, and the one that the part ends in
+    const long long w = edgeW[e];
+    if (edgeW[0] >= edgeW[1] || (e == 1 && c.x.tiles == 0)) break;
+    const int skip = c.x.skipped(G, c.kt), here = c.x.blocks - skip;
+    const long long start = w - (c.b0 - skip);
+    // a part of the first tile, if that began earlier; the beginning of the one that the part ends in
+    if (c.b0 == skip || (e == 1 && start < edgeW[0])) continue;
+    const long long p0 = start / share;
+    const int parts = (int)((start + here - 1) / share - p0) + 1;
+    __threadfence();
+    __syncthreads();
+    if (tid == 0) {
+      lastS = atomicAdd(a.count + p0, 1) == parts - 1;
+      if (lastS) a.count[p0] = 0;
+    }
+    __syncthreads();
+    if (lastS && tid < WT_KEYS) {
+      __threadfence();
+      const int tp = c.kt * WT_KEYS + tid;
+      if (tp < c.x.ctx) {
+        float sum = 0.f;
+        for (int p = 0; p < parts; ++p) sum += __ldcg(a.part + ((p0 + p) * 2 + (p == 0)) * WT_KEYS + tid);
+        float* const to = a.mass + ((long long)c.s * H + c.h) * a.positions + tp;
+        *to = (tp < c.x.len ? *to : 0.f) + sum;
+      }
+    }
+    __syncthreads();
+  }
+}
+
+template <int D>
+cudaError_t launch(const WeighTcArgs& a, int grid, cudaStream_t stream) {
+  auto k = paged_weigh_tc_kernel<D>;
+  static std::atomic<unsigned long long> raised{0};
+  const cudaError_t e = raise_smem_limit_once(raised, k, WL<D>::BYTES);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3(WT_THREADS);
+  cfg.dynamicSmemBytes = WL<D>::BYTES;
+  cfg.stream = stream;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, k, a);
+}
+
+}  // namespace
+
+size_t paged_weigh_workspace(int sms) { return (size_t)sms * 2 * WT_KEYS * 4; }
+
+cudaError_t launch_paged_weigh_tc(const Pool& pool, const Batch& b, const void* q, long long q_ts, long long q_hs,
+                                  int HQ, const float* lse, float* mass, long long positions, int least, int* count,
+                                  float* part, int sms, int32_t* err, cudaStream_t stream) {
+  WeighTcArgs a{};
+  a.pool = pool;
+  a.b = b;
+  a.q = static_cast<const bf16*>(q);
+  a.q_ts = q_ts;
+  a.q_hs = q_hs;
+  a.lse = lse;
+  a.mass = mass;
+  a.positions = positions;
+  a.part = part;
+  a.count = count;
+  a.err = err;
+  a.c = (float)(1.4426950408889634 / sqrt((double)pool.d));
+  a.G = HQ / pool.H;
+  a.least = least;
+  return pool.d == 128 ? launch<128>(a, sms, stream) : launch<64>(a, sms, stream);
+}
+
+}  // namespace kvpop

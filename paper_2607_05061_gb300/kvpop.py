@@ -119,7 +119,7 @@ _SIGS = {
     "kvpop_paged_shared_bytes": (c_size_t, [_P, _P, c_int32, c_int32]),
     "kvpop_paged_attend_shared": (ctypes.c_int, [_P, _P, _P, c_int32, _P, _P, c_int32, _P, ctypes.c_int, _P, _P,
                                                  c_size_t, _P, c_size_t, _P]),
-    "kvpop_paged_weigh": (ctypes.c_int, [_P, _P, _P, c_int32, _P, _P, ctypes.c_int64, _P]),
+    "kvpop_paged_weigh": (ctypes.c_int, [_P, _P, _P, c_int32, _P, _P, ctypes.c_int64, _P, c_size_t, _P]),
     "kvpop_paged_evict": (ctypes.c_int, [_P, _P, _P, ctypes.c_int64, _P, ctypes.c_int64, c_int32, c_int32, c_int32,
                                          c_int32, _P, _P, ctypes.c_int64, _P, _P]),
     "kvpop_standalone_status": (ctypes.c_int, [_P]),

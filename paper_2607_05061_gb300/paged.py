@@ -56,8 +56,8 @@ def _output(shape, dtype, device, stream):
 class PagedCache:
     """One layer's pages.  ``k_pages, v_pages [n_pages][H][page][d]`` (float8_e4m3fn) and
     ``k_scale, v_scale [n_pages][H][page / 16]`` (fp32) stay the caller's; ``PagedCache.empty``
-    makes them.  ``workspace``: another cache's, to share (some 90 MB).  Calls of ``attend`` that use
-    one workspace have to follow each other, on one stream or ordered by events, as those of a
+    makes them.  ``workspace``: another cache's, to share (some 90 MB).  Calls of ``attend`` and ``weigh``
+    that use one workspace have to follow each other, on one stream or ordered by events, as those of a
     model's layers do; the class does not see to it.  That goes for one cache used on two streams."""
 
     def __init__(self, k_pages, v_pages, k_scale, v_scale, workspace: Optional[torch.Tensor] = None):
@@ -297,7 +297,8 @@ class PagedCache:
         self._mass(what, "mass", mass, table.shape[0], table.shape[1] * self.page)
         self._elsewhere(what, table, lens, starts, q, lse, mass)
         on = self._on(what, stream)
-        status = kvpop_paged_weigh(self._pool_ptr, batch, qr, heads, lse.data_ptr(), mass.data_ptr(), mass.shape[2], on)
+        status = kvpop_paged_weigh(self._pool_ptr, batch, qr, heads, lse.data_ptr(), mass.data_ptr(), mass.shape[2],
+                                   *self._work, on)
         if status != 0:
             _ck(status, "kvpop_paged_weigh")
         return mass

@@ -22,10 +22,10 @@ def append_at(kv, p=None, b=None, q=None, k=None, v=None, **kw):
 
 
 def weigh(kv, p=None, b=None, q=None, **kw):
-    a = dict(heads=4, lse=PTR, mass=PTR + 2048, positions=64)
+    a = dict(heads=4, lse=PTR, mass=PTR + 2048, positions=64, ws=PTR, nbytes=1 << 40)
     a.update(kw)
     return kv.kvpop_paged_weigh(ctypes.byref(p or pool(kv)), ctypes.byref(b or batch(kv)), ctypes.byref(q or rows(kv)),
-                                a["heads"], a["lse"], a["mass"], a["positions"], None)
+                                a["heads"], a["lse"], a["mass"], a["positions"], a["ws"], a["nbytes"], None)
 
 
 def evict(kv, p=None, b=None, **kw):
@@ -70,7 +70,8 @@ def test_axes_that_are_none(kv):
 
 
 @pytest.mark.parametrize("kw", [dict(heads=0), dict(heads=3), dict(lse=None), dict(mass=None), dict(positions=63),
-                                dict(positions=-1), dict(positions=1 << 60), dict(mass=PTR), dict(lse=PTR + 2048)])
+                                dict(positions=-1), dict(positions=1 << 60), dict(mass=PTR), dict(lse=PTR + 2048),
+                                dict(ws=None)])
 def test_weigh_arguments_that_are_refused(kv, kw):
     assert weigh(kv, **kw) == 1
 
@@ -95,6 +96,7 @@ def test_eviction_of_more_than_a_grid_numbers(kv):
 
 def test_misaligned(kv):
     assert append_at(kv, at=PTR + 2) == 2 and append_at(kv, cos=PTR + 4) == 2 and append_at(kv, q_out=PTR + 8) == 2
+    assert weigh(kv, ws=PTR + 64) == 2
     assert weigh(kv, lse=PTR + 2) == 2 and weigh(kv, mass=PTR + 2050) == 2
     assert weigh(kv, q=rows(kv, data_dev=PTR + 2)) == 2 and weigh(kv, p=pool(kv, k_pages_dev=PTR + 8)) == 2
     assert evict(kv, kept=PTR + 1026) == 2 and evict(kv, to=PTR + 2) == 2 and evict(kv, lens=PTR + 3074) == 2
