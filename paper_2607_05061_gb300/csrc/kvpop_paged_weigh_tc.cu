@@ -14,7 +14,7 @@
 //  * 16 softmax warps, which also bring the next tile's positions into the other half of the
 //    operand's tensor memory (their bytes are on their way one tile before, their pages two);
 //  * 1 MMA warp: S = K Q^T (M 128, N 128, K d) per half of the tile, one buffer a half;
-//  * 2 producer warps: query rows by 16-byte cp.async into 128B-swizzled slots, with lse and the last
+//  * 3 producer warps: query rows by 16-byte cp.async into 128B-swizzled slots, with lse and the last
 //    position that each row sees beside them.  Where all of a sequence's rows fit the slots they stay
 //    there for all tiles of the head.
 // Tensor memory: S 2 x 128 columns, operands 2 x (2 x d / 2).
@@ -30,7 +30,7 @@ using namespace paged;
 using namespace tc05;
 
 constexpr int WT_HALF = 128, WT_KEYS = 256, WT_BN = 128;
-constexpr int WT_SOFT = 16, WT_MMA_WARP = WT_SOFT, WT_COPY_WARP = WT_SOFT + 1, WT_COPY = 2;
+constexpr int WT_SOFT = 16, WT_MMA_WARP = WT_SOFT, WT_COPY_WARP = WT_SOFT + 1, WT_COPY = 3;
 constexpr int WT_THREADS = 32 * (WT_COPY_WARP + WT_COPY);
 constexpr int WT_WHOLE = 8;                              // tiles of up to that many blocks are not cut
 constexpr float kLog2E = 1.4426950408889634f;
@@ -55,8 +55,8 @@ struct WL {
   static constexpr int ST = D == 128 ? 5 : 8, SLOT = WT_BN * D * 2;
   static constexpr int OFF_NL = ST * SLOT;               // [slot][128] -lse log2 e
   static constexpr int OFF_LIM = OFF_NL + ST * WT_BN * 4;   // [slot][128] last position seen, -1: none
-  static constexpr int OFF_FLAG = OFF_LIM + ST * WT_BN * 4; // [slot][copy warp] whether one sees none
-  static constexpr int OFF_X = OFF_FLAG + ST * WT_COPY * 4; // [2][256] sums of the upper columns
+  static constexpr int OFF_FLAG = OFF_LIM + ST * WT_BN * 4; // [slot][4] whether one of 32 rows sees none
+  static constexpr int OFF_X = OFF_FLAG + ST * 16; // [2][256] sums of the upper columns
   static constexpr int OFF_BAR = (OFF_X + 2 * WT_KEYS * 4 + 7) / 8 * 8;
   static constexpr int FULL = 0, EMPTY = ST, SFULL = 2 * ST, PFULL = SFULL + 2, AFULL = PFULL + 2, XFULL = AFULL + 2,
                        END = XFULL + 8, N_BAR = END + 1;
@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) paged_weigh_tc_kernel(WeighTcAr
   }
   if (tid == 64) {
     for (int i = 0; i < ST; ++i) {
-      mbar_init(bar(L::FULL + i), 32 * WT_COPY + WT_COPY);
+      mbar_init(bar(L::FULL + i), 4 * 32 + 4);
       mbar_init(bar(L::EMPTY + i), 1 + WT_SOFT);
     }
     for (int i = 0; i < 2; ++i) {
@@ -234,64 +234,67 @@ __global__ void __launch_bounds__(WT_THREADS, 1) paged_weigh_tc_kernel(WeighTcAr
 
   if (warp >= WT_COPY_WARP) {
     // ---------------------------------------------------------------- query rows
+    // The warps take groups of 32 rows in turn.  A group's addresses and normalisers are asked for one
+    // group ahead.
     const int cw = warp - WT_COPY_WARP;
-    auto load = [&](const Tile& x, int b) {
-      const int st = pos % ST;
-      if (pos >= (uint32_t)ST && !wait(L::EMPTY + st, (pos / ST - 1) & 1)) return false;
-      // a lane knows two of the warp's 64 rows
-      long long off[2];
-      int lim[2];
-      float nl[2];
-      bool none = false;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const long long r = (long long)b * WT_BN + cw * 64 + 32 * i + lane, rows = (long long)x.x.n * G;
-        off[i] = -1;
-        lim[i] = -1;
-        nl[i] = 0.f;
-        if (r < rows) {
-          const int tok = (int)(r / G), g = (int)(r - (long long)tok * G);
-          off[i] = (x.x.first + tok) * a.q_ts + (long long)(x.h * G + g) * a.q_hs;
-          const float l = a.lse[((long long)(x.x.first + tok) * H + x.h) * G + g];
-          if (l != -INFINITY) {
-            lim[i] = last_seen(x.x.len, tok, x.x.ctx);
-            nl[i] = -l * kLog2E;
-          }
-        }
-        none |= lim[i] < 0;
+    struct Group {
+      long long off;
+      float l;
+      int lim;
+    };
+    int b = t.b0;                                        // the load of number `pos`: block b of tile t
+    auto end = [&] { return stays(t) ? t.x.blocks : t.b1; };
+    auto next_load = [&] {
+      ++pos;
+      if (++b < end()) return;
+      const Tile was = t;
+      do advance(a, t);
+      while (t.valid() && stays(t) && t.same_head(was));
+      b = t.b0;
+    };
+    auto group = [&](int k) {
+      Group x;
+      const long long r = (long long)b * WT_BN + 32 * k + lane;
+      const bool in = t.valid() && r < (long long)t.x.n * G;
+      const int tok = in ? (int)((uint32_t)r / (uint32_t)G) : 0, g = in ? (int)r - tok * G : 0;
+      x.off = in ? (t.x.first + tok) * a.q_ts + (long long)(t.h * G + g) * a.q_hs : -1;
+      x.l = in ? a.lse[((long long)(t.x.first + tok) * H + t.h) * G + g] : -INFINITY;
+      x.lim = last_seen(t.x.len, tok, t.x.ctx);
+      return x;
+    };
+    int k = cw;
+    bool more = t.valid();
+    Group x = group(k);
+    while (more && ok) {
+      const uint32_t p = pos;
+      const int st = p % ST, kk = k;
+      const Group y = x;
+      if ((k += WT_COPY) >= 4) {                         // the group after this one
+        k -= 4;
+        next_load();
       }
+      more = t.valid();
+      x = group(k);
+      if (p >= (uint32_t)ST && !(ok = wait(L::EMPTY + st, (p / ST - 1) & 1))) break;
       const uint32_t dst = sb + st * L::SLOT;
       constexpr int LPR = D / 8, RPI = 32 / LPR;         // lanes of a row, rows at a time
       const int c = lane % LPR, sub = lane / LPR;
 #pragma unroll
-      for (int i = 0; i < 64 / RPI; ++i) {
+      for (int i = 0; i < LPR; ++i) {
         const int rr = i * RPI + sub;
-        const long long o = __shfl_sync(0xffffffffu, off[i * RPI / 32], rr & 31);
-        cp_async16(dst + tile_off(cw * 64 + rr, c, WT_BN), a.q + (o < 0 ? 0 : o) + 8 * c, o < 0 ? 0 : 16);
+        const long long o = __shfl_sync(0xffffffffu, y.off, rr);
+        cp_async16(dst + tile_off(kk * 32 + rr, c, WT_BN), a.q + (o < 0 ? 0 : o) + 8 * c, o < 0 ? 0 : 16);
       }
       cp_async_arrive_noinc(bar(L::FULL + st));
-      float* nls = reinterpret_cast<float*>(smt + L::OFF_NL) + st * WT_BN + cw * 64;
-      int* lims = reinterpret_cast<int*>(smt + L::OFF_LIM) + st * WT_BN + cw * 64;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        nls[32 * i + lane] = nl[i];
-        lims[32 * i + lane] = lim[i];
-      }
-      none = __any_sync(0xffffffffu, none);
-      if (lane == 0) reinterpret_cast<int*>(smt + L::OFF_FLAG)[st * WT_COPY + cw] = none;
+      const bool gone = y.l == -INFINITY;
+      reinterpret_cast<float*>(smt + L::OFF_NL)[st * WT_BN + kk * 32 + lane] = gone ? 0.f : -y.l * kLog2E;
+      reinterpret_cast<int*>(smt + L::OFF_LIM)[st * WT_BN + kk * 32 + lane] = gone ? -1 : y.lim;
+      const bool none = __any_sync(0xffffffffu, gone);
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar(L::FULL + st));
-      ++pos;
-      return true;
-    };
-    Tile head = t;                                       // the first tile of the head
-    bool fresh = true;
-    while (t.valid() && ok) {
-      if (!stays(t) || fresh)
-        for (int b = t.b0; b < (stays(t) ? t.x.blocks : t.b1) && ok; ++b) ok = load(t, b);
-      advance(a, t);
-      fresh = !t.valid() || !t.same_head(head);
-      if (fresh) head = t;
+      if (lane == 0) {
+        reinterpret_cast<int*>(smt + L::OFF_FLAG)[st * 4 + kk] = none;
+        mbar_arrive(bar(L::FULL + st));
+      }
     }
     cp_wait<0>();
   } else if (warp == WT_MMA_WARP) {
@@ -423,6 +426,8 @@ __global__ void __launch_bounds__(WT_THREADS, 1) paged_weigh_tc_kernel(WeighTcAr
       fetch();
       look();
       const int t0 = t.kt * WT_KEYS, tp = t0 + r, t1 = min(t0 + WT_KEYS, t.x.ctx) - 1;
+      // blocks from here on have rows that see the whole tile: tokens from t1 - len on
+      const int all_see = t1 <= t.x.len ? 0 : (int)(((long long)(t1 - t.x.len) * G + WT_BN - 1) / WT_BN);
       float* const to = a.mass + ((long long)t.s * H + t.h) * a.positions + tp;
       const bool whole = t.b0 == t.x.skipped(G, t.kt) && t.b1 == t.x.blocks;
       float before = 0.f;
@@ -445,7 +450,8 @@ __global__ void __launch_bounds__(WT_THREADS, 1) paged_weigh_tc_kernel(WeighTcAr
         if (lane == 0) mbar_arrive(bar(L::PFULL + hh));
         const float4* nl = reinterpret_cast<const float4*>(nlS + st * WT_BN);
         uint64_t s0 = 0ull, s1 = 0ull;
-        const bool edge = last_seen(t.x.len, (int)((long long)b * WT_BN / G), t.x.ctx) < t1 || flagS[st * WT_COPY] || flagS[st * WT_COPY + 1];
+        const bool edge = b < all_see ||
+                          (flagS[4 * st] | flagS[4 * st + 1] | flagS[4 * st + 2] | flagS[4 * st + 3]);
         if (!edge) {
 #pragma unroll
           for (int k = 0; k < 16; ++k) {
