@@ -3,7 +3,7 @@
 // The mathematics is that of kvpop_paged_weigh.cu.  Positions are the rows of the products: a tile is
 // 256 positions of one (sequence, KV head), as bf16 (which holds every e4m3 value) in tensor memory,
 // and its query rows (token, query head) come as blocks of 128 columns, unchanged.  A thread owns one
-// position and 64 columns of every block:
+// position:
 //   x = S ks c - lse log2 e,   sum += 2^x,
 // one fma, one exponential and one addition a value; there is no maximum to keep, since a weight is
 // no more than 1.  A position's sum is added to its weight at the end of the tile.
@@ -11,13 +11,15 @@
 // All (tile, block) pairs form one list, tile after tile, that is cut evenly over the SMs; a tile that
 // lies in several CTAs' parts is added up, in their order, by the CTA that arrives last, at its end.
 // Roles:
-//  * 16 softmax warps, which also bring the next tile's positions into the other half of the
-//    operand's tensor memory (their bytes are on their way one tile before, their pages two);
+//  * 8 softmax warps, which also bring the next tile's positions into the other half of the
+//    operand's tensor memory (their bytes are on their way two tiles before, their pages three);
 //  * 1 MMA warp: S = K Q^T (M 128, N 128, K d) per half of the tile, one buffer a half;
 //  * 3 producer warps: query rows by 16-byte cp.async into 128B-swizzled slots, with lse and the last
 //    position that each row sees beside them.  Where all of a sequence's rows fit the slots they stay
 //    there for all tiles of the head.
 // Tensor memory: S 2 x 128 columns, operands 2 x (2 x d / 2).
+#include <type_traits>
+
 #include "kvpop_mma.cuh"
 #include "kvpop_paged.cuh"
 #include "kvpop_ptx.cuh"
@@ -30,9 +32,12 @@ using namespace paged;
 using namespace tc05;
 
 constexpr int WT_HALF = 128, WT_KEYS = 256, WT_BN = 128;
-constexpr int WT_SOFT = 16, WT_MMA_WARP = WT_SOFT, WT_COPY_WARP = WT_SOFT + 1, WT_COPY = 3;
+constexpr int WT_SOFT = 8, WT_MMA_WARP = WT_SOFT, WT_COPY_WARP = WT_SOFT + 1, WT_COPY = 3;
 constexpr int WT_THREADS = 32 * (WT_COPY_WARP + WT_COPY);
 constexpr int WT_WHOLE = 8;                              // tiles of up to that many blocks are not cut
+#ifndef WT_ENDS
+#define WT_ENDS 4
+#endif
 constexpr float kLog2E = 1.4426950408889634f;
 
 struct WeighTcArgs {
@@ -52,14 +57,17 @@ struct WeighTcArgs {
 
 template <int D>
 struct WL {
-  static constexpr int ST = D == 128 ? 5 : 8, SLOT = WT_BN * D * 2;
+  static constexpr int ST = D == 128 ? 4 : 8, SLOT = WT_BN * D * 2;
   static constexpr int OFF_NL = ST * SLOT;               // [slot][128] -lse log2 e
   static constexpr int OFF_LIM = OFF_NL + ST * WT_BN * 4;   // [slot][128] last position seen, -1: none
-  static constexpr int OFF_FLAG = OFF_LIM + ST * WT_BN * 4; // [slot][4] whether one of 32 rows sees none
-  static constexpr int OFF_X = OFF_FLAG + ST * 16; // [2][256] sums of the upper columns
-  static constexpr int OFF_BAR = (OFF_X + 2 * WT_KEYS * 4 + 7) / 8 * 8;
-  static constexpr int FULL = 0, EMPTY = ST, SFULL = 2 * ST, PFULL = SFULL + 2, AFULL = PFULL + 2, XFULL = AFULL + 2,
-                       END = XFULL + 8, N_BAR = END + 1;
+  static constexpr int OFF_FLAG = OFF_LIM + ST * WT_BN * 4; // [slot] a byte for each 32 rows: whether one sees none
+  static constexpr int OFF_RAW = (OFF_FLAG + ST * 4 + 15) / 16 * 16;   // [2] bytes of tiles to come, a thread's pieces apart
+  // a thread's page of a tile to come, and scale and weight so far of tiles there and to come: in registers
+  // they were spilled, and a load that is spilled is waited for
+  static constexpr int OFF_ID = OFF_RAW + 2 * WT_KEYS * D, OFF_SC = OFF_ID + 2 * WT_KEYS * 4, OFF_OLD = OFF_SC + 4 * WT_KEYS * 4;
+  static constexpr int OFF_BAR = OFF_OLD + 4 * WT_KEYS * 4;
+  static constexpr int FULL = 0, EMPTY = ST, SFULL = 2 * ST, PFULL = SFULL + 2, AFULL = PFULL + 2,
+                       END = AFULL + 2, N_BAR = END + 1;
   static constexpr int OFF_TMEM = OFF_BAR + 8 * N_BAR, BYTES = OFF_TMEM + 16;
   static_assert(ST <= WT_WHOLE, "");
 };
@@ -72,7 +80,7 @@ struct WSeqT {
     return t0 <= len ? 0 : (int)((t0 - len) * G / WT_BN);
   }
   __device__ __forceinline__ int here(int G, int kt) const { return blocks - skipped(G, kt); }
-  // blocks of the tiles before kt
+  // places of the tiles before kt: their blocks, and what a tile's ends cost, in blocks
   __device__ __forceinline__ long long before(int G, int kt) const {
     const int full = min(kt, min(tiles, len / WT_KEYS + 1));
     long long w = (long long)full * blocks;
@@ -80,7 +88,7 @@ struct WSeqT {
       const long long up = ((long long)len * G + WT_BN - 1) / WT_BN, k = kt - full;
       w += k * (blocks + up) - (long long)G * ((long long)kt * (kt - 1) - (long long)full * (full - 1));
     }
-    return w;
+    return w + (long long)WT_ENDS * kt;
   }
 };
 __device__ __forceinline__ WSeqT wseq_t(const WeighTcArgs& a, int s) {
@@ -101,13 +109,13 @@ __device__ __forceinline__ WSeqT wseq_t(const WeighTcArgs& a, int s) {
 struct Tile {
   WSeqT x;
   int s, h, kt, b0, b1;
-  long long at, end;                                     // list positions of b0, and of the CTA's end
+  long long at, end;                                     // places of b0, and of the CTA's end, in the list
   __device__ __forceinline__ bool valid() const { return at < end; }
   __device__ __forceinline__ void cut() { b1 = (int)min((long long)x.blocks, b0 + (end - at)); }
   __device__ __forceinline__ bool same_head(const Tile& o) const { return s == o.s && h == o.h; }
 };
 __device__ __forceinline__ void advance(const WeighTcArgs& a, Tile& t) {
-  t.at += t.b1 - t.b0;
+  t.at += t.x.blocks - t.b0 + WT_ENDS;
   if (t.at >= t.end) return;
   if (++t.kt == t.x.tiles) {
     t.kt = 0;
@@ -120,7 +128,8 @@ __device__ __forceinline__ void advance(const WeighTcArgs& a, Tile& t) {
   t.b0 = t.x.skipped(a.G, t.kt);
   t.cut();
 }
-// The tile that list position w lies in (by a whole warp); w: below the total.
+// The tile that place w of the list lies in (by a whole warp); w: below the total.  b0 may lie behind its
+// blocks.
 __device__ Tile find(const WeighTcArgs& a, long long w, int lane) {
   Tile t;
   long long base = 0;
@@ -161,7 +170,7 @@ __device__ Tile find(const WeighTcArgs& a, long long w, int lane) {
 template <int D>
 __global__ void __launch_bounds__(WT_THREADS, 1) paged_weigh_tc_kernel(WeighTcArgs a) {
   using L = WL<D>;
-  constexpr int ST = L::ST, RAW = D / 32;                // 16-byte pieces of a thread's half of a row
+  constexpr int ST = L::ST, RAW = D / 16;                // 16-byte pieces of a row
   extern __shared__ __align__(1024) unsigned char smt[];
   __shared__ Tile edgeS[2], aheadS[WT_SOFT];
   __shared__ long long edgeW[2], shareS;
@@ -187,8 +196,8 @@ __global__ void __launch_bounds__(WT_THREADS, 1) paged_weigh_tc_kernel(WeighTcAr
     if (w < total) {
       t = find(a, w, lane);
       const int skip = t.x.skipped(G, t.kt);
-      if (t.b0 > skip && t.x.blocks - skip <= WT_WHOLE) {
-        w += t.x.blocks - t.b0;
+      if (t.b0 >= t.x.blocks || (t.b0 > skip && t.x.blocks - skip <= WT_WHOLE)) {
+        w += t.x.blocks - t.b0 + WT_ENDS;
         t = w < total ? find(a, w, lane) : Tile{};
       }
     }
@@ -208,7 +217,6 @@ __global__ void __launch_bounds__(WT_THREADS, 1) paged_weigh_tc_kernel(WeighTcAr
       mbar_init(bar(L::PFULL + i), WT_SOFT / 2);
       mbar_init(bar(L::AFULL + i), WT_SOFT);
     }
-    for (int i = 0; i < 8; ++i) mbar_init(bar(L::XFULL + i), 1);
     mbar_init(bar(L::END), 1);
     mbar_fence_init();
   }
@@ -292,7 +300,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) paged_weigh_tc_kernel(WeighTcAr
       const bool none = __any_sync(0xffffffffu, gone);
       __syncwarp();
       if (lane == 0) {
-        reinterpret_cast<int*>(smt + L::OFF_FLAG)[st * 4 + kk] = none;
+        (smt + L::OFF_FLAG)[st * 4 + kk] = none;
         mbar_arrive(bar(L::FULL + st));
       }
     }
@@ -348,132 +356,154 @@ __global__ void __launch_bounds__(WT_THREADS, 1) paged_weigh_tc_kernel(WeighTcAr
     wait(L::END, 0);
   } else {
     // ---------------------------------------------------------------- softmax
-    // warp: half hh of the tile, rows 32 (warp mod 4) + lane, columns 64 cs .. of every block
-    const int hh = (warp >> 2) & 1, cs = warp >> 3, r = hh * WT_HALF + (warp & 3) * 32 + lane;
+    // a thread: one position, in half hh of the tile, and all columns.  While one half's warps work on
+    // their logits the tensor core forms the other's.
+    const int hh = warp >> 2, r = tid;
     const uint32_t tl = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-    const float* const nlS = reinterpret_cast<const float*>(smt + L::OFF_NL) + 64 * cs;
-    const int* const limS = reinterpret_cast<const int*>(smt + L::OFF_LIM) + 64 * cs;
+    const float* const nlS = reinterpret_cast<const float*>(smt + L::OFF_NL);
+    const int* const limS = reinterpret_cast<const int*>(smt + L::OFF_LIM);
     const int* const flagS = reinterpret_cast<const int*>(smt + L::OFF_FLAG);
-    float* const xS = reinterpret_cast<float*>(smt + L::OFF_X);
-    // the tiles to come: the page of one, the bytes and scale of the one before it
+    // Tiles to come, by their number: the page of j + 3, the bytes of j + 2 and of j + 1.
     if (lane == 0) aheadS[warp] = t;
     __syncwarp();
-    int id = -1, id_t = 0, id_h = 0;
-    uint4 raw[RAW];
-    float raw_scale = 0.f, next_scale = 0.f;
-    auto look = [&] {                                    // the page of the row in `ahead`
-      id = -1;
+    int pos_of = -1, head_of = 0;                        // of the tile whose page is on its way: the thread's position,
+    const float* old_of = nullptr;                       // head and weight so far
+    auto mine = [&](int off, int n) { return reinterpret_cast<float*>(smt + off) + n * WT_KEYS + r; };
+    auto look = [&](int j) {                             // the page of the row in `ahead`
+      pos_of = -1;
+      old_of = nullptr;
       Tile ahead = aheadS[warp];
       if (!ahead.valid()) return;
-      id_t = ahead.kt * WT_KEYS + r;
-      id_h = ahead.h;
-      if (id_t < ahead.x.ctx) {
-        id = a.b.table[(long long)ahead.s * a.b.table_stride + (id_t >> a.pool.page_shift)];
-        if ((unsigned)id >= (unsigned)a.pool.n_pages) {
-          report(a.err, ERR_PAGE);
-          id = -1;
-        }
+      const int at = ahead.kt * WT_KEYS + r;
+      if (at < ahead.x.ctx) {
+        pos_of = at;
+        head_of = ahead.h;
+        if (at < ahead.x.len) old_of = a.mass + ((long long)ahead.s * H + ahead.h) * a.positions + at;
+        cp_async4(smem_u32(mine(L::OFF_ID, j & 1)), a.b.table + (long long)ahead.s * a.b.table_stride + (at >> a.pool.page_shift));
       }
       advance(a, ahead);
       __syncwarp();
       if (lane == 0) aheadS[warp] = ahead;
       __syncwarp();
     };
-    auto fetch = [&] {                                   // its bytes
-      raw_scale = 0.f;
-#pragma unroll
-      for (int i = 0; i < RAW; ++i) raw[i] = make_uint4(0, 0, 0, 0);
-      if (id >= 0) {
-        const long long at = ((long long)id * H + id_h) * a.pool.page + (id_t & (a.pool.page - 1));
-        const uint4* p = reinterpret_cast<const uint4*>(a.pool.k + at * D + cs * (D / 2));
-#pragma unroll
-        for (int i = 0; i < RAW; ++i) raw[i] = p[i];
-        raw_scale = a.pool.ks[at / BLK];
-      }
-    };
-    auto store = [&](int buf) {                          // into the operand
-      float w[D / 4];
-#pragma unroll
-      for (int i = 0; i < RAW; ++i) {
-        const uint32_t u[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          uint32_t lo, hi;
-          cvt4(u[k], lo, hi);
-          const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&lo));
-          const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-          w[8 * i + 2 * k] = __uint_as_float(pack_bf16(x.x, x.y));
-          w[8 * i + 2 * k + 1] = __uint_as_float(pack_bf16(y.x, y.y));
+    const uint32_t rawS = sb + L::OFF_RAW + tid * 16;
+    auto fetch = [&](int j) {                            // its bytes (the page is there)
+      int id = -1;
+      if (pos_of >= 0) {
+        id = __float_as_int(*mine(L::OFF_ID, j & 1));
+        if ((unsigned)id >= (unsigned)a.pool.n_pages) {
+          report(a.err, ERR_PAGE);
+          id = -1;
         }
       }
-      const uint32_t to = tl + 256 + buf * D + hh * (D / 2) + cs * (D / 4);
-      if constexpr (D == 128) tmem_st32(to, w); else tmem_st16(to, w);
+      const long long at = id < 0 ? 0 : ((long long)id * H + head_of) * a.pool.page + (pos_of & (a.pool.page - 1));
+      const unsigned char* p = a.pool.k + at * D;
+#pragma unroll
+      for (int i = 0; i < RAW; ++i)
+        cp_async16(rawS + (j & 1) * (WT_KEYS * D) + i * (32 * WT_SOFT * 16), p + 16 * i, id < 0 ? 0 : 16);
+      if (id >= 0) cp_async4(smem_u32(mine(L::OFF_SC, j & 3)), a.pool.ks + at / BLK);
+      else *mine(L::OFF_SC, j & 3) = 0.f;
+      if (old_of) cp_async4(smem_u32(mine(L::OFF_OLD, j & 3)), old_of);
+      else *mine(L::OFF_OLD, j & 3) = 0.f;
+    };
+    auto store = [&](int buf) {                          // into the operand
+#pragma unroll
+      for (int c = 0; c < RAW; c += 2) {
+        float w[16];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint4 v = *reinterpret_cast<const uint4*>(smt + L::OFF_RAW + tid * 16 + buf * (WT_KEYS * D) + (c + i) * (32 * WT_SOFT * 16));
+          const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            uint32_t lo, hi;
+            cvt4(u[k], lo, hi);
+            const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&lo));
+            const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+            w[8 * i + 2 * k] = __uint_as_float(pack_bf16(x.x, x.y));
+            w[8 * i + 2 * k + 1] = __uint_as_float(pack_bf16(y.x, y.y));
+          }
+        }
+        tmem_st16(tl + 256 + buf * D + hh * (D / 2) + 8 * c, w);
+      }
       tmem_wait_st();
       fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(L::AFULL + buf));
-      next_scale = raw_scale;
     };
-    look();
-    fetch();
-    look();
+    look(0);
+    cp_commit();
+#pragma unroll 1
+    for (int j = 0; j < 2; ++j) {
+      cp_wait<0>();
+      fetch(j);
+      look(j + 1);
+      cp_commit();
+    }
+    cp_wait<1>();
     if (t.valid()) store(0);
     uint32_t step = 0;
     int first = t.b0;
     for (uint32_t i = 0; t.valid() && ok; ++i) {
-      const float scale = next_scale;                    // 0: no position, or a bad page
+      cp_wait<0>();                                      // (asked for a tile ago)
+      const float scale = *mine(L::OFF_SC, i & 3);       // 0: no position, or a bad page
       const uint64_t cc = f2_pack(a.c * scale, a.c * scale);
-      fetch();
-      look();
+      fetch(i + 2);                                      // (that buffer's bytes are in the operand)
+      look(i + 3);
+      cp_commit();
       const int t0 = t.kt * WT_KEYS, tp = t0 + r, t1 = min(t0 + WT_KEYS, t.x.ctx) - 1;
       // blocks from here on have rows that see the whole tile: tokens from t1 - len on
       const int all_see = t1 <= t.x.len ? 0 : (int)(((long long)(t1 - t.x.len) * G + WT_BN - 1) / WT_BN);
       float* const to = a.mass + ((long long)t.s * H + t.h) * a.positions + tp;
       const bool whole = t.b0 == t.x.skipped(G, t.kt) && t.b1 == t.x.blocks;
-      float before = 0.f;
-      if (cs == 0 && whole && tp < t.x.ctx && tp < t.x.len) before = *to;
       const bool stay = stays(t);
       float sum = 0.f;
       for (int b = t.b0; b < t.b1; ++b, ++step) {
         const uint32_t p = stay ? pos + (b - first) : pos;
         const int st = p % ST;
-        if (!(ok = wait(L::SFULL + hh, step & 1) && wait(L::FULL + st, p / ST & 1))) break;
+        if (!(ok = wait(L::FULL + st, p / ST & 1) && wait(L::SFULL + hh, step & 1))) break;
         fence_after();
         // (all products of the tile before are done: the other operand is free)
-        if (b == t.b1 - 1 && t.at + (t.b1 - t.b0) < t.end) store((i + 1) & 1);
-        float s[64];
-        tmem_ld32(tl + hh * 128 + 64 * cs, *reinterpret_cast<float(*)[32]>(s));
-        tmem_ld32(tl + hh * 128 + 64 * cs + 32, *reinterpret_cast<float(*)[32]>(s + 32));
+        if (b == t.b1 - 1 && t.at + (t.x.blocks - t.b0 + WT_ENDS) < t.end) store((i + 1) & 1);
+        const bool edge = b < all_see || flagS[st] != 0;
+        uint64_t s0 = 0ull, s1 = 0ull;
+        const uint32_t tS = tl + hh * 128;
+        const float4* const nl = reinterpret_cast<const float4*>(nlS + st * WT_BN);
+        const int4* const lim = reinterpret_cast<const int4*>(limS + st * WT_BN);
+        float v[4][32];
+        tmem_ld32(tS, v[0]);
+        tmem_ld32(tS + 32, v[1]);
+        tmem_ld32(tS + 64, v[2]);
+        tmem_ld32(tS + 96, v[3]);
         tmem_wait_ld();
-        fence_before();
+        fence_before();                                  // the logits are in registers
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(L::PFULL + hh));
-        const float4* nl = reinterpret_cast<const float4*>(nlS + st * WT_BN);
-        uint64_t s0 = 0ull, s1 = 0ull;
-        const bool edge = b < all_see ||
-                          (flagS[4 * st] | flagS[4 * st + 1] | flagS[4 * st + 2] | flagS[4 * st + 3]);
-        if (!edge) {
+        auto columns = [&](auto at_edge, int u) {
+          float (&w)[32] = v[u];
 #pragma unroll
-          for (int k = 0; k < 16; ++k) {
-            const float4 n4 = nl[k];
+          for (int k = 0; k < 8; ++k) {
+            const float4 n4 = nl[8 * u + k];
             float x0, x1, x2, x3;
-            f2_unpack(f2_fma(f2_pack(s[4 * k], s[4 * k + 1]), cc, f2_pack(n4.x, n4.y)), x0, x1);
-            f2_unpack(f2_fma(f2_pack(s[4 * k + 2], s[4 * k + 3]), cc, f2_pack(n4.z, n4.w)), x2, x3);
+            f2_unpack(f2_fma(f2_pack(w[4 * k], w[4 * k + 1]), cc, f2_pack(n4.x, n4.y)), x0, x1);
+            f2_unpack(f2_fma(f2_pack(w[4 * k + 2], w[4 * k + 3]), cc, f2_pack(n4.z, n4.w)), x2, x3);
+            if constexpr (decltype(at_edge)::value) {
+              const int4 l4 = lim[8 * u + k];
+              x0 = tp <= l4.x ? x0 : -INFINITY;
+              x1 = tp <= l4.y ? x1 : -INFINITY;
+              x2 = tp <= l4.z ? x2 : -INFINITY;
+              x3 = tp <= l4.w ? x3 : -INFINITY;
+            }
             s0 = f2_add(s0, f2_pack(ex2(x0), ex2(x1)));
             s1 = f2_add(s1, f2_pack(ex2(x2), ex2(x3)));
           }
-        } else {
-          const int4* lim = reinterpret_cast<const int4*>(limS + st * WT_BN);
+        };
+        if (edge) {
 #pragma unroll
-          for (int k = 0; k < 16; ++k) {
-            const float4 n4 = nl[k];
-            const int4 l4 = lim[k];
-            float x0, x1, x2, x3;
-            f2_unpack(f2_fma(f2_pack(s[4 * k], s[4 * k + 1]), cc, f2_pack(n4.x, n4.y)), x0, x1);
-            f2_unpack(f2_fma(f2_pack(s[4 * k + 2], s[4 * k + 3]), cc, f2_pack(n4.z, n4.w)), x2, x3);
-            s0 = f2_add(s0, f2_pack(ex2(tp <= l4.x ? x0 : -INFINITY), ex2(tp <= l4.y ? x1 : -INFINITY)));
-            s1 = f2_add(s1, f2_pack(ex2(tp <= l4.z ? x2 : -INFINITY), ex2(tp <= l4.w ? x3 : -INFINITY)));
-          }
+          for (int u = 0; u < 4; ++u) columns(std::true_type{}, u);
+        } else {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) columns(std::false_type{}, u);
         }
         float y0, y1;
         f2_unpack(f2_add(s0, s1), y0, y1);
@@ -485,22 +515,12 @@ __global__ void __launch_bounds__(WT_THREADS, 1) paged_weigh_tc_kernel(WeighTcAr
         }
       }
       if (!ok) break;
-      // ---- the columns' halves meet
-      float* const x = xS + (i & 1) * WT_KEYS + r;
-      if (cs == 1) {
-        *x = sum;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(L::XFULL + (warp & 7)));
-      } else {
-        if (!(ok = wait(L::XFULL + warp, i & 1))) break;
-        sum += *x;
-        if (scale == 0.f) sum = 0.f;
-        if (whole) {
-          if (tp < t.x.ctx) *to = before + sum;
-        } else {                                         // (the part's first tile, or its last)
-          const bool begins = t.b0 == t.x.skipped(G, t.kt);
-          __stcg(a.part + ((long long)blockIdx.x * 2 + begins) * WT_KEYS + r, sum);
-        }
+      if (scale == 0.f) sum = 0.f;
+      if (whole) {
+        if (tp < t.x.ctx) *to = *mine(L::OFF_OLD, i & 3) + sum;
+      } else {                                           // (the part's first tile, or its last)
+        const bool begins = t.b0 == t.x.skipped(G, t.kt);
+        __stcg(a.part + ((long long)blockIdx.x * 2 + begins) * WT_KEYS + r, sum);
       }
       const Tile was = t;
       advance(a, t);
