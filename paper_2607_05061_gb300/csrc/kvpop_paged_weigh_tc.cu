@@ -386,7 +386,10 @@ __global__ void __launch_bounds__(WT_THREADS, 1) paged_weigh_tc_kernel(WeighTcAr
       if (lane == 0) aheadS[warp] = ahead;
       __syncwarp();
     };
-    const uint32_t rawS = sb + L::OFF_RAW + tid * 16;
+    // A warp copies its 32 rows as whole lines (a row a lane, each copy touches 32 of them: 2200 clocks a
+    // tile); chunk c of row r lies at chunk c ^ r of the row's 128 (64) bytes.
+    unsigned char* const rawS = smt + L::OFF_RAW + warp * (32 * D);
+    auto chunk_of = [&](int row, int c) { return row * D + ((c ^ (row & (RAW - 1))) << 4); };
     auto fetch = [&](int j) {                            // its bytes (the page is there)
       int id = -1;
       if (pos_of >= 0) {
@@ -396,23 +399,27 @@ __global__ void __launch_bounds__(WT_THREADS, 1) paged_weigh_tc_kernel(WeighTcAr
           id = -1;
         }
       }
-      const long long at = id < 0 ? 0 : ((long long)id * H + head_of) * a.pool.page + (pos_of & (a.pool.page - 1));
-      const unsigned char* p = a.pool.k + at * D;
+      const long long at = id < 0 ? -1 : ((long long)id * H + head_of) * a.pool.page + (pos_of & (a.pool.page - 1));
+      const uint32_t dst = smem_u32(rawS) + (j & 1) * (WT_KEYS * D);
 #pragma unroll
-      for (int i = 0; i < RAW; ++i)
-        cp_async16(rawS + (j & 1) * (WT_KEYS * D) + i * (32 * WT_SOFT * 16), p + 16 * i, id < 0 ? 0 : 16);
+      for (int i = 0; i < RAW; ++i) {
+        const int row = i * (32 / RAW) + lane / RAW, c = lane % RAW;
+        const long long o = __shfl_sync(0xffffffffu, at, row);
+        cp_async16(dst + chunk_of(row, c), a.pool.k + (o < 0 ? 0 : o) * D + 16 * c, o < 0 ? 0 : 16);
+      }
       if (id >= 0) cp_async4(smem_u32(mine(L::OFF_SC, j & 3)), a.pool.ks + at / BLK);
       else *mine(L::OFF_SC, j & 3) = 0.f;
       if (old_of) cp_async4(smem_u32(mine(L::OFF_OLD, j & 3)), old_of);
       else *mine(L::OFF_OLD, j & 3) = 0.f;
     };
     auto store = [&](int buf) {                          // into the operand
+      __syncwarp();
 #pragma unroll
       for (int c = 0; c < RAW; c += 2) {
         float w[16];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const uint4 v = *reinterpret_cast<const uint4*>(smt + L::OFF_RAW + tid * 16 + buf * (WT_KEYS * D) + (c + i) * (32 * WT_SOFT * 16));
+          const uint4 v = *reinterpret_cast<const uint4*>(rawS + buf * (WT_KEYS * D) + chunk_of(lane, c + i));
           const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
