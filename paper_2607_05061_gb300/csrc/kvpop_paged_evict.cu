@@ -52,9 +52,10 @@ __device__ __forceinline__ uint32_t key_of(float m) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-__global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(EvictArgs a) {
+// (four CTAs an SM: with 40 registers 512 rows of 4200 took two waves)
+__global__ void __launch_bounds__(EV_THREADS, 4) evict_select_kernel(EvictArgs a) {
   extern __shared__ uint32_t keyS[];
-  __shared__ uint32_t histS[2][EV_BINS];
+  __shared__ __align__(16) uint32_t histS[EV_BINS], sumS[EV_BINS];   // the CTA's counts, and its share of the cluster's
   __shared__ uint32_t warpS[2][EV_WARPS], foundS[2], sumsS[2];
   cg::cluster_group cluster = cg::this_cluster();
   const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
@@ -81,39 +82,51 @@ __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(EvictArgs a) {
   auto key = [&](int i) { return cached ? keyS[i] : key_of(m[i]); };
   if (cached)
     for (int i = tid; i < n; i += EV_THREADS) keyS[i] = key_of(m[i]);
-  for (int i = tid; i < 2 * EV_BINS; i += EV_THREADS) (&histS[0][0])[i] = 0;
-  __syncthreads();
+  for (int i = tid; i < EV_BINS; i += EV_THREADS) histS[i] = sumS[i] = 0;
+  if (C > 1) cluster.sync(); else __syncthreads();
 
   // ---- the want-th largest key, digit by digit
   uint32_t prefix = 0, left = (uint32_t)want;          // of the keys that begin with prefix, left are wanted
 #pragma unroll
   for (int p = 0; p < 3; ++p) {
     const int shift = p == 0 ? 21 : p == 1 ? 10 : 0, bins = p == 2 ? 1024 : 2048;
-    uint32_t* const hist = histS[p & 1];
     for (int i = tid; i < n; i += EV_THREADS) {
       const uint32_t k = key(i);
-      if (p == 0 || k >> (shift + (p == 2 ? 10 : 11)) == prefix) atomicAdd(hist + (k >> shift & (bins - 1)), 1u);
+      if (p == 0 || k >> (shift + (p == 2 ? 10 : 11)) == prefix) atomicAdd(histS + (k >> shift & (bins - 1)), 1u);
     }
-    if (C > 1) cluster.sync(); else __syncthreads();
-    if (p == 1)                                        // (all have read the first pass's)
-      for (int i = tid; i < EV_BINS; i += EV_THREADS) histS[0][i] = 0;
+    __syncthreads();
     // the bins from the highest down, 4 (or 2) a thread
     constexpr int PER = EV_BINS / EV_THREADS;
-    const int mine = p == 2 ? PER / 2 : PER;
+    const int mine = p == 2 ? PER / 2 : PER, low = bins - mine * (tid + 1);   // bins low .. low + mine - 1
     uint32_t c[PER], sum = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      c[i] = 0;
-      if (i < mine) {
-        const int bin = bins - 1 - (tid * mine + i);
-        if (C == 1) {
-          c[i] = hist[bin];
-        } else {
-          for (int r = 0; r < C; ++r) c[i] += cluster.map_shared_rank(hist, r)[bin];
-        }
+    if (C > 1) {
+      // The cluster's counts of a pass come together in one of its CTAs: few bins are not empty.  (Read from
+      // all CTAs by all, they took 7 us a pass.)
+      uint32_t* const all = cluster.map_shared_rank(sumS, p);
+      for (int i = tid; i < bins; i += EV_THREADS) {
+        const uint32_t x = histS[i];
+        if (x) atomicAdd(all + i, x);
+        histS[i] = 0;
       }
-      sum += c[i];
+      cluster.sync();
+      const uint2 lo2 = *reinterpret_cast<const uint2*>(all + low);
+      c[0] = lo2.x;
+      c[1] = lo2.y;
+      c[2] = c[3] = 0;
+      if (mine == PER) {
+        const uint2 hi2 = *reinterpret_cast<const uint2*>(all + low + 2);
+        c[2] = hi2.x;
+        c[3] = hi2.y;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        c[i] = i < mine ? histS[low + i] : 0;
+        if (i < mine) histS[low + i] = 0;
+      }
     }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) sum += c[i];
     uint32_t pre = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -126,9 +139,9 @@ __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(EvictArgs a) {
     uint32_t above = pre - sum;
     if (above < left && left <= pre) {
 #pragma unroll
-      for (int i = 0; i < PER; ++i) {
+      for (int i = PER - 1; i >= 0; --i) {
         if (above < left && left <= above + c[i]) {
-          foundS[0] = (uint32_t)(bins - 1 - (tid * mine + i));
+          foundS[0] = (uint32_t)(low + i);
           foundS[1] = above;
         }
         above += c[i];
@@ -317,9 +330,9 @@ cudaError_t launch_paged_evict(const Pool& pool, const Batch& b, const PagedEvic
   a.e = e;
   a.err = err;
   const long long rows = (long long)b.n_seq * pool.H, cap = (long long)b.max_pages << pool.page_shift;
-  // CTAs of a row: more than one where the rows alone do not fill the SMs and may be long
-  int C = 1;
-  while (C < 8 && rows * C * 2 <= 2 * sms && cap / C > 4096) C *= 2;
+  // CTAs of a row: more than one where the rows alone do not fill the SMs and may be long (20 rows of up to
+  // 60000 positions: 53 us in all with all CTAs' counts read by each, 29 with the counts brought together)
+  const int C = cap > 32768 && rows * 8 <= 4 * sms ? 8 : cap > 8192 && rows * 4 <= 4 * sms ? 4 : 1;
   a.cached = (int)std::min<long long>((cap + C - 1) / C, EV_CACHED);
   const size_t smem = (size_t)a.cached * 4;
   static std::atomic<unsigned long long> raised{0};
@@ -336,7 +349,7 @@ cudaError_t launch_paged_evict(const Pool& pool, const Batch& b, const PagedEvic
   launch_ex(cfg, at, 1, stream);
   err_ = cudaLaunchKernelEx(&cfg, evict_select_kernel, a);
   if (err_ != cudaSuccess) return err_;
-  const int blocks = (int)std::min<long long>((e.keep + BLK - 1) / BLK, (cap + BLK - 1) / BLK);
+  const int blocks = (int)((std::min<long long>(e.keep, cap) + BLK - 1) / BLK);
   const long long units = rows * blocks;
   cfg.gridDim = dim3((unsigned)((units + MV_WARPS - 1) / MV_WARPS));
   cfg.blockDim = dim3(32 * MV_WARPS);
