@@ -3,9 +3,12 @@
 Per layer: q, k, v projections, ``PagedCache.append`` (rotation and write), ``PagedCache.attend``,
 output projection and residual; no norms and no MLP blocks, as in ``DecodeStack``.  Prompts of
 different lengths come in chunks, other sequences' single tokens among them; then every sequence
-takes one token a step, captured into a CUDA graph.
+takes one token a step, captured into a CUDA graph.  With ``--shared`` all prompts begin with the same
+tokens, which are read once for all of them; with ``--keep`` the weights of positions are added up, and
+the caches cut down to the heaviest ones before the steps.
 
     python examples/paged_stack.py --layers 4 --batch 16 --prompt 2000 --steps 64
+    python examples/paged_stack.py --batch 32 --shared 8192 --prompt 300 --keep 1024
 """
 from __future__ import annotations
 
@@ -36,7 +39,7 @@ class PagedStack:
     """``layers`` layers of random weights; all share one page table, each has its own pages."""
 
     def __init__(self, layers: int, batch: int, hidden: int, n_kv_heads: int, q_per_kv: int, head_dim: int,
-                 max_tokens: int, page: int = 64, seed: int = 0, device="cuda"):
+                 max_tokens: int, page: int = 64, seed: int = 0, device="cuda", weights: bool = False):
         self.H, self.HQ, self.d, self.hidden, self.b = n_kv_heads, n_kv_heads * q_per_kv, head_dim, hidden, batch
         g = torch.Generator(device=device).manual_seed(seed)
 
@@ -52,17 +55,24 @@ class PagedStack:
                                                 workspace=self.caches[0].workspace if self.caches else None))
         self.cos, self.sin = rotation_tables(max_tokens, head_dim, device=device)
         self.graph = None
+        # with `weights`: what each position of each layer and KV head has been given, and room to shed
+        self.mass = [torch.zeros((batch, n_kv_heads, per * page), device=device) for _ in range(layers if weights else 0)]
+        self.groups = (None, None)
 
-    def forward(self, x, starts=None, max_new=None, lse=None):
+    def forward(self, x, starts=None, max_new=None, lse=None, positions=None):
         """Hidden states ``x [tokens][hidden]`` (bf16) of the new tokens through all layers; the
-        table has pages for them, and ``advance`` is the caller's."""
+        table has pages for them, and ``advance`` is the caller's.  ``positions``: where they are not
+        the tokens' places."""
         n, HQ, H, d = x.shape[0], self.HQ, self.H, self.d
-        for W, cache in zip(self.layers, self.caches):
+        table, lens, (groups, prefix) = self.table.dev, self.table.lens, self.groups
+        for i, (W, cache) in enumerate(zip(self.layers, self.caches)):
             qkv = torch.matmul(x, W["Wqkv"]).view(n, HQ + 2 * H, d)
-            q = cache.append(self.table.dev, self.table.lens, qkv[:, :HQ], qkv[:, HQ:HQ + H], qkv[:, HQ + H:],
-                             self.cos, self.sin, starts=starts, max_new=max_new)
-            o, _ = cache.attend(self.table.dev, self.table.lens, q, starts=starts, max_new=max_new,
-                                out_dtype=torch.bfloat16, lse=lse)
+            q = cache.append(table, lens, qkv[:, :HQ], qkv[:, HQ:HQ + H], qkv[:, HQ + H:],
+                             self.cos, self.sin, starts=starts, max_new=max_new, positions=positions)
+            o, l = cache.attend(table, lens, q, starts=starts, max_new=max_new, out_dtype=torch.bfloat16, lse=lse,
+                                want_lse=bool(self.mass), groups=groups, prefix=prefix)
+            if self.mass:
+                cache.weigh(table, lens, q, l, self.mass[i], starts=starts, max_new=max_new)
             x = x + torch.matmul(o.view(n, HQ * d), W["Wo"])
         return x
 
@@ -73,14 +83,43 @@ class PagedStack:
         if x.shape[0] != sum(counts):
             raise ValueError(f"PagedStack.chunk: {x.shape[0]} rows for {sum(counts)} tokens of the open places")
         self.table.grow(new)
-        y = self.forward(x, self.table.starts(new), max(counts))
+        kw = {"positions": self.table.positions(new)} if self.table.held != self.table.seen else {}   # (some were shed)
+        y = self.forward(x, self.table.starts(new), max(counts), **kw)
         self.table.advance(new)
         return y
+
+    def share(self, s: int, places, tokens: int) -> int:
+        """Sequences at ``places`` that begin as the one at s does; what they share is read once from then on
+        (until a place is opened or closed: then ``regroup``).  Weights of shared positions start as what s's tokens have given them so far."""
+        for t in places:
+            n = self.table.share(s, t, tokens)
+            for mass in self.mass:
+                mass[t, :, :n] = mass[s, :, :n]
+        self.regroup()
+        return n
+
+    def _turns(self):
+        """What turns the tokens of a step: not their places once tokens may be shed."""
+        return self.table.pos if self.mass else None
+
+    def regroup(self):
+        self.groups = self.table.groups()
+
+    def shed(self, keep: int, sinks: int = 4, window: int = 64):
+        """Every layer and KV head keeps the ``keep`` positions of every place that got most weight.  A step
+        that was captured before stays good, but with shared prefixes (there are none behind it)."""
+        to = self.table.shrink(keep)
+        for cache, mass in zip(self.caches, self.mass):
+            new = torch.zeros_like(mass)
+            cache.evict(self.table.dev, self.table.lens, mass, to, keep, sinks=sinks, window=window, new_mass=new)
+            mass.copy_(new)
+        self.table.shrunk()
+        self.regroup()
 
     def step(self, x):
         """One more token of every place (an idle one's row passes through the residual only)."""
         self.table.grow(1)
-        y = self.forward(x)
+        y = self.forward(x, positions=self._turns())
         self.table.advance(1)
         return y
 
@@ -93,7 +132,7 @@ class PagedStack:
         with torch.cuda.stream(stream):
             torch.matmul(x_in, self.layers[0]["Wqkv"])          # cuBLAS sets itself up outside a capture only
             with torch.cuda.graph(self.graph, stream=stream):
-                y = self.forward(x_in)
+                y = self.forward(x_in, positions=self._turns())
                 self.table.advance_lens()
         torch.cuda.current_stream().wait_stream(stream)
         return y
@@ -112,16 +151,22 @@ class PagedStack:
 def main():
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     for name, value in (("layers", 4), ("batch", 16), ("hidden", 4096), ("kv-heads", 8), ("q-per-kv", 4),
-                        ("head-dim", 128), ("prompt", 2000), ("chunk", 512), ("steps", 64)):
+                        ("head-dim", 128), ("prompt", 2000), ("chunk", 512), ("steps", 64), ("shared", 0), ("keep", 0)):
         ap.add_argument("--" + name, type=int, default=value)
     a = ap.parse_args()
-    st = PagedStack(a.layers, a.batch, a.hidden, a.kv_heads, a.q_per_kv, a.head_dim, a.prompt + a.steps + 2)
+    st = PagedStack(a.layers, a.batch, a.hidden, a.kv_heads, a.q_per_kv, a.head_dim, a.shared + a.prompt + a.steps + 2,
+                    weights=a.keep > 0)
     g = torch.Generator(device="cuda").manual_seed(1)
     left = [max(1, a.prompt - 37 * s) for s in range(a.batch)]
+    torch.cuda.synchronize()
+    t0, tokens = time.perf_counter(), sum(left) + a.shared
     for s in range(a.batch):
         st.table.open(s)
-    torch.cuda.synchronize()
-    t0, tokens = time.perf_counter(), sum(left)
+    for at in range(0, a.shared, a.chunk):                     # the first place reads what all begin with
+        n = min(a.chunk, a.shared - at)
+        st.chunk(torch.randn((n, a.hidden), generator=g, device="cuda").bfloat16(), [n] + [0] * (a.batch - 1))
+    if a.shared:
+        st.share(0, range(1, a.batch), a.shared)
     while any(left):
         new = [min(a.chunk, k) for k in left]
         st.chunk(torch.randn((sum(new), a.hidden), generator=g, device="cuda").bfloat16(), new)
@@ -129,6 +174,8 @@ def main():
     st.check()
     t1 = time.perf_counter()
     print(f"prompts: {tokens} tokens through {a.layers} layers in {1e3 * (t1 - t0):.1f} ms")
+    if a.keep:
+        st.shed(a.keep)
     x = torch.randn((a.batch, a.hidden), generator=g, device="cuda").bfloat16()
     st.table.grow(a.steps + 1)
     st.capture(x)

@@ -346,17 +346,23 @@ class PagedCache:
 
 
 class PageTable:
-    """Pages of a batch's sequences, handed out on the host: ``dev [n][max_pages]`` and
-    ``lens [n]`` (int32, on the device) are what the caches take.  A place of the batch is idle
-    (length -1) until ``open``."""
+    """Pages of a batch's sequences, handed out on the host: ``dev [n][max_pages]``, ``lens [n]``
+    and ``pos [n]`` (int32, on the device; tokens held, and the position of the next one, which is the
+    same until tokens are shed) are what the caches take.  A place of the batch is idle (length -1)
+    until ``open``.  Sequences can share the pages that they begin with (``share``); a page is free
+    again when the last of them has given it back."""
 
     def __init__(self, n_seq: int, max_pages: int, n_pages: int, page: int = 64, device="cuda"):
         self.page, self.max_pages = page, max_pages
         self.held: List[int] = [-1] * n_seq
+        self.seen: List[int] = [-1] * n_seq                # tokens since open, shed ones among them
         self.pages: List[List[int]] = [[] for _ in range(n_seq)]
+        self.users: List[int] = [0] * n_pages
         self.free: List[int] = list(range(n_pages - 1, -1, -1))
         self.dev = torch.full((n_seq, max_pages), -1, dtype=torch.int32, device=device)
         self.lens = torch.full((n_seq,), -1, dtype=torch.int32, device=device)
+        self.pos = torch.full((n_seq,), -1, dtype=torch.int32, device=device)
+        self._shrink: Optional[List[List[int]]] = None     # pages that ``shrink`` handed out
 
     def counts(self, new) -> List[int]:
         """Tokens of every place (``new``: a number, or one for each place): none of idle ones, which
@@ -367,23 +373,91 @@ class PageTable:
             raise ValueError(f"PageTable: {len(counts)} token counts for {n} places, none below 0")
         return [c if h >= 0 else 0 for c, h in zip(counts, self.held)]
 
+    def _take(self) -> int:
+        page = self.free.pop()
+        self.users[page] = 1
+        return page
+
+    def _give(self, pages: Sequence[int]):
+        for page in reversed(pages):
+            self.users[page] -= 1
+            if self.users[page] == 0:
+                self.free.append(page)
+
+    def _settled(self, what):
+        if self._shrink is not None:
+            raise ValueError(f"PageTable.{what}: tokens are being shed (shrink without shrunk)")
+
     def open(self, s: int):
         """A new sequence at place s."""
         self.close(s)
-        self.held[s] = 0
+        self.held[s] = self.seen[s] = 0
         self.lens[s] = 0
+        self.pos[s] = 0
 
     def close(self, s: int):
         """Gives place s's pages back and leaves it idle."""
-        self.free.extend(reversed(self.pages[s]))
+        self._settled("close")
+        self._give(self.pages[s])
         self.pages[s] = []
-        self.held[s] = -1
+        self.held[s] = self.seen[s] = -1
         self.lens[s] = -1
+        self.pos[s] = -1
         self.dev[s] = -1
+
+    def share(self, s: int, t: int, tokens: int) -> int:
+        """A sequence at place t that begins with the first ``tokens`` tokens of the one at s, as far as they
+        fill whole pages, which both then read.  Returns their number.  (Not of one that has shed tokens:
+        its heads hold different ones.)"""
+        self._settled("share")
+        if s == t or self.held[s] < 0 or tokens < 0:
+            raise ValueError(f"PageTable.share: {tokens} tokens of place {s} (holds {self.held[s]}) for place {t}")
+        if self.held[s] != self.seen[s]:
+            raise ValueError(f"PageTable.share: place {s} has shed {self.seen[s] - self.held[s]} of its tokens")
+        self.close(t)
+        k = min(tokens, self.held[s]) // self.page
+        self.pages[t] = self.pages[s][:k]
+        for page in self.pages[t]:
+            self.users[page] += 1
+        self.held[t] = self.seen[t] = k * self.page
+        if k:
+            self.dev[t, :k] = self.dev[s, :k]
+        self.lens[t] = k * self.page
+        self.pos[t] = k * self.page
+        return k * self.page
+
+    def groups(self):
+        """(groups, prefix) for ``PagedCache.attend``: runs of places whose sequences begin with the same
+        pages.  (None, None) where none do."""
+        runs, i, n = [], 0, len(self.held)
+        while i < n:
+            common, live, end = self.pages[i][:max(self.held[i], 0) // self.page], 1, i + 1
+            for j in range(i + 1, n if common else 0):
+                if self.held[j] < 0:
+                    continue                               # (an idle place within a run does not matter)
+                other = self.pages[j][:self.held[j] // self.page]
+                k = next((m for m, (a, b) in enumerate(zip(common, other)) if a != b), min(len(common), len(other)))
+                if live * k < (live - 1) * len(common) or k == 0:
+                    break                                  # (fewer pages for more sequences would be read more often)
+                common, live, end = common[:k], live + 1, j + 1
+            runs.append((i, end, len(common) * self.page if live > 1 else 0))
+            i = end
+        if not any(p for _, _, p in runs):
+            return None, None
+        first, prefix = [0], []
+        for k, (_, end, p) in enumerate(runs):
+            if p == 0 and prefix and prefix[-1] == 0:
+                first[-1] = end                            # (places that share nothing, together)
+            else:
+                first.append(end)
+                prefix.append(p)
+        dev = self.dev.device
+        return torch.tensor(first, dtype=torch.int32, device=dev), torch.tensor(prefix, dtype=torch.int32, device=dev)
 
     def grow(self, new):
         """Pages for ``new`` more tokens of every sequence (a number, or one for each place); none
         are handed out when they do not suffice (MemoryError)."""
+        self._settled("grow")
         counts = self.counts(new)
         need = [max(0, -(-(max(h, 0) + c) // self.page) - len(p)) for h, c, p in zip(self.held, counts, self.pages)]
         if any(len(p) + k > self.max_pages for p, k in zip(self.pages, need)):
@@ -394,29 +468,71 @@ class PageTable:
         for s, k in enumerate(need):
             for _ in range(k):
                 where.append((s, len(self.pages[s])))
-                ids.append(self.free.pop())
+                ids.append(self._take())
                 self.pages[s].append(ids[-1])
         if ids:
             at = torch.tensor(where, dtype=torch.int64, device=self.dev.device)
             self.dev[at[:, 0], at[:, 1]] = torch.tensor(ids, dtype=torch.int32, device=self.dev.device)
 
+    def shrink(self, keep: int) -> torch.Tensor:
+        """New pages for at most ``keep`` tokens of every open place, as the table that ``PagedCache.evict`` of
+        every layer writes to; ``shrunk`` then makes it the table.  MemoryError when they do not suffice.  (Asked
+        again before that, the earlier ones are given back.)"""
+        if keep < 1:
+            raise ValueError(f"PageTable.shrink: {keep} tokens")
+        self._drop_shrink()
+        need = [-(-min(max(h, 0), keep) // self.page) for h in self.held]
+        if sum(need) > len(self.free):
+            raise MemoryError(f"PageTable: {sum(need)} pages wanted, {len(self.free)} free")
+        width = -(-keep // self.page)
+        self._shrink = [[self._take() for _ in range(k)] for k in need]
+        self._keep = keep
+        rows = [p + [-1] * (width - len(p)) for p in self._shrink]
+        return torch.tensor(rows, dtype=torch.int32, device=self.dev.device)
+
+    def _drop_shrink(self):
+        for pages in self._shrink or []:
+            self._give(pages)
+        self._shrink = None
+
+    def shrunk(self):
+        """Every layer has written its tokens to the pages of ``shrink``: the others are given back."""
+        if self._shrink is None:
+            raise ValueError("PageTable.shrunk: no shrink before it")
+        new, self._shrink = self._shrink, None
+        for s, pages in enumerate(new):
+            self._give(self.pages[s])
+            self.pages[s] = pages
+            self.held[s] = min(self.held[s], self._keep)
+        rows = [p + [-1] * (self.max_pages - len(p)) for p in self.pages]
+        self.dev.copy_(torch.tensor(rows, dtype=torch.int32))
+        self.lens.copy_(torch.tensor(self.held, dtype=torch.int32))
+
     def advance_lens(self):
         """One more token of every open place, on the device alone: what a captured step ends with
         (``advance_held`` then tells the host at each replay)."""
-        self.lens += (self.lens >= 0).to(torch.int32)
+        live = (self.lens >= 0).to(torch.int32)
+        self.lens += live
+        self.pos += live
 
     def advance_held(self, new):
         """The host's part of ``advance``, for tokens by which a replayed graph moved ``lens``."""
-        self.held = [h + c if h >= 0 else h for h, c in zip(self.held, self.counts(new))]
+        counts = self.counts(new)
+        self.held = [h + c if h >= 0 else h for h, c in zip(self.held, counts)]
+        self.seen = [h + c if h >= 0 else h for h, c in zip(self.seen, counts)]
 
     def advance(self, new):
         """The new tokens are in every layer's cache."""
+        self._settled("advance")
         counts = self.counts(new)
         self.advance_held(counts)
         if len(set(counts)) == 1 and min(self.held) >= 0:
             self.lens += counts[0]
+            self.pos += counts[0]
         else:
-            self.lens += torch.tensor(counts, dtype=torch.int32, device=self.lens.device)
+            more = torch.tensor(counts, dtype=torch.int32, device=self.lens.device)
+            self.lens += more
+            self.pos += more
 
     def starts(self, new: Sequence[int]) -> torch.Tensor:
         """First token of every place, for the calls' ``starts``: the rows of the open places, one
@@ -424,4 +540,10 @@ class PageTable:
         at = [0]
         for c in self.counts(new):
             at.append(at[-1] + c)
+        return torch.tensor(at, dtype=torch.int32, device=self.dev.device)
+
+    def positions(self, new: Sequence[int]) -> torch.Tensor:
+        """Positions of the coming tokens, rows as those of ``starts`` (with one token of every place they
+        are ``pos``)."""
+        at = [h + i for h, c in zip(self.seen, self.counts(new)) for i in range(c)]
         return torch.tensor(at, dtype=torch.int32, device=self.dev.device)
