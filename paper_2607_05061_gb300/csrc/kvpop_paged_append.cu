@@ -153,6 +153,48 @@ __device__ __forceinline__ Turn turn_at(const AppendArgs& a, const Lane& n, cons
     for (int i = 0; i < 8; ++i) t.sn[i] = -t.sn[i];
   return t;
 }
+// The same by the rows of the tables that its two groups of 4 pairs turn by.
+__device__ __forceinline__ Turn turn_by(const AppendArgs& a, const Lane& n, int r0, int r1) {
+  Turn t;
+  if (!n.turned) return t;
+  const long long half = a.rot >> 1, o0 = r0 * half + n.angle, o1 = r1 * half + n.angle + (a.interleaved ? 0 : 4);
+  Raw<float> cs, sn;
+  cs.a = ld16f(a.cosT + o0);
+  cs.b = ld16f(a.cosT + o1);
+  sn.a = ld16f(a.sinT + o0);
+  sn.b = ld16f(a.sinT + o1);
+  cs.get(t.cs);
+  sn.get(t.sn);
+  if (n.low && !a.interleaved)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t.sn[i] = -t.sn[i];
+  return t;
+}
+// The positions of a block's (at most 16) new tokens, two of up to 64 a lane.  Read where they are used, each
+// was waited for before its cosines could be asked for (14500 image tokens 77 us).
+struct Places {
+  int v[2];
+  unsigned bad[2];                                  // which of them lie outside the tables
+  __device__ __forceinline__ void load(const AppendArgs& a, long long tok, int rows, int lane) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int i = lane + 32 * e;
+      v[e] = i < rows * a.n_axes ? a.at[tok * a.n_axes + i] : 0;
+      bad[e] = __ballot_sync(0xffffffffu, (unsigned)v[e] >= (unsigned)a.max_pos);
+    }
+    if (bad[0] | bad[1]) report(a.err, ERR_ROTATION);
+  }
+  // (by all lanes)
+  __device__ __forceinline__ int of(const AppendArgs& a, int row, int axis) const {
+    const int i = row * a.n_axes + axis;
+    const int x = __shfl_sync(0xffffffffu, v[0], i & 31), y = __shfl_sync(0xffffffffu, v[1], i & 31);
+    return i < 32 ? x : y;
+  }
+  __device__ __forceinline__ bool ok(const AppendArgs& a, int row) const {
+    const unsigned long long all = (unsigned long long)bad[1] << 32 | bad[0];
+    return (all >> (row * a.n_axes & 63) & ((1u << a.n_axes) - 1u)) == 0;
+  }
+};
 // Whether all of a token's positions are in the tables.
 __device__ __forceinline__ bool in_tables(const AppendArgs& a, const int32_t* at) {
   bool ok = true;
@@ -255,6 +297,18 @@ __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendAr
   if (AT && ONE && p0 < end && !in_tables(a, a.at + (long long)t.first * a.n_axes)) end = p0;
   const bool some = p0 < end;
   if (!ONE && !some) return;                        // warp-uniform
+  Places places;
+  if (AT && !ONE) places.load(a, t.first + (p0 - t.len), end - p0, lane);
+  // what turns row `it` of the lane: two rows of the tables, or, where 4 pairs are of several axes, all of them
+  struct Axes {
+    int a0, a1;
+    bool mixed;
+  };
+  auto axes_of = [&](const Lane& n) {
+    const uint32_t x = a.axes[n.angle >> 2 & 15], y = a.axes[(n.angle >> 2) + 1 & 15];
+    return Axes{(int)(x & 255), (int)((a.interleaved ? x : y) & 255),
+                x != (x & 255) * 0x01010101u || (!a.interleaved && y != (y & 255) * 0x01010101u)};
+  };
 
   if (slot >= 2 * a.pool.H) {                       // ------------------------------ queries
     const int h0 = (slot - 2 * a.pool.H) * QH;
@@ -266,11 +320,18 @@ __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendAr
     const float* sinR = AT ? nullptr : a.sinT + (cosR - a.cosT);
     bf16* to = a.q_out + (tok * a.HQ + h0) * D + n.own;
     if (!ONE) ahead<T, IT, RPI, QH>(from + n.own, a.q_ts, a.q_hs, min(a.HQ - h0, QH), end - pos, c);
+    const Axes ax = AT && !ONE ? axes_of(n) : Axes{};
 #pragma unroll 1
     for (int it = 0; it < IT; ++it) {
       const int32_t* at = AT ? a.at + (t.first + (pos - t.len)) * (long long)a.n_axes : nullptr;
-      if (pos < end && (!AT || ONE || in_tables(a, at))) {
-        const Turn turn = AT ? turn_at(a, n, at) : turn_of(a, n, cosR, sinR);
+      int r0 = 0, r1 = 0;
+      if (AT && !ONE) {
+        const int row = min(pos, end - 1) - p0;
+        r0 = places.of(a, row, ax.a0);
+        r1 = places.of(a, row, ax.a1);
+      }
+      if (pos < end && (!AT || ONE || places.ok(a, pos - p0))) {
+        const Turn turn = !AT ? turn_of(a, n, cosR, sinR) : ONE || ax.mixed ? turn_at(a, n, at) : turn_by(a, n, r0, r1);
         Raw<T> own[QH], other[QH];
 #pragma unroll
         for (int e = 0; e < QH; ++e) {
@@ -320,24 +381,31 @@ __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendAr
   const long long angle0 = (long long)pos0 * (a.rot >> 1) + n.angle;
   if (!ONE && id >= 0) ahead<T, IT, RPI, 1>(from + n.own, ts, 0, 1, end - pos0, c);
   const int32_t* const at0 = AT ? a.at + (t.first + (pos0 - t.len)) * (long long)a.n_axes : nullptr;
-  uint32_t ok = 0;                                  // AT: the lane's rows whose positions are in the tables
-  if (AT && id >= 0)
-#pragma unroll
-    for (int it = 0; it < IT; ++it)
-      if (pos0 + it * RPI < end && (ONE || in_tables(a, at0 + (long long)it * RPI * a.n_axes))) ok |= 1u << it;
-  auto taken = [&](int it) { return AT ? (ok >> it & 1u) != 0 : pos0 + it * RPI < end; };
-  auto read = [&](int it, float (&x)[8]) {
+  const Axes ax = AT && !ONE ? axes_of(n) : Axes{};
+  auto taken = [&](int it) {
+    return pos0 + it * RPI < end && (!AT || ONE || places.ok(a, pos0 + it * RPI - p0));
+  };
+  auto turns = [&](int it, int& r0, int& r1) {      // (by all lanes, before the rows that are none are passed over)
+    r0 = r1 = 0;
+    if (AT && !ONE && !is_v) {
+      const int row = min(pos0 + it * RPI, end - 1) - p0;
+      r0 = places.of(a, row, ax.a0);
+      r1 = places.of(a, row, ax.a1);
+    }
+  };
+  auto read = [&](int it, int r0, int r1, float (&x)[8]) {
     const T* row = from + it * RPI * ts;
     const long long at = angle0 + it * RPI * (a.rot >> 1);
     Raw<T> own, other;
     own.load(row + n.own);
     other.load(row + n.other);
-    rotated(a, n, AT ? turn_at(a, n, at0 + (long long)it * RPI * a.n_axes) : turn_of(a, n, a.cosT + at, a.sinT + at),
+    rotated(a, n, !AT ? turn_of(a, n, a.cosT + at, a.sinT + at)
+                  : ONE || ax.mixed ? turn_at(a, n, at0 + (long long)it * RPI * a.n_axes) : turn_by(a, n, r0, r1),
             own, other, x);
   };
-  auto value = [&](int it, float (&x)[8], bool again) {
+  auto value = [&](int it, int r0, int r1, float (&x)[8], bool again) {
     if (!KEEP || !again) {
-      read(it, x);
+      read(it, r0, r1, x);
     } else {
       const float4 u = keepS[threadIdx.x >> 5][2 * it][lane], w = keepS[threadIdx.x >> 5][2 * it + 1][lane];
       x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
@@ -348,10 +416,12 @@ __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendAr
     float m = 0.f;
     if (id >= 0)
 #pragma unroll 2
-      for (int it = 0; it < IT; ++it)
+      for (int it = 0; it < IT; ++it) {
+        int r0, r1;
+        turns(it, r0, r1);
         if (taken(it)) {
           float x[8];
-          value(it, x, limit > 0.f);
+          value(it, r0, r1, x, limit > 0.f);
           if (KEEP && limit == 0.f) {
             keepS[threadIdx.x >> 5][2 * it][lane] = make_float4(x[0], x[1], x[2], x[3]);
             keepS[threadIdx.x >> 5][2 * it + 1][lane] = make_float4(x[4], x[5], x[6], x[7]);
@@ -359,6 +429,7 @@ __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendAr
 #pragma unroll
           for (int i = 0; i < 8; ++i) m = fmaxf(m, limit > 0.f && !(fabsf(x[i]) < limit) ? 0.f : fabsf(x[i]));
         }
+      }
 #pragma unroll
     for (int o = ONE ? LPR / 2 : 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     return m;
@@ -387,12 +458,15 @@ __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendAr
   const float inv = 1.f / sc;                       // exact: sc is a power of two
   unsigned char* to = rows + (head + (pos0 - p0)) * D + n.own;
 #pragma unroll 2
-  for (int it = 0; it < IT; ++it)
+  for (int it = 0; it < IT; ++it) {
+    int r0, r1;
+    turns(it, r0, r1);
     if (taken(it)) {
       float x[8];
-      value(it, x, true);
+      value(it, r0, r1, x, true);
       *reinterpret_cast<uint2*>(to + it * RPI * D) = codes8(x, inv, special);
     }
+  }
   if (lane == lead) *scale = sc;
 }
 

@@ -542,6 +542,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) paged_weigh_tc_kernel(WeighTcAr
         first = t.b0;
       }
     }
+    cp_wait<0>();
   }
   fence_before();
   __syncthreads();
