@@ -11,8 +11,9 @@
 // All (tile, block) pairs form one list, tile after tile, that is cut evenly over the SMs; a tile that
 // lies in several CTAs' parts is added up, in their order, by the CTA that arrives last, at its end.
 // Roles:
-//  * 8 softmax warps, which also bring the next tile's positions into the other half of the
-//    operand's tensor memory (their bytes are on their way two tiles before, their pages three);
+//  * 8 softmax warps;
+//  * 4 warps that bring the positions of the tiles to come into the other half of the operand's tensor
+//    memory: their pages two tiles before, their bytes one;
 //  * 1 MMA warp: S = K Q^T (M 128, N 128, K d) per half of the tile, one buffer a half;
 //  * 3 producer warps: query rows by 16-byte cp.async into 128B-swizzled slots, with lse and the last
 //    position that each row sees beside them.  Where all of a sequence's rows fit the slots they stay
@@ -33,7 +34,9 @@ using namespace tc05;
 
 constexpr int WT_HALF = 128, WT_KEYS = 256, WT_BN = 128;
 constexpr int WT_SOFT = 8, WT_MMA_WARP = WT_SOFT, WT_COPY_WARP = WT_SOFT + 1, WT_COPY = 3;
-constexpr int WT_THREADS = 32 * (WT_COPY_WARP + WT_COPY);
+constexpr int WT_KEY_WARP = WT_COPY_WARP + WT_COPY, WT_KEY = 4;
+constexpr int WT_THREADS = 32 * (WT_KEY_WARP + WT_KEY);
+constexpr int WT_OLD = 8;                                // tiles whose scales and weights so far are held
 constexpr int WT_WHOLE = 8;                              // tiles of up to that many blocks are not cut
 #ifndef WT_ENDS
 #define WT_ENDS 4
@@ -64,10 +67,10 @@ struct WL {
   static constexpr int OFF_RAW = (OFF_FLAG + ST * 4 + 15) / 16 * 16;   // [2] bytes of tiles to come, a thread's pieces apart
   // a thread's page of a tile to come, and scale and weight so far of tiles there and to come: in registers
   // they were spilled, and a load that is spilled is waited for
-  static constexpr int OFF_ID = OFF_RAW + 2 * WT_KEYS * D, OFF_SC = OFF_ID + 2 * WT_KEYS * 4, OFF_OLD = OFF_SC + 4 * WT_KEYS * 4;
-  static constexpr int OFF_BAR = OFF_OLD + 4 * WT_KEYS * 4;
-  static constexpr int FULL = 0, EMPTY = ST, SFULL = 2 * ST, PFULL = SFULL + 2, AFULL = PFULL + 2,
-                       END = AFULL + 2, N_BAR = END + 1;
+  static constexpr int OFF_ID = OFF_RAW + 2 * WT_KEYS * D, OFF_SC = OFF_ID + 2 * WT_KEYS * 4, OFF_OLD = OFF_SC + WT_OLD * WT_KEYS * 4;
+  static constexpr int OFF_BAR = OFF_OLD + WT_OLD * WT_KEYS * 4;
+  static constexpr int FULL = 0, EMPTY = ST, SFULL = 2 * ST, PFULL = SFULL + 2, AFULL = PFULL + 2, AEMPTY = AFULL + 2,
+                       END = AEMPTY + 2, N_BAR = END + 1;
   static constexpr int OFF_TMEM = OFF_BAR + 8 * N_BAR, BYTES = OFF_TMEM + 16;
   static_assert(ST <= WT_WHOLE, "");
 };
@@ -172,7 +175,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) paged_weigh_tc_kernel(WeighTcAr
   using L = WL<D>;
   constexpr int ST = L::ST, RAW = D / 16;                // 16-byte pieces of a row
   extern __shared__ __align__(1024) unsigned char smt[];
-  __shared__ Tile edgeS[2], aheadS[WT_SOFT];
+  __shared__ Tile edgeS[2], aheadS[WT_KEY];
   __shared__ long long edgeW[2], shareS;
   __shared__ int lastS;
   const uint32_t sb = smem_u32(smt);
@@ -215,7 +218,8 @@ __global__ void __launch_bounds__(WT_THREADS, 1) paged_weigh_tc_kernel(WeighTcAr
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar(L::SFULL + i), 1);
       mbar_init(bar(L::PFULL + i), WT_SOFT / 2);
-      mbar_init(bar(L::AFULL + i), WT_SOFT);
+      mbar_init(bar(L::AFULL + i), WT_KEY);
+      mbar_init(bar(L::AEMPTY + i), 1);
     }
     mbar_init(bar(L::END), 1);
     mbar_fence_init();
@@ -240,7 +244,115 @@ __global__ void __launch_bounds__(WT_THREADS, 1) paged_weigh_tc_kernel(WeighTcAr
   uint32_t pos = 0;
   bool ok = true;
 
-  if (warp >= WT_COPY_WARP) {
+  if (warp >= WT_KEY_WARP) {
+    // ---------------------------------------------------------------- positions
+    // Tiles by their number j: the pages of j + 2, the bytes of j + 1, and tile j into the operand.  A
+    // thread: rows `lane` of the warp's 32 in either half, whose pages, scales and weights so far it asks
+    // for; their bytes the warp copies as whole lines.
+    const int kw = warp - WT_KEY_WARP;
+    const uint32_t tl = tmem + ((uint32_t)(kw * 32) << 16);
+    if (lane == 0) aheadS[kw] = t;
+    __syncwarp();
+    int pos_of[2] = {-1, -1}, head_of = 0;               // of the tile whose pages are on their way
+    const float* old_of = nullptr;                       // weight so far of position 0 of its head
+    int old_len = 0;
+    auto mine = [&](int off, int n, int hh) { return reinterpret_cast<float*>(smt + off) + n * WT_KEYS + hh * WT_HALF + kw * 32 + lane; };
+    auto look = [&](int j) {
+      pos_of[0] = pos_of[1] = -1;
+      Tile ahead = aheadS[kw];
+      if (!ahead.valid()) return;
+      head_of = ahead.h;
+      old_of = a.mass + ((long long)ahead.s * H + ahead.h) * a.positions;
+      old_len = ahead.x.len;
+      const int32_t* const row = a.b.table + (long long)ahead.s * a.b.table_stride;
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh) {
+        const int at = ahead.kt * WT_KEYS + hh * WT_HALF + kw * 32 + lane;
+        if (at < ahead.x.ctx) {
+          pos_of[hh] = at;
+          cp_async4(smem_u32(mine(L::OFF_ID, j & 1, hh)), row + (at >> a.pool.page_shift));
+        }
+      }
+      advance(a, ahead);
+      __syncwarp();
+      if (lane == 0) aheadS[kw] = ahead;
+      __syncwarp();
+    };
+    // chunk c of row r lies at chunk c ^ r of the row's 128 (64) bytes
+    auto chunk_of = [&](int row, int c) { return row * D + ((c ^ (row & (RAW - 1))) << 4); };
+    auto fetch = [&](int j) {                            // (the pages are there)
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh) {
+        int id = -1;
+        if (pos_of[hh] >= 0) {
+          id = __float_as_int(*mine(L::OFF_ID, j & 1, hh));
+          if ((unsigned)id >= (unsigned)a.pool.n_pages) {
+            report(a.err, ERR_PAGE);
+            id = -1;
+          }
+        }
+        const long long at = id < 0 ? -1 : ((long long)id * H + head_of) * a.pool.page + (pos_of[hh] & (a.pool.page - 1));
+        const uint32_t dst = sb + L::OFF_RAW + (j & 1) * (WT_KEYS * D) + (hh * WT_HALF + kw * 32) * D;
+#pragma unroll
+        for (int i = 0; i < RAW; ++i) {
+          const int row = i * (32 / RAW) + lane / RAW, c = lane % RAW;
+          const long long o = __shfl_sync(0xffffffffu, at, row);
+          cp_async16(dst + chunk_of(row, c), a.pool.k + (o < 0 ? 0 : o) * D + 16 * c, o < 0 ? 0 : 16);
+        }
+        if (id >= 0) cp_async4(smem_u32(mine(L::OFF_SC, j % WT_OLD, hh)), a.pool.ks + at / BLK);
+        else *mine(L::OFF_SC, j % WT_OLD, hh) = 0.f;
+        if (pos_of[hh] >= 0 && pos_of[hh] < old_len) cp_async4(smem_u32(mine(L::OFF_OLD, j % WT_OLD, hh)), old_of + pos_of[hh]);
+        else *mine(L::OFF_OLD, j % WT_OLD, hh) = 0.f;
+      }
+    };
+    auto store = [&](int buf) {
+      __syncwarp();
+#pragma unroll 1
+      for (int hh = 0; hh < 2; ++hh) {
+        const unsigned char* const raw = smt + L::OFF_RAW + buf * (WT_KEYS * D) + (hh * WT_HALF + kw * 32) * D;
+#pragma unroll
+        for (int c = 0; c < RAW; c += 2) {
+          float w[16];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint4 v = *reinterpret_cast<const uint4*>(raw + chunk_of(lane, c + i));
+            const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              uint32_t lo, hi;
+              cvt4(u[k], lo, hi);
+              const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&lo));
+              const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+              w[8 * i + 2 * k] = __uint_as_float(pack_bf16(x.x, x.y));
+              w[8 * i + 2 * k + 1] = __uint_as_float(pack_bf16(y.x, y.y));
+            }
+          }
+          tmem_st16(tl + 256 + buf * D + hh * (D / 2) + 8 * c, w);
+        }
+      }
+      tmem_wait_st();
+      fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(L::AFULL + buf));
+    };
+    look(0);
+    cp_commit();
+    cp_wait<0>();
+    fetch(0);
+    look(1);
+    cp_commit();
+    for (int j = 0; t.valid() && ok; ++j) {
+      cp_wait<0>();
+      fetch(j + 1);                                      // (the bytes before them are in the operand)
+      look(j + 2);
+      cp_commit();
+      if (j >= 2 && !(ok = wait(L::AEMPTY + (j & 1), (j / 2 - 1) & 1))) break;
+      fence_after();
+      store(j & 1);
+      advance(a, t);
+    }
+    cp_wait<0>();
+  } else if (warp >= WT_COPY_WARP) {
     // ---------------------------------------------------------------- query rows
     // The warps take groups of 32 rows in turn.  A group's addresses and normalisers are asked for one
     // group ahead.
@@ -338,6 +450,8 @@ __global__ void __launch_bounds__(WT_THREADS, 1) paged_weigh_tc_kernel(WeighTcAr
         }
         if (!stay) ++pos;
       }
+      if (lead) commit(bar(L::AEMPTY + (i & 1)));
+      __syncwarp();
       const Tile was = t;
       advance(a, t);
       if (!t.valid() || !t.same_head(was)) {
@@ -363,101 +477,14 @@ __global__ void __launch_bounds__(WT_THREADS, 1) paged_weigh_tc_kernel(WeighTcAr
     const float* const nlS = reinterpret_cast<const float*>(smt + L::OFF_NL);
     const int* const limS = reinterpret_cast<const int*>(smt + L::OFF_LIM);
     const int* const flagS = reinterpret_cast<const int*>(smt + L::OFF_FLAG);
-    // Tiles to come, by their number: the page of j + 3, the bytes of j + 2 and of j + 1.
-    if (lane == 0) aheadS[warp] = t;
-    __syncwarp();
-    int pos_of = -1, head_of = 0;                        // of the tile whose page is on its way: the thread's position,
-    const float* old_of = nullptr;                       // head and weight so far
-    auto mine = [&](int off, int n) { return reinterpret_cast<float*>(smt + off) + n * WT_KEYS + r; };
-    auto look = [&](int j) {                             // the page of the row in `ahead`
-      pos_of = -1;
-      old_of = nullptr;
-      Tile ahead = aheadS[warp];
-      if (!ahead.valid()) return;
-      const int at = ahead.kt * WT_KEYS + r;
-      if (at < ahead.x.ctx) {
-        pos_of = at;
-        head_of = ahead.h;
-        if (at < ahead.x.len) old_of = a.mass + ((long long)ahead.s * H + ahead.h) * a.positions + at;
-        cp_async4(smem_u32(mine(L::OFF_ID, j & 1)), a.b.table + (long long)ahead.s * a.b.table_stride + (at >> a.pool.page_shift));
-      }
-      advance(a, ahead);
-      __syncwarp();
-      if (lane == 0) aheadS[warp] = ahead;
-      __syncwarp();
-    };
-    // A warp copies its 32 rows as whole lines (a row a lane, each copy touches 32 of them: 2200 clocks a
-    // tile); chunk c of row r lies at chunk c ^ r of the row's 128 (64) bytes.
-    unsigned char* const rawS = smt + L::OFF_RAW + warp * (32 * D);
-    auto chunk_of = [&](int row, int c) { return row * D + ((c ^ (row & (RAW - 1))) << 4); };
-    auto fetch = [&](int j) {                            // its bytes (the page is there)
-      int id = -1;
-      if (pos_of >= 0) {
-        id = __float_as_int(*mine(L::OFF_ID, j & 1));
-        if ((unsigned)id >= (unsigned)a.pool.n_pages) {
-          report(a.err, ERR_PAGE);
-          id = -1;
-        }
-      }
-      const long long at = id < 0 ? -1 : ((long long)id * H + head_of) * a.pool.page + (pos_of & (a.pool.page - 1));
-      const uint32_t dst = smem_u32(rawS) + (j & 1) * (WT_KEYS * D);
-#pragma unroll
-      for (int i = 0; i < RAW; ++i) {
-        const int row = i * (32 / RAW) + lane / RAW, c = lane % RAW;
-        const long long o = __shfl_sync(0xffffffffu, at, row);
-        cp_async16(dst + chunk_of(row, c), a.pool.k + (o < 0 ? 0 : o) * D + 16 * c, o < 0 ? 0 : 16);
-      }
-      if (id >= 0) cp_async4(smem_u32(mine(L::OFF_SC, j & 3)), a.pool.ks + at / BLK);
-      else *mine(L::OFF_SC, j & 3) = 0.f;
-      if (old_of) cp_async4(smem_u32(mine(L::OFF_OLD, j & 3)), old_of);
-      else *mine(L::OFF_OLD, j & 3) = 0.f;
-    };
-    auto store = [&](int buf) {                          // into the operand
-      __syncwarp();
-#pragma unroll
-      for (int c = 0; c < RAW; c += 2) {
-        float w[16];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint4 v = *reinterpret_cast<const uint4*>(rawS + buf * (WT_KEYS * D) + chunk_of(lane, c + i));
-          const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            uint32_t lo, hi;
-            cvt4(u[k], lo, hi);
-            const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&lo));
-            const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-            w[8 * i + 2 * k] = __uint_as_float(pack_bf16(x.x, x.y));
-            w[8 * i + 2 * k + 1] = __uint_as_float(pack_bf16(y.x, y.y));
-          }
-        }
-        tmem_st16(tl + 256 + buf * D + hh * (D / 2) + 8 * c, w);
-      }
-      tmem_wait_st();
-      fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(L::AFULL + buf));
-    };
-    look(0);
-    cp_commit();
-#pragma unroll 1
-    for (int j = 0; j < 2; ++j) {
-      cp_wait<0>();
-      fetch(j);
-      look(j + 1);
-      cp_commit();
-    }
-    cp_wait<1>();
-    if (t.valid()) store(0);
     uint32_t step = 0;
     int first = t.b0;
     for (uint32_t i = 0; t.valid() && ok; ++i) {
-      cp_wait<0>();                                      // (asked for a tile ago)
-      const float scale = *mine(L::OFF_SC, i & 3);       // 0: no position, or a bad page
+      if (!(ok = wait(L::AFULL + (i & 1), i >> 1 & 1))) break;
+      const float* const of = reinterpret_cast<const float*>(smt) + (i % WT_OLD) * WT_KEYS + r;
+      const float scale = of[L::OFF_SC / 4];             // 0: no position, or a bad page
+      const float before = of[L::OFF_OLD / 4];
       const uint64_t cc = f2_pack(a.c * scale, a.c * scale);
-      fetch(i + 2);                                      // (that buffer's bytes are in the operand)
-      look(i + 3);
-      cp_commit();
       const int t0 = t.kt * WT_KEYS, tp = t0 + r, t1 = min(t0 + WT_KEYS, t.x.ctx) - 1;
       // blocks from here on have rows that see the whole tile: tokens from t1 - len on
       const int all_see = t1 <= t.x.len ? 0 : (int)(((long long)(t1 - t.x.len) * G + WT_BN - 1) / WT_BN);
@@ -470,24 +497,19 @@ __global__ void __launch_bounds__(WT_THREADS, 1) paged_weigh_tc_kernel(WeighTcAr
         const int st = p % ST;
         if (!(ok = wait(L::FULL + st, p / ST & 1) && wait(L::SFULL + hh, step & 1))) break;
         fence_after();
-        // (all products of the tile before are done: the other operand is free)
-        if (b == t.b1 - 1 && t.at + (t.x.blocks - t.b0 + WT_ENDS) < t.end) store((i + 1) & 1);
         const bool edge = b < all_see || flagS[st] != 0;
         uint64_t s0 = 0ull, s1 = 0ull;
         const uint32_t tS = tl + hh * 128;
         const float4* const nl = reinterpret_cast<const float4*>(nlS + st * WT_BN);
         const int4* const lim = reinterpret_cast<const int4*>(limS + st * WT_BN);
-        float v[4][32];
+        // two groups of 32 columns are on their way while a third is worked on
+        float v[3][32];
         tmem_ld32(tS, v[0]);
         tmem_ld32(tS + 32, v[1]);
-        tmem_ld32(tS + 64, v[2]);
-        tmem_ld32(tS + 96, v[3]);
         tmem_wait_ld();
-        fence_before();                                  // the logits are in registers
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(L::PFULL + hh));
+        tmem_ld32(tS + 64, v[2]);
         auto columns = [&](auto at_edge, int u) {
-          float (&w)[32] = v[u];
+          float (&w)[32] = v[u % 3];
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
             const float4 n4 = nl[8 * u + k];
@@ -505,13 +527,18 @@ __global__ void __launch_bounds__(WT_THREADS, 1) paged_weigh_tc_kernel(WeighTcAr
             s1 = f2_add(s1, f2_pack(ex2(x2), ex2(x3)));
           }
         };
-        if (edge) {
-#pragma unroll
-          for (int u = 0; u < 4; ++u) columns(std::true_type{}, u);
-        } else {
-#pragma unroll
-          for (int u = 0; u < 4; ++u) columns(std::false_type{}, u);
-        }
+        auto all = [&](auto at_edge) {
+          columns(at_edge, 0);
+          tmem_ld32(tS + 96, v[0]);
+          columns(at_edge, 1);
+          tmem_wait_ld();
+          fence_before();                                // the logits are in registers
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(L::PFULL + hh));
+          columns(at_edge, 2);
+          columns(at_edge, 3);
+        };
+        if (edge) all(std::true_type{}); else all(std::false_type{});
         float y0, y1;
         f2_unpack(f2_add(s0, s1), y0, y1);
         sum += y0 + y1;
@@ -524,7 +551,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) paged_weigh_tc_kernel(WeighTcAr
       if (!ok) break;
       if (scale == 0.f) sum = 0.f;
       if (whole) {
-        if (tp < t.x.ctx) *to = *mine(L::OFF_OLD, i & 3) + sum;
+        if (tp < t.x.ctx) *to = before + sum;
       } else {                                           // (the part's first tile, or its last)
         const bool begins = t.b0 == t.x.skipped(G, t.kt);
         __stcg(a.part + ((long long)blockIdx.x * 2 + begins) * WT_KEYS + r, sum);
@@ -542,7 +569,6 @@ __global__ void __launch_bounds__(WT_THREADS, 1) paged_weigh_tc_kernel(WeighTcAr
         first = t.b0;
       }
     }
-    cp_wait<0>();
   }
   fence_before();
   __syncthreads();
