@@ -21,7 +21,11 @@ namespace {
 using namespace paged;
 
 constexpr int WG_WARPS = 8, WG_CTAS = 2;
-constexpr int WG_ROWS = 32;            // rows of a sequence from which on it goes to the tcgen05 kernel
+// Rows of a sequence above which it goes to the tcgen05 kernel, whose time hardly depends on them.  us here for
+// up to 8, 32, 64 rows / there: 16 sequences of 10000 positions and 4 heads, d = 128 18, 36, 64 / 49; d = 64 15,
+// 25, 45 / 40; 64 of 2000 and 8 heads 31, 57, 107 / 75; d = 64 23, 38, 72 / 60; 2 of 3000 and 2 heads 5.7, 9.4,
+// 16 / 12.
+constexpr int WG_ROWS = 32;
 
 struct WeighArgs {
   Pool pool;
@@ -318,9 +322,11 @@ cudaError_t launch_paged_weigh(const Pool& pool, const Batch& b, const void* q, 
   a.c = (float)(1.4426950408889634 / sqrt((double)pool.d));
   a.G = G;
   const int grid = WG_CTAS * sms;
-  const bool few = most_rows <= 8;
-  if (pool.d == 128) return few ? launch<128, 1>(a, grid, stream) : launch<128, 4>(a, grid, stream);
-  return few ? launch<64, 1>(a, grid, stream) : launch<64, 4>(a, grid, stream);
+  // groups of 8 rows at once, by the most that a sequence here has
+  const int nt = most_rows <= 8 ? 1 : most_rows <= 16 ? 2 : 4;
+  if (pool.d == 128)
+    return nt == 1 ? launch<128, 1>(a, grid, stream) : nt == 2 ? launch<128, 2>(a, grid, stream) : launch<128, 4>(a, grid, stream);
+  return nt == 1 ? launch<64, 1>(a, grid, stream) : nt == 2 ? launch<64, 2>(a, grid, stream) : launch<64, 4>(a, grid, stream);
 }
 
 }  // namespace kvpop
