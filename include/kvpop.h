@@ -502,7 +502,7 @@ kvpop_status kvpop_paged_append(const kvpop_paged_pool* pool, const kvpop_paged_
  * has shed tokens, or tokens with positions on several axes (time, height and width of an image's).
  * Pair j of token i turns by row positions[i][axes[j]] of the tables; the token's place is
  * lens + i of its sequence as before.
- *   positions_dev [n_tokens][n_axes] int32, contiguous, n_axes 1 .. 4; rot_dim >= 16
+ *   positions_dev [n_tokens][n_axes] int32, contiguous, n_axes 1 .. 4, no memory of q_out; rot_dim >= 16
  *   axes (host, read by the call) [rot_dim / 2] bytes, each below n_axes; NULL: all 0
  * A token with a position outside 0 .. max_pos - 1, used by a pair or not, is recorded and left out:
  * its query row, keys and values keep what they held, and its block's scale does not count it. */

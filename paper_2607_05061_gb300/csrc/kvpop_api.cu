@@ -846,6 +846,11 @@ static bool rows_meet(const kvpop_rows* r, long long tokens, long long heads, lo
   }
   return false;
 }
+// Whether two ranges of memory share a byte.
+static bool ranges_meet(const void* p, long long p_bytes, const void* q, long long q_bytes) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return a < b + (uintptr_t)q_bytes && b < a + (uintptr_t)p_bytes;
+}
 static paged::Pool paged_pool(const kvpop_paged_pool* p) {
   paged::Pool q;
   q.k = static_cast<unsigned char*>(p->k_pages_dev);
@@ -938,7 +943,8 @@ static kvpop_status paged_append(const kvpop_paged_pool* pool, const kvpop_paged
   const long long out_bytes = 2ll * batch->n_tokens * n_q_heads * pool->head_dim;
   if (q && (rows_meet(q, batch->n_tokens, n_q_heads, pool->head_dim, esz, q_out, out_bytes) ||
             rows_meet(k, batch->n_tokens, pool->n_kv_heads, pool->head_dim, esz, q_out, out_bytes) ||
-            rows_meet(v, batch->n_tokens, pool->n_kv_heads, pool->head_dim, esz, q_out, out_bytes)))
+            rows_meet(v, batch->n_tokens, pool->n_kv_heads, pool->head_dim, esz, q_out, out_bytes) ||
+            (at && ranges_meet(positions, 4ll * batch->n_tokens * n_axes, q_out, out_bytes))))
     return KVPOP_ERR_INVALID_ARG;
   const PagedDevice dev = paged_device();
   if (dev.sms <= 0) return KVPOP_ERR_CUDA;
@@ -1050,11 +1056,6 @@ kvpop_status kvpop_paged_attend_shared(const kvpop_paged_pool* pool, const kvpop
                                             out_dtype == KVPOP_F32, lse, workspace, scratch, dev.sms, dev.err, stream)));
 }
 
-// Whether two ranges of memory share a byte.
-static bool ranges_meet(const void* p, long long p_bytes, const void* q, long long q_bytes) {
-  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
-  return a < b + (uintptr_t)q_bytes && b < a + (uintptr_t)p_bytes;
-}
 // Whether [n_seq][H][positions] floats can be counted in bytes, and have room for what the table holds.
 static bool mass_ok(const kvpop_paged_pool* p, long long n_seq, long long positions, long long pages) {
   return positions >= pages * p->page && (__int128)n_seq * p->n_kv_heads * positions < ((__int128)1 << 60);

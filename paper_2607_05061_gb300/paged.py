@@ -85,6 +85,7 @@ class PagedCache:
                 torch.cuda.current_stream().synchronize()      # zero for whatever stream comes first
         self.workspace = workspace
         self._index = k_pages.get_device()
+        self._scratch = {}
         self._pool_ptr = ctypes.addressof(self._pool)
         self._work = (0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
 
@@ -265,7 +266,14 @@ class PagedCache:
         _want(what, "groups", groups, torch.int32, (n_groups + 1,))
         self._elsewhere(what, groups, prefix)
         on = self._on(what, stream)
-        need = kvpop_paged_shared_bytes(self._pool_ptr, batch, n_groups, heads)
+        # (sizes decide: asked for once for each)
+        sizes = (batch[24:], batch[16:24] == bytes(8), n_groups, heads)
+        need = self._scratch.get(sizes)
+        if need is None:
+            need = kvpop_paged_shared_bytes(self._pool_ptr, batch, n_groups, heads)
+            if len(self._scratch) >= 64:
+                self._scratch.clear()
+            self._scratch[sizes] = need
         scratch = _output((max(need, 1),), torch.uint8, out.device, stream)
         status = kvpop_paged_attend_shared(self._pool_ptr, batch, qr, heads, groups.data_ptr(), prefix.data_ptr(),
                                            n_groups, out.data_ptr(), code, None if lse is None else lse.data_ptr(),

@@ -228,3 +228,17 @@ def test_captured_and_replayed(dev):
         for h in range(H):
             at = op.kept(mass[s, h, :p].tolist(), keep, 1, 3)
             assert kept[s, h].tolist() == at + [-1] * (keep - len(at))
+
+
+def test_rows_that_shared_memory_does_not_hold(dev):
+    """More keys than a CTA has room for are read again in each pass."""
+    H, page, d, keep, L = 160, 1024, 64, 300, 50001
+    need = -(-L // page)
+    cache = make_cache(dev, need + 1, H, d, page, seed=5)
+    table, lens, _ = tables([L], [0], page, need, dev, spare=0)
+    mass = torch.randint(0, 5000, (1, H, need * page), generator=torch.Generator().manual_seed(4)).float()
+    to = to_table(table.cpu(), 1, 1, need + 1).to(dev)
+    n, kept = cache.evict(table, lens, mass.to(dev), to, keep, sinks=2, window=20)
+    assert n.tolist() == [keep] and status()[0] == 0
+    for h in range(H):
+        assert kept[0, h].tolist() == fast_kept(mass[0, h, :L].numpy(), keep, 2, 20)

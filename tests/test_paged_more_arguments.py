@@ -12,7 +12,7 @@ AXES = (ctypes.c_char * 32)()
 
 def append_at(kv, p=None, b=None, q=None, k=None, v=None, **kw):
     a = dict(n_q_heads=4, dtype=kv.KVPOP_BF16, cos=PTR, sin=PTR, rot=64, max_pos=8, inter=0, at=PTR, n_axes=3,
-             axes=ctypes.addressof(AXES), q_out=PTR)
+             axes=ctypes.addressof(AXES), q_out=PTR + 2048)
     a.update(kw)
     ref = ctypes.byref
     return kv.kvpop_paged_append_at(
@@ -57,7 +57,7 @@ def test_batches_that_eviction_refuses(kv, bad):
 
 
 @pytest.mark.parametrize("kw", [dict(at=None), dict(n_axes=0), dict(n_axes=5), dict(rot=0), dict(cos=None),
-                                dict(max_pos=0), dict(q_out=None)])
+                                dict(max_pos=0), dict(q_out=None), dict(q_out=PTR), dict(at=PTR + 2048 + 1016)])
 def test_append_at_arguments_that_are_refused(kv, kw):
     assert append_at(kv, **kw) == 1
 
@@ -95,7 +95,7 @@ def test_eviction_of_more_than_a_grid_numbers(kv):
 
 
 def test_misaligned(kv):
-    assert append_at(kv, at=PTR + 2) == 2 and append_at(kv, cos=PTR + 4) == 2 and append_at(kv, q_out=PTR + 8) == 2
+    assert append_at(kv, at=PTR + 2) == 2 and append_at(kv, cos=PTR + 4) == 2 and append_at(kv, q_out=PTR + 2056) == 2
     assert weigh(kv, ws=PTR + 64) == 2
     assert weigh(kv, lse=PTR + 2) == 2 and weigh(kv, mass=PTR + 2050) == 2
     assert weigh(kv, q=rows(kv, data_dev=PTR + 2)) == 2 and weigh(kv, p=pool(kv, k_pages_dev=PTR + 8)) == 2
