@@ -183,13 +183,14 @@ struct Entry {
   int place;                           // first tile of the tcgen05 kernel, -1: has few rows
 };
 constexpr int SHARED_STEP = 64;        // blocks of the tcgen05 kernel
+enum : int { TILES_ALL, TILES_SHARE, TILES_FEW, TILES_PARTS };   // all tiles; blocks of a part at most; CTAs of the other kernel
 struct Parts {
   const Entry* entries;                // [groups + sequences]
   int n_groups;
   long long rows;                      // n_tokens * query heads
   float* sums;                         // [own, group's][rows][d]
   float2* ml;                          // [own, group's][rows] what the sums are relative to, and the weights' sums
-  int* tiles;                          // tiles there are, blocks of a part at most, and for each tile its parts
+  int* tiles;                          // what the plan says of the tcgen05 kernel's tiles: TILES_..., then each tile's parts
   int room;                            // places for sums of parts
 };
 

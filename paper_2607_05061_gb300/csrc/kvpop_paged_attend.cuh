@@ -265,7 +265,10 @@ __global__ void __launch_bounds__(32 * W, AT_CTAS) paged_attend_kernel(AttendArg
     leave();
     return;
   }
-  const long long share = max(div_pos(total + gridDim.x - 1, gridDim.x), (long long)W);   // a block a warp at least
+  int ctas = gridDim.x;                                    // (PARTS: those that run beside the other kernel)
+  if constexpr (PARTS)
+    if (a.skip_long) ctas = a.to.tiles[TILES_FEW];
+  const long long share = max(div_pos(total + ctas - 1, ctas), (long long)W);   // a block a warp at least
   long long w0 = share * blockIdx.x, w1 = min(w0 + share, total);
   if (w0 >= total) {
     leave();

@@ -249,7 +249,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
   int all_tiles = 0;
   if constexpr (PARTS) {
     // all tiles' first parts, then their second ones, ...; the plan has made the list
-    all_tiles = a.to.tiles[0];
+    all_tiles = a.to.tiles[TILES_ALL];
     if (all_tiles == 0) return;
     part = (int)(blockIdx.x / (unsigned)all_tiles);
     const int tile = all_tiles - 1 - (int)(blockIdx.x % (unsigned)all_tiles);
@@ -285,7 +285,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     }
   }
   if (s < 0) return;                                     // (offsets that do not ascend)
-  int share = PARTS ? a.to.tiles[1] : INT32_MAX;         // blocks of a part at most
+  int share = PARTS ? a.to.tiles[TILES_SHARE] : INT32_MAX;         // blocks of a part at most
   if (!PARTS && gridDim.y > 1) {
     tiles = __reduce_add_sync(0xffffffffu, tiles);
     most = __reduce_max_sync(0xffffffffu, most);
@@ -346,7 +346,7 @@ __global__ void __launch_bounds__(PP_THREADS, 1) paged_prompt_kernel(PromptArgs 
     keep[7] = -1;
     if (PARTS) {
       keep[8] = s;
-      if (part == 0) a.to.tiles[2 + place * H + h] = cut;
+      if (part == 0) a.to.tiles[TILES_PARTS + place * H + h] = cut;
     }
   }
   if (warp == PP_MMA_WARP) tmem_alloc(sb + L::OFF_TMEM, PP_TMEM);

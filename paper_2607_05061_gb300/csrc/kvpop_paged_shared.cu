@@ -11,6 +11,13 @@
 // positions are cut over all SMs, and beside them the stream for few rows; the join reads each row's
 // sums.  The number of shared positions is a multiple of 64 (blocks of the tcgen05 kernel): what is
 // left of a prefix counts as the sequences' own.
+//
+// 64 sequences over 32768 shared positions with 100 to 2000 of their own (8 KV and 32 query heads, fp32
+// results): 100 us, 565 for the same table without groups.  3 of them are the plan, 9 the join; between them
+// the shared part on tcgen05 (the second product twice) runs beside the own ones, each on SMs of its own.
+// Sharing pays from some 65000 positions saved on (members times prefix, 8 KV heads, d = 128: re-reading
+// below that comes from L2): 16 members over 4096 positions 27 us either way, over 16384 48 and 71, 4 over
+// 16384 26 and 25, 64 over 1024 34 and 34, over 16384 50 and 253.
 #include "kvpop_paged_attend.cuh"
 #include "kvpop_paged_prompt.cuh"
 
@@ -30,6 +37,8 @@ struct PlanArgs {
   int own_tiles;                       // whether it takes sequences' own parts
   int* tiles_out;                      // Parts::tiles
   int room, sms;                       // CTAs that parts may take
+  int rows, one;                       // rows that the other kernel takes at once, and groups of one token
+  float block_us;                      // of the tcgen05 kernel
 };
 
 __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(PlanArgs a) {
@@ -132,12 +141,42 @@ __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(PlanArgs a) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) all_blocks += __shfl_xor_sync(0xffffffffu, all_blocks, o);
     const int all = place * a.pool.H;
-    int share = INT32_MAX;
-    if (all > 0 && a.room / all > 1)
-      share = max(share_of<false>(all, most, all_blocks, a.sms, min(a.room / all, PP_MORE_PARTS), lane), 1);
+    int share = INT32_MAX, few = AT_CTAS * a.sms;
+    const int most_parts = all > 0 ? min(a.room / all, PP_MORE_PARTS) : 0;
+    if (most_parts > 1) share = max(share_of<false>(all, most, all_blocks, a.sms, most_parts, lane), 1);
+    // Both kernels fill the SMs, one after the other, unless this leaves some of them to the other: then
+    // they run side by side.  us of a place of its list and CTA, and of both kernels' ends (64 sequences over
+    // 32768 positions with 100 to 2000 own ones: one after the other 116 us, side by side 100; three ragged
+    // groups 58, 49; drafted tokens over two prefixes 28, 26.  With 0.1 or 0.2 us a place, ends of 6 or 12,
+    // within 12% of that).
+    constexpr float PLACE_US = 0.14f, FEW_US = 10.f, ENDS_US = 9.f;
+    float work = 0.f;
+    for (int i = lane; i < ng + n; i += 32) {
+      const Entry& e = a.entries[i];
+      if (e.place >= 0) continue;
+      const float units = e.n > 1 ? ceilf((float)e.n * (float)a.G / (float)a.rows) : (float)(e.n * a.one);
+      work += units * (float)(max((e.ctx + BLK - 1) / BLK - e.begin / BLK, 1) + AT_ENDS);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) work += __shfl_xor_sync(0xffffffffu, work, o);
+    work *= (float)a.pool.H * PLACE_US / (float)AT_CTAS;
+    if (all > 0 && all < a.sms) {
+      const int c = lane + 1, used = all * c, b = (most - 1) / c + 1;
+      const bool can = c <= most_parts && used <= a.sms - 8 && (c == 1 || b >= PP_LEAST);
+      const float cost = can ? fmaxf(ENDS_US + (float)b * a.block_us, FEW_US + work / (float)(a.sms - used)) : 3e38f;
+      const unsigned key = __reduce_min_sync(0xffffffffu, (__float_as_uint(cost) & ~31u) | (unsigned)lane);
+      const int at = key & 31u;
+      const float best = __shfl_sync(0xffffffffu, cost, at);
+      const float alone = ENDS_US + (float)min(share, most) * a.block_us + FEW_US + work / (float)a.sms;
+      if (best < alone && best < 3e38f) {
+        share = max(__shfl_sync(0xffffffffu, b, at), 1);
+        few = AT_CTAS * (a.sms - all * (at + 1));
+      }
+    }
     if (lane == 0) {
-      a.tiles_out[0] = all;
-      a.tiles_out[1] = share;
+      a.tiles_out[TILES_ALL] = all;
+      a.tiles_out[TILES_SHARE] = share;
+      a.tiles_out[TILES_FEW] = few;
     }
   }
 }
@@ -173,7 +212,7 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) shared_join_kernel(JoinArgs a
     }
     s = lo;
   }
-  const int all = a.part ? a.from.tiles[0] : 0;  // a tile's parts lie that far apart
+  const int all = a.part ? a.from.tiles[TILES_ALL] : 0;  // a tile's parts lie that far apart
   // a row's sums: one row of `sums`, or a tile's parts
   struct Source {
     const float* p;
@@ -184,7 +223,7 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) shared_join_kernel(JoinArgs a
     Source x;
     const int r = (tok - e.first) * a.G + g;
     const int pair = e.place >= 0 ? (e.place + r / PP_ROWS) * a.H + h : 0;
-    x.n = e.place >= 0 ? a.from.tiles[2 + pair] : 1;
+    x.n = e.place >= 0 ? a.from.tiles[TILES_PARTS + pair] : 1;
     const long long at = row + (group ? a.from.rows : 0), slot0 = all - 1 - pair;
     x.p = x.n > 1 ? a.part + (slot0 * PP_ROWS + r % PP_ROWS) * D + 4 * cc : a.from.sums + at * D + 4 * cc;
     x.ml = x.n > 1 ? a.part_ml + slot0 * PP_ROWS + r % PP_ROWS : a.from.ml + at;
@@ -293,18 +332,20 @@ Layout layout(const Batch& b, int n_groups, int HQ, int H, int d) {
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   Layout l;
   l.tiles = up((size_t)((long long)n_groups + b.n_seq) * sizeof(Entry));
-  l.ml = l.tiles + up((size_t)(tiles + 2) * 4);
+  l.ml = l.tiles + up((size_t)(tiles + TILES_PARTS) * 4);
   l.sums = l.ml + up((size_t)rows * 2 * sizeof(float2));
   l.bytes = l.sums + (size_t)rows * 2 * d * 4;
   return l;
 }
 
+// Groups of 8 rows that the kernel for few rows takes at once.
+int groups_of_8(const Batch& b, int G, bool beside) {
+  const long long rows = !b.starts || beside ? G : ((long long)b.n_tokens * G + b.n_seq - 1) / b.n_seq;
+  return rows <= 8 ? 1 : 2;
+}
 template <int D>
-cudaError_t launch_few(AttendArgs& a, int n_groups, int sms, bool precise, cudaStream_t stream) {
+cudaError_t launch_few(const AttendArgs& a, int nt, int sms, bool precise, cudaStream_t stream) {
   const int grid = AT_CTAS * sms;
-  const long long rows = !a.b.starts || a.skip_long ? a.G : ((long long)a.b.n_tokens * a.G + a.b.n_seq - 1) / a.b.n_seq;
-  const int nt = rows <= 8 ? 1 : 2;
-  a.one = (a.G + 8 * nt - 1) / (8 * nt);
   if (precise)
     return nt == 1 ? launch_attend<D, 1, D == 64 ? 8 : 6, true, true>(a, grid, stream) : launch_attend<D, 2, 4, true, true>(a, grid, stream);
   return nt == 1 ? launch_attend<D, 1, D == 64 ? 8 : 6, false, true>(a, grid, stream) : launch_attend<D, 2, 6, false, true>(a, grid, stream);
@@ -346,6 +387,10 @@ cudaError_t launch_paged_shared(const Pool& pool, const Batch& b, const int32_t*
   const long long grid_tc = tiles * H + sms;
   plan.room = (int)std::min<long long>(grid_tc, slots_of(sms));
   plan.sms = sms;
+  const int nt = groups_of_8(b, G, tiles > 0), one = (G + 8 * nt - 1) / (8 * nt);
+  plan.rows = 8 * nt;
+  plan.one = one;
+  plan.block_us = pool.d == 128 ? (out_f32 ? 1.5f : 0.95f) : out_f32 ? 1.f : 0.7f;
   cudaError_t e = launch_after(shared_plan_kernel, 1, PLAN_THREADS, plan, stream);
   if (e != cudaSuccess) return e;
   Parts to{};
@@ -407,8 +452,9 @@ cudaError_t launch_paged_shared(const Pool& pool, const Batch& b, const int32_t*
   a.G = G;
   a.inv_g = 1.f / (float)G;
   a.skip_long = tiles > 0;
+  a.one = one;
   a.to = to;
-  e = pool.d == 128 ? launch_few<128>(a, n_groups, sms, out_f32 != 0, stream) : launch_few<64>(a, n_groups, sms, out_f32 != 0, stream);
+  e = pool.d == 128 ? launch_few<128>(a, nt, sms, out_f32 != 0, stream) : launch_few<64>(a, nt, sms, out_f32 != 0, stream);
   if (e != cudaSuccess) return e;
   join.b = b;
   join.from = to;
