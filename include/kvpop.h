@@ -588,7 +588,7 @@ kvpop_status kvpop_paged_weigh(const kvpop_paged_pool* pool, const kvpop_paged_b
  *   kept_dev [n_seq][H][keep] int32 out: the positions kept, -1 behind them
  *   new_mass_dev [n_seq][H][new_positions] fp32 out or NULL: their mass (new_positions >= keep; what
  *   lies behind them stays); no memory of mass_dev or kept_dev
- *   new_lens_dev [n_seq] int32 out or NULL: tokens held now, -1 for idle places; not lens_dev
+ *   new_lens_dev [n_seq] int32 out or NULL: tokens held now, -1 for idle places; no memory of the others
  * The token's positions are no longer their places: kvpop_paged_append_at takes what comes next.  Bad
  * entries of either table are recorded (kvpop_standalone_status) and the rows that they concern left
  * out.  Asynchronous on `stream`; no allocation, no workspace. */

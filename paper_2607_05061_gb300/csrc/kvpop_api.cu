@@ -1110,13 +1110,16 @@ kvpop_status kvpop_paged_evict(const kvpop_paged_pool* pool, const kvpop_paged_b
       !aligned4(mass_dev) || !aligned4(to_table_dev) || !aligned4(kept_dev) || !aligned4(new_mass_dev) ||
       !aligned4(new_lens_dev))
     return KVPOP_ERR_ALIGN;
-  // weights are read while others' are written, and lengths
+  // weights are read while others' are written, and lengths; positions that were kept are read again
   const long long mass_bytes = 4 * rows * positions, kept_bytes = 4 * rows * keep;
   const long long new_bytes = new_mass_dev ? 4 * rows * new_positions : 0, lens_bytes = 4ll * batch->n_seq;
   if (ranges_meet(mass_dev, mass_bytes, kept_dev, kept_bytes) ||
       (new_mass_dev && (ranges_meet(mass_dev, mass_bytes, new_mass_dev, new_bytes) ||
                         ranges_meet(kept_dev, kept_bytes, new_mass_dev, new_bytes))) ||
-      (new_lens_dev && ranges_meet(batch->lens_dev, lens_bytes, new_lens_dev, lens_bytes)))
+      (new_lens_dev && (ranges_meet(batch->lens_dev, lens_bytes, new_lens_dev, lens_bytes) ||
+                        ranges_meet(kept_dev, kept_bytes, new_lens_dev, lens_bytes) ||
+                        ranges_meet(mass_dev, mass_bytes, new_lens_dev, lens_bytes) ||
+                        (new_mass_dev && ranges_meet(new_mass_dev, new_bytes, new_lens_dev, lens_bytes)))))
     return KVPOP_ERR_INVALID_ARG;
   const PagedDevice dev = paged_device();
   if (dev.sms <= 0) return KVPOP_ERR_CUDA;

@@ -13,8 +13,8 @@
 // positions in order: a warp counts what it keeps of its stretch, and numbers it behind the others.
 // A cluster of CTAs takes a row where there are few.  The second moves 16 slots of K and V a warp:
 // rows come as whole 128 or 64 bytes.  Bound by memory: the weights once, each kept row read and
-// written once.  64 sequences of 4160 to 4224 tokens and 8 heads (d = 128) to 4096: 207 us, 14 of them the
-// selection; 1.1 GB, 0.79 of the copy rate.
+// written once.  64 sequences of 4160 to 4224 tokens and 8 heads (d = 128) to 4096: 183 us, 14 of them the
+// selection; 1.1 GB, 0.89 of the copy rate.
 #include <cooperative_groups.h>
 
 #include "kvpop_paged.cuh"
@@ -30,7 +30,7 @@ using namespace paged;
 
 constexpr int EV_WARPS = 16, EV_THREADS = 32 * EV_WARPS, EV_BINS = 2048;
 constexpr int EV_CACHED = 48 * 1024;   // keys that a CTA holds at most (192 KB)
-constexpr int MV_WARPS = 8;
+constexpr int MV_WARPS = 4;             // 64 sequences: 182.9 us (184.4 with 8, 190 with 16)
 
 struct EvictArgs {
   Pool pool;
@@ -316,7 +316,7 @@ __global__ void __launch_bounds__(32 * MV_WARPS) evict_move_kernel(EvictArgs a, 
     unsigned char* const to = (kv ? a.pool.v : a.pool.k) + dst * D + 16 * c;
 #pragma unroll
     for (int i = 0; i < IT; ++i)
-      if (from[i] >= 0) __stcs(reinterpret_cast<uint4*>(to + (i * RPI + sub) * D), w[kv][i]);   // (used once, both: 213 us without, 207)
+      if (from[i] >= 0) __stcs(reinterpret_cast<uint4*>(to + (i * RPI + sub) * D), w[kv][i]);   // (used once, both: 3% of the time)
     if (lane == 0) (kv ? a.pool.vs : a.pool.ks)[dst / BLK] = pow2(e);
   }
 }

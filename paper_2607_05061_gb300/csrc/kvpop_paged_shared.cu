@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) shared_join_kernel(JoinArgs a
   if (tok >= a.b.n_tokens) return;
   int s = tok;
   if (a.b.starts) {
-    if (tok >= a.b.starts[a.b.n_seq]) return;    // nobody's
+    if (tok < a.b.starts[0] || tok >= a.b.starts[a.b.n_seq]) return;   // nobody's
     int lo = 0, hi = a.b.n_seq - 1;              // the last sequence that starts at or before the token
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;

@@ -195,6 +195,21 @@ def test_idle_and_nobodys_rows(dev):
     assert status()[0] == 0
 
 
+def test_rows_before_the_first_sequence_stay(dev):
+    """Many rows a sequence (tcgen05, positions in parts) and few, behind rows that are nobody's."""
+    H, G, page, d, skip = 1, 4, 64, 128, 70
+    first, prefix, held, counts = [0, 3], [512], [512, 600, 700], [90, 3, 40]
+    table, lens, starts, total = shared_tables(first, prefix, held, counts, page, dev, seed=3)
+    cache = make_cache(dev, total, H, d, page, seed=2)
+    hide_rest(cache, table, held, counts, page)
+    n = skip + sum(counts)
+    q = (torch.randn((n, H * G, d), generator=torch.Generator().manual_seed(5)) * 0.02).bfloat16().to(dev)
+    out, lse = torch.full((n, H * G, d), 7.0, device=dev), torch.full((n, H * G), 7.0, device=dev)
+    cache.attend(table, lens, q, starts=starts + skip, out=out, lse=lse, groups=ints(first, dev), prefix=ints(prefix, dev))
+    assert status()[0] == 0 and (out[:skip] == 7).all() and (lse[:skip] == 7).all()
+    check(out[skip:], lse[skip:], attend_reference(cache, table, held, counts, q[skip:], page), torch.float32)
+
+
 def test_bad_groups_and_tables(dev):
     H, G, page, d = 1, 2, 16, 64
     first, prefix, held = [0, 3, 5], [64, 64], [70, 64, 90, 66, 65]

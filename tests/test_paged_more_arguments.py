@@ -84,7 +84,8 @@ def test_weigh_of_more_rows_than_an_int_numbers(kv):
                                 dict(keep=0), dict(keep=33), dict(sinks=-1), dict(window=-1), dict(sinks=20, window=13),
                                 dict(kept=None), dict(kept=PTR + 512), dict(new=PTR + 512, new_positions=32),
                                 dict(new=PTR + 1024, new_positions=32), dict(new=PTR + 2048, new_positions=31),
-                                dict(lens=PTR + 4), dict(sinks=2 ** 31 - 1, window=2 ** 31 - 1)])
+                                dict(lens=PTR + 4), dict(lens=PTR + 1028),
+                                dict(lens=PTR + 252), dict(new=PTR + 8192, new_positions=32, lens=PTR + 8196), dict(sinks=2 ** 31 - 1, window=2 ** 31 - 1)])
 def test_evict_arguments_that_are_refused(kv, kw):
     assert evict(kv, **kw) == 1
 
