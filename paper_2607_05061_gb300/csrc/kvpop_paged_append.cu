@@ -15,7 +15,7 @@
 // the tables.  Its place in the cache stays p.
 //
 // Bound by memory: K, V and q are read once, codes and rotated queries written once.  One warp
-// takes one head of K or V, or two of q, over the (at most 16) new tokens of one block, so that a
+// takes one head of K or V, or a few of q, over the (at most 16) new tokens of one block, so that a
 // block's scale and codes have one writer; with one token a sequence, D / 8 lanes take a head.  16384
 // tokens of 5 prompts with 32 query and 8 KV heads (bf16) take 88 us, 413 MB at 4.7 TB/s: the warps
 // wait for their loads (less since they send their rows to L2 ahead: 98 before), and the issue slots
@@ -30,7 +30,7 @@ namespace {
 
 using namespace paged;
 
-constexpr int AP_WARPS = 4, AP_QH = 2;
+constexpr int AP_WARPS = 4;
 
 struct AppendArgs {
   Pool pool;
@@ -170,27 +170,26 @@ __device__ __forceinline__ Turn turn_by(const AppendArgs& a, const Lane& n, int 
     for (int i = 0; i < 8; ++i) t.sn[i] = -t.sn[i];
   return t;
 }
-// The positions of a block's (at most 16) new tokens, two of up to 64 a lane.  Read where they are used, each
-// was waited for before its cosines could be asked for (14500 image tokens 77 us).
+// The positions of a block's (at most 16) new tokens, up to 64, in shared memory.  (Read where they are used, each
+// was waited for before its cosines could be asked for: 14500 image tokens 77 us; from lanes' registers by
+// shuffles 67; so, with four heads of queries at once and the rows one after the other, which leaves
+// registers to the loads, 58.)
 struct Places {
-  int v[2];
+  const int* v;
   unsigned bad[2];                                  // which of them lie outside the tables
-  __device__ __forceinline__ void load(const AppendArgs& a, long long tok, int rows, int lane) {
+  __device__ __forceinline__ void load(const AppendArgs& a, long long tok, int rows, int lane, int* to) {
+    v = to;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      const int i = lane + 32 * e;
-      v[e] = i < rows * a.n_axes ? a.at[tok * a.n_axes + i] : 0;
-      bad[e] = __ballot_sync(0xffffffffu, (unsigned)v[e] >= (unsigned)a.max_pos);
+      const int i = lane + 32 * e, x = i < rows * a.n_axes ? a.at[tok * a.n_axes + i] : 0;
+      to[i] = x;
+      bad[e] = __ballot_sync(0xffffffffu, (unsigned)x >= (unsigned)a.max_pos);
     }
     if (bad[0] | bad[1]) report(a.err, ERR_ROTATION);
-  }
-  // (by all lanes)
-  __device__ __forceinline__ int of(const AppendArgs& a, int row, int axis) const {
-    const int i = row * a.n_axes + axis;
-    const int x = __shfl_sync(0xffffffffu, v[0], i & 31), y = __shfl_sync(0xffffffffu, v[1], i & 31);
-    return i < 32 ? x : y;
+    __syncwarp();
   }
   __device__ __forceinline__ bool ok(const AppendArgs& a, int row) const {
+    if ((bad[0] | bad[1]) == 0) return true;
     const unsigned long long all = (unsigned long long)bad[1] << 32 | bad[0];
     return (all >> (row * a.n_axes & 63) & ((1u << a.n_axes) - 1u)) == 0;
   }
@@ -247,11 +246,16 @@ __device__ __forceinline__ void ahead(const T* p, long long ts, long long hs, in
       if (it * RPI < rows && e < heads) prefetch_l2_line(p + it * RPI * ts + e * hs);
 }
 
+// Heads of q that a warp takes at once: more of them share a row's cosines and sines, as registers allow
+// (14500 image tokens with 1, 2, 3, 4: 76, 62, 59, 58 us).
+template <typename T, bool AT>
+constexpr int HEADS_AT_ONCE = AT && sizeof(T) == 2 ? 4 : 2;
+
 // ONE: one token a sequence.  D / 8 lanes per row; a warp takes one (block, head) of up to 16 rows,
 // or, with ONE, 32 / (D / 8) of them with one row each.  AT: positions are given.
 template <typename T, int D, bool ONE, bool AT>
-__global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendArgs a) {
-  constexpr int LPR = D / 8, RPI = 32 / LPR, IT = ONE ? 1 : BLK / RPI, QH = ONE ? 1 : AP_QH;
+__global__ void __launch_bounds__(32 * AP_WARPS, AT && !ONE ? 7 : 8) paged_append_kernel(AppendArgs a) {
+  constexpr int LPR = D / 8, RPI = 32 / LPR, IT = ONE ? 1 : BLK / RPI, QH = ONE ? 1 : HEADS_AT_ONCE<T, AT>;
   const int lane = threadIdx.x & 31, c = lane % LPR, sub = lane / LPR;
   constexpr bool KEEP = !ONE && D == 64;            // rotated rows stay in shared memory: 8 values a lane and turn
   __shared__ float4 keepS[KEEP ? AP_WARPS : 1][KEEP ? 2 * IT : 1][32];
@@ -298,7 +302,8 @@ __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendAr
   const bool some = p0 < end;
   if (!ONE && !some) return;                        // warp-uniform
   Places places;
-  if (AT && !ONE) places.load(a, t.first + (p0 - t.len), end - p0, lane);
+  __shared__ int placeS[AT && !ONE ? AP_WARPS : 1][64];
+  if (AT && !ONE) places.load(a, t.first + (p0 - t.len), end - p0, lane, placeS[threadIdx.x >> 5]);
   // what turns row `it` of the lane: two rows of the tables, or, where 4 pairs are of several axes, all of them
   struct Axes {
     int a0, a1;
@@ -308,6 +313,10 @@ __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendAr
     const uint32_t x = a.axes[n.angle >> 2 & 15], y = a.axes[(n.angle >> 2) + 1 & 15];
     return Axes{(int)(x & 255), (int)((a.interleaved ? x : y) & 255),
                 x != (x & 255) * 0x01010101u || (!a.interleaved && y != (y & 255) * 0x01010101u)};
+  };
+
+  auto turned_by = [&](const Lane& n, int row, const Axes& x) {
+    return turn_by(a, n, places.v[row * a.n_axes + x.a0], places.v[row * a.n_axes + x.a1]);
   };
 
   if (slot >= 2 * a.pool.H) {                       // ------------------------------ queries
@@ -324,14 +333,8 @@ __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendAr
 #pragma unroll 1
     for (int it = 0; it < IT; ++it) {
       const int32_t* at = AT ? a.at + (t.first + (pos - t.len)) * (long long)a.n_axes : nullptr;
-      int r0 = 0, r1 = 0;
-      if (AT && !ONE) {
-        const int row = min(pos, end - 1) - p0;
-        r0 = places.of(a, row, ax.a0);
-        r1 = places.of(a, row, ax.a1);
-      }
       if (pos < end && (!AT || ONE || places.ok(a, pos - p0))) {
-        const Turn turn = !AT ? turn_of(a, n, cosR, sinR) : ONE || ax.mixed ? turn_at(a, n, at) : turn_by(a, n, r0, r1);
+        const Turn turn = !AT ? turn_of(a, n, cosR, sinR) : ONE || ax.mixed ? turn_at(a, n, at) : turned_by(n, pos - p0, ax);
         Raw<T> own[QH], other[QH];
 #pragma unroll
         for (int e = 0; e < QH; ++e) {
@@ -385,27 +388,20 @@ __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendAr
   auto taken = [&](int it) {
     return pos0 + it * RPI < end && (!AT || ONE || places.ok(a, pos0 + it * RPI - p0));
   };
-  auto turns = [&](int it, int& r0, int& r1) {      // (by all lanes, before the rows that are none are passed over)
-    r0 = r1 = 0;
-    if (AT && !ONE && !is_v) {
-      const int row = min(pos0 + it * RPI, end - 1) - p0;
-      r0 = places.of(a, row, ax.a0);
-      r1 = places.of(a, row, ax.a1);
-    }
-  };
-  auto read = [&](int it, int r0, int r1, float (&x)[8]) {
+  auto read = [&](int it, float (&x)[8]) {
     const T* row = from + it * RPI * ts;
     const long long at = angle0 + it * RPI * (a.rot >> 1);
     Raw<T> own, other;
     own.load(row + n.own);
     other.load(row + n.other);
     rotated(a, n, !AT ? turn_of(a, n, a.cosT + at, a.sinT + at)
-                  : ONE || ax.mixed ? turn_at(a, n, at0 + (long long)it * RPI * a.n_axes) : turn_by(a, n, r0, r1),
+                  : ONE || ax.mixed ? turn_at(a, n, at0 + (long long)it * RPI * a.n_axes)
+                                    : turned_by(n, pos0 + it * RPI - p0, ax),
             own, other, x);
   };
-  auto value = [&](int it, int r0, int r1, float (&x)[8], bool again) {
+  auto value = [&](int it, float (&x)[8], bool again) {
     if (!KEEP || !again) {
-      read(it, r0, r1, x);
+      read(it, x);
     } else {
       const float4 u = keepS[threadIdx.x >> 5][2 * it][lane], w = keepS[threadIdx.x >> 5][2 * it + 1][lane];
       x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
@@ -415,13 +411,11 @@ __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendAr
   auto largest = [&](float limit) {
     float m = 0.f;
     if (id >= 0)
-#pragma unroll 2
-      for (int it = 0; it < IT; ++it) {
-        int r0, r1;
-        turns(it, r0, r1);
+#pragma unroll (AT ? 1 : 2)
+      for (int it = 0; it < IT; ++it)
         if (taken(it)) {
           float x[8];
-          value(it, r0, r1, x, limit > 0.f);
+          value(it, x, limit > 0.f);
           if (KEEP && limit == 0.f) {
             keepS[threadIdx.x >> 5][2 * it][lane] = make_float4(x[0], x[1], x[2], x[3]);
             keepS[threadIdx.x >> 5][2 * it + 1][lane] = make_float4(x[4], x[5], x[6], x[7]);
@@ -429,7 +423,6 @@ __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendAr
 #pragma unroll
           for (int i = 0; i < 8; ++i) m = fmaxf(m, limit > 0.f && !(fabsf(x[i]) < limit) ? 0.f : fabsf(x[i]));
         }
-      }
 #pragma unroll
     for (int o = ONE ? LPR / 2 : 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     return m;
@@ -457,23 +450,21 @@ __global__ void __launch_bounds__(32 * AP_WARPS, 8) paged_append_kernel(AppendAr
   }
   const float inv = 1.f / sc;                       // exact: sc is a power of two
   unsigned char* to = rows + (head + (pos0 - p0)) * D + n.own;
-#pragma unroll 2
-  for (int it = 0; it < IT; ++it) {
-    int r0, r1;
-    turns(it, r0, r1);
+#pragma unroll (AT ? 1 : 2)
+  for (int it = 0; it < IT; ++it)
     if (taken(it)) {
       float x[8];
-      value(it, r0, r1, x, true);
+      value(it, x, true);
       *reinterpret_cast<uint2*>(to + it * RPI * D) = codes8(x, inv, special);
     }
-  }
   if (lane == lead) *scale = sc;
 }
 
 template <typename T, int D>
 cudaError_t launch(AppendArgs& a, cudaStream_t stream) {
   const bool one = a.b.starts == nullptr;
-  const long long tasks = (2 * a.pool.H + (one ? a.HQ : (a.HQ + AP_QH - 1) / AP_QH)) * (one ? (long long)a.b.n_seq : a.b.n_tokens / BLK + 2ll * a.b.n_seq);
+  const int qh = a.at ? HEADS_AT_ONCE<T, true> : HEADS_AT_ONCE<T, false>;
+  const long long tasks = (2 * a.pool.H + (one ? a.HQ : (a.HQ + qh - 1) / qh)) * (one ? (long long)a.b.n_seq : a.b.n_tokens / BLK + 2ll * a.b.n_seq);
   if (tasks > INT32_MAX - 32 * AP_WARPS) return cudaErrorInvalidValue;   // (refused before)
   a.tasks = (int)tasks;
   const int per_block = AP_WARPS * (one ? 32 / (D / 8) : 1), grid = (a.tasks + per_block - 1) / per_block;
