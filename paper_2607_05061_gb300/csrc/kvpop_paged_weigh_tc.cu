@@ -18,6 +18,12 @@
 //  * 3 producer warps: query rows by 16-byte cp.async into 128B-swizzled slots, with lse and the last
 //    position that each row sees beside them.  Where all of a sequence's rows fit the slots they stay
 //    there for all tiles of the head.
+// A wait by parity misses a phase when the one after it is complete too, so a barrier's next phase needs an
+// arrival of everyone who waits for this one.  Operands (AFULL) are given back (AEMPTY) by the MMA warp, when
+// their products are done, and by each softmax warp, as it begins the tile: the position warps are two tiles
+// ahead of the last of them at most.  Query slots (FULL) are given back (EMPTY) by both, so that the producers
+// are ST blocks ahead at most.  Logits (SFULL) are given back (PFULL) by their half's warps: the MMA warp is
+// one block ahead.
 // Tensor memory: S 2 x 128 columns, operands 2 x (2 x d / 2).
 //
 // A block of 256 positions by 128 rows takes the tensor cores 1024 clocks at d = 128 and the exponential
@@ -228,7 +234,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) paged_weigh_tc_kernel(WeighTcAr
       mbar_init(bar(L::SFULL + i), 1);
       mbar_init(bar(L::PFULL + i), WT_SOFT / 2);
       mbar_init(bar(L::AFULL + i), WT_KEY);
-      mbar_init(bar(L::AEMPTY + i), 1);
+      mbar_init(bar(L::AEMPTY + i), 1 + WT_SOFT);
     }
     mbar_init(bar(L::END), 1);
     mbar_fence_init();
@@ -493,6 +499,8 @@ __global__ void __launch_bounds__(WT_THREADS, 1) paged_weigh_tc_kernel(WeighTcAr
       const float* const of = reinterpret_cast<const float*>(smt) + (i % WT_OLD) * WT_KEYS + r;
       const float scale = of[L::OFF_SC / 4];             // 0: no position, or a bad page
       const float before = of[L::OFF_OLD / 4];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(L::AEMPTY + (i & 1)));
       const uint64_t cc = f2_pack(a.c * scale, a.c * scale);
       const int t0 = t.kt * WT_KEYS, tp = t0 + r, t1 = min(t0 + WT_KEYS, t.x.ctx) - 1;
       // blocks from here on have rows that see the whole tile: tokens from t1 - len on
