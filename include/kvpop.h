@@ -505,7 +505,8 @@ kvpop_status kvpop_paged_append(const kvpop_paged_pool* pool, const kvpop_paged_
  *   positions_dev [n_tokens][n_axes] int32, contiguous, n_axes 1 .. 4, no memory of q_out; rot_dim >= 16
  *   axes (host, read by the call) [rot_dim / 2] bytes, each below n_axes; NULL: all 0
  * A token with a position outside 0 .. max_pos - 1, used by a pair or not, is recorded and left out:
- * its query row, keys and values keep what they held, and its block's scale does not count it. */
+ * its query row, keys and values keep what they held, and its block's scale does not count it (a block
+ * that begins with it starts from the least scale, whatever the page's earlier owner left). */
 kvpop_status kvpop_paged_append_at(const kvpop_paged_pool* pool, const kvpop_paged_batch* batch,
                                    const kvpop_rows* q, int32_t n_q_heads, const kvpop_rows* k,
                                    const kvpop_rows* v, kvpop_dtype dtype, const float* cos_dev,

@@ -298,8 +298,10 @@ __global__ void __launch_bounds__(32 * AP_WARPS, AT && !ONE ? 7 : 8) paged_appen
       }
     }
   }
-  if (AT && ONE && p0 < end && !in_tables(a, a.at + (long long)t.first * a.n_axes)) end = p0;
   const bool some = p0 < end;
+  // one token that is left out: it only starts its block's scale, if it is the first, as a block of several does
+  const bool gone = AT && ONE && some && !in_tables(a, a.at + (long long)t.first * a.n_axes);
+  if (gone) end = p0;
   if (!ONE && !some) return;                        // warp-uniform
   Places places;
   __shared__ int placeS[AT && !ONE ? AP_WARPS : 1][64];
@@ -364,7 +366,8 @@ __global__ void __launch_bounds__(32 * AP_WARPS, AT && !ONE ? 7 : 8) paged_appen
   const bool kv = slot < 2 * a.pool.H && some;      // (ONE: lanes of queries stay for the shuffles)
   const bool is_v = slot >= a.pool.H;
   const int h = is_v ? slot - a.pool.H : slot;
-  const int id = kv ? page_of(a.b, a.pool, s, p0, a.err) : -1;   // a block lies in one page
+  // a block lies in one page
+  const int id = kv && !(gone && (p0 & (BLK - 1)) != 0) ? page_of(a.b, a.pool, s, p0, a.err) : -1;
   const T* src = static_cast<const T*>(is_v ? a.v : a.k) + h * (is_v ? a.v_hs : a.k_hs);
   const long long ts = is_v ? a.v_ts : a.k_ts;
   const long long at = ((long long)max(id, 0) * a.pool.H + h) * a.pool.page;
