@@ -293,7 +293,9 @@ __global__ void __launch_bounds__(32 * MV_WARPS) evict_move_kernel(EvictArgs a, 
     bool far = false, same = true;
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
-      f[i] *= inv;
+      // (codes that are not 0 are at least 2^-9 and become 448 at most: above 2^18 there are zeros and NaN alone,
+      // and times inf, which 2^100 / 2^-96 would be, a zero is none)
+      f[i] = fminf(f[i] * inv, 1048576.f);
       far |= f[i] > 32768.f;
       same &= f[i] == 1.f || from[i] < 0;
     }
