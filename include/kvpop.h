@@ -545,7 +545,8 @@ kvpop_status kvpop_paged_attend(const kvpop_paged_pool* pool, const kvpop_paged_
  *     (their rows of the table need not be: one member's are read; idle places do not matter).  What
  *     passes the shortest member's tokens is not taken as shared, nor is what is left of a multiple
  *     of 64; a group with fewer than two members that have tokens, or fewer than 64 positions, is none
- * Offsets that do not ascend are recorded, and what they concern is left out.  Other arguments and the
+ * Offsets that do not ascend (a group that begins before an earlier offset) are recorded, and what they
+ * concern is left out: those places are computed without a group.  Other arguments and the
  * precision as kvpop_paged_attend, whose workspace it shares.
  *   scratch_dev: kvpop_paged_shared_bytes(...) bytes (0: arguments that the call refuses; some
  *     8 (d + 2) a token and query head), 256-byte aligned, of no content before or after

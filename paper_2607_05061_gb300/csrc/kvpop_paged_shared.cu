@@ -59,8 +59,10 @@ __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(PlanArgs a) {
   }
   __syncthreads();
   for (int g = warp; g < ng; g += PLAN_THREADS / 32) {
-    int from = a.groups[g], to = a.groups[g + 1];
-    if (from < 0 || to < from || to > n) {
+    int from = a.groups[g], to = a.groups[g + 1], before = 0;   // (places of two groups would have neither's sums)
+    for (int i = lane; i < g; i += 32) before = max(before, a.groups[i]);
+    before = __reduce_max_sync(0xffffffffu, before);
+    if (from < before || to < from || to > n) {
       if (lane == 0) report(a.err, ERR_BATCH);
       from = to = 0;
     }
