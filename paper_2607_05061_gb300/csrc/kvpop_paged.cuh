@@ -233,7 +233,8 @@ cudaError_t launch_paged_evict(const paged::Pool& pool, const paged::Batch& b, c
 cudaError_t launch_paged_weigh(const paged::Pool& pool, const paged::Batch& b, const void* q, long long q_ts,
                                long long q_hs, int HQ, const float* lse, float* mass, long long positions,
                                void* workspace, int sms, int32_t* err, cudaStream_t stream);
-// The same for sequences with more than `least` rows: counters of a CTA each, zero between calls, and sums.
+// The same for sequences with more than `least` rows: counters of a CTA each (one an SM), zero between calls,
+// and bytes of sums.
 size_t paged_weigh_workspace(int sms);
 cudaError_t launch_paged_weigh_tc(const paged::Pool& pool, const paged::Batch& b, const void* q, long long q_ts,
                                   long long q_hs, int HQ, const float* lse, float* mass, long long positions,

@@ -29,10 +29,12 @@ cudaError_t launch_d(AttendArgs& a, int sms, cudaStream_t stream) {
 }  // namespace
 
 // [counters here][there] [partial results here][there]
-size_t paged_attend_workspace(int sms) {
-  return counter_bytes(sms) + paged_prompt_counters(sms) + part_bytes(sms) + paged_prompt_parts(sms);
-}
 size_t paged_attend_parts(int sms) { return counter_bytes(sms) + paged_prompt_counters(sms); }
+// The weights' counters and sums lie in the same places.
+static_assert(AT_CTAS * 8 >= (int)sizeof(int), "a counter an SM");
+size_t paged_attend_workspace(int sms) {
+  return paged_attend_parts(sms) + std::max(part_bytes(sms) + paged_prompt_parts(sms), paged_weigh_workspace(sms));
+}
 
 cudaError_t launch_paged_attend(const Pool& pool, const Batch& b, const void* q, long long q_ts, long long q_hs,
                                 int HQ, void* out, int out_f32, float* lse, void* workspace, int sms,

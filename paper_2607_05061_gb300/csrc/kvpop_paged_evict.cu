@@ -323,13 +323,13 @@ __global__ void __launch_bounds__(32 * MV_WARPS) evict_move_kernel(EvictArgs a, 
   }
 }
 
-cudaError_t launch_ex(cudaLaunchConfig_t& cfg, cudaLaunchAttribute* at, int n, cudaStream_t stream) {
+// The launch's last attribute (after `n` others), and its stream.
+void after_the_last(cudaLaunchConfig_t& cfg, cudaLaunchAttribute* at, int n, cudaStream_t stream) {
   at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[n].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = n + 1;
   cfg.stream = stream;
-  return cudaSuccess;
 }
 
 }  // namespace
@@ -358,7 +358,7 @@ cudaError_t launch_paged_evict(const Pool& pool, const Batch& b, const PagedEvic
   at[0].id = cudaLaunchAttributeClusterDimension;
   at[0].val.clusterDim.x = C;
   at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-  launch_ex(cfg, at, 1, stream);
+  after_the_last(cfg, at, 1, stream);
   err_ = cudaLaunchKernelEx(&cfg, evict_select_kernel, a);
   if (err_ != cudaSuccess) return err_;
   const int blocks = (int)((std::min<long long>(e.keep, cap) + BLK - 1) / BLK);
@@ -366,7 +366,7 @@ cudaError_t launch_paged_evict(const Pool& pool, const Batch& b, const PagedEvic
   cfg.gridDim = dim3((unsigned)((units + MV_WARPS - 1) / MV_WARPS));
   cfg.blockDim = dim3(32 * MV_WARPS);
   cfg.dynamicSmemBytes = 0;
-  launch_ex(cfg, at, 0, stream);
+  after_the_last(cfg, at, 0, stream);
   return pool.d == 128 ? cudaLaunchKernelEx(&cfg, evict_move_kernel<128>, a, blocks, units)
                        : cudaLaunchKernelEx(&cfg, evict_move_kernel<64>, a, blocks, units);
 }
