@@ -20,6 +20,7 @@ import ctypes
 import struct
 from typing import List, Optional, Sequence
 
+import numpy as np
 import torch
 
 from .kvpop import (KVPOP_BF16, KVPOP_F32, _ck, _ptr, _raw_stream, _stream, kvpop_paged_append, kvpop_paged_append_at,
@@ -437,19 +438,36 @@ class PageTable:
     def groups(self):
         """(groups, prefix) for ``PagedCache.attend``: runs of places whose sequences begin with the same
         pages.  (None, None) where none do."""
-        runs, i, n = [], 0, len(self.held)
-        while i < n:
-            common, live, end = self.pages[i][:max(self.held[i], 0) // self.page], 1, i + 1
-            for j in range(i + 1, n if common else 0):
-                if self.held[j] < 0:
-                    continue                               # (an idle place within a run does not matter)
-                other = self.pages[j][:self.held[j] // self.page]
-                k = next((m for m, (a, b) in enumerate(zip(common, other)) if a != b), min(len(common), len(other)))
-                if live * k < (live - 1) * len(common) or k == 0:
-                    break                                  # (fewer pages for more sequences would be read more often)
-                common, live, end = common[:k], live + 1, j + 1
-            runs.append((i, end, len(common) * self.page if live > 1 else 0))
-            i = end
+        live = [s for s, h in enumerate(self.held) if h >= 0]
+        whole = [self.pages[s][:self.held[s] // self.page] for s in live]
+        # (what neighbours have in common; a run has the least of it)
+        common = [next((m for m, (x, y) in enumerate(zip(a, b)) if x != y), min(len(a), len(b)))
+                  for a, b in zip(whole, whole[1:])]
+        # the runs that save most reads of pages, the fewest of those that save alike: for the first k live places
+        # what they are worth, pages saved before runs, and where the last run begins
+        k_all = len(live)
+        worth, begin = np.zeros(k_all + 1, np.int64), [0] * (k_all + 1)
+        least, others = np.zeros(k_all, np.int64), np.arange(k_all, -1, -1)
+        for k in range(1, k_all + 1):
+            if k > 1:
+                least[k - 2] = common[k - 2]
+                np.minimum(least[:k - 2], common[k - 2], out=least[:k - 2])
+            each = worth[:k] + others[k_all - k + 1:k_all + 1] * least[:k] * (k_all + 1)
+            begin[k] = int(each.argmax())
+            worth[k] = each[begin[k]] - 1
+        cuts, k = [], len(live)
+        while k > 0:
+            cuts.append((begin[k], k))
+            k = begin[k]
+        runs, at, n = [], 0, len(self.held)
+        for i, k in reversed(cuts):                        # (idle places within a run do not matter)
+            first, end = live[i], live[k - 1] + 1
+            if first > at:
+                runs.append((at, first, 0))
+            runs.append((first, end, min(common[i:k - 1]) * self.page if k - i > 1 else 0))
+            at = end
+        if at < n:
+            runs.append((at, n, 0))
         if not any(p for _, _, p in runs):
             return None, None
         first, prefix = [0], []
