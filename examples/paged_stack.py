@@ -16,6 +16,7 @@ import argparse
 import os
 import sys
 import time
+from typing import Optional
 
 import torch
 
@@ -39,7 +40,8 @@ class PagedStack:
     """``layers`` layers of random weights; all share one page table, each has its own pages."""
 
     def __init__(self, layers: int, batch: int, hidden: int, n_kv_heads: int, q_per_kv: int, head_dim: int,
-                 max_tokens: int, page: int = 64, seed: int = 0, device="cuda", weights: bool = False):
+                 max_tokens: int, page: int = 64, seed: int = 0, device="cuda", weights: bool = False,
+                 keep: Optional[int] = None):
         self.H, self.HQ, self.d, self.hidden, self.b = n_kv_heads, n_kv_heads * q_per_kv, head_dim, hidden, batch
         g = torch.Generator(device=device).manual_seed(seed)
 
@@ -48,14 +50,17 @@ class PagedStack:
         nq, nkv = self.HQ * head_dim, self.H * head_dim
         self.layers = [{"Wqkv": weight(hidden, nq + 2 * nkv), "Wo": weight(nq, hidden)} for _ in range(layers)]
         per = -(-max_tokens // page)
-        self.table = PageTable(batch, per, batch * per, page, device=device)
+        # with `weights` there is room for what ``shed`` moves, `keep` tokens of every place at most (none given: all)
+        move = -(-min(max_tokens if keep is None else keep, max_tokens) // page) if weights else 0
+        n_pages = batch * (per + move)
+        self.table = PageTable(batch, per, n_pages, page, device=device)
         self.caches = []
         for _ in range(layers):                    # calls of one stack follow each other: one workspace
-            self.caches.append(PagedCache.empty(batch * per, n_kv_heads, head_dim, page, device=device,
+            self.caches.append(PagedCache.empty(n_pages, n_kv_heads, head_dim, page, device=device,
                                                 workspace=self.caches[0].workspace if self.caches else None))
         self.cos, self.sin = rotation_tables(max_tokens, head_dim, device=device)
         self.graph = None
-        # with `weights`: what each position of each layer and KV head has been given, and room to shed
+        # with `weights`: what each position of each layer and KV head has been given
         self.mass = [torch.zeros((batch, n_kv_heads, per * page), device=device) for _ in range(layers if weights else 0)]
         self.groups = (None, None)
 
@@ -108,6 +113,8 @@ class PagedStack:
     def shed(self, keep: int, sinks: int = 4, window: int = 64):
         """Every layer and KV head keeps the ``keep`` positions of every place that got most weight.  A step
         that was captured before stays good, but with shared prefixes (there are none behind it)."""
+        if not 0 <= sinks + window <= keep or min(sinks, window) < 0:
+            raise ValueError(f"PagedStack.shed: {sinks} sinks and a window of {window} are not among {keep} tokens")
         to = self.table.shrink(keep)
         for cache, mass in zip(self.caches, self.mass):
             new = torch.zeros_like(mass)
@@ -155,7 +162,7 @@ def main():
         ap.add_argument("--" + name, type=int, default=value)
     a = ap.parse_args()
     st = PagedStack(a.layers, a.batch, a.hidden, a.kv_heads, a.q_per_kv, a.head_dim, a.shared + a.prompt + a.steps + 2,
-                    weights=a.keep > 0)
+                    weights=a.keep > 0, keep=a.keep)
     g = torch.Generator(device="cuda").manual_seed(1)
     left = [max(1, a.prompt - 37 * s) for s in range(a.batch)]
     torch.cuda.synchronize()
@@ -175,7 +182,7 @@ def main():
     t1 = time.perf_counter()
     print(f"prompts: {tokens} tokens through {a.layers} layers in {1e3 * (t1 - t0):.1f} ms")
     if a.keep:
-        st.shed(a.keep)
+        st.shed(a.keep, window=max(0, min(64, a.keep // 2)), sinks=min(4, a.keep // 2))
     x = torch.randn((a.batch, a.hidden), generator=g, device="cuda").bfloat16()
     st.table.grow(a.steps + 1)
     st.capture(x)
