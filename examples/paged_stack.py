@@ -95,7 +95,9 @@ class PagedStack:
 
     def share(self, s: int, places, tokens: int) -> int:
         """Sequences at ``places`` that begin as the one at s does; what they share is read once from then on
-        (until a place is opened or closed: then ``regroup``).  Weights of shared positions start as what s's tokens have given them so far."""
+        (until a place is opened or closed: then ``regroup``).  Weights of shared positions start as what s's tokens
+        have given them so far.  Returns the number of shared tokens (0 without places)."""
+        n = 0
         for t in places:
             n = self.table.share(s, t, tokens)
             for mass in self.mass:
