@@ -62,13 +62,16 @@ class PagedStack:
         self.graph = None
         # with `weights`: what each position of each layer and KV head has been given
         self.mass = [torch.zeros((batch, n_kv_heads, per * page), device=device) for _ in range(layers if weights else 0)]
-        self.groups = (None, None)
+        self.groups, self._grouped = (None, None), 0        # and the table's changes that they are of
+        self._captured = (None, None)                       # groups that the captured step reads
 
     def forward(self, x, starts=None, max_new=None, lse=None, positions=None):
         """Hidden states ``x [tokens][hidden]`` (bf16) of the new tokens through all layers; the
         table has pages for them, and ``advance`` is the caller's.  ``positions``: where they are not
         the tokens' places."""
         n, HQ, H, d = x.shape[0], self.HQ, self.H, self.d
+        if self._grouped != self.table.changes:
+            self.regroup()
         table, lens, (groups, prefix) = self.table.dev, self.table.lens, self.groups
         for i, (W, cache) in enumerate(zip(self.layers, self.caches)):
             qkv = torch.matmul(x, W["Wqkv"]).view(n, HQ + 2 * H, d)
@@ -94,9 +97,9 @@ class PagedStack:
         return y
 
     def share(self, s: int, places, tokens: int) -> int:
-        """Sequences at ``places`` that begin as the one at s does; what they share is read once from then on
-        (until a place is opened or closed: then ``regroup``).  Weights of shared positions start as what s's tokens
-        have given them so far.  Returns the number of shared tokens (0 without places)."""
+        """Sequences at ``places`` that begin as the one at s does; what they share is read once from then on.
+        Weights of shared positions start as what s's tokens have given them so far.  Returns the number of shared
+        tokens (0 without places)."""
         n = 0
         for t in places:
             n = self.table.share(s, t, tokens)
@@ -110,11 +113,23 @@ class PagedStack:
         return self.table.pos if self.mass else None
 
     def regroup(self):
-        self.groups = self.table.groups()
+        """Groups of the sequences that share what they begin with, as the table is now (calls see to it when
+        places have begun anew).  A captured step's stay where they are and become these, as far as there is room
+        for them: the others' sequences read for themselves until the step is captured again."""
+        self.groups, self._grouped = self.table.groups(), self.table.changes
+        first, prefix = self._captured
+        if first is None:
+            return
+        prefix.zero_()
+        if self.groups[0] is not None:
+            n = min(len(prefix), len(self.groups[1]))
+            first[:n + 1] = self.groups[0][:n + 1]
+            first[n + 1:] = self.groups[0][n]
+            prefix[:n] = self.groups[1][:n]
 
     def shed(self, keep: int, sinks: int = 4, window: int = 64):
         """Every layer and KV head keeps the ``keep`` positions of every place that got most weight.  A step
-        that was captured before stays good, but with shared prefixes (there are none behind it)."""
+        that was captured before stays good (there are no shared prefixes behind it)."""
         if not 0 <= sinks + window <= keep or min(sinks, window) < 0:
             raise ValueError(f"PagedStack.shed: {sinks} sinks and a window of {window} are not among {keep} tokens")
         to = self.table.shrink(keep)
@@ -137,6 +152,9 @@ class PagedStack:
         ``replay`` runs it."""
         stream = torch.cuda.Stream()
         stream.wait_stream(torch.cuda.current_stream())
+        self._captured = (None, None)
+        self.regroup()
+        self._captured = self.groups                            # (a step captured earlier has its own)
         self.graph = torch.cuda.CUDAGraph()
         with torch.cuda.stream(stream):
             torch.matmul(x_in, self.layers[0]["Wqkv"])          # cuBLAS sets itself up outside a capture only
@@ -148,6 +166,8 @@ class PagedStack:
 
     def replay(self):
         """The captured step: one more token of every open place, as ``step``."""
+        if self._grouped != self.table.changes:
+            self.regroup()
         self.table.grow(1)
         self.graph.replay()
         self.table.advance_held(1)

@@ -372,6 +372,7 @@ class PageTable:
         self.lens = torch.full((n_seq,), -1, dtype=torch.int32, device=device)
         self.pos = torch.full((n_seq,), -1, dtype=torch.int32, device=device)
         self._shrink: Optional[List[List[int]]] = None     # pages that ``shrink`` handed out
+        self.changes = 0                                   # places that began anew on other pages: ``groups`` of before do not hold
 
     def counts(self, new) -> List[int]:
         """Tokens of every place (``new``: a number, or one for each place): none of idle ones, which
@@ -400,6 +401,7 @@ class PageTable:
     def open(self, s: int):
         """A new sequence at place s."""
         self.close(s)
+        self.changes += 1
         self.held[s] = self.seen[s] = 0
         self.lens[s] = 0
         self.pos[s] = 0
@@ -424,6 +426,7 @@ class PageTable:
         if self.held[s] != self.seen[s]:
             raise ValueError(f"PageTable.share: place {s} has shed {self.seen[s] - self.held[s]} of its tokens")
         self.close(t)
+        self.changes += 1
         k = min(tokens, self.held[s]) // self.page
         self.pages[t] = self.pages[s][:k]
         for page in self.pages[t]:
@@ -437,7 +440,10 @@ class PageTable:
 
     def groups(self):
         """(groups, prefix) for ``PagedCache.attend``: runs of places whose sequences begin with the same
-        pages.  (None, None) where none do."""
+        pages.  (None, None) where none do.  They hold as long as ``changes`` stays what it is (more tokens and
+        closed places do not matter).  Whether a group pays is not asked: it does from some 65000 positions that
+        are not read again on, at 8 KV heads and d = 128, and calls of few sequences over short prefixes are faster
+        without (4 over 512: 11 us, 15 with)."""
         live = [s for s, h in enumerate(self.held) if h >= 0]
         whole = [self.pages[s][:self.held[s] // self.page] for s in live]
         # (what neighbours have in common; a run has the least of it)
@@ -526,6 +532,7 @@ class PageTable:
         if self._shrink is None:
             raise ValueError("PageTable.shrunk: no shrink before it")
         new, self._shrink = self._shrink, None
+        self.changes += 1
         for s, pages in enumerate(new):
             self._give(self.pages[s])
             self.pages[s] = pages
