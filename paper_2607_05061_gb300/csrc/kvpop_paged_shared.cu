@@ -25,6 +25,7 @@ namespace kvpop {
 namespace {
 
 constexpr int PLAN_THREADS = 256;
+constexpr int FEW_ROWS = 8;            // that the kernel for few rows takes at once
 constexpr int ANY_LEN = 0x7fffff00;    // as a length: its tokens see all positions there are
 
 struct PlanArgs {
@@ -37,7 +38,7 @@ struct PlanArgs {
   int own_tiles;                       // whether it takes sequences' own parts
   int* tiles_out;                      // Parts::tiles
   int room, sms;                       // CTAs that parts may take
-  int rows, one;                       // rows that the other kernel takes at once, and groups of one token
+  int one;                             // groups of rows of one token, for the other kernel
   float block_us;                      // of the tcgen05 kernel
 };
 
@@ -147,16 +148,18 @@ __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(PlanArgs a) {
     const int most_parts = all > 0 ? min(a.room / all, PP_MORE_PARTS) : 0;
     if (most_parts > 1) share = max(share_of<false>(all, most, all_blocks, a.sms, most_parts, lane), 1);
     // Both kernels fill the SMs, one after the other, unless this leaves some of them to the other: then
-    // they run side by side.  us of a place of its list and CTA, and of both kernels' ends (64 sequences over
-    // 32768 positions with 100 to 2000 own ones: one after the other 116 us, side by side 100; three ragged
-    // groups 58, 49; drafted tokens over two prefixes 28, 26.  With 0.1 or 0.2 us a place, ends of 6 or 12,
-    // within 12% of that).
+    // they run side by side.  us of a place of its list and CTA, and of both kernels' ends, set on 64 sequences over
+    // 32768 positions with 100 to 2000 own ones (one after the other 116 us, side by side 100), three ragged
+    // groups (58, 49) and drafted tokens over two prefixes (28, 26); with 0.1 or 0.2 us a place, ends of 6 or 12,
+    // within 12% of that.  Over 24 to 128 sequences of 100 to 4000 own positions over 4096 to 65536 shared ones, both
+    // types and head sizes, 1 to 8 KV heads, 1 and 4 groups (86 measured): what this chooses takes 0.70 to 1.03
+    // of one after the other, but once 1.11 (64 of 100 over 4096, fp32: 36.9, 33.2).
     constexpr float PLACE_US = 0.14f, FEW_US = 10.f, ENDS_US = 9.f;
     float work = 0.f;
     for (int i = lane; i < ng + n; i += 32) {
       const Entry& e = a.entries[i];
       if (e.place >= 0) continue;
-      const float units = e.n > 1 ? ceilf((float)e.n * (float)a.G / (float)a.rows) : (float)(e.n * a.one);
+      const float units = e.n > 1 ? ceilf((float)e.n * (float)a.G / (float)FEW_ROWS) : (float)(e.n * a.one);
       work += units * (float)(max((e.ctx + BLK - 1) / BLK - e.begin / BLK, 1) + AT_ENDS);
     }
 #pragma unroll
@@ -340,17 +343,16 @@ Layout layout(const Batch& b, int n_groups, int HQ, int H, int d) {
   return l;
 }
 
-// Groups of 8 rows that the kernel for few rows takes at once.
-int groups_of_8(const Batch& b, int G, bool beside) {
-  const long long rows = !b.starts || beside ? G : ((long long)b.n_tokens * G + b.n_seq - 1) / b.n_seq;
-  return rows <= 8 ? 1 : 2;
-}
+// The kernel for few rows, FEW_ROWS at once.  us so / 16 at once, over 4096 shared positions and 4 KV heads:
+// 32 sequences with 1000 own positions, 16 query heads, d = 128 fp32 36.3 / 37.4, bf16 32.3 / 37.9, d = 64 31.2 /
+// 31.3, 27.5 / 30.9; 3 with 3000 21.3 / 27.0, 20.7 / 25.7, 18.8 / 21.0, 18.7 / 21.4; 7 of 2 tokens and 4 heads
+// 22.1 / 29.1, 21.8 / 26.6, 20.2 / 22.0, 19.8 / 22.2; 5 of 3 tokens over 8192 28.7 / 32.8, 27.0 / 29.2, 26.1 /
+// 24.5, 25.4 / 23.5.
 template <int D>
-cudaError_t launch_few(const AttendArgs& a, int nt, int sms, bool precise, cudaStream_t stream) {
+cudaError_t launch_few(const AttendArgs& a, int sms, bool precise, cudaStream_t stream) {
   const int grid = AT_CTAS * sms;
-  if (precise)
-    return nt == 1 ? launch_attend<D, 1, D == 64 ? 8 : 6, true, true>(a, grid, stream) : launch_attend<D, 2, 4, true, true>(a, grid, stream);
-  return nt == 1 ? launch_attend<D, 1, D == 64 ? 8 : 6, false, true>(a, grid, stream) : launch_attend<D, 2, 6, false, true>(a, grid, stream);
+  constexpr int W = D == 64 ? 8 : 6;
+  return precise ? launch_attend<D, 1, W, true, true>(a, grid, stream) : launch_attend<D, 1, W, false, true>(a, grid, stream);
 }
 
 }  // namespace
@@ -389,9 +391,7 @@ cudaError_t launch_paged_shared(const Pool& pool, const Batch& b, const int32_t*
   const long long grid_tc = tiles * H + sms;
   plan.room = (int)std::min<long long>(grid_tc, slots_of(sms));
   plan.sms = sms;
-  const int nt = groups_of_8(b, G, tiles > 0), one = (G + 8 * nt - 1) / (8 * nt);
-  plan.rows = 8 * nt;
-  plan.one = one;
+  plan.one = (G + FEW_ROWS - 1) / FEW_ROWS;
   plan.block_us = pool.d == 128 ? (out_f32 ? 1.5f : 0.95f) : out_f32 ? 1.f : 0.7f;
   cudaError_t e = launch_after(shared_plan_kernel, 1, PLAN_THREADS, plan, stream);
   if (e != cudaSuccess) return e;
@@ -454,9 +454,9 @@ cudaError_t launch_paged_shared(const Pool& pool, const Batch& b, const int32_t*
   a.G = G;
   a.inv_g = 1.f / (float)G;
   a.skip_long = tiles > 0;
-  a.one = one;
+  a.one = plan.one;
   a.to = to;
-  e = pool.d == 128 ? launch_few<128>(a, nt, sms, out_f32 != 0, stream) : launch_few<64>(a, nt, sms, out_f32 != 0, stream);
+  e = pool.d == 128 ? launch_few<128>(a, sms, out_f32 != 0, stream) : launch_few<64>(a, sms, out_f32 != 0, stream);
   if (e != cudaSuccess) return e;
   join.b = b;
   join.from = to;

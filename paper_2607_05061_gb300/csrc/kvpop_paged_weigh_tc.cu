@@ -53,7 +53,10 @@ constexpr int WT_SOFT = 8, WT_MMA_WARP = WT_SOFT, WT_COPY_WARP = WT_SOFT + 1, WT
 constexpr int WT_KEY_WARP = WT_COPY_WARP + WT_COPY, WT_KEY = 4;
 constexpr int WT_THREADS = 32 * (WT_KEY_WARP + WT_KEY);
 constexpr int WT_OLD = 8;                                // tiles whose scales and weights so far are held
-constexpr int WT_WHOLE = 8;                              // tiles of up to that many blocks are not cut
+// Tiles of up to that many blocks are not cut.  us with 8, 16, 32 (d = 128, 4 heads a KV head): 3 sequences of 9000
+// with 600 new tokens (19 blocks) 141, 149, 142; 6 of 3000 with 500 (16) 95, 102, 102; one of 2000 with 700 (22)
+// 30, 39, 42; 2 of 16000 with 1000 (32) 138, 140, 159; d = 64 alike.  (Rows that stay in the slots are whole tiles.)
+constexpr int WT_WHOLE = 8;
 // What a tile's ends cost beside its blocks, in blocks (a prompt of 6001 tokens: 0 177 us, 2 150, 3 145, 4 147, 6 149).
 constexpr int WT_ENDS = 3;
 constexpr float kLog2E = 1.4426950408889634f;

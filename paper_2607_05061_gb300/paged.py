@@ -24,7 +24,8 @@ import numpy as np
 import torch
 
 from .kvpop import (KVPOP_BF16, KVPOP_F32, _ck, _ptr, _raw_stream, _stream, kvpop_paged_append, kvpop_paged_append_at,
-                    kvpop_paged_attend_shared, kvpop_paged_evict, kvpop_paged_shared_bytes, kvpop_paged_weigh, kvpop_paged_attend, kvpop_paged_batch, kvpop_paged_pool, kvpop_paged_workspace_bytes, kvpop_rows)
+                    kvpop_paged_attend, kvpop_paged_attend_shared, kvpop_paged_batch, kvpop_paged_evict,
+                    kvpop_paged_pool, kvpop_paged_shared_bytes, kvpop_paged_weigh, kvpop_paged_workspace_bytes, kvpop_rows)
 
 BLOCK = 16               # tokens that share a scale
 _F8 = torch.float8_e4m3fn
